@@ -1,7 +1,6 @@
 """Sequence operators beside the blurry window: what is measured of them, and their plain forms.
 
-Three operators, each with the call that reads a prompt and the call that takes one token per row, and the backward
-pass of the two that a model around the blurry window is trained with:
+Three operators, each with the call that reads a prompt, its backward pass, and the call that takes one token per row:
 
   window  softmax attention over the last `window` tokens and the first `sinks` tokens of the sequence; heads share
           keys and values in groups; a row's past lies in a ring of sinks + window slots
@@ -9,7 +8,7 @@ pass of the two that a model around the blurry window is trained with:
   conv    the short causal convolution of each channel in front of a sequence operator, with bias and SiLU
           (conv_forward, conv_backward, conv_step)
   ssm     the selective state space scan h_t = exp(dt_t A) h_{t-1} + dt_t B_t x_t^T, y_t = C_t h_t + D x_t of each head
-          (ssm_forward, ssm_step)
+          (ssm_forward, ssm_backward, ssm_step)
 
 The plain forms compute in float32 (running sums of decays in float64) and round once, at the end.
 """
@@ -49,15 +48,15 @@ def listed():
         # its gradient in a training step
         {"name": "conv training", "kind": "conv_backward", "dtype": "bf16", "B": 8, "H": 16, "L": 4096, "d": 64, "taps": 4,
          "silu": True, "state": False, "ragged": False},
-        # and its decode step
-        {"name": "conv step", "kind": "conv_step", "dtype": "bf16", "B": 512, "H": 16, "L": 1, "d": 64, "taps": 4,
-         "silu": True, "state": True, "ragged": False},
         # a prompt batch of the LM layer's shape through the scan
         {"name": "ssm prompt", "kind": "ssm_forward", "dtype": "bf16", "B": 8, "H": 16, "G": 1, "L": 4096, "d": 64, "N": 128,
          "state": False, "ragged": False},
         # two long rows in float32 that continue from their states, of lengths that no tile divides
         {"name": "ssm long", "kind": "ssm_forward", "dtype": "f32", "B": 2, "H": 8, "G": 2, "L": 16411, "d": 64, "N": 64,
          "state": True, "ragged": True},
+        # the backward pass of a training step through the scan
+        {"name": "ssm training", "kind": "ssm_backward", "dtype": "bf16", "B": 8, "H": 16, "G": 2, "L": 2048, "d": 64, "N": 64,
+         "state": False, "ragged": False},
         # a decode step of a full serving batch: reads and writes every row's state
         {"name": "ssm step", "kind": "ssm_step", "dtype": "bf16", "B": 512, "H": 16, "G": 1, "L": 1, "d": 64, "N": 128,
          "state": True, "ragged": False},
@@ -70,11 +69,13 @@ def _log(rng, lo, hi):
 
 def draw(rng):
     kind = rng.choice(["window_forward", "window_forward", "window_backward", "window_step", "window_step", "conv_forward",
-                       "conv_backward", "conv_step", "ssm_forward", "ssm_forward", "ssm_step"])
+                       "conv_backward", "conv_step", "ssm_forward", "ssm_forward", "ssm_backward", "ssm_step"])
     c = {"kind": kind, "dtype": rng.choice(["bf16", "bf16", "f32"]), "d": rng.choice([32, 64, 128]), "ragged": rng.random() < 0.4}
     step = kind.endswith("step")
-    c["L"] = 1 if step else _log(rng, 1, 65536 if kind != "window_backward" else 8192)
+    c["L"] = 1 if step else _log(rng, 1, 65536 if not kind.endswith("backward") else 8192)
     c["H"] = rng.choice([1, 2, 4, 8, 12, 16])
+    if kind.endswith("backward"):  # nobody trains on a token, and some of its gradients are nothing but roundings
+        c["L"] = max(c["L"], 16)
     c["B"] = _log(rng, 1, 512 if step else 16)
     if kind.startswith("window"):
         c["Hkv"] = rng.choice([g for g in (1, 2, 3, 4, 8, 16) if c["H"] % g == 0])
@@ -82,7 +83,7 @@ def draw(rng):
         c["sinks"] = rng.choice([0, 1, 4, 7, 64])
         c["cached"] = step or (kind == "window_forward" and rng.random() < 0.4)
         if kind == "window_backward":  # a query with one key has no gradient but roundings
-            c["L"], c["window"] = max(c["L"], 16), max(c["window"], 8)
+            c["window"] = max(c["window"], 8)
     elif kind.startswith("conv"):
         c["taps"] = rng.choice([1, 2, 3, 4, 4, 7])
         c["silu"] = rng.random() < 0.7
@@ -165,6 +166,9 @@ def work(case):
     st = B * H * N * d * 4
     if c["kind"] == "ssm_step":
         return {"bytes": 2 * st + B * (2 * H * d * e + 4 * H + 2 * G * N * e), "flops": 6 * B * H * N * d}
+    if c["kind"] == "ssm_backward":  # 64-token chunks: C B^T, dy x^T, three products with them; six with the states
+        return {"bytes": toks * (3 * H * d * e + 8 * H + 4 * G * N * e) + st * (3 if c["state"] else 0),
+                "flops": toks * H * (2 * 64 * (3 * N + 2 * d) + 12 * N * d)}
     # 64-token chunks: C B^T, its product with x, the state's reading and its update
     return {"bytes": toks * (2 * H * d * e + 4 * H + 2 * G * N * e) + st * (2 if c["state"] else 1),
             "flops": toks * H * (2 * 64 * N + 2 * 64 * d + 4 * N * d)}
@@ -219,6 +223,9 @@ def prepare(case, seed):
         s["A"], s["D"] = -uniform(1, 16, H), uniform(0.5, 1.5, H)
         s["Bm"], s["Cm"] = normal(B, G, *tok, N), normal(B, G, *tok, N)
         s["state"] = normal(B, H, N, d, dtype=F32, std=0.3) if c["state"] else None
+        if c["kind"] == "ssm_backward":
+            s["dy"] = normal(B, H, L, d)
+            s["dstate"] = normal(B, H, N, d, dtype=F32, std=0.3) if c["state"] else None
         if one:
             s["state_out"] = torch.empty_like(s["state"])
     return s
@@ -252,6 +259,10 @@ def _own(s):
         return [y, s["state_out"]]
     if kind == "ssm_forward":
         return list(bla.ssm_forward(s["x"], s["dt"], s["A"], s["Bm"], s["Cm"], s["D"], state=s["state"], lengths=s["lengths"]))
+    if kind == "ssm_backward":
+        got = bla.ssm_backward(s["x"], s["dt"], s["A"], s["Bm"], s["Cm"], s["dy"], s["D"], state=s["state"], dstate=s["dstate"],
+                               lengths=s["lengths"], want_state_grad=c["state"])
+        return list(got) if c["state"] else list(got[:6])
     y = bla.ssm_step(s["x"], s["dt"], s["A"], s["Bm"], s["Cm"], s["state"], s["D"], state_out=s["state_out"])
     return [y, s["state_out"]]
 
@@ -424,7 +435,8 @@ def _conv_backward(s):
     return [dx, dw, db] + ([dext[:, :, :K - 1].contiguous()] if c["state"] else [])
 
 
-def _ssm_forward(s):
+def _ssm_parts(s):
+    """64-token chunks: the inputs of each, the exponents of the decays and the states that enter the chunks (and leave the last)."""
     c = s["case"]
     B, H, L, d = s["x"].shape
     G, N, n = c["G"], c["N"], 64
@@ -432,28 +444,69 @@ def _ssm_forward(s):
     lens = torch.full((B,), L, dtype=torch.int64, device=s["x"].device) if s["lengths"] is None else s["lengths"].long()
     ok = (torch.arange(L, device=lens.device)[None] < lens[:, None])[:, None]
     pad = nb * n - L
-    cut = lambda x: torch.nn.functional.pad(x, (0, 0, 0, pad)).reshape(x.shape[0], x.shape[1], nb, n, x.shape[-1])  # noqa: E731
-    dt = torch.where(ok, s["dt"], torch.zeros_like(s["dt"]))
-    dt = torch.nn.functional.pad(dt, (0, pad)).reshape(B, H, nb, n)
-    zero = lambda x: torch.where(ok[..., None], x.float(), torch.zeros(1, device=x.device))  # noqa: E731
-    x, bm, cm = cut(zero(s["x"])), cut(zero(s["Bm"])), cut(zero(s["Cm"]))
-    a = torch.cumsum(dt.double() * s["A"].double()[None, :, None, None], -1)              # decay exponents in a chunk
+    cut = lambda x: torch.nn.functional.pad(torch.where(ok[..., None], x.float(), 0.0), (0, 0, 0, pad)).reshape(  # noqa: E731
+        B, x.shape[1], nb, n, x.shape[-1])
+    dt = torch.nn.functional.pad(torch.where(ok, s["dt"], 0.0), (0, pad)).reshape(B, H, nb, n)
     heads = lambda t: t.repeat_interleave(H // G, 1)  # noqa: E731
+    x, bm, cm = cut(s["x"]), cut(s["Bm"]), cut(s["Cm"])
+    a = torch.cumsum(dt.double() * s["A"].double()[None, :, None, None], -1)              # decay exponents in a chunk
     low = torch.tril(torch.ones(n, n, dtype=torch.bool, device=x.device))
     decay = torch.where(low, torch.exp(torch.where(low, a[..., :, None] - a[..., None, :], 0.0)), 0.0).float()
-    y = torch.matmul(heads(torch.matmul(cm, bm.transpose(-1, -2))) * decay * dt[..., None, :], x)
-    to_end = (torch.exp(a[..., -1:] - a) * dt).float()
-    own_state = torch.matmul((heads(bm) * to_end[..., None]).transpose(-1, -2), x)        # [B, H, nb, N, d]
     total = torch.cumsum(a[..., -1], -1)                                                  # [B, H, nb]
     ends = torch.nn.functional.pad(total, (1, 0))                                         # exponent before chunk 0 .. nb
     past = torch.ones(nb + 1, nb, dtype=torch.bool, device=x.device).tril(-1)
     carry = torch.where(past, torch.exp(torch.where(past, ends[..., :, None] - total[..., None, :], 0.0)), 0.0).float()
+    to_end = torch.exp(a[..., -1:] - a).float()
+    own_state = torch.matmul((heads(bm) * (to_end * dt)[..., None]).transpose(-1, -2), x)  # [B, H, nb, N, d]
     enter = torch.matmul(carry, own_state.reshape(B, H, nb, N * d)).reshape(B, H, nb + 1, N, d)
     if s["state"] is not None:
         enter = enter + torch.exp(ends).float()[..., None, None] * s["state"][:, :, None]
+    return cut, heads, x, bm, cm, dt, a, decay, to_end, ends, enter, (nb, n)
+
+
+def _ssm_forward(s):
+    cut, heads, x, bm, cm, dt, a, decay, to_end, ends, enter, (nb, n) = _ssm_parts(s)
+    B, H, L, d = s["x"].shape
+    y = torch.matmul(heads(torch.matmul(cm, bm.transpose(-1, -2))) * decay * dt[..., None, :], x)
     y = y + torch.matmul(heads(cm), enter[:, :, :nb]) * torch.exp(a).float()[..., None]
     y = y + s["D"][None, :, None, None, None] * x
     return [y.reshape(B, H, nb * n, d)[:, :, :L].to(s["x"].dtype), enter[:, :, nb].contiguous()]
+
+
+def _ssm_backward(s):
+    cut, heads, x, bm, cm, dt, a, decay, to_end, ends, enter, (nb, n) = _ssm_parts(s)
+    B, H, L, d = s["x"].shape
+    G, N = s["case"]["G"], s["case"]["N"]
+    dy, bh, ch = cut(s["dy"]), heads(bm), heads(cm)
+    down = torch.exp(a).float()
+    A = s["A"][None, :, None, None]
+    # the gradient of the state that leaves each chunk
+    own_grad = torch.matmul((ch * down[..., None]).transpose(-1, -2), dy).reshape(B, H, nb, N * d)
+    later = torch.ones(nb + 1, nb, dtype=torch.bool, device=x.device).triu(0)
+    back = torch.where(later, torch.exp(torch.where(later, ends[..., None, :-1] - ends[..., :, None], 0.0)), 0.0).float()
+    g = torch.matmul(back, own_grad).reshape(B, H, nb + 1, N, d)                          # before chunk 0 .. nb
+    if s["dstate"] is not None:
+        g = g + torch.exp(ends[..., -1:] - ends).float()[..., None, None] * s["dstate"][:, :, None]
+    gout, hin = g[:, :, 1:], enter[:, :, :nb]
+    cb, yx = heads(torch.matmul(cm, bm.transpose(-1, -2))) * decay, torch.matmul(dy, x.transpose(-1, -2)) * decay
+    gb, hy = torch.matmul(bh, gout) * to_end[..., None], torch.matmul(dy, hin.transpose(-1, -2)) * down[..., None]
+    gx = torch.matmul(x, gout.transpose(-1, -2)) * to_end[..., None]
+    dx = dt[..., None] * (torch.matmul(cb.transpose(-1, -2), dy) + gb) + s["D"][None, :, None, None, None] * dy
+    dc = torch.matmul(yx * dt[..., None, :], bh) + hy
+    db = dt[..., None] * (torch.matmul(yx.transpose(-1, -2), ch) + gx)
+    pair = yx.double() * heads(torch.matmul(cm, bm.transpose(-1, -2))).double()
+    late = (gx * bh).double().sum(-1)
+    direct = pair.sum(-2) + late
+    ds = (pair * dt[..., None, :]).sum(-1) + (hy * ch).double().sum(-1) - dt * direct
+    end = (dt * late).sum(-1) + torch.exp(a[..., -1]) * (gout * hin).double().sum((-1, -2))
+    da = ds.flip(-1).cumsum(-1).flip(-1) + end[..., None]
+    ddt = direct + A * da
+    flat = lambda t: t.reshape(t.shape[0], t.shape[1], nb * n, *t.shape[4:])[:, :, :L]  # noqa: E731
+    shared = lambda t: flat(t.reshape(B, G, H // G, nb, n, N).sum(2)).to(s["x"].dtype)  # noqa: E731
+    ok = torch.arange(L, device=x.device)[None, None] < (L if s["lengths"] is None else s["lengths"].long()[:, None, None])
+    got = [flat(dx).to(s["x"].dtype), torch.where(ok, flat(ddt), 0.0).float(), (da * dt).sum((0, 2, 3)).float(), shared(db), shared(dc),
+           (dy * x).double().sum((0, 2, 3, 4)).float()]
+    return got + ([g[:, :, 0].contiguous()] if s["case"]["state"] else [])
 
 
 def _ssm_step(s):
@@ -483,7 +536,8 @@ def run(state):
     if kind == "window_forward":
         return _window_forward(state) + (list(_rings(state)) if state["case"]["cached"] else [])
     return {"window_backward": _window_backward, "window_step": _window_step, "conv_forward": _conv_forward,
-            "conv_backward": _conv_backward, "conv_step": _conv_forward, "ssm_forward": _ssm_forward, "ssm_step": _ssm_step}[kind](state)
+            "conv_backward": _conv_backward, "conv_step": _conv_forward, "ssm_forward": _ssm_forward, "ssm_backward": _ssm_backward,
+            "ssm_step": _ssm_step}[kind](state)
 
 
 # ---- the definitions in 64 bits, row by row and token by token ----
@@ -578,19 +632,44 @@ def _exact_ssm(s):
     lens = torch.tensor(_lengths(c) or [L] * B, device=x.device)[:, None]
     h = torch.zeros(B, H, N, d, dtype=F64, device=x.device) if s["state"] is None else s["state"].double()
     y = torch.zeros_like(x)
+    kept = [h]
     for t in range(L):
         go = (t < lens).double()
         step = dt[:, :, t] * go
         h = torch.exp(step * A)[..., None, None] * h
         h = torch.addcmul(h, (step[..., None] * bm[:, :, t].repeat_interleave(rep, 1))[..., None], x[:, :, t, None, :])
         y[:, :, t] = ((cm[:, :, t].repeat_interleave(rep, 1)[..., None] * h).sum(-2) + D * x[:, :, t]) * go[..., None]
-    return [y.squeeze(2) if one else y, h]
+        if c["kind"] == "ssm_backward":
+            kept.append(h)
+    if c["kind"] != "ssm_backward":
+        return [y.squeeze(2) if one else y, h]
+    g = torch.zeros_like(h) if s["dstate"] is None else s["dstate"].double()
+    dx, ddt, db, dc = torch.zeros_like(x), torch.zeros_like(dt), torch.zeros_like(bm), torch.zeros_like(cm)
+    dA, dD = torch.zeros(H, dtype=F64, device=x.device), torch.zeros(H, dtype=F64, device=x.device)
+    shared = lambda w: w.reshape(B, c["G"], rep, N).sum(2)  # noqa: E731
+    for t in reversed(range(L)):
+        go = (t < lens).double()
+        step = dt[:, :, t] * go
+        dy = s["dy"][:, :, t].double() * go[..., None]
+        bh, ch, xt = bm[:, :, t].repeat_interleave(rep, 1), cm[:, :, t].repeat_interleave(rep, 1), x[:, :, t] * go[..., None]
+        dh = torch.addcmul(g, ch[..., None], dy[..., None, :])
+        g = torch.exp(step * A)[..., None, None] * dh
+        along = (g * kept[t]).sum((-1, -2))
+        bdh = (bh[..., None] * dh).sum(-2)
+        dx[:, :, t] = step[..., None] * bdh + D * dy
+        ddt[:, :, t] = ((bdh * xt).sum(-1) + A * along) * go
+        db[:, :, t] = shared(step[..., None] * (dh * xt[..., None, :]).sum(-1))
+        dc[:, :, t] = shared((kept[t + 1] * dy[..., None, :]).sum(-1))
+        dA, dD = dA + (step * along).sum(0), dD + (xt * dy).sum((0, 2))
+    return [dx, ddt, dA, db, dc, dD] + ([g] if c["state"] else [])
 
 
 def exact(case, seed):
     c = dict(case)
-    s = prepare(c, seed)
     kind = c["kind"]
+    if kind == "ssm_backward" and c["B"] * c["H"] * c["L"] * c["N"] * c["d"] * 8 > 6e10:  # every token's state
+        return None
+    s = prepare(c, seed)
     if kind == "window_step":
         return _exact_window(s) + [None, None]
     if kind.startswith("window"):
