@@ -315,6 +315,69 @@ bla_status bla_layer_forward_timed(const bla_params* p, const double* T, const v
                                    float* state_k_out, float* state_v_out, void* workspace,
                                    size_t workspace_bytes, void* stream, void* const* events);
 
+/*
+ * Window attention with sinks: exact softmax attention on the near past (the attention of Sec. 2.1 over the sliding
+ * window that the state-decay form has as its limit).  The query at absolute position p sees the keys at positions j <= p with
+ * p - j < window, and those with j < sinks:
+ *     o_p = sum_j softmax_j(scale <q_p, k_j>) v_j.
+ * Query heads share keys and values in groups: query head h reads key head h / (H / H_kv).
+ *   q, o: [B, H, L, d]   k, v: [B, H_kv, L, d]   (bla_window_step: L is absent)
+ * The past of a row is a ring of sinks + window slots in the io dtype,
+ *   cache_k, cache_v: [B, H_kv, sinks + window, d],
+ * which holds position j in slot j while j < sinks, and in slot sinks + (j - sinks) mod window after.  Slots that no
+ * token has reached are never read.
+ *   lengths (device int32 [B], NULL = L): row b has only its first lengths[b] tokens (clamped to 0 .. L).  The rest is padding: its
+ *   q, k, v (and dO) are not read, its outputs are zeros (lse: minus infinity; gradients: zeros).
+ *   pos (device int64 [B], NULL = t0): the absolute position of row b's token 0.  A row whose position is negative or past
+ *   2^62 has no tokens in this call (an idle row of a serving batch): zeros as for padding, and its ring stays.
+ * A non-finite value in a token of the sequence may reach the outputs of other queries that share a tile of keys with it.
+ * Supported: float32 or bfloat16; d in {32, 64, 128}; H a multiple of H_kv; window >= 1, sinks >= 0, window + sinks <= 2^30; 1e-6 <=
+ * |scale| <= 1e6.  Alignment, ownership, streams, workspaces and errors follow the conventions above; the outputs must not
+ * overlap the inputs (BLA_ERR_INVALID_ARG).
+ */
+typedef struct {
+    int32_t B, H, H_kv, L; /* batch rows, query heads, key heads, tokens in this call       */
+    int32_t d;             /* head width                                                  */
+    int32_t window, sinks; /* keys of the window (the query's own is one), first keys kept  */
+    int32_t io_dtype;      /* bla_dtype of q, k, v, o and the rings                         */
+    int64_t t0;            /* absolute position of token 0 of every row (pos = NULL)        */
+    float scale;           /* softmax scale; 0 selects 1/sqrt(d)                            */
+} bla_window_params;
+
+/* BLA_OK if the shape in *p has kernels, else the error it would get. */
+bla_status bla_window_supported(const bla_window_params* p);
+
+/* Bytes of device workspace bla_window_forward needs (0: none, or *p is not supported). */
+size_t bla_window_workspace_size(const bla_window_params* p);
+
+/*
+ * L tokens of every row.  cache_k_in / cache_v_in: the rings before token 0 (both or neither; NULL: nothing before token 0
+ * exists).  lse [B, H, L] float32 (NULL = not wanted) receives log sum_j exp(scale <q, k_j>), which bla_window_backward
+ * takes.  cache_k_out / cache_v_out receive the rings after the call (both or neither; slots without a token are copied from
+ * the input rings, or zero).
+ */
+bla_status bla_window_forward(const bla_window_params* p, const void* q, const void* k, const void* v,
+                              const int32_t* lengths, const int64_t* pos, const void* cache_k_in,
+                              const void* cache_v_in, void* o, float* lse, void* cache_k_out, void* cache_v_out,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace bla_window_step needs (p->L is ignored). */
+size_t bla_window_step_workspace_size(const bla_window_params* p);
+
+/* One token for every row: the rings take its key and value in place. */
+bla_status bla_window_step(const bla_window_params* p, const void* q, const void* k, const void* v, const int64_t* pos,
+                           void* cache_k, void* cache_v, void* o, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/*
+ * Gradients of bla_window_forward without rings and with t0 = 0 (BLA_ERR_UNSUPPORTED otherwise): o and lse are its outputs,
+ * dO = dLoss/dO.  dk and dv are summed over the query heads of a group.  The sums run in a fixed order (no atomics).
+ */
+size_t bla_window_backward_workspace_size(const bla_window_params* p);
+bla_status bla_window_backward(const bla_window_params* p, const void* q, const void* k, const void* v, const void* o,
+                               const float* lse, const void* dO, const int32_t* lengths, void* dq, void* dk, void* dv,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

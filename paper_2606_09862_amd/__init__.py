@@ -36,6 +36,13 @@ class Params(ctypes.Structure):
                 ("phase_anchor", ctypes.c_int32), ("reuse_tables", ctypes.c_int32)]
 
 
+class WindowParams(ctypes.Structure):
+    """Mirror of ``bla_window_params``."""
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("L", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("t0", ctypes.c_int64), ("scale", ctypes.c_float)]
+
+
 _lib = None
 _dp = ctypes.POINTER(ctypes.c_double)
 _vp = ctypes.c_void_p
@@ -87,6 +94,16 @@ def lib():
         L.bla_layer_forward_timed.argtypes = [P, _dp] + [_vp] * 9 + [ctypes.c_size_t, _vp,
                                                                        ctypes.POINTER(ctypes.c_void_p)]
         L.bla_layer_forward_timed.restype = ctypes.c_int
+        W = ctypes.POINTER(WindowParams)
+        for name in ("bla_window_workspace_size", "bla_window_step_workspace_size", "bla_window_backward_workspace_size"):
+            getattr(L, name).argtypes = [W]
+            getattr(L, name).restype = ctypes.c_size_t
+        L.bla_window_supported.argtypes = [W]
+        L.bla_window_forward.argtypes = [W] + [_vp] * 12 + [ctypes.c_size_t, _vp]
+        L.bla_window_step.argtypes = [W] + [_vp] * 8 + [ctypes.c_size_t, _vp]
+        L.bla_window_backward.argtypes = [W] + [_vp] * 11 + [ctypes.c_size_t, _vp]
+        for name in ("bla_window_supported", "bla_window_forward", "bla_window_step", "bla_window_backward"):
+            getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -396,3 +413,130 @@ def layer_forward(x, w_qkv, w_o, T, H: int, M: int, S: int, t0: int = 0, scale: 
     if st != 0:
         raise BlaError(st, "bla_layer_forward")
     return y, sk, sv
+
+
+# ---- window attention, the short convolution and the selective scan ----
+
+def _check_on(t, shape, dtype, name, dev):
+    """_check, and that the tensor lies on the call's device."""
+    _check(t, shape, dtype, name)
+    if t.device != dev:
+        raise ValueError(f"{name}: expected a tensor on {dev}, got {t.device}")
+
+
+def _io(t, name):
+    if t.dtype == torch.bfloat16:
+        return BLA_BF16
+    if t.dtype == torch.float32:
+        return BLA_F32
+    raise ValueError(f"{name}: expected torch.float32 or torch.bfloat16, got {t.dtype}")
+
+
+def _call(fn, what, dev, *args):
+    """The library's call on the tensors' device (which need not be the current one) and its current stream."""
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            st = fn(*args, _stream(dev))
+    else:
+        st = fn(*args, _stream(dev))
+    if st != 0:
+        raise BlaError(st, what)
+
+
+def _room(workspace, need, dev):
+    """The caller's workspace where it is large enough (a uint8 tensor on the call's device), else a fresh one."""
+    if workspace is not None and workspace.numel() >= need:
+        _check_on(workspace, workspace.shape, torch.uint8, "workspace", dev)
+        return workspace
+    return torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+
+
+def _window_params(q, k, window, sinks, t0, scale):
+    B, H, d = q.shape[0], q.shape[1], q.shape[-1]
+    L = q.shape[2] if q.dim() == 4 else 1
+    return WindowParams(B, H, k.shape[1] if k.dim() == q.dim() else 0, L, d, int(window), int(sinks), _io(q, "q"),
+                        int(t0), 0.0 if scale is None else float(scale))
+
+
+def _window_check(st, what):
+    if st != 0:
+        raise BlaError(st, f"{what} (shape check)")
+
+
+def window_forward(q, k, v, window: int, sinks: int = 0, t0: int = 0, scale: float | None = None, lengths=None, pos=None,
+                   cache_k=None, cache_v=None, want_lse: bool = False, want_cache: bool = False, workspace=None,
+                   out=None):
+    """bla_window_forward: softmax attention over the last `window` tokens and the first `sinks` tokens.
+
+    q [B,H,L,d], k and v [B,H_kv,L,d] (float32 or bfloat16), H a multiple of H_kv.  lengths (int32 [B]): tokens of each
+    row, the rest is padding (zeros in the output).  pos (int64 [B]) or t0: the position of each row's first token.
+    cache_k / cache_v [B,H_kv,sinks+window,d]: the rings before the call.  Returns (o, lse, cache_k_out, cache_v_out);
+    lse is float32 [B,H,L] (None unless want_lse), the rings are those after the call (None unless want_cache).
+    """
+    B, H, L, d = q.shape
+    Hkv, dt, dev = k.shape[1], q.dtype, q.device
+    p = _window_params(q, k, window, sinks, t0, scale)
+    _check_on(q, (B, H, L, d), dt, "q", dev)
+    _check_on(k, (B, Hkv, L, d), dt, "k", dev)
+    _check_on(v, (B, Hkv, L, d), dt, "v", dev)
+    ring = (B, Hkv, int(sinks) + int(window), d)
+    if (cache_k is None) != (cache_v is None):
+        raise ValueError("cache_k and cache_v: both or neither")
+    for name, t in (("cache_k", cache_k), ("cache_v", cache_v)):
+        if t is not None:
+            _check_on(t, ring, dt, name, dev)
+    if lengths is not None:
+        _check_on(lengths, (B,), torch.int32, "lengths", dev)
+    if pos is not None:
+        _check_on(pos, (B,), torch.int64, "pos", dev)
+    _window_check(lib().bla_window_supported(ctypes.byref(p)), "bla_window_forward")
+    o = _out(out, q, (B, H, L, d))
+    lse = torch.empty((B, H, L), dtype=torch.float32, device=dev) if want_lse else None
+    ck = torch.empty(ring, dtype=dt, device=dev) if want_cache else None
+    cv = torch.empty(ring, dtype=dt, device=dev) if want_cache else None
+    ws = _room(workspace, lib().bla_window_workspace_size(ctypes.byref(p)), dev)
+    _call(lib().bla_window_forward, "bla_window_forward", dev, ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(lengths),
+          _ptr(pos), _ptr(cache_k), _ptr(cache_v), _ptr(o), _ptr(lse), _ptr(ck), _ptr(cv), _ptr(ws), ws.numel())
+    return o, lse, ck, cv
+
+
+def window_step(q, k, v, window: int, sinks: int, cache_k, cache_v, pos=None, t0: int = 0, scale: float | None = None,
+                workspace=None, out=None):
+    """bla_window_step: one decode token per row, q [B,H,d], k and v [B,H_kv,d]; the rings cache_k / cache_v
+    [B,H_kv,sinks+window,d] take its key and value in place.  A row with a negative pos is idle (zeros)."""
+    B, H, d = q.shape
+    Hkv, dt, dev = k.shape[1], q.dtype, q.device
+    p = _window_params(q, k, window, sinks, t0, scale)
+    _check_on(q, (B, H, d), dt, "q", dev)
+    _check_on(k, (B, Hkv, d), dt, "k", dev)
+    _check_on(v, (B, Hkv, d), dt, "v", dev)
+    ring = (B, Hkv, int(sinks) + int(window), d)
+    _check_on(cache_k, ring, dt, "cache_k", dev)
+    _check_on(cache_v, ring, dt, "cache_v", dev)
+    if pos is not None:
+        _check_on(pos, (B,), torch.int64, "pos", dev)
+    _window_check(lib().bla_window_supported(ctypes.byref(p)), "bla_window_step")
+    o = _out(out, q, (B, H, d))
+    ws = _room(workspace, lib().bla_window_step_workspace_size(ctypes.byref(p)), dev)
+    _call(lib().bla_window_step, "bla_window_step", dev, ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(pos),
+          _ptr(cache_k), _ptr(cache_v), _ptr(o), _ptr(ws), ws.numel())
+    return o
+
+
+def window_backward(q, k, v, o, lse, dO, window: int, sinks: int = 0, scale: float | None = None, lengths=None,
+                    workspace=None):
+    """bla_window_backward: (dq, dk, dv) of window_forward without rings from its outputs o and lse and dO = dLoss/dO."""
+    B, H, L, d = q.shape
+    Hkv, dt, dev = k.shape[1], q.dtype, q.device
+    p = _window_params(q, k, window, sinks, 0, scale)
+    for name, t, h in (("q", q, H), ("k", k, Hkv), ("v", v, Hkv), ("o", o, H), ("dO", dO, H)):
+        _check_on(t, (B, h, L, d), dt, name, dev)
+    _check_on(lse, (B, H, L), torch.float32, "lse", dev)
+    if lengths is not None:
+        _check_on(lengths, (B,), torch.int32, "lengths", dev)
+    _window_check(lib().bla_window_supported(ctypes.byref(p)), "bla_window_backward")
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    ws = _room(workspace, lib().bla_window_backward_workspace_size(ctypes.byref(p)), dev)
+    _call(lib().bla_window_backward, "bla_window_backward", dev, ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
+          _ptr(lse), _ptr(dO), _ptr(lengths), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel())
+    return dq, dk, dv
