@@ -378,6 +378,92 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
                                const float* lse, const void* dO, const int32_t* lengths, void* dq, void* dk, void* dv,
                                void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * The short causal convolution of each channel, as the paper's models apply it to queries, keys and values ahead of the
+ * operator:
+ *     z_t = bias + sum_{j < taps} w[j] x_{t - taps + 1 + j},   y_t = z_t (silu = 0) or z_t sigmoid(z_t) (silu = 1).
+ *   x, y: [B, H, L, d] in the io dtype (bla_conv_step: L is absent; a tensor [B, L, C] is H = 1, d = C)
+ *   w: float32 [H, d, taps]   bias: float32 [H, d] (NULL = zero)
+ *   state: float32 [B, H, taps - 1, d], the taps - 1 tokens before the call, oldest first (NULL = zeros)
+ *   lengths: as for bla_window_forward; the state after the call is that after the row's last token.
+ * Supported: float32 or bfloat16, 1 <= taps <= 8, d a multiple of 8.  Sums are float32.  Outputs must not overlap inputs;
+ * bla_conv_step's state_out may be its state_in (updated in place).  Other conventions as above.
+ */
+typedef struct {
+    int32_t B, H, L, d;
+    int32_t taps;
+    int32_t silu;     /* 0 or 1 */
+    int32_t io_dtype; /* bla_dtype of x, y, dx, dy */
+} bla_conv_params;
+
+/* BLA_OK if the shape in *p has kernels, else the error it would get. */
+bla_status bla_conv_supported(const bla_conv_params* p);
+
+/* state_out (NULL = not wanted) receives the state after the call. */
+bla_status bla_conv_forward(const bla_conv_params* p, const void* x, const float* w, const float* bias,
+                            const int32_t* lengths, const float* state_in, void* y, float* state_out, void* stream);
+
+/* One token for every row (p->L is ignored). */
+bla_status bla_conv_step(const bla_conv_params* p, const void* x, const float* w, const float* bias,
+                         const float* state_in, void* y, float* state_out, void* stream);
+
+/*
+ * Gradients of bla_conv_forward from its inputs, dy = dLoss/dy and dstate_out = dLoss/d(state after the call) (NULL = zero):
+ * dx [B, H, L, d] (zeros in padding), dw [H, d, taps], dbias [H, d] (NULL = not wanted), dstate_in [B, H, taps - 1, d] (NULL = not
+ * wanted).  The sums over tokens and rows run in a fixed order.  B = 0 is BLA_ERR_UNSUPPORTED (dw would be left unwritten).
+ */
+size_t bla_conv_backward_workspace_size(const bla_conv_params* p);
+bla_status bla_conv_backward(const bla_conv_params* p, const void* x, const float* w, const float* bias, const void* dy,
+                             const int32_t* lengths, const float* state_in, const float* dstate_out, void* dx, float* dw,
+                             float* dbias, float* dstate_in, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The selective state space scan (the discrete state space model of Eq. ssm with a decay and an input matrix of each token):
+ * per row and head, with h the state (N x d),
+ *     h_t = exp(dt_t A) h_{t-1} + dt_t B_t x_t^T,   y_t = h_t^T C_t + D x_t.
+ * Heads share B and C in groups: head h uses group h / (H / G).
+ *   x, y: [B, H, L, d]   Bm, Cm: [B, G, L, N]   in the io dtype (bla_ssm_step: L is absent)
+ *   dt: float32 [B, H, L]   A: float32 [H]   D: float32 [H] (NULL = zero)   state: float32 [B, H, N, d] (NULL = zero)
+ *   lengths: as for bla_window_forward (padding is not read, y and the gradients are zero there, and the state after the call
+ *   is that after the row's last token).
+ * A is expected to be <= 0 with dt >= 0 (a decay); the formula is computed for any sign, and overflows where it does.
+ * A non-finite value in a token may reach the other tokens of its 64-token chunk.
+ * Supported: float32 or bfloat16; d in {32, 64, 128}; N a multiple of 8 up to 128; H a multiple of G.  The state and every sum are
+ * float32, the sums of dt A float64.  Outputs must not overlap inputs; bla_ssm_step's state_out may be its state_in
+ * (updated in place).  Other conventions as above.
+ */
+typedef struct {
+    int32_t B, H, G, L, d, N;
+    int32_t io_dtype; /* bla_dtype of x, Bm, Cm, y and their gradients */
+} bla_ssm_params;
+
+/* BLA_OK if the shape in *p has kernels, else the error it would get. */
+bla_status bla_ssm_supported(const bla_ssm_params* p);
+
+/* Bytes of device workspace bla_ssm_forward needs (0: none, or *p is not supported). */
+size_t bla_ssm_workspace_size(const bla_ssm_params* p);
+
+/* L tokens of every row; state_out (NULL = not wanted) receives the state after them. */
+bla_status bla_ssm_forward(const bla_ssm_params* p, const void* x, const float* dt, const float* A, const void* Bm,
+                           const void* Cm, const float* D, const int32_t* lengths, const float* state_in, void* y,
+                           float* state_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token for every row (p->L is ignored). */
+bla_status bla_ssm_step(const bla_ssm_params* p, const void* x, const float* dt, const float* A, const void* Bm,
+                        const void* Cm, const float* D, const float* state_in, void* y, float* state_out, void* stream);
+
+/*
+ * Gradients of bla_ssm_forward from its inputs, dy = dLoss/dy and dstate_out = dLoss/d(state after the call) (NULL = zero):
+ * dx, dB, dC in the io dtype (dB and dC summed over the heads of a group), ddt [B, H, L], dA [H], dD [H] (NULL = not wanted) and
+ * dstate_in [B, H, N, d] (NULL = not wanted) in float32.  The sums run in a fixed order (no atomics).  The workspace holds two
+ * states of every 64 tokens and head.  B = 0 or L = 0 is BLA_ERR_UNSUPPORTED.
+ */
+size_t bla_ssm_backward_workspace_size(const bla_ssm_params* p);
+bla_status bla_ssm_backward(const bla_ssm_params* p, const void* x, const float* dt, const float* A, const void* Bm,
+                            const void* Cm, const float* D, const void* dy, const int32_t* lengths, const float* state_in,
+                            const float* dstate_out, void* dx, float* ddt, float* dA, void* dB, void* dC, float* dD,
+                            float* dstate_in, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -43,6 +43,18 @@ class WindowParams(ctypes.Structure):
                 ("io_dtype", ctypes.c_int32), ("t0", ctypes.c_int64), ("scale", ctypes.c_float)]
 
 
+class ConvParams(ctypes.Structure):
+    """Mirror of ``bla_conv_params``."""
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("taps", ctypes.c_int32), ("silu", ctypes.c_int32), ("io_dtype", ctypes.c_int32)]
+
+
+class SsmParams(ctypes.Structure):
+    """Mirror of ``bla_ssm_params``."""
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("G", ctypes.c_int32), ("L", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("N", ctypes.c_int32), ("io_dtype", ctypes.c_int32)]
+
+
 _lib = None
 _dp = ctypes.POINTER(ctypes.c_double)
 _vp = ctypes.c_void_p
@@ -103,6 +115,25 @@ def lib():
         L.bla_window_step.argtypes = [W] + [_vp] * 8 + [ctypes.c_size_t, _vp]
         L.bla_window_backward.argtypes = [W] + [_vp] * 11 + [ctypes.c_size_t, _vp]
         for name in ("bla_window_supported", "bla_window_forward", "bla_window_step", "bla_window_backward"):
+            getattr(L, name).restype = ctypes.c_int
+        C = ctypes.POINTER(ConvParams)
+        L.bla_conv_backward_workspace_size.argtypes = [C]
+        L.bla_conv_backward_workspace_size.restype = ctypes.c_size_t
+        L.bla_conv_supported.argtypes = [C]
+        L.bla_conv_forward.argtypes = [C] + [_vp] * 8
+        L.bla_conv_step.argtypes = [C] + [_vp] * 7
+        L.bla_conv_backward.argtypes = [C] + [_vp] * 12 + [ctypes.c_size_t, _vp]
+        for name in ("bla_conv_supported", "bla_conv_forward", "bla_conv_step", "bla_conv_backward"):
+            getattr(L, name).restype = ctypes.c_int
+        S = ctypes.POINTER(SsmParams)
+        for name in ("bla_ssm_workspace_size", "bla_ssm_backward_workspace_size"):
+            getattr(L, name).argtypes = [S]
+            getattr(L, name).restype = ctypes.c_size_t
+        L.bla_ssm_supported.argtypes = [S]
+        L.bla_ssm_forward.argtypes = [S] + [_vp] * 11 + [ctypes.c_size_t, _vp]
+        L.bla_ssm_step.argtypes = [S] + [_vp] * 10
+        L.bla_ssm_backward.argtypes = [S] + [_vp] * 18 + [ctypes.c_size_t, _vp]
+        for name in ("bla_ssm_supported", "bla_ssm_forward", "bla_ssm_step", "bla_ssm_backward"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -540,3 +571,161 @@ def window_backward(q, k, v, o, lse, dO, window: int, sinks: int = 0, scale: flo
     _call(lib().bla_window_backward, "bla_window_backward", dev, ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
           _ptr(lse), _ptr(dO), _ptr(lengths), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel())
     return dq, dk, dv
+
+
+def _conv_check(x, w, bias, silu, what):
+    """The checks that the convolution's calls share; returns its parameters."""
+    H, d = x.shape[1], x.shape[-1]
+    if w.dim() != 3:
+        raise ValueError(f"w: expected [H, d, taps], got {tuple(w.shape)}")
+    K, dev = w.shape[2], x.device
+    p = ConvParams(x.shape[0], H, x.shape[2] if x.dim() == 4 else 1, d, K, int(silu), _io(x, "x"))
+    _check_on(w, (H, d, K), torch.float32, "w", dev)
+    if bias is not None:
+        _check_on(bias, (H, d), torch.float32, "bias", dev)
+    st = lib().bla_conv_supported(ctypes.byref(p))
+    if st != 0:
+        raise BlaError(st, f"{what} (shape check)")
+    return p, K
+
+
+def conv_forward(x, w, bias=None, silu: bool = True, state=None, lengths=None, want_state: bool = True, out=None):
+    """bla_conv_forward: the causal convolution of each channel of x [B,H,L,d] (float32 or bfloat16) with w [H,d,taps] and
+    bias [H,d] (float32), then SiLU if silu.  state [B,H,taps-1,d] float32: the tokens before the call (None = zeros).
+    lengths (int32 [B]): tokens of each row.  Returns (y, state after the call or None)."""
+    B, H, L, d = x.shape
+    dev = x.device
+    _check_on(x, (B, H, L, d), x.dtype, "x", dev)
+    p, K = _conv_check(x, w, bias, silu, "bla_conv_forward")
+    if state is not None:
+        _check_on(state, (B, H, K - 1, d), torch.float32, "state", dev)
+    if lengths is not None:
+        _check_on(lengths, (B,), torch.int32, "lengths", dev)
+    y = _out(out, x, (B, H, L, d))
+    so = torch.empty((B, H, K - 1, d), dtype=torch.float32, device=dev) if want_state else None
+    _call(lib().bla_conv_forward, "bla_conv_forward", dev, ctypes.byref(p), _ptr(x), _ptr(w), _ptr(bias), _ptr(lengths),
+          _ptr(state), _ptr(y), _ptr(so))
+    return y, so
+
+
+def conv_step(x, w, state, bias=None, silu: bool = True, state_out=None, out=None):
+    """bla_conv_step: one token per row, x [B,H,d].  The state [B,H,taps-1,d] is updated in place, or left alone where
+    state_out receives it."""
+    B, H, d = x.shape
+    dev = x.device
+    _check_on(x, (B, H, d), x.dtype, "x", dev)
+    p, K = _conv_check(x, w, bias, silu, "bla_conv_step")
+    state_out = state if state_out is None else state_out
+    _check_on(state, (B, H, K - 1, d), torch.float32, "state", dev)
+    _check_on(state_out, (B, H, K - 1, d), torch.float32, "state_out", dev)
+    y = _out(out, x, (B, H, d))
+    _call(lib().bla_conv_step, "bla_conv_step", dev, ctypes.byref(p), _ptr(x), _ptr(w), _ptr(bias), _ptr(state), _ptr(y),
+          _ptr(state_out))
+    return y
+
+
+def conv_backward(x, w, dy, bias=None, silu: bool = True, state=None, dstate=None, lengths=None,
+                  want_state_grad: bool = True, workspace=None):
+    """bla_conv_backward: gradients of conv_forward for dy = dLoss/dy and dstate = dLoss/d(state after the call) (None =
+    zero).  Returns (dx, dw, dbias, dLoss/d(state before the call) or None); dbias is that of a zero bias where bias is
+    None."""
+    B, H, L, d = x.shape
+    dev = x.device
+    _check_on(x, (B, H, L, d), x.dtype, "x", dev)
+    _check_on(dy, (B, H, L, d), x.dtype, "dy", dev)
+    p, K = _conv_check(x, w, bias, silu, "bla_conv_backward")
+    for name, t in (("state", state), ("dstate", dstate)):
+        if t is not None:
+            _check_on(t, (B, H, K - 1, d), torch.float32, name, dev)
+    if lengths is not None:
+        _check_on(lengths, (B,), torch.int32, "lengths", dev)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    db = torch.empty((H, d), dtype=torch.float32, device=dev)
+    ds = torch.empty((B, H, K - 1, d), dtype=torch.float32, device=dev) if want_state_grad else None
+    ws = _room(workspace, lib().bla_conv_backward_workspace_size(ctypes.byref(p)), dev)
+    _call(lib().bla_conv_backward, "bla_conv_backward", dev, ctypes.byref(p), _ptr(x), _ptr(w), _ptr(bias), _ptr(dy),
+          _ptr(lengths), _ptr(state), _ptr(dstate), _ptr(dx), _ptr(dw), _ptr(db), _ptr(ds), _ptr(ws), ws.numel())
+    return dx, dw, db, ds
+
+
+def _ssm_check(x, dt, A, Bm, Cm, D, what):
+    """The checks that the scan's calls share; returns its parameters and the shape of a state."""
+    tok = x.shape[2:-1]
+    B, H, d = x.shape[0], x.shape[1], x.shape[-1]
+    if Bm.dim() != x.dim():
+        raise ValueError(f"Bm: expected {x.dim()} dimensions, got {tuple(Bm.shape)}")
+    G, N, dev = Bm.shape[1], Bm.shape[-1], x.device
+    p = SsmParams(B, H, G, tok[0] if tok else 1, d, N, _io(x, "x"))
+    _check_on(Bm, (B, G, *tok, N), x.dtype, "Bm", dev)
+    _check_on(Cm, (B, G, *tok, N), x.dtype, "Cm", dev)
+    _check_on(dt, (B, H, *tok), torch.float32, "dt", dev)
+    _check_on(A, (H,), torch.float32, "A", dev)
+    if D is not None:
+        _check_on(D, (H,), torch.float32, "D", dev)
+    st = lib().bla_ssm_supported(ctypes.byref(p))
+    if st != 0:
+        raise BlaError(st, f"{what} (shape check)")
+    return p, (B, H, N, d)
+
+
+def ssm_forward(x, dt, A, Bm, Cm, D=None, state=None, lengths=None, want_state: bool = True, workspace=None, out=None):
+    """bla_ssm_forward: the selective state space scan h_t = exp(dt_t A) h_{t-1} + dt_t B_t x_t^T, y_t = C_t h_t + D x_t.
+
+    x [B,H,L,d], Bm and Cm [B,G,L,N] (float32 or bfloat16), dt [B,H,L], A and D [H] (float32; D None = zero), state
+    [B,H,N,d] float32 before the call (None = zero), lengths (int32 [B]): tokens of each row.  Returns (y, state after
+    the call or None)."""
+    B, H, L, d = x.shape
+    dev = x.device
+    _check_on(x, (B, H, L, d), x.dtype, "x", dev)
+    p, shape = _ssm_check(x, dt, A, Bm, Cm, D, "bla_ssm_forward")
+    if state is not None:
+        _check_on(state, shape, torch.float32, "state", dev)
+    if lengths is not None:
+        _check_on(lengths, (B,), torch.int32, "lengths", dev)
+    y = _out(out, x, (B, H, L, d))
+    so = torch.empty(shape, dtype=torch.float32, device=dev) if want_state else None
+    ws = _room(workspace, lib().bla_ssm_workspace_size(ctypes.byref(p)), dev)
+    _call(lib().bla_ssm_forward, "bla_ssm_forward", dev, ctypes.byref(p), _ptr(x), _ptr(dt), _ptr(A), _ptr(Bm), _ptr(Cm),
+          _ptr(D), _ptr(lengths), _ptr(state), _ptr(y), _ptr(so), _ptr(ws), ws.numel())
+    return y, so
+
+
+def ssm_step(x, dt, A, Bm, Cm, state, D=None, state_out=None, out=None):
+    """bla_ssm_step: one token per row, x [B,H,d], dt [B,H], Bm and Cm [B,G,N].  The state [B,H,N,d] is updated in place, or
+    left alone where state_out receives it."""
+    B, H, d = x.shape
+    dev = x.device
+    _check_on(x, (B, H, d), x.dtype, "x", dev)
+    p, shape = _ssm_check(x, dt, A, Bm, Cm, D, "bla_ssm_step")
+    state_out = state if state_out is None else state_out
+    _check_on(state, shape, torch.float32, "state", dev)
+    _check_on(state_out, shape, torch.float32, "state_out", dev)
+    y = _out(out, x, (B, H, d))
+    _call(lib().bla_ssm_step, "bla_ssm_step", dev, ctypes.byref(p), _ptr(x), _ptr(dt), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D),
+          _ptr(state), _ptr(y), _ptr(state_out))
+    return y
+
+
+def ssm_backward(x, dt, A, Bm, Cm, dy, D=None, state=None, dstate=None, lengths=None, want_state_grad: bool = True,
+                 workspace=None):
+    """bla_ssm_backward: gradients of ssm_forward for dy = dLoss/dy and dstate = dLoss/d(state after the call) (None =
+    zero).  Returns (dx, ddt, dA, dBm, dCm, dD, dLoss/d(state before the call) or None); dD is that of a zero D where D is
+    None."""
+    B, H, L, d = x.shape
+    dev = x.device
+    _check_on(x, (B, H, L, d), x.dtype, "x", dev)
+    _check_on(dy, (B, H, L, d), x.dtype, "dy", dev)
+    p, shape = _ssm_check(x, dt, A, Bm, Cm, D, "bla_ssm_backward")
+    for name, t in (("state", state), ("dstate", dstate)):
+        if t is not None:
+            _check_on(t, shape, torch.float32, name, dev)
+    if lengths is not None:
+        _check_on(lengths, (B,), torch.int32, "lengths", dev)
+    dx, ddt, dA = torch.empty_like(x), torch.empty_like(dt), torch.empty_like(A)
+    dB, dC, dD = torch.empty_like(Bm), torch.empty_like(Cm), torch.empty_like(A)
+    ds = torch.empty(shape, dtype=torch.float32, device=dev) if want_state_grad else None
+    ws = _room(workspace, lib().bla_ssm_backward_workspace_size(ctypes.byref(p)), dev)
+    _call(lib().bla_ssm_backward, "bla_ssm_backward", dev, ctypes.byref(p), _ptr(x), _ptr(dt), _ptr(A), _ptr(Bm), _ptr(Cm),
+          _ptr(D), _ptr(dy), _ptr(lengths), _ptr(state), _ptr(dstate), _ptr(dx), _ptr(ddt), _ptr(dA), _ptr(dB), _ptr(dC),
+          _ptr(dD), _ptr(ds), _ptr(ws), ws.numel())
+    return dx, ddt, dA, dB, dC, dD, ds

@@ -1,0 +1,128 @@
+// The selective state space scan: kernel arguments and what its kernels share.
+//
+//   h_t = exp(dt_t A) h_{t-1} + dt_t B_t x_t^T   (h: N x d),   y_t = h_t^T C_t + D x_t
+// per row and head; the heads of a group share B and C.  In chunks of 64 tokens, with s_t the sum of dt A over the chunk's tokens
+// up to t and s_c its whole sum:
+//   y_t   = sum_{u <= t} e^{s_t - s_u} dt_u (C_t . B_u) x_u + e^{s_t} h_in^T C_t + D x_t
+//   h_out = e^{s_c} h_in + sum_u e^{s_c - s_u} dt_u B_u x_u^T
+// Only differences s_t - s_u of a chunk are exponentiated, so nothing overflows where A <= 0.  The sums s run in float64.
+#pragma once
+
+#include "bla_seq.h"
+
+namespace bla {
+
+constexpr int kSsmChunk = 64;
+
+struct SsmArgs {
+    const void *x, *Bm, *Cm;        // [B, H, L, D], [B, G, L, N]
+    const float *dt, *A, *Dm;       // [B, H, L], [H], [H] or null
+    const float* state_in;          // [B, H, N, D] or null
+    const int32_t* lengths;
+    void* y;
+    float* state_out;               // or null
+    float* seg_state;               // [nseg - 1][B H][N][D]: segment summaries, then the states entering segments 1 ..
+    float* seg_decay;               // [nseg - 1][B H]
+    int B, H, G, L, N;
+    int nch, cps, nseg;
+    long long units, per;
+};
+
+struct SsmStepArgs {
+    const void *x, *Bm, *Cm;        // [B, H, D], [B, G, N]
+    const float *dt, *A, *Dm;       // [B, H], [H], [H] or null
+    const float* state_in;
+    void* y;
+    float* state_out;
+    int B, H, G, N;
+};
+
+struct SsmBwdArgs {
+    const void *x, *Bm, *Cm, *dy;
+    const float *dt, *A, *Dm, *state_in, *dstate_out;
+    const int32_t* lengths;
+    void *dx, *dBm, *dCm;
+    float *ddt, *dA, *dD, *dstate_in;  // dD, dstate_in: or null
+    float* enter;                   // [B H][nch][N][D]: the states entering the chunks
+    float* leave;                   // [B H][nch][N][D]: the gradients of the states leaving them
+    float* part_head;               // [B H][nch][2]: a chunk's parts of dA and dD
+    float* part_bc;                 // hsplit > 1: [hsplit][B][G][nch][2][64][N]
+    int B, H, G, L, N, nch, hsplit;
+    long long walk_units, walk_per, units, per;
+};
+
+// Eight products of a float32 weight and an operand value, as an operand of a contraction whose float32 results keep the weight's
+// precision: in bf16 as a sum of two roundings (2^-17 relative; two products), in float32 as it is.
+template <typename T> struct Split;
+template <> struct Split<bf16> {
+    bf16x8 hi, lo;
+    __device__ __forceinline__ void set(floatx8 v)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            hi[e] = (bf16)v[e];
+            lo[e] = (bf16)(v[e] - (float)hi[e]);
+        }
+    }
+};
+template <> struct Split<float> {
+    floatx8 hi;
+    __device__ __forceinline__ void set(floatx8 v) { hi = v; }
+};
+__device__ __forceinline__ floatx4 mma_split(bf16x8 a, const Split<bf16>& b, floatx4 c) { return mma(a, b.hi, mma(a, b.lo, c)); }
+__device__ __forceinline__ floatx4 mma_split(floatx8 a, const Split<float>& b, floatx4 c) { return mma(a, b.hi, c); }
+__device__ __forceinline__ floatx8 to_f8(bf16x8 x)
+{
+    floatx8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = (float)x[e];
+    return r;
+}
+__device__ __forceinline__ floatx8 to_f8(floatx8 x) { return x; }
+
+// Fragments in the accumulator order of rows of N real columns in memory (zeros past them): the halves lie 16 columns apart.
+template <typename T> __device__ __forceinline__ typename Frag<T>::type ld_acc_row(const T* row, int kb, int g, int N)
+{
+    const int k = 32 * kb + 4 * g;
+    return join(k < N ? ld4<T>(row + k) : zero_half<T>(), k + 16 < N ? ld4<T>(row + k + 16) : zero_half<T>());
+}
+// The same of an LDS tile in the dual layout (row x0 + r, x0 a multiple of 16).
+__device__ __forceinline__ bf16x8 ld_acc_dual(const bf16* M, int ld, int x0, int kb, int g, int r)
+{
+    return ld_frag_2x8_sw(M + (x0 + r) * ld, kb, g, r);
+}
+__device__ __forceinline__ floatx8 ld_acc_dual(const float* M, int ld, int x0, int kb, int g, int r)
+{
+    return ld_frag<float>(M + (x0 + r) * ld, 32 * kb, g);
+}
+
+// e^x of a float64 exponent to float32 precision: the part of x that float32 cannot hold goes in as a factor 1 + x_lo.
+__device__ __forceinline__ float exp_f64(double x)
+{
+    const double y = x * 1.4426950408889634;
+    const float hi = (float)y;
+    const float e = exp2_fast(hi);
+    return __builtin_fmaf(e, (float)(y - (double)hi) * kLn2, e);
+}
+
+// Inclusive sum over the wave's lanes (lane = token).
+__device__ __forceinline__ double wave_scan(double x, int lane)
+{
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const double y = __shfl_up(x, off);
+        x += lane >= off ? y : 0.0;
+    }
+    return x;
+}
+
+__device__ __forceinline__ int ssm_length(const int32_t* lengths, int b, int L) { return lengths ? min(max(lengths[b], 0), L) : L; }
+
+hipError_t launch_ssm_forward(int bf16_io, int D, const SsmArgs& a, hipStream_t s);
+hipError_t launch_ssm_step(int bf16_io, int D, const SsmStepArgs& a, hipStream_t s);
+hipError_t launch_ssm_backward(int bf16_io, int D, const SsmBwdArgs& a, hipStream_t s);
+
+// State rows of a kernel: N padded to 64 or 128 (rows past N are zero and not stored).
+inline int ssm_rows(int N) { return N <= 64 ? 64 : 128; }
+
+}  // namespace bla

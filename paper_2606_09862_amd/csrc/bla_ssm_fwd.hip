@@ -1,0 +1,327 @@
+// The selective scan over a prompt and for single tokens (bla_ssm_forward, bla_ssm_step).
+#include "bla_ssm.h"
+
+namespace bla {
+namespace {
+
+// A workgroup of four waves walks the chunks of one segment of one head with the state in registers.
+//
+// Wave w owns 16 tokens of a chunk (columns t of every tile) and NP / 4 rows n of the state, held transposed (accumulator rows d,
+// columns n) in float32.  Per chunk:
+//   G^T = B C^T (rows u, columns t; tiles u <= t only), weighted by e^{s_t - s_u} dt_u: the operand of the second product;
+//   Y^T = h^T C^T scaled by e^{s_t}, plus X^T (weighted G)^T: h is published in LDS in the operand type;
+//   h^T <- e^{s_c} h^T + X^T (w B)^T with w_u = e^{s_c - s_u} dt_u: the transposed fragments of X serve both products.
+// In bf16 the weighted G and the published h are rounded to 2^-9 relative, as y is; the weights of the state's update are kept to 2^-17
+// (Split), since the state is a float32 result and is carried on.
+// SUM: the segment's own state from zero and its decay, for the scan over the segments; no outputs.
+template <typename T, int D, int NP, bool SUM> struct SsmGeo {
+    static constexpr int PE = 16 / (int)sizeof(T);
+    static constexpr int CHX = D / PE, CHB = NP / PE;        // 16-byte pieces of a row
+    static constexpr int PX = 64 * CHX / 256, PB = 64 * CHB / 256;
+    static constexpr int LX = red_ld<T>(D), LB = dual_ld<T>(NP), LH = red_ld<T>(D);
+    static constexpr int TNW = NP / 64, TD = D / 16;
+};
+
+template <typename T, int D, int NP, bool SUM>
+__global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
+{
+    typedef SsmGeo<T, D, NP, SUM> G;
+    typedef typename Frag<T>::type F;
+    __shared__ __attribute__((aligned(16))) T sX[64 * G::LX];
+    __shared__ __attribute__((aligned(16))) T sB[64 * G::LB];
+    __shared__ __attribute__((aligned(16))) T sH[SUM ? 8 : NP * G::LH];
+    __shared__ __attribute__((aligned(16))) float sS[64], sSl[64], sDt[64], sE[64], sW[64];
+    __shared__ float sTot;
+
+    long long u = xcd_unit(blockIdx.x, a.per);
+    if (u >= a.units) return;
+    const int h = (int)(u % a.H);
+    u /= a.H;
+    const int nsg = SUM ? a.nseg - 1 : a.nseg;
+    const int seg = (int)(u % nsg), b = (int)(u / nsg);
+    const int bh = b * a.H + h, grp = h / (a.H / a.G);
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
+    const int len = ssm_length(a.lengths, b, a.L);
+    const T* x = (const T*)a.x + (size_t)bh * a.L * D;
+    const T* Bm = (const T*)a.Bm + ((size_t)b * a.G + grp) * a.L * a.N;
+    const T* Cm = (const T*)a.Cm + ((size_t)b * a.G + grp) * a.L * a.N;
+    T* y = SUM ? nullptr : (T*)a.y + (size_t)bh * a.L * D;
+    const float* dt = a.dt + (size_t)bh * a.L;
+    const double A = a.A[h];
+    const float skip = a.Dm ? a.Dm[h] : 0.f;
+    const int c0 = seg * a.cps, c1 = min(a.nch, c0 + a.cps);
+    const int cend = min(c1, (len + 63) / 64);  // chunks past it are padding
+    const size_t BH = (size_t)a.B * a.H;
+
+    floatx4 hs[G::TNW][G::TD];  // h[n = 16 (TNW wave + nt) + r][d = 16 dt + 4g ..]
+    const float* from = SUM ? nullptr : seg == 0 ? (a.state_in ? a.state_in + (size_t)bh * a.N * D : nullptr)
+                                                 : a.seg_state + ((size_t)(seg - 1) * BH + bh) * a.N * D;
+#pragma unroll
+    for (int nt = 0; nt < G::TNW; ++nt) {
+        const int n = 16 * (G::TNW * wave + nt) + r;
+#pragma unroll
+        for (int d = 0; d < G::TD; ++d)
+            hs[nt][d] = from && n < a.N ? ld4f(from + (size_t)n * D + 16 * d + 4 * g) : zero4();
+    }
+
+    intx4 xr[G::PX], br[G::PB];
+    F cf[NP / 32], cn[NP / 32];
+    float dtr = 0.f;
+    auto load = [&](int c) {
+        const int n = min(64, len - 64 * c);
+#pragma unroll
+        for (int i = 0; i < G::PX; ++i) {
+            const int row = (i * 256 + tid) / G::CHX, ch = (i * 256 + tid) % G::CHX;
+            xr[i] = intx4{0, 0, 0, 0};
+            if (row < n) xr[i] = *(const intx4*)(x + (size_t)(64 * c + row) * D + ch * G::PE);
+        }
+#pragma unroll
+        for (int i = 0; i < G::PB; ++i) {
+            const int row = (i * 256 + tid) / G::CHB, ch = (i * 256 + tid) % G::CHB;
+            br[i] = intx4{0, 0, 0, 0};
+            if (row < n && ch * G::PE < a.N) br[i] = *(const intx4*)(Bm + (size_t)(64 * c + row) * a.N + ch * G::PE);
+        }
+        if (!SUM) {
+            const int t = 16 * wave + r;
+#pragma unroll
+            for (int kb = 0; kb < NP / 32; ++kb)
+                cn[kb] = t < n ? ld_acc_row<T>(Cm + (size_t)(64 * c + t) * a.N, kb, g, a.N) : zero_frag<T>();
+        }
+        if (wave == 0) dtr = lane < n ? dt[64 * c + lane] : 0.f;
+    };
+
+    double decay = 0.0;
+    if (c0 < cend) load(c0);
+    for (int c = c0; c < cend; ++c) {
+#pragma unroll
+        for (int i = 0; i < G::PX; ++i) {
+            const int row = (i * 256 + tid) / G::CHX, ch = (i * 256 + tid) % G::CHX;
+            *(intx4*)(sX + row * G::LX + ch * G::PE) = xr[i];
+        }
+#pragma unroll
+        for (int i = 0; i < G::PB; ++i) {
+            const int row = (i * 256 + tid) / G::CHB, ch = (i * 256 + tid) % G::CHB;
+            *(intx4*)(sB + row * G::LB + dual_col<T>(row, ch * G::PE)) = br[i];
+        }
+        if (wave == 0) {
+            const double s = wave_scan((double)dtr * A, lane), tot = __shfl(s, 63);
+            decay += tot;
+            sS[lane] = (float)s;
+            sSl[lane] = (float)(s - (double)(float)s);
+            sDt[lane] = dtr;
+            sE[lane] = exp_f64(s);
+            sW[lane] = exp_f64(tot - s) * dtr;
+            if (lane == 0) sTot = exp_f64(tot);
+        }
+        if (!SUM) {
+#pragma unroll
+            for (int kb = 0; kb < NP / 32; ++kb) cf[kb] = cn[kb];
+#pragma unroll
+            for (int nt = 0; nt < G::TNW; ++nt)
+#pragma unroll
+                for (int d = 0; d < G::TD; ++d)
+                    st4(sH + (16 * (G::TNW * wave + nt) + r) * G::LH + 16 * d + 4 * g, hs[nt][d]);
+        }
+        __syncthreads();
+        if (c + 1 < cend) load(c + 1);
+
+        F pf[2] = {zero_frag<T>(), zero_frag<T>()};
+        if (!SUM) {
+            const int t = 16 * wave + r;
+            const float st = sS[t], stl = sSl[t];
+            floatx4 p[4];
+#pragma unroll
+            for (int ut = 0; ut < 4; ++ut) {
+                p[ut] = zero4();
+                if (ut <= wave) {
+#pragma unroll
+                    for (int kb = 0; kb < NP / 32; ++kb) p[ut] = mma(ld_acc_dual(sB, G::LB, 16 * ut, kb, g, r), cf[kb], p[ut]);
+                    const floatx4 su = ld4f(sS + 16 * ut + 4 * g), du = ld4f(sDt + 16 * ut + 4 * g);
+                    floatx4 sl = zero4();
+                    if (sizeof(T) == 4) sl = ld4f(sSl + 16 * ut + 4 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float df = st - su[e];
+                        if (sizeof(T) == 4) df += stl - sl[e];
+                        const float w = exp2_fast(df * kLog2e) * du[e] * p[ut][e];
+                        p[ut][e] = 16 * ut + 4 * g + e <= t ? w : 0.f;
+                    }
+                }
+            }
+            pf[0] = frag_from_acc<T>(p[0], p[1]);
+            pf[1] = frag_from_acc<T>(p[2], p[3]);
+        }
+        Split<T> wb[G::TNW][2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const floatx8 w = join(ld4f(sW + 32 * kb + 4 * g), ld4f(sW + 32 * kb + 16 + 4 * g));
+#pragma unroll
+            for (int nt = 0; nt < G::TNW; ++nt)
+                wb[nt][kb].set(w * to_f8(ld_red_dual(sB, G::LB, 16 * (G::TNW * wave + nt), kb, g, r)));
+        }
+        const float es = sE[16 * wave + r], tot = sTot;
+#pragma unroll
+        for (int d = 0; d < G::TD; ++d) {
+            const F xf[2] = {ld_red(sX, G::LX, 16 * d, 0, g, r), ld_red(sX, G::LX, 16 * d, 1, g, r)};
+            if (!SUM) {
+                floatx4 o = zero4();
+#pragma unroll
+                for (int kb = 0; kb < NP / 32; ++kb) o = mma(ld_red(sH, G::LH, 16 * d, kb, g, r), cf[kb], o);
+                o *= es;
+                o = mma(xf[0], pf[0], o);
+                if (wave >= 2) o = mma(xf[1], pf[1], o);
+                const int t = 64 * c + 16 * wave + r;
+                const floatx4 xt = to_f4(ld4<T>(sX + (16 * wave + r) * G::LX + 16 * d + 4 * g));
+                if (t < a.L) st4(y + (size_t)t * D + 16 * d + 4 * g, t < len ? o + skip * xt : zero4());
+            }
+#pragma unroll
+            for (int nt = 0; nt < G::TNW; ++nt) {
+                hs[nt][d] *= tot;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) hs[nt][d] = mma_split(xf[kb], wb[nt][kb], hs[nt][d]);
+            }
+        }
+        __syncthreads();
+    }
+
+    if (!SUM) {  // padding
+        const int t0 = 64 * max(c0, cend), t1 = min(a.L, 64 * c1);
+        for (int i = tid; i < (t1 - t0) * G::CHX; i += 256) *(intx4*)(y + (size_t)t0 * D + (size_t)i * G::PE) = intx4{0, 0, 0, 0};
+    }
+    float* to = SUM ? a.seg_state + ((size_t)seg * BH + bh) * a.N * D
+                    : seg == a.nseg - 1 && a.state_out ? a.state_out + (size_t)bh * a.N * D : nullptr;
+    if (to) {
+#pragma unroll
+        for (int nt = 0; nt < G::TNW; ++nt) {
+            const int n = 16 * (G::TNW * wave + nt) + r;
+            if (n < a.N)
+#pragma unroll
+                for (int d = 0; d < G::TD; ++d) st4f(to + (size_t)n * D + 16 * d + 4 * g, hs[nt][d]);
+        }
+    }
+    if (SUM && tid == 0) a.seg_decay[(size_t)seg * BH + bh] = exp_f64(decay);
+}
+
+// States entering segments 1 .. in place of the segments' own states: four elements of a head's state per lane.
+__global__ void __launch_bounds__(256) ssm_scan_kernel(SsmArgs a, int D)
+{
+    const size_t n4 = (size_t)a.N * D / 4, BH = (size_t)a.B * a.H;
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= BH * n4) return;
+    const size_t bh = i / n4;
+    floatx4 c = a.state_in ? ld4f(a.state_in + 4 * i) : zero4();
+    for (int s = 0; s < a.nseg - 1; ++s) {
+        float* p = a.seg_state + ((size_t)s * BH * n4 + i) * 4;
+        c = c * a.seg_decay[s * BH + bh] + ld4f(p);
+        st4f(p, c);
+    }
+}
+
+// One token: a workgroup reads and writes a head's state once, four columns of a row per lane; y is summed over the row groups through LDS.
+// Bound: the state's bytes.
+template <typename T, int D, int PASSES> __global__ void __launch_bounds__(256) ssm_step_kernel(SsmStepArgs a)
+{
+    constexpr int NQ = D / 4, RPP = 256 / NQ;
+    __shared__ __attribute__((aligned(16))) float red[RPP * D];
+    const int bh = blockIdx.x, h = bh % a.H, b = bh / a.H, grp = h / (a.H / a.G);
+    const int tid = threadIdx.x, qd = tid % NQ, rg = tid / NQ;
+    const float* in = a.state_in + (size_t)bh * a.N * D;
+    float* out = a.state_out + (size_t)bh * a.N * D;
+    floatx4 s[PASSES];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) s[p] = ld4f(in + (size_t)min(p * RPP + rg, a.N - 1) * D + 4 * qd);
+    const T* Bm = (const T*)a.Bm + ((size_t)b * a.G + grp) * a.N;
+    const T* Cm = (const T*)a.Cm + ((size_t)b * a.G + grp) * a.N;
+    const float dt = a.dt[bh];
+    const float keep = exp_f64((double)dt * (double)a.A[h]);
+    const floatx4 x = to_f4(ld4<T>((const T*)a.x + (size_t)bh * D + 4 * qd)), xd = dt * x;
+    floatx4 y = zero4();
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int n = p * RPP + rg;
+        if (n < a.N) {
+            const floatx4 v = keep * s[p] + (float)Bm[n] * xd;
+            st4f(out + (size_t)n * D + 4 * qd, v);
+            y += (float)Cm[n] * v;
+        }
+    }
+    st4f(red + rg * D + 4 * qd, y);
+    __syncthreads();
+    if (tid < NQ) {
+        floatx4 o = (a.Dm ? a.Dm[h] : 0.f) * x;
+        for (int i = 0; i < RPP; ++i) o += ld4f(red + i * D + 4 * tid);
+        st4((T*)a.y + (size_t)bh * D + 4 * tid, o);
+    }
+}
+
+template <typename T, int D, int NP> hipError_t forward_n(const SsmArgs& a, hipStream_t s)
+{
+    if (a.nseg > 1) {
+        SsmArgs z = a;
+        z.units = (long long)a.B * a.H * (a.nseg - 1);
+        z.per = (z.units + 7) / 8;
+        hipLaunchKernelGGL((ssm_forward_kernel<T, D, NP, true>), dim3((unsigned)(8 * z.per)), dim3(256), 0, s, z);
+        const size_t n = (size_t)a.B * a.H * a.N * D / 4;
+        hipLaunchKernelGGL(ssm_scan_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a, D);
+    }
+    hipLaunchKernelGGL((ssm_forward_kernel<T, D, NP, false>), dim3((unsigned)(8 * a.per)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T, int D> hipError_t forward_d(const SsmArgs& a, hipStream_t s)
+{
+    return a.N <= 64 ? forward_n<T, D, 64>(a, s) : forward_n<T, D, 128>(a, s);
+}
+
+template <typename T, int D> hipError_t step_d(const SsmStepArgs& a, hipStream_t s)
+{
+    const dim3 grid((unsigned)(a.B * a.H));
+    constexpr int RPP = 256 / (D / 4);
+    const int passes = (a.N + RPP - 1) / RPP;
+#define BLA_STEP(P)                                                                            \
+    if constexpr (P * RPP < 256) {                                                             \
+        if (passes <= P) {                                                                     \
+            hipLaunchKernelGGL((ssm_step_kernel<T, D, P>), grid, dim3(256), 0, s, a);          \
+            return hipGetLastError();                                                          \
+        }                                                                                      \
+    }
+    BLA_STEP(1)
+    BLA_STEP(2)
+    BLA_STEP(4)
+    BLA_STEP(8)
+    BLA_STEP(16)
+#undef BLA_STEP
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_ssm_forward(int bf16_io, int D, const SsmArgs& a, hipStream_t s)
+{
+    if (bf16_io) {
+        if (D == 32) return forward_d<bf16, 32>(a, s);
+        if (D == 64) return forward_d<bf16, 64>(a, s);
+        if (D == 128) return forward_d<bf16, 128>(a, s);
+    } else {
+        if (D == 32) return forward_d<float, 32>(a, s);
+        if (D == 64) return forward_d<float, 64>(a, s);
+        if (D == 128) return forward_d<float, 128>(a, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_ssm_step(int bf16_io, int D, const SsmStepArgs& a, hipStream_t s)
+{
+    if (bf16_io) {
+        if (D == 32) return step_d<bf16, 32>(a, s);
+        if (D == 64) return step_d<bf16, 64>(a, s);
+        if (D == 128) return step_d<bf16, 128>(a, s);
+    } else {
+        if (D == 32) return step_d<float, 32>(a, s);
+        if (D == 64) return step_d<float, 64>(a, s);
+        if (D == 128) return step_d<float, 128>(a, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace bla
