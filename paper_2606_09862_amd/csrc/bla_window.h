@@ -62,7 +62,7 @@ __device__ __forceinline__ int row_tokens(const int32_t* lengths, const int64_t*
     return lengths ? min(max(lengths[b], 0), L) : L;
 }
 
-hipError_t launch_window_forward(int bf16_io, int D, int qt, const WindowArgs& a, hipStream_t s);
+hipError_t launch_window_forward(int bf16_io, int D, int waves, const WindowArgs& a, hipStream_t s);
 hipError_t launch_window_ring(int bf16_io, int D, const WindowArgs& a, hipStream_t s);
 hipError_t launch_window_step(int bf16_io, int D, const WindowStepArgs& a, hipStream_t s);
 hipError_t launch_window_backward(int bf16_io, int D, const WindowBwdArgs& a, hipStream_t s);

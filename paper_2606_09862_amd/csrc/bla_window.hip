@@ -32,7 +32,7 @@ float scale_of(const bla_window_params* p) { return p->scale == 0.f ? 1.f / sqrt
 // Forward: 128 queries to a workgroup (each fragment of keys serves two query tiles), 64 where that fills the device better;
 // the keys of a block in parts of at least four tiles where the blocks alone do not fill it.
 struct ForwardPlan {
-    int qt, nqb, nsplit;
+    int waves, nqb, nsplit;
     long long units;
     size_t total;
 };
@@ -40,10 +40,10 @@ ForwardPlan forward_plan(const bla_window_params* p, bool cached)
 {
     ForwardPlan f;
     const long long bh = (long long)p->B * p->H;
-    f.qt = bh * ((p->L + 127) / 128) >= kFill ? 2 : 1;
-    f.nqb = (p->L + 64 * f.qt - 1) / (64 * f.qt);
+    f.waves = bh * ((p->L + 127) / 128) >= kFill ? 8 : 4;
+    f.nqb = (p->L + 16 * f.waves - 1) / (16 * f.waves);
     const long long blocks = bh * f.nqb;
-    long long keys = (long long)p->window - 1 + 64 * f.qt + p->sinks;
+    long long keys = (long long)p->window - 1 + 16 * f.waves + p->sinks;
     if (!cached && keys > p->L) keys = p->L;
     const long long tiles = (keys + kWinKeys - 1) / kWinKeys;
     long long n = 1;
@@ -146,7 +146,7 @@ bla_status bla_window_forward(const bla_window_params* p, const void* q, const v
     a.part_o = (float*)workspace;
     a.part_ml = f.nsplit > 1 ? a.part_o + (size_t)f.nsplit * rows * p->d : nullptr;
     hipStream_t s = (hipStream_t)stream;
-    if (p->L > 0 && launch_window_forward(bf16, p->d, f.qt, a, s) != hipSuccess) return BLA_ERR_HIP;
+    if (p->L > 0 && launch_window_forward(bf16, p->d, f.waves, a, s) != hipSuccess) return BLA_ERR_HIP;
     if (p->L > 0 && f.nsplit > 1) {
         const JoinArgs j = {a.part_o, a.part_ml, o, lse, (long long)rows, f.nsplit};
         if (launch_window_join(bf16, p->d, j, s) != hipSuccess) return BLA_ERR_HIP;

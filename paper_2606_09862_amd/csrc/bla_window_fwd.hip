@@ -1,4 +1,6 @@
 // Window attention over a prompt (bla_window_forward).
+#include <type_traits>
+
 #include "bla_window.h"
 
 namespace bla {
@@ -6,29 +8,32 @@ namespace {
 
 // One pass over a query block's keys with the running maximum and sum of the softmax.
 //
-// A workgroup of four waves takes 64 QT queries of one head (wave w the 16 QT queries from 16 QT w on) and walks
-// the keys that any of them sees: first the sinks before the window of its first query, then the window's keys,
-// as one row of `total` keys in tiles of 64.  The new tokens' keys are read from k, v and the past's from the ring, so
-// that a tile may hold sinks, past and new keys alike.  Tiles are loaded into registers one ahead and pass through two LDS
-// buffers, one barrier per tile.
+// A workgroup of NW waves takes 16 NW queries of one head (wave w the 16 from 16 w on) and walks the keys that any of them
+// sees: first the sinks before the window of its first query, then the window's keys, as one row of `total` keys in tiles of
+// 64.  With a ring (RING) the past's keys are read from it and the new tokens' from k, v, so that a tile may hold sinks,
+// past and new keys alike.  Tiles are loaded into registers one ahead and pass through two LDS buffers, one
+// barrier per tile.
 // S^T = K Q^T gives each lane four keys of one query (accumulator rows: keys), so the softmax runs down a column
 // (in the lane, then over the four row groups), and the accumulators, rounded to the operand type, are the
 // operand of O^T = V^T P without leaving the registers.  In bf16 the weights are rounded to 2^-9 relative, as their
 // values are; maxima, sums and outputs are float32.
-template <typename T, int D, int QT> struct WinGeo {
-    static constexpr int BQ = 64 * QT;
+// The maximum that the weights are taken against follows the true one only once that is more than 2^kLag above it: the
+// weights stay below 2^kLag, no precision is lost, and a tile needs neither a reduction over the lanes nor a rescaling
+// unless some lane has found such a score.
+template <typename T, int D, int NW> struct WinGeo {
+    static constexpr int BQ = 16 * NW, NT = 64 * NW;
     static constexpr int LK = nat_ld<T>(D), LV = red_ld<T>(D);
-    static constexpr int CH = D * (int)sizeof(T) / 16;  // 16-byte pieces of a row
-    static constexpr int RPP = 256 / CH;                // rows per pass of the workgroup's loads
-    static constexpr int NP = kWinKeys / RPP;
-    static constexpr int PE = 16 / (int)sizeof(T);
-    static constexpr int BUF = kWinKeys * (LK + LV);    // elements of one buffer
+    static constexpr int PE = 16 / (int)sizeof(T), CH = D / PE;  // 16-byte pieces of a row
+    static constexpr int NPC = kWinKeys * CH;                    // pieces of a tile
+    static constexpr int NP = (NPC + NT - 1) / NT, RPP = NT / CH;
+    static constexpr int BUF = kWinKeys * (LK + LV);             // elements of one buffer
 };
+constexpr float kLag = 8.f;
 
-template <typename T, int D, int QT>
-__global__ void __launch_bounds__(256) window_forward_kernel(WindowArgs a)
+template <typename T, int D, int NW, bool RING>
+__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) window_forward_kernel(WindowArgs a)
 {
-    typedef WinGeo<T, D, QT> G;
+    typedef WinGeo<T, D, NW> G;
     typedef typename Frag<T>::type F;
     __shared__ __attribute__((aligned(16))) T lds[2 * G::BUF];
 
@@ -50,14 +55,14 @@ __global__ void __launch_bounds__(256) window_forward_kernel(WindowArgs a)
     const int nq = min(G::BQ, len - q0);
     const size_t row0 = ((size_t)b * a.H + h) * a.L + q0;  // the block's first row of q, o, lse
     T* const out = (T*)a.o + row0 * D;
-    const int a0 = 16 * QT * wave;                         // the wave's first query in the block
+    const int a0 = 16 * wave;                              // the wave's first query in the block
 
     if (nq <= 0) {  // padding: zeros
         const int rows = min(G::BQ, a.L - q0);
-        for (int i = tid; i < rows * G::CH; i += 256) {
+        for (int i = tid; i < rows * G::CH; i += G::NT) {
             if (a.nsplit == 1) *(intx4*)(out + (size_t)i * G::PE) = intx4{0, 0, 0, 0};
         }
-        for (int i = tid; i < rows; i += 256) {
+        for (int i = tid; i < rows; i += G::NT) {
             if (a.nsplit == 1) {
                 if (a.lse) a.lse[row0 + i] = -INFINITY;
             } else {
@@ -71,7 +76,7 @@ __global__ void __launch_bounds__(256) window_forward_kernel(WindowArgs a)
 
     // The block's keys: sinks [s0, s0 + ns), then positions [lo, p0 + nq).
     const int64_t p0 = pos + q0;
-    const int64_t first = a.ck ? 0 : pos;                   // the first position whose key exists
+    const int64_t first = RING ? 0 : pos;                   // the first position whose key exists
     const int64_t lo = max(first, p0 - (a.W - 1));
     const int64_t s0 = min(first, (int64_t)a.S);
     const int ns = (int)(min((int64_t)a.S, lo) > s0 ? min((int64_t)a.S, lo) - s0 : 0);
@@ -80,8 +85,12 @@ __global__ void __launch_bounds__(256) window_forward_kernel(WindowArgs a)
     const int sb = (int)min((int64_t)0x40000000, max((int64_t)0, a.S - lo));  // window keys that are sinks too
     const int neu = (int)(pos - lo > 0 ? pos - lo : 0);     // window keys that come from the ring
     const int back = (int)(lo > pos ? lo - pos : 0);        // the new token of window key 0
-    const int64_t rlo = max(lo, (int64_t)a.S);              // ring slot of the first window key past the sinks
-    const int r0 = (int)((rlo - a.S) % a.W), rj = (int)(rlo - lo < 0x40000000 ? rlo - lo : 0x40000000);
+    int r0 = 0, rj = 0;
+    if (RING) {                                             // ring slot of the first window key past the sinks
+        const int64_t rlo = max(lo, (int64_t)a.S);
+        r0 = (int)((rlo - a.S) % a.W);
+        rj = (int)(rlo - lo < 0x40000000 ? rlo - lo : 0x40000000);
+    }
     const size_t kvrow = ((size_t)b * a.Hkv + hk) * a.L, crow = ((size_t)b * a.Hkv + hk) * ((size_t)a.S + a.W);
 
     const int ntile = (total + kWinKeys - 1) / kWinKeys;
@@ -89,6 +98,8 @@ __global__ void __launch_bounds__(256) window_forward_kernel(WindowArgs a)
     const int tb = part * each, te = min(ntile, tb + each);
 
     const int ch = tid % G::CH, lrow = tid / G::CH;
+    const T *knew = (const T*)a.k + kvrow * D + ch * G::PE, *vnew = (const T*)a.v + kvrow * D + ch * G::PE;
+    const T *kold = (const T*)a.ck + crow * D + ch * G::PE, *vold = (const T*)a.cv + crow * D + ch * G::PE;
     intx4 kr[G::NP], vr[G::NP];
     auto load = [&](int tile) {
 #pragma unroll
@@ -96,12 +107,12 @@ __global__ void __launch_bounds__(256) window_forward_kernel(WindowArgs a)
             const int i = tile * kWinKeys + ps * G::RPP + lrow;
             const int j = i - ns;
             kr[ps] = vr[ps] = intx4{0, 0, 0, 0};
-            if (i < total) {
-                const bool fresh = j >= neu || (j < 0 && s0 + i >= pos);
-                if (fresh) {
-                    const size_t at = (kvrow + (size_t)(j < 0 ? (int)(s0 + i - pos) : j - neu + back)) * D + ch * G::PE;
-                    kr[ps] = *(const intx4*)((const T*)a.k + at);
-                    vr[ps] = *(const intx4*)((const T*)a.v + at);
+            if (i < total && (G::NPC >= G::NT || lrow < kWinKeys)) {
+                const int spos = (int)(s0 - pos) + i;       // a sink as a new token, if it is one
+                if (!RING || j >= neu || (j < 0 && s0 + i >= pos)) {
+                    const size_t at = (size_t)(j < 0 ? spos : j - neu + back) * D;
+                    kr[ps] = *(const intx4*)(knew + at);
+                    vr[ps] = *(const intx4*)(vnew + at);
                 } else {
                     int slot;
                     if (j < 0) {
@@ -112,9 +123,9 @@ __global__ void __launch_bounds__(256) window_forward_kernel(WindowArgs a)
                         slot = r0 + (j - rj);
                         slot = a.S + (slot >= a.W ? slot - a.W : slot);
                     }
-                    const size_t at = (crow + slot) * D + ch * G::PE;
-                    kr[ps] = *(const intx4*)((const T*)a.ck + at);
-                    vr[ps] = *(const intx4*)((const T*)a.cv + at);
+                    const size_t at = (size_t)slot * D;
+                    kr[ps] = *(const intx4*)(kold + at);
+                    vr[ps] = *(const intx4*)(vold + at);
                 }
             }
         }
@@ -123,132 +134,121 @@ __global__ void __launch_bounds__(256) window_forward_kernel(WindowArgs a)
 #pragma unroll
         for (int ps = 0; ps < G::NP; ++ps) {
             const int i = ps * G::RPP + lrow;
-            *(intx4*)(buf + i * G::LK + ch * G::PE) = kr[ps];
-            *(intx4*)(buf + kWinKeys * G::LK + i * G::LV + ch * G::PE) = vr[ps];
+            if (G::NPC >= G::NT || lrow < kWinKeys) {
+                *(intx4*)(buf + i * G::LK + ch * G::PE) = kr[ps];
+                *(intx4*)(buf + kWinKeys * G::LK + i * G::LV + ch * G::PE) = vr[ps];
+            }
         }
     };
 
     // queries, sign of the scale folded in (exact), as the second operand of K Q^T
-    F qf[QT][D / 32];
-    const float sgn = a.scale < 0.f ? -1.f : 1.f;
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-        const int i = min(a0 + 16 * qt + r, nq - 1);
-        const T* qrow = (const T*)a.q + (row0 + i) * D;
+    F qf[D / 32];
+    {
+        const T* qrow = (const T*)a.q + (row0 + min(a0 + r, nq - 1)) * D;
 #pragma unroll
         for (int kb = 0; kb < D / 32; ++kb) {
-            qf[qt][kb] = ld_nat(qrow, kb, g);
+            qf[kb] = ld_nat(qrow, kb, g);
             if (a.scale < 0.f)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) qf[qt][kb][e] = (T)(sgn * (float)qf[qt][kb][e]);
+                for (int e = 0; e < 8; ++e) qf[kb][e] = (T)(-(float)qf[kb][e]);
         }
     }
-    const float sc = fabsf(a.scale) * kLog2e;
+    const float sc = fabsf(a.scale) * kLog2e, lag = kLag / sc;
 
-    floatx4 acc[QT][D / 16];
-    float mx[QT], sum[QT];
+    floatx4 acc[D / 16];
+    float mx = kNoMax, sum = 0.f, limit = kNoMax;           // limit: mx + lag
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-        mx[qt] = kNoMax;
-        sum[qt] = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] = zero4();
-    }
+    for (int dt = 0; dt < D / 16; ++dt) acc[dt] = zero4();
 
-    const int aend = min(a0 + 16 * QT, nq) - 1;  // the wave's last query
+    const int aend = min(a0 + 16, nq) - 1;  // the wave's last query
+    const int ca = c + a0 + r;              // the lane's query as a window key
+    // NK tiles of 16 keys from the tile's key 16 k0 on; `edge`: some pair of them is not visible
+    auto keys = [&](const T* sK, const T* sV, int j0, auto nk, auto edge, int k0) {
+        constexpr int NK = decltype(nk)::value;
+        floatx4 s[NK];
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt) {
+            s[kt] = zero4();
+#pragma unroll
+            for (int kb = 0; kb < D / 32; ++kb) s[kt] = mma(ld_nat(sK + (16 * (k0 + kt) + r) * G::LK, kb, g), qf[kb], s[kt]);
+        }
+        if (decltype(edge)::value) {
+#pragma unroll
+            for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = j0 + 16 * (k0 + kt) + 4 * g + e;
+                    const bool seen = (j < 0) | ((j <= ca) & ((ca - j < a.W) | (j < sb)));  // no branches
+                    s[kt][e] = seen ? s[kt][e] : -INFINITY;
+                }
+        }
+        float m = kNoMax;
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt) m = fmaxf(m, fmaxf(fmaxf(s[kt][0], s[kt][1]), fmaxf(s[kt][2], s[kt][3])));
+        if (__any(m > limit)) {
+            m = fmaxf(mx, rows_max(m));
+            const float al = exp2_fast((mx - m) * sc);
+            sum *= al;
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) acc[dt] *= al;
+            mx = m;
+            limit = m == kNoMax ? kNoMax : m + lag;
+        }
+        const float nm = -mx * sc;
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p = exp2_fast(__builtin_fmaf(s[kt][e], sc, nm));
+                s[kt][e] = p;
+                sum += p;
+            }
+#pragma unroll
+        for (int kb = 0; kb < NK / 2; ++kb) {
+            const F pf = frag_from_acc<T>(s[2 * kb], s[2 * kb + 1]);
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) acc[dt] = mma(ld_red(sV, G::LV, 16 * dt, k0 / 2 + kb, g, r), pf, acc[dt]);
+        }
+    };
+    typedef std::integral_constant<int, 4> Four;
+    typedef std::integral_constant<int, 2> Two;
+
     if (tb < te) load(tb);
     for (int t = tb; t < te; ++t) {
         T* buf = lds + (t & 1) * G::BUF;
         store(buf);
         __syncthreads();
         if (t + 1 < te) load(t + 1);
+        const T *sK = buf, *sV = buf + kWinKeys * G::LK;
         const int j0 = t * kWinKeys - ns, j1 = j0 + kWinKeys - 1;  // the tile's window keys (negative: sinks)
-        // no key of the tile is seen by the wave: past its last query, or before its first window
-        if (a0 >= nq || j0 > c + aend || (j0 >= sb && j1 <= c + a0 - a.W)) continue;
-        const bool whole = j1 < 0 || (j0 >= 0 && j1 <= c + a0 && (c + aend - j0 < a.W || j1 < sb));
-        const T* sK = buf;
-        const T* sV = buf + kWinKeys * G::LK;
-
-        floatx4 s[QT][4];
+        if (a0 >= nq) continue;
+        if (j1 < 0 || (j0 >= 0 && j1 <= c + a0 && (c + aend - j0 < a.W || j1 < sb))) {
+            keys(sK, sV, j0, Four(), std::false_type(), 0);
+        } else {  // halves of the tile, those that the wave sees: up to its last query, from its first window or a sink on
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-#pragma unroll
-            for (int qt = 0; qt < QT; ++qt) s[qt][kt] = zero4();
-#pragma unroll
-            for (int kb = 0; kb < D / 32; ++kb) {
-                const F kf = ld_nat(sK + (16 * kt + r) * G::LK, kb, g);
-#pragma unroll
-                for (int qt = 0; qt < QT; ++qt) s[qt][kt] = mma(kf, qf[qt][kb], s[qt][kt]);
-            }
-        }
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-            if (!whole) {
-                const int ca = c + a0 + 16 * qt + r;  // the query as a window key
-#pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int j = j0 + 16 * kt + 4 * g + e;
-                        const bool seen = (j < 0) | ((j <= ca) & ((ca - j < a.W) | (j < sb)));  // no branches
-                        s[qt][kt][e] = seen ? s[qt][kt][e] : -INFINITY;
-                    }
-            }
-            float m = kNoMax;
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-                m = fmaxf(m, fmaxf(fmaxf(s[qt][kt][0], s[qt][kt][1]), fmaxf(s[qt][kt][2], s[qt][kt][3])));
-            m = fmaxf(mx[qt], rows_max(m));
-            if (__any(m > mx[qt])) {
-                const float al = exp2_fast((mx[qt] - m) * sc);
-                sum[qt] *= al;
-#pragma unroll
-                for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] *= al;
-                mx[qt] = m;
-            }
-            const float nm = -m * sc;
-#pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = exp2_fast(__builtin_fmaf(s[qt][kt][e], sc, nm));
-                    s[qt][kt][e] = p;
-                    sum[qt] += p;
-                }
-        }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            F pf[QT];
-#pragma unroll
-            for (int qt = 0; qt < QT; ++qt) pf[qt] = frag_from_acc<T>(s[qt][2 * kb], s[qt][2 * kb + 1]);
-#pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) {
-                const F vf = ld_red(sV, G::LV, 16 * dt, kb, g, r);
-#pragma unroll
-                for (int qt = 0; qt < QT; ++qt) acc[qt][dt] = mma(vf, pf[qt], acc[qt][dt]);
+            for (int hf = 0; hf < 2; ++hf) {
+                const int i0 = j0 + 32 * hf, i1 = i0 + 31;
+                if (i0 <= c + aend && (i0 < sb || i1 > c + a0 - a.W)) keys(sK, sV, j0, Two(), std::true_type(), 2 * hf);
             }
         }
     }
 
+    const int i = a0 + r;
+    const float l = rows_sum(sum);
+    if (i >= min(G::BQ, a.L - q0)) return;
+    const bool real = i < nq;
+    if (a.nsplit == 1) {
+        const float inv = real ? 1.f / l : 0.f;
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-        const int i = a0 + 16 * qt + r;
-        const float l = rows_sum(sum[qt]);
-        if (i >= min(G::BQ, a.L - q0)) continue;
-        const bool real = i < nq;
-        if (a.nsplit == 1) {
-            const float inv = real ? 1.f / l : 0.f;
+        for (int dt = 0; dt < D / 16; ++dt) st4(out + (size_t)i * D + 16 * dt + 4 * g, real ? acc[dt] * inv : zero4());
+        if (a.lse && g == 0) a.lse[row0 + i] = real ? (mx * sc + __log2f(l)) * kLn2 : -INFINITY;
+    } else {
+        const size_t at = (size_t)part * a.B * a.H * a.L + row0 + i;
 #pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) st4(out + (size_t)i * D + 16 * dt + 4 * g, real ? acc[qt][dt] * inv : zero4());
-            if (a.lse && g == 0) a.lse[row0 + i] = real ? (mx[qt] * sc + __log2f(l)) * kLn2 : -INFINITY;
-        } else {
-            const size_t at = (size_t)part * a.B * a.H * a.L + row0 + i;
-#pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) st4f(a.part_o + at * D + 16 * dt + 4 * g, acc[qt][dt]);
-            if (g == 0) {
-                a.part_ml[2 * at] = real ? mx[qt] * sc : kNoMax;
-                a.part_ml[2 * at + 1] = real ? l : 0.f;
-            }
+        for (int dt = 0; dt < D / 16; ++dt) st4f(a.part_o + at * D + 16 * dt + 4 * g, acc[dt]);
+        if (g == 0) {
+            a.part_ml[2 * at] = real ? mx * sc : kNoMax;
+            a.part_ml[2 * at + 1] = real ? l : 0.f;
         }
     }
 }
@@ -316,14 +316,19 @@ template <typename T, int D> __global__ void __launch_bounds__(256) window_ring_
     *(intx4*)((T*)a.cv_out + to) = vx;
 }
 
-template <typename T, int D> hipError_t forward_d(int qt, const WindowArgs& a, hipStream_t s)
+template <typename T, int D, bool RING> hipError_t forward_r(int waves, const WindowArgs& a, hipStream_t s)
 {
     const dim3 grid((unsigned)(8 * a.per));
-    if (qt == 2)
-        hipLaunchKernelGGL((window_forward_kernel<T, D, 2>), grid, dim3(256), 0, s, a);
+    if (waves == 8)
+        hipLaunchKernelGGL((window_forward_kernel<T, D, 8, RING>), grid, dim3(512), 0, s, a);
     else
-        hipLaunchKernelGGL((window_forward_kernel<T, D, 1>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((window_forward_kernel<T, D, 4, RING>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
+}
+
+template <typename T, int D> hipError_t forward_d(int waves, const WindowArgs& a, hipStream_t s)
+{
+    return a.ck ? forward_r<T, D, true>(waves, a, s) : forward_r<T, D, false>(waves, a, s);
 }
 
 template <typename T, int D> hipError_t join_d(const JoinArgs& a, hipStream_t s)
@@ -354,9 +359,9 @@ template <typename T, int D> hipError_t ring_d(const WindowArgs& a, hipStream_t 
     }                                                          \
     return hipErrorInvalidValue;
 
-hipError_t launch_window_forward(int bf16_io, int D, int qt, const WindowArgs& a, hipStream_t s)
+hipError_t launch_window_forward(int bf16_io, int D, int waves, const WindowArgs& a, hipStream_t s)
 {
-#define BLA_CALL(T, DD) forward_d<T, DD>(qt, a, s)
+#define BLA_CALL(T, DD) forward_d<T, DD>(waves, a, s)
     BLA_BY_TYPE(BLA_CALL)
 #undef BLA_CALL
 }
