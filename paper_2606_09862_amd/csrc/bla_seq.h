@@ -69,6 +69,12 @@ __device__ __forceinline__ floatx8 ld_red_dual(const float* M, int ld, int x0, i
     return ld_red(M, ld, x0, kb, g, r);
 }
 
+// The largest of three, a NaN if one of them is (v_maximum3_f32; fmaxf would first quiet each operand, an instruction apiece).
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Work index of a workgroup: workgroups are dealt to the eight XCDs by index mod 8, so index w works on

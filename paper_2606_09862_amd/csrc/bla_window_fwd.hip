@@ -1,6 +1,4 @@
 // Window attention over a prompt (bla_window_forward).
-#include <type_traits>
-
 #include "bla_window.h"
 
 namespace bla {
@@ -104,29 +102,26 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
     auto load = [&](int tile) {
 #pragma unroll
         for (int ps = 0; ps < G::NP; ++ps) {
-            const int i = tile * kWinKeys + ps * G::RPP + lrow;
-            const int j = i - ns;
-            kr[ps] = vr[ps] = intx4{0, 0, 0, 0};
-            if (i < total && (G::NPC >= G::NT || lrow < kWinKeys)) {
-                const int spos = (int)(s0 - pos) + i;       // a sink as a new token, if it is one
-                if (!RING || j >= neu || (j < 0 && s0 + i >= pos)) {
-                    const size_t at = (size_t)(j < 0 ? spos : j - neu + back) * D;
-                    kr[ps] = *(const intx4*)(knew + at);
-                    vr[ps] = *(const intx4*)(vnew + at);
+            // rows past the last key repeat it: the mask hides them
+            const int i = min(tile * kWinKeys + ps * G::RPP + lrow, total - 1), j = i - ns;
+            if (G::NPC < G::NT && lrow >= kWinKeys) continue;
+            if (!RING || j >= neu || (j < 0 && s0 + i >= pos)) {
+                const size_t at = (size_t)(j < 0 ? (int)(s0 - pos) + i : j - neu + back) * D;
+                kr[ps] = *(const intx4*)(knew + at);
+                vr[ps] = *(const intx4*)(vnew + at);
+            } else {
+                int slot;
+                if (j < 0) {
+                    slot = (int)s0 + i;
+                } else if (j < rj) {
+                    slot = (int)lo + j;
                 } else {
-                    int slot;
-                    if (j < 0) {
-                        slot = (int)s0 + i;
-                    } else if (j < rj) {
-                        slot = (int)lo + j;
-                    } else {
-                        slot = r0 + (j - rj);
-                        slot = a.S + (slot >= a.W ? slot - a.W : slot);
-                    }
-                    const size_t at = (size_t)slot * D;
-                    kr[ps] = *(const intx4*)(kold + at);
-                    vr[ps] = *(const intx4*)(vold + at);
+                    slot = r0 + (j - rj);
+                    slot = a.S + (slot >= a.W ? slot - a.W : slot);
                 }
+                const size_t at = (size_t)slot * D;
+                kr[ps] = *(const intx4*)(kold + at);
+                vr[ps] = *(const intx4*)(vold + at);
             }
         }
     };
@@ -161,58 +156,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
     for (int dt = 0; dt < D / 16; ++dt) acc[dt] = zero4();
 
     const int aend = min(a0 + 16, nq) - 1;  // the wave's last query
-    const int ca = c + a0 + r;              // the lane's query as a window key
-    // NK tiles of 16 keys from the tile's key 16 k0 on; `edge`: some pair of them is not visible
-    auto keys = [&](const T* sK, const T* sV, int j0, auto nk, auto edge, int k0) {
-        constexpr int NK = decltype(nk)::value;
-        floatx4 s[NK];
-#pragma unroll
-        for (int kt = 0; kt < NK; ++kt) {
-            s[kt] = zero4();
-#pragma unroll
-            for (int kb = 0; kb < D / 32; ++kb) s[kt] = mma(ld_nat(sK + (16 * (k0 + kt) + r) * G::LK, kb, g), qf[kb], s[kt]);
-        }
-        if (decltype(edge)::value) {
-#pragma unroll
-            for (int kt = 0; kt < NK; ++kt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = j0 + 16 * (k0 + kt) + 4 * g + e;
-                    const bool seen = (j < 0) | ((j <= ca) & ((ca - j < a.W) | (j < sb)));  // no branches
-                    s[kt][e] = seen ? s[kt][e] : -INFINITY;
-                }
-        }
-        float m = kNoMax;
-#pragma unroll
-        for (int kt = 0; kt < NK; ++kt) m = fmaxf(m, fmaxf(fmaxf(s[kt][0], s[kt][1]), fmaxf(s[kt][2], s[kt][3])));
-        if (__any(m > limit)) {
-            m = fmaxf(mx, rows_max(m));
-            const float al = exp2_fast((mx - m) * sc);
-            sum *= al;
-#pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) acc[dt] *= al;
-            mx = m;
-            limit = m == kNoMax ? kNoMax : m + lag;
-        }
-        const float nm = -mx * sc;
-#pragma unroll
-        for (int kt = 0; kt < NK; ++kt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float p = exp2_fast(__builtin_fmaf(s[kt][e], sc, nm));
-                s[kt][e] = p;
-                sum += p;
-            }
-#pragma unroll
-        for (int kb = 0; kb < NK / 2; ++kb) {
-            const F pf = frag_from_acc<T>(s[2 * kb], s[2 * kb + 1]);
-#pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) acc[dt] = mma(ld_red(sV, G::LV, 16 * dt, k0 / 2 + kb, g, r), pf, acc[dt]);
-        }
-    };
-    typedef std::integral_constant<int, 4> Four;
-    typedef std::integral_constant<int, 2> Two;
-
+    const int jhi = c + a0 + r, jlo = jhi - (a.W - 1);  // the lane's query sees the window keys jlo .. jhi, and those below sb up to jhi
     if (tb < te) load(tb);
     for (int t = tb; t < te; ++t) {
         T* buf = lds + (t & 1) * G::BUF;
@@ -220,16 +164,54 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
         __syncthreads();
         if (t + 1 < te) load(t + 1);
         const T *sK = buf, *sV = buf + kWinKeys * G::LK;
-        const int j0 = t * kWinKeys - ns, j1 = j0 + kWinKeys - 1;  // the tile's window keys (negative: sinks)
         if (a0 >= nq) continue;
-        if (j1 < 0 || (j0 >= 0 && j1 <= c + a0 && (c + aend - j0 < a.W || j1 < sb))) {
-            keys(sK, sV, j0, Four(), std::false_type(), 0);
-        } else {  // halves of the tile, those that the wave sees: up to its last query, from its first window or a sink on
+        // 32 keys at a time: those up to the wave's last query, from its first query's window or a sink on
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                const int i0 = j0 + 32 * hf, i1 = i0 + 31;
-                if (i0 <= c + aend && (i0 < sb || i1 > c + a0 - a.W)) keys(sK, sV, j0, Two(), std::true_type(), 2 * hf);
+        for (int hf = 0; hf < 2; ++hf) {
+            const int i0 = t * kWinKeys - ns + 32 * hf, i1 = i0 + 31;  // window keys (negative: sinks)
+            if (i0 > c + aend || (i0 >= sb && i1 <= c + a0 - a.W)) continue;
+            floatx4 s[2];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                s[kt] = zero4();
+#pragma unroll
+                for (int kb = 0; kb < D / 32; ++kb) s[kt] = mma(ld_nat(sK + (32 * hf + 16 * kt + r) * G::LK, kb, g), qf[kb], s[kt]);
             }
+            if (i1 > c + a0 || (i0 <= c + aend - a.W && i1 >= sb)) {  // some pair is not visible
+                const int j = i0 + 4 * g;
+                if (i0 >= sb) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        s[e >> 2][e & 3] = (unsigned)(j + 16 * (e >> 2) + (e & 3) - jlo) < (unsigned)a.W ? s[e >> 2][e & 3] : -INFINITY;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int k = j + 16 * (e >> 2) + (e & 3);
+                        s[e >> 2][e & 3] = (k <= jhi) & ((k >= jlo) | (k < sb)) ? s[e >> 2][e & 3] : -INFINITY;
+                    }
+                }
+            }
+            float m = max3(max3(s[0][0], s[0][1], s[0][2]), max3(s[0][3], s[1][0], s[1][1]), max3(s[1][2], s[1][3], s[1][3]));
+            if (__any(m > limit)) {
+                m = fmaxf(mx, rows_max(m));
+                const float al = exp2_fast((mx - m) * sc);
+                sum *= al;
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) acc[dt] *= al;
+                mx = m;
+                limit = m == kNoMax ? kNoMax : m + lag;
+            }
+            const float nm = -mx * sc;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[kt][e] = exp2_fast(__builtin_fmaf(s[kt][e], sc, nm));
+                    sum += s[kt][e];
+                }
+            const F pf = frag_from_acc<T>(s[0], s[1]);
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) acc[dt] = mma(ld_red(sV, G::LV, 16 * dt, hf, g, r), pf, acc[dt]);
         }
     }
 
