@@ -43,28 +43,19 @@ __device__ __forceinline__ floatx8 ld_red(const float* M, int ld, int x0, int kb
 template <typename T> __host__ __device__ constexpr int nat_ld(int D) { return D + 16 / (int)sizeof(T); }
 template <typename T> __host__ __device__ constexpr int red_ld(int D) { return sizeof(T) == 2 ? D + 16 : D + 4; }
 
-// A tile read both ways: row stride dual_ld, and in bf16 the eight-column groups of rows with bit 3 set lie at column
-// XOR 8, which moves rows r and r + 8 of a fragment off each other's banks (the transposing reads stay
-// conflict-free: swz_col).  dual_col is where a column (a multiple of a 16-byte piece) of a row lies.
-template <typename T> __host__ __device__ constexpr int dual_ld(int D) { return red_ld<T>(D); }
-template <typename T> __device__ __forceinline__ int dual_col(int row, int col)
-{
-    return sizeof(T) == 2 ? swz_col(row, col) : col;
-}
-// rows x0 .. x0+15 (x0 a multiple of 16, row x0 + r of the lane) as a natural-order fragment
-__device__ __forceinline__ bf16x8 ld_nat_dual(const bf16* M, int ld, int x0, int kb, int g, int r)
-{
-    return *reinterpret_cast<const bf16x8*>(M + (x0 + r) * ld + 32 * kb + ((8 * g) ^ ((r >> 3) << 3)));
-}
-__device__ __forceinline__ floatx8 ld_nat_dual(const float* M, int ld, int x0, int kb, int g, int r)
+// A tile read both ways.  In bf16 rows padded by 16 bytes put the sixteen rows of a fragment on different banks and leave the
+// transposing reads one overlap in eight rows (the 8 x odd dwords that avoid it need a swizzle for the row reads and a sixth
+// more LDS, which costs a workgroup per compute unit).
+template <typename T> __host__ __device__ constexpr int dual_ld(int D) { return nat_ld<T>(D); }
+template <typename T> __device__ __forceinline__ int dual_col(int, int col) { return col; }
+// rows x0 .. x0+15 as a natural-order fragment
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type ld_nat_dual(const T* M, int ld, int x0, int kb, int g, int r)
 {
     return ld_nat(M + (x0 + r) * ld, kb, g);
 }
-__device__ __forceinline__ bf16x8 ld_red_dual(const bf16* M, int ld, int x0, int kb, int g, int r)
-{
-    return ld_frag_tr_sw(M, ld, x0, kb, g, r);
-}
-__device__ __forceinline__ floatx8 ld_red_dual(const float* M, int ld, int x0, int kb, int g, int r)
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type ld_red_dual(const T* M, int ld, int x0, int kb, int g, int r)
 {
     return ld_red(M, ld, x0, kb, g, r);
 }

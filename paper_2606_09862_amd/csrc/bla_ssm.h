@@ -89,7 +89,7 @@ template <typename T> __device__ __forceinline__ typename Frag<T>::type ld_acc_r
 // The same of an LDS tile in the dual layout (row x0 + r, x0 a multiple of 16).
 __device__ __forceinline__ bf16x8 ld_acc_dual(const bf16* M, int ld, int x0, int kb, int g, int r)
 {
-    return ld_frag_2x8_sw(M + (x0 + r) * ld, kb, g, r);
+    return ld_frag_2x8(M + (x0 + r) * ld, kb, g);
 }
 __device__ __forceinline__ floatx8 ld_acc_dual(const float* M, int ld, int x0, int kb, int g, int r)
 {

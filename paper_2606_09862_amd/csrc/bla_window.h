@@ -66,8 +66,7 @@ hipError_t launch_window_forward(int bf16_io, int D, int waves, const WindowArgs
 hipError_t launch_window_ring(int bf16_io, int D, const WindowArgs& a, hipStream_t s);
 hipError_t launch_window_step(int bf16_io, int D, const WindowStepArgs& a, hipStream_t s);
 hipError_t launch_window_backward(int bf16_io, int D, const WindowBwdArgs& a, hipStream_t s);
-int window_bwd_keys(int bf16_io, int D);     // keys per block of the key pass
-int window_bwd_queries(int bf16_io, int D);  // queries per block of the query pass
+int window_bwd_block(int D);  // queries (keys) per block of the query (key) pass
 
 // Join of nsplit parts of a softmax: o = sum_s e^{m_s - m} O_s / sum_s e^{m_s - m} l_s (m in the base-2 domain).
 struct JoinArgs {

@@ -83,9 +83,9 @@ struct BackwardPlan {
 BackwardPlan backward_plan(const bla_window_params* p)
 {
     BackwardPlan b;
-    const int bf16 = p->io_dtype == BLA_BF16, nk = window_bwd_keys(bf16, p->d), bq = window_bwd_queries(bf16, p->d);
     const long long bh = (long long)p->B * p->H, bk = (long long)p->B * p->H_kv;
-    b.nqb = (p->L + bq - 1) / bq;
+    const int nk = window_bwd_block(p->d);
+    b.nqb = (p->L + nk - 1) / nk;
     b.nkb = (p->L + nk - 1) / nk;
     const int sinks = p->sinks < p->L ? p->sinks : p->L;
     b.nsb = (sinks + nk - 1) / nk;

@@ -11,11 +11,14 @@
 namespace bla {
 namespace {
 
+// Tiles of 16 queries (query pass) or keys (key pass) that a wave owns: two where the registers hold them, so that each fragment read
+// from LDS serves two products.
+template <typename T, int D> constexpr int bwd_tiles() { return D == 128 ? 1 : 2; }
+// Four waves to a workgroup: with eight one workgroup fills a compute unit and its waves wait for each other at every tile (128 x 4096 tokens,
+// d = 64, window 511: query pass 229 us with eight waves, 167 with four; key pass 310 and 259).
 template <typename T, int D> struct BwdGeo {
-    static constexpr int CH = D * (int)sizeof(T) / 16, RPP = 256 / CH, NP = 64 / RPP, PE = 16 / (int)sizeof(T);
-    static constexpr int QT = D == 128 ? 1 : 2;  // query tiles of a wave in the query pass
-    static constexpr int KT = D == 128 ? 1 : 2;  // key tiles of a wave in the key pass
-    static constexpr int BQ = 64 * QT, NK = 64 * KT;
+    static constexpr int NT = 256, PE = 16 / (int)sizeof(T), CH = D / PE, RPP = NT / CH, NP = 64 / RPP;
+    static constexpr int XT = bwd_tiles<T, D>(), NB = 64 * XT;
     static constexpr int LD = dual_ld<T>(D), LN = nat_ld<T>(D);
 };
 
@@ -25,7 +28,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
 {
     typedef BwdGeo<T, D> G;
     typedef typename Frag<T>::type F;
-    constexpr int QT = G::QT, BUF = 64 * (G::LD + G::LN);
+    constexpr int QT = G::XT, BUF = 64 * (G::LD + G::LN);
     __shared__ __attribute__((aligned(16))) T lds[2 * BUF];
 
     long long u = xcd_unit(blockIdx.x, a.q_per);
@@ -33,37 +36,35 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
     const int grp = a.H / a.Hkv;
     const int hg = (int)(u % grp);
     u /= grp;
-    const int q0 = (int)(u % a.nqb) * G::BQ;
+    const int q0 = (int)(u % a.nqb) * G::NB;
     u /= a.nqb;
     const int hk = (int)(u % a.Hkv), b = (int)(u / a.Hkv);
     const int h = hk * grp + hg;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
     const int len = a.lengths ? min(max(a.lengths[b], 0), a.L) : a.L;
-    const int nq = min(G::BQ, len - q0);
+    const int nq = min(G::NB, len - q0);
     const size_t row0 = ((size_t)b * a.H + h) * a.L + q0;
     T* const out = (T*)a.dq + row0 * D;
     const int ch = tid % G::CH, lrow = tid / G::CH;
     if (nq <= 0) {
-        const int rows = min(G::BQ, a.L - q0);
-        for (int i = tid; i < rows * G::CH; i += 256) *(intx4*)(out + (size_t)i * G::PE) = intx4{0, 0, 0, 0};
+        const int rows = min(G::NB, a.L - q0);
+        for (int i = tid; i < rows * G::CH; i += G::NT) *(intx4*)(out + (size_t)i * G::PE) = intx4{0, 0, 0, 0};
         return;
     }
     const int lo = q0 - (a.W - 1) > 0 ? q0 - (a.W - 1) : 0;
     const int ns = min(a.S, lo), c = q0 - lo, total = ns + c + nq, sb = max(0, a.S - lo);
     const size_t kvrow = ((size_t)b * a.Hkv + hk) * a.L;
+    const T *kp = (const T*)a.k + kvrow * D + ch * G::PE, *vp = (const T*)a.v + kvrow * D + ch * G::PE;
     const int ntile = (total + 63) / 64;
 
     intx4 kr[G::NP], vr[G::NP];
     auto load = [&](int tile) {
 #pragma unroll
         for (int ps = 0; ps < G::NP; ++ps) {
-            const int i = tile * 64 + ps * G::RPP + lrow;
-            kr[ps] = vr[ps] = intx4{0, 0, 0, 0};
-            if (i < total) {
-                const size_t at = (kvrow + (i < ns ? i : lo + i - ns)) * D + ch * G::PE;
-                kr[ps] = *(const intx4*)((const T*)a.k + at);
-                vr[ps] = *(const intx4*)((const T*)a.v + at);
-            }
+            const int i = min(tile * 64 + ps * G::RPP + lrow, total - 1);
+            const size_t at = (size_t)(i < ns ? i : lo + i - ns) * D;
+            kr[ps] = *(const intx4*)(kp + at);
+            vr[ps] = *(const intx4*)(vp + at);
         }
     };
 
@@ -106,11 +107,11 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
         }
         __syncthreads();
         if (t + 1 < ntile) load(t + 1);
-        const int j0 = t * 64 - ns, j1 = j0 + 63;
-        if (a0 >= nq || j0 > c + aend || (j0 >= sb && j1 <= c + a0 - a.W)) continue;
-        const bool whole = j1 < 0 || (j0 >= 0 && j1 <= c + a0 && (c + aend - j0 < a.W || j1 < sb));
+        if (a0 >= nq) continue;
 #pragma unroll
-        for (int kb2 = 0; kb2 < 2; ++kb2) {
+        for (int hf = 0; hf < 2; ++hf) {
+            const int i0 = t * 64 - ns + 32 * hf, i1 = i0 + 31;  // window keys (negative: sinks)
+            if (i0 > c + aend || (i0 >= sb && i1 <= c + a0 - a.W)) continue;
             floatx4 s[QT][2], dp[QT][2];
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
@@ -118,8 +119,8 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
                 for (int qt = 0; qt < QT; ++qt) s[qt][kt] = dp[qt][kt] = zero4();
 #pragma unroll
                 for (int kb = 0; kb < D / 32; ++kb) {
-                    const F kf = ld_nat_dual(sK, G::LD, 32 * kb2 + 16 * kt, kb, g, r);
-                    const F vf = ld_nat(sV + (32 * kb2 + 16 * kt + r) * G::LN, kb, g);
+                    const F kf = ld_nat_dual(sK, G::LD, 32 * hf + 16 * kt, kb, g, r);
+                    const F vf = ld_nat(sV + (32 * hf + 16 * kt + r) * G::LN, kb, g);
 #pragma unroll
                     for (int qt = 0; qt < QT; ++qt) {
                         s[qt][kt] = mma(kf, qf[qt][kb], s[qt][kt]);
@@ -127,26 +128,37 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
                     }
                 }
             }
-            F sf[QT];
 #pragma unroll
-            for (int qt = 0; qt < QT; ++qt) {
-                const int ca = c + a0 + 16 * qt + r;
+            for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float p = exp2_fast(__builtin_fmaf(s[qt][kt][e], sc, -lse2[qt])) * (dp[qt][kt][e] - delta[qt]);
-                        if (!whole) {
-                            const int j = j0 + 32 * kb2 + 16 * kt + 4 * g + e;
-                            p = (j < 0) | ((j <= ca) & ((ca - j < a.W) | (j < sb))) ? p : 0.f;
+                    for (int e = 0; e < 4; ++e)
+                        s[qt][kt][e] = exp2_fast(__builtin_fmaf(s[qt][kt][e], sc, -lse2[qt])) * (dp[qt][kt][e] - delta[qt]);
+            if (i1 > c + a0 || (i0 <= c + aend - a.W && i1 >= sb)) {  // some pair is not visible
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt) {
+                    const int jhi = c + a0 + 16 * qt + r, jlo = jhi - (a.W - 1), j = i0 + 4 * g;
+                    if (i0 >= sb) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            s[qt][e >> 2][e & 3] =
+                                (unsigned)(j + 16 * (e >> 2) + (e & 3) - jlo) < (unsigned)a.W ? s[qt][e >> 2][e & 3] : 0.f;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int k = j + 16 * (e >> 2) + (e & 3);
+                            s[qt][e >> 2][e & 3] = (k <= jhi) & ((k >= jlo) | (k < sb)) ? s[qt][e >> 2][e & 3] : 0.f;
                         }
-                        s[qt][kt][e] = p;
                     }
-                sf[qt] = frag_from_acc<T>(s[qt][0], s[qt][1]);
+                }
             }
+            F sf[QT];
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) sf[qt] = frag_from_acc<T>(s[qt][0], s[qt][1]);
 #pragma unroll
             for (int dt = 0; dt < D / 16; ++dt) {
-                const F kf = ld_red_dual(sK, G::LD, 16 * dt, kb2, g, r);
+                const F kf = ld_red_dual(sK, G::LD, 16 * dt, hf, g, r);
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt) acc[qt][dt] = mma(kf, sf[qt], acc[qt][dt]);
             }
@@ -155,7 +167,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         const int i = a0 + 16 * qt + r;
-        if (i >= min(G::BQ, a.L - q0)) continue;
+        if (i >= min(G::NB, a.L - q0)) continue;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt)
             st4(out + (size_t)i * D + 16 * dt + 4 * g, i < nq ? acc[qt][dt] * a.scale : zero4());
@@ -172,7 +184,7 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
 {
     typedef BwdGeo<T, D> G;
     typedef typename Frag<T>::type F;
-    constexpr int KT = G::KT, BUF = 64 * 2 * G::LD;
+    constexpr int KT = G::XT, BUF = 64 * 2 * G::LD;
     __shared__ __attribute__((aligned(16))) T lds[2 * BUF];
     __shared__ __attribute__((aligned(16))) float sStat[2][2][64];
 
@@ -185,28 +197,31 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
     const int hk = (int)(u % a.Hkv), b = (int)(u / a.Hkv);
     const bool sink = job < a.nsb * a.ssplit;
     const int nb = sink ? job / a.ssplit : job - a.nsb * a.ssplit + a.nsb, part = sink ? job % a.ssplit : 0;
-    const int n0 = nb * G::NK;
+    const int n0 = nb * G::NB;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
     const int len = a.lengths ? min(max(a.lengths[b], 0), a.L) : a.L;
     const size_t kvrow = ((size_t)b * a.Hkv + hk) * a.L;
     const int ch = tid % G::CH, lrow = tid / G::CH;
 
     // 64-query tiles of the walk, from query n0 on
-    const int qend = sink ? len : (int)min((long long)len, (long long)n0 + G::NK - 1 + a.W);
+    const int qend = sink ? len : (int)min((long long)len, (long long)n0 + G::NB - 1 + a.W);
     int tb = 0, te = qend > n0 ? (qend - n0 + 63) / 64 : 0;
     if (sink) {
         const int each = (te + a.ssplit - 1) / a.ssplit;
         tb = part * each;
         te = min(te, tb + each);
     }
-    const int nt = max(0, te - tb), steps = nt * grp;
+    const int nt = max(0, te - tb);
 
-    const int k0 = n0 + 16 * KT * wave;  // the wave's first key
+    const int k0 = n0 + 16 * KT * wave, kend = k0 + 16 * KT - 1;  // the wave's keys
     F kf[KT][D / 32], vf[KT][D / 32];
+    unsigned span[KT];                                            // key j is seen by the queries j .. j + span - 1
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-        const size_t at = (kvrow + min(k0 + 16 * kt + r, a.L - 1)) * D;
-        const bool in = k0 + 16 * kt + r < len;
+        const int j = k0 + 16 * kt + r;
+        const size_t at = (kvrow + min(j, a.L - 1)) * D;
+        const bool in = j < len;
+        span[kt] = in ? (unsigned)(j < a.S ? len - j : min(len - j, a.W)) : 0u;
 #pragma unroll
         for (int kb = 0; kb < D / 32; ++kb) {
             kf[kt][kb] = in ? ld_nat((const T*)a.k + at, kb, g) : zero_frag<T>();
@@ -222,97 +237,106 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
 
     intx4 qr[G::NP], dr[G::NP];
     float st = 0.f;
-    auto load = [&](int step) {
-        const int hg = step / nt, q0 = n0 + 64 * (tb + step % nt);
-        const size_t row0 = ((size_t)b * a.H + hk * grp + hg) * a.L + q0;
+    const T *qp = (const T*)a.q + ch * G::PE, *dp_ = (const T*)a.dO + ch * G::PE;
+    auto load = [&](int hg, int t) {  // queries past the row's last repeat it: the masks hide them
+        const size_t row0 = ((size_t)b * a.H + hk * grp + hg) * a.L;
+        const int q0 = n0 + 64 * (tb + t);
 #pragma unroll
         for (int ps = 0; ps < G::NP; ++ps) {
-            const int i = ps * G::RPP + lrow;
-            qr[ps] = dr[ps] = intx4{0, 0, 0, 0};
-            if (q0 + i < len) {
-                const size_t at = (row0 + i) * D + ch * G::PE;
-                qr[ps] = *(const intx4*)((const T*)a.q + at);
-                dr[ps] = *(const intx4*)((const T*)a.dO + at);
-            }
+            const size_t at = (row0 + min(q0 + ps * G::RPP + lrow, len - 1)) * D;
+            qr[ps] = *(const intx4*)(qp + at);
+            dr[ps] = *(const intx4*)(dp_ + at);
         }
         if (tid < 128) {
-            const int i = tid & 63;
-            st = q0 + i < len ? (tid < 64 ? a.lse[row0 + i] * kLog2e : a.delta[row0 + i]) : 0.f;
+            const size_t at = row0 + min(q0 + (tid & 63), len - 1);
+            st = tid < 64 ? a.lse[at] * kLog2e : a.delta[at];
         }
     };
 
-    if (steps > 0) load(0);
-    for (int step = 0; step < steps; ++step) {
-        T *sQ = lds + (step & 1) * BUF, *sD = sQ + 64 * G::LD;
-        float(*stat)[64] = sStat[step & 1];
+    if (nt > 0) load(0, 0);
+    int buf = 0;
+    for (int hg = 0; hg < grp; ++hg)
+        for (int t = 0; t < nt; ++t, buf ^= 1) {
+            T *sQ = lds + buf * BUF, *sD = sQ + 64 * G::LD;
+            float(*stat)[64] = sStat[buf];
 #pragma unroll
-        for (int ps = 0; ps < G::NP; ++ps) {
-            const int i = ps * G::RPP + lrow, at = i * G::LD + dual_col<T>(i, ch * G::PE);
-            *(intx4*)(sQ + at) = qr[ps];
-            *(intx4*)(sD + at) = dr[ps];
-        }
-        if (tid < 128) stat[tid >> 6][tid & 63] = st;
-        __syncthreads();
-        if (step + 1 < steps) load(step + 1);
-        const int q0 = n0 + 64 * (tb + step % nt), q1 = min(q0 + 63, len - 1);
-        const int kend = k0 + 16 * KT - 1;
-        if (k0 > q1 || (k0 >= a.S && q0 - kend >= a.W)) continue;
-        const bool whole = kend <= q0 && q0 + 63 < len && (q0 + 63 - k0 < a.W || kend < a.S);
-#pragma unroll
-        for (int kb2 = 0; kb2 < 2; ++kb2) {
-            floatx4 s[KT][2], dp[KT][2];
-#pragma unroll
-            for (int qt = 0; qt < 2; ++qt) {
-#pragma unroll
-                for (int kt = 0; kt < KT; ++kt) s[kt][qt] = dp[kt][qt] = zero4();
-#pragma unroll
-                for (int kb = 0; kb < D / 32; ++kb) {
-                    const F qf = ld_nat_dual(sQ, G::LD, 32 * kb2 + 16 * qt, kb, g, r);
-                    const F df = ld_nat_dual(sD, G::LD, 32 * kb2 + 16 * qt, kb, g, r);
-#pragma unroll
-                    for (int kt = 0; kt < KT; ++kt) {
-                        s[kt][qt] = mma(qf, kf[kt][kb], s[kt][qt]);
-                        dp[kt][qt] = mma(df, vf[kt][kb], dp[kt][qt]);
-                    }
-                }
+            for (int ps = 0; ps < G::NP; ++ps) {
+                    const int i = ps * G::RPP + lrow, at = i * G::LD + dual_col<T>(i, ch * G::PE);
+                *(intx4*)(sQ + at) = qr[ps];
+                *(intx4*)(sD + at) = dr[ps];
             }
-            F pf[KT], sf[KT];
+            if (tid < 128) stat[tid >> 6][tid & 63] = st;
+            __syncthreads();
+            if (t + 1 < nt)
+                load(hg, t + 1);
+            else if (hg + 1 < grp)
+                load(hg + 1, 0);
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
+            for (int hf = 0; hf < 2; ++hf) {
+                const int q0 = n0 + 64 * (tb + t) + 32 * hf, q1 = q0 + 31;
+                if (q0 >= len || k0 > q1 || (k0 >= a.S && q0 - kend >= a.W)) continue;
+                floatx4 s[KT][2], dp[KT][2];
 #pragma unroll
                 for (int qt = 0; qt < 2; ++qt) {
-                    const floatx4 lse2 = ld4f(stat[0] + 32 * kb2 + 16 * qt + 4 * g);
-                    const floatx4 delta = ld4f(stat[1] + 32 * kb2 + 16 * qt + 4 * g);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float p = exp2_fast(__builtin_fmaf(s[kt][qt][e], sc, -lse2[e]));
-                        if (!whole) {
-                            const int q = q0 + 32 * kb2 + 16 * qt + 4 * g + e, j = k0 + 16 * kt + r;
-                            p = (q < len) & (j <= q) & ((q - j < a.W) | (j < a.S)) ? p : 0.f;
+                    for (int kt = 0; kt < KT; ++kt) s[kt][qt] = dp[kt][qt] = zero4();
+#pragma unroll
+                    for (int kb = 0; kb < D / 32; ++kb) {
+                        const F qf = ld_nat_dual(sQ, G::LD, 32 * hf + 16 * qt, kb, g, r);
+                        const F df = ld_nat_dual(sD, G::LD, 32 * hf + 16 * qt, kb, g, r);
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt) {
+                            s[kt][qt] = mma(qf, kf[kt][kb], s[kt][qt]);
+                            dp[kt][qt] = mma(df, vf[kt][kb], dp[kt][qt]);
                         }
-                        s[kt][qt][e] = p;
-                        dp[kt][qt][e] = p * (dp[kt][qt][e] - delta[e]);
                     }
                 }
-                pf[kt] = frag_from_acc<T>(s[kt][0], s[kt][1]);
-                sf[kt] = frag_from_acc<T>(dp[kt][0], dp[kt][1]);
-            }
 #pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) {
-                const F df = ld_red_dual(sD, G::LD, 16 * dt, kb2, g, r), qf = ld_red_dual(sQ, G::LD, 16 * dt, kb2, g, r);
+                for (int qt = 0; qt < 2; ++qt) {
+                    const floatx4 lse2 = ld4f(stat[0] + 32 * hf + 16 * qt + 4 * g);
+                    const floatx4 delta = ld4f(stat[1] + 32 * hf + 16 * qt + 4 * g);
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            s[kt][qt][e] = exp2_fast(__builtin_fmaf(s[kt][qt][e], sc, -lse2[e]));
+                            dp[kt][qt][e] = s[kt][qt][e] * (dp[kt][qt][e] - delta[e]);
+                        }
+                }
+                if (kend > q0 || q1 >= len || (q1 - k0 >= a.W && kend >= a.S)) {  // some pair is not visible
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt) {
+                        const int q = q0 + 4 * g - (k0 + 16 * kt + r);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const bool seen = (unsigned)(q + 16 * (e >> 2) + (e & 3)) < span[kt];
+                            s[kt][e >> 2][e & 3] = seen ? s[kt][e >> 2][e & 3] : 0.f;
+                            dp[kt][e >> 2][e & 3] = seen ? dp[kt][e >> 2][e & 3] : 0.f;
+                        }
+                    }
+                }
+                F pf[KT], sf[KT];
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
-                    dv[kt][dt] = mma(df, pf[kt], dv[kt][dt]);
-                    dk[kt][dt] = mma(qf, sf[kt], dk[kt][dt]);
+                    pf[kt] = frag_from_acc<T>(s[kt][0], s[kt][1]);
+                    sf[kt] = frag_from_acc<T>(dp[kt][0], dp[kt][1]);
+                }
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) {
+                    const F df = ld_red_dual(sD, G::LD, 16 * dt, hf, g, r), qf = ld_red_dual(sQ, G::LD, 16 * dt, hf, g, r);
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt) {
+                        dv[kt][dt] = mma(df, pf[kt], dv[kt][dt]);
+                        dk[kt][dt] = mma(qf, sf[kt], dk[kt][dt]);
+                    }
                 }
             }
         }
-    }
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
         const int key = k0 + 16 * kt + r;
         if (sink) {
-            float* to = a.part + ((((size_t)part * a.B + b) * a.Hkv + hk) * a.nsb * G::NK + key) * 2 * D;
+            float* to = a.part + ((((size_t)part * a.B + b) * a.Hkv + hk) * a.nsb * G::NB + key) * 2 * D;
 #pragma unroll
             for (int dt = 0; dt < D / 16; ++dt) {
                 st4f(to + 16 * dt + 4 * g, dk[kt][dt]);
@@ -330,9 +354,9 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
 }
 
 // dk and dv of the keys of the blocks with sinks: the parts, added in order.
-template <typename T, int D> __global__ void __launch_bounds__(256) window_bwd_sum_kernel(WindowBwdArgs a)
+template <typename T, int D> __global__ void __launch_bounds__(256) window_bwd_sum_kernel(WindowBwdArgs a, int block)
 {
-    const int keys = a.nsb * BwdGeo<T, D>::NK;
+    const int keys = a.nsb * block;
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     const int c = 4 * (int)(i % (2 * D / 4));
     const long long row = i / (2 * D / 4);  // (b, hk, key)
@@ -350,19 +374,19 @@ template <typename T, int D> __global__ void __launch_bounds__(256) window_bwd_s
 
 template <typename T, int D> hipError_t backward_d(const WindowBwdArgs& a, hipStream_t s)
 {
-    hipLaunchKernelGGL((window_bwd_q_kernel<T, D>), dim3((unsigned)(8 * a.q_per)), dim3(256), 0, s, a);
-    hipLaunchKernelGGL((window_bwd_k_kernel<T, D>), dim3((unsigned)(8 * a.k_per)), dim3(256), 0, s, a);
+    typedef BwdGeo<T, D> G;
+    hipLaunchKernelGGL((window_bwd_q_kernel<T, D>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
+    hipLaunchKernelGGL((window_bwd_k_kernel<T, D>), dim3((unsigned)(8 * a.k_per)), dim3(G::NT), 0, s, a);
     if (a.nsb > 0) {
-        const long long n = (long long)a.B * a.Hkv * a.nsb * BwdGeo<T, D>::NK * (2 * D / 4);
-        hipLaunchKernelGGL((window_bwd_sum_kernel<T, D>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
+        const long long n = (long long)a.B * a.Hkv * a.nsb * G::NB * (2 * D / 4);
+        hipLaunchKernelGGL((window_bwd_sum_kernel<T, D>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a, G::NB);
     }
     return hipGetLastError();
 }
 
 }  // namespace
 
-int window_bwd_keys(int, int D) { return D == 128 ? BwdGeo<bf16, 128>::NK : BwdGeo<bf16, 64>::NK; }
-int window_bwd_queries(int, int D) { return D == 128 ? BwdGeo<bf16, 128>::BQ : BwdGeo<bf16, 64>::BQ; }
+int window_bwd_block(int D) { return D == 128 ? BwdGeo<bf16, 128>::NB : BwdGeo<bf16, 64>::NB; }
 
 hipError_t launch_window_backward(int bf16_io, int D, const WindowBwdArgs& a, hipStream_t s)
 {
