@@ -447,51 +447,68 @@ def layer_forward(x, w_qkv, w_o, T, H: int, M: int, S: int, t0: int = 0, scale: 
 
 
 # ---- window attention, the short convolution and the selective scan ----
+#
+# A decode step of these runs for a few microseconds on the device as well, so what depends on shapes alone (the
+# parameter block, whether the shape is supported, the workspace's size) is kept per shape.
 
 def _check_on(t, shape, dtype, name, dev):
-    """_check, and that the tensor lies on the call's device."""
-    _check(t, shape, dtype, name)
-    if t.device != dev:
-        raise ValueError(f"{name}: expected a tensor on {dev}, got {t.device}")
+    """A contiguous tensor of this shape and type on GPU number dev."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or dev < 0 or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{max(dev, 0)}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _io(t, name):
-    if t.dtype == torch.bfloat16:
+def _io(dtype, name):
+    if dtype is torch.bfloat16:
         return BLA_BF16
-    if t.dtype == torch.float32:
+    if dtype is torch.float32:
         return BLA_F32
-    raise ValueError(f"{name}: expected torch.float32 or torch.bfloat16, got {t.dtype}")
+    raise ValueError(f"{name}: expected torch.float32 or torch.bfloat16, got {dtype}")
 
 
 def _call(fn, what, dev, *args):
     """The library's call on the tensors' device (which need not be the current one) and its current stream."""
-    if dev.index != torch.cuda.current_device():
+    stream = torch._C._cuda_getCurrentRawStream(dev)
+    if dev != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
-            st = fn(*args, _stream(dev))
+            st = fn(*args, stream)
     else:
-        st = fn(*args, _stream(dev))
+        st = fn(*args, stream)
     if st != 0:
         raise BlaError(st, what)
 
 
-def _room(workspace, need, dev):
-    """The caller's workspace where it is large enough (a uint8 tensor on the call's device), else a fresh one."""
+def _result(out, like, shape, name="out"):
+    """A fresh tensor like `like`, or the caller's after the checks of an input."""
+    if out is None:
+        return torch.empty_like(like)
+    _check_on(out, shape, like.dtype, name, like.get_device())
+    return out
+
+
+def _room(workspace, need, like):
+    """The caller's workspace where it is large enough (a uint8 tensor on the call's device), a fresh one otherwise, or
+    None where none is needed: (tensor, address, bytes)."""
+    if need == 0:
+        return None, None, 0
     if workspace is not None and workspace.numel() >= need:
-        _check_on(workspace, workspace.shape, torch.uint8, "workspace", dev)
-        return workspace
-    return torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+        _check_on(workspace, workspace.shape, torch.uint8, "workspace", like.get_device())
+    else:
+        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+    return workspace, workspace.data_ptr(), workspace.numel()
 
 
-def _window_params(q, k, window, sinks, t0, scale):
-    B, H, d = q.shape[0], q.shape[1], q.shape[-1]
-    L = q.shape[2] if q.dim() == 4 else 1
-    return WindowParams(B, H, k.shape[1] if k.dim() == q.dim() else 0, L, d, int(window), int(sinks), _io(q, "q"),
-                        int(t0), 0.0 if scale is None else float(scale))
-
-
-def _window_check(st, what):
+def _shape_status(st, what):
     if st != 0:
         raise BlaError(st, f"{what} (shape check)")
+
+
+@functools.lru_cache(maxsize=256)
+def _window_plan(size, what, B, H, Hkv, L, d, window, sinks, t0, scale, dtype):
+    """(parameters by reference, workspace bytes by the library function `size`)."""
+    p = ctypes.byref(WindowParams(B, H, Hkv, L, d, window, sinks, _io(dtype, "q"), t0, scale))
+    _shape_status(lib().bla_window_supported(p), what)
+    return p, getattr(lib(), size)(p)
 
 
 def window_forward(q, k, v, window: int, sinks: int = 0, t0: int = 0, scale: float | None = None, lengths=None, pos=None,
@@ -505,29 +522,29 @@ def window_forward(q, k, v, window: int, sinks: int = 0, t0: int = 0, scale: flo
     lse is float32 [B,H,L] (None unless want_lse), the rings are those after the call (None unless want_cache).
     """
     B, H, L, d = q.shape
-    Hkv, dt, dev = k.shape[1], q.dtype, q.device
-    p = _window_params(q, k, window, sinks, t0, scale)
+    Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
+    p, need = _window_plan("bla_window_workspace_size", "bla_window_forward", B, H, Hkv, L, d, int(window), int(sinks),
+                           int(t0), 0.0 if scale is None else float(scale), dt)
     _check_on(q, (B, H, L, d), dt, "q", dev)
     _check_on(k, (B, Hkv, L, d), dt, "k", dev)
     _check_on(v, (B, Hkv, L, d), dt, "v", dev)
-    ring = (B, Hkv, int(sinks) + int(window), d)
+    ring = (B, Hkv, sinks + window, d)
     if (cache_k is None) != (cache_v is None):
         raise ValueError("cache_k and cache_v: both or neither")
-    for name, t in (("cache_k", cache_k), ("cache_v", cache_v)):
-        if t is not None:
-            _check_on(t, ring, dt, name, dev)
+    if cache_k is not None:
+        _check_on(cache_k, ring, dt, "cache_k", dev)
+        _check_on(cache_v, ring, dt, "cache_v", dev)
     if lengths is not None:
         _check_on(lengths, (B,), torch.int32, "lengths", dev)
     if pos is not None:
         _check_on(pos, (B,), torch.int64, "pos", dev)
-    _window_check(lib().bla_window_supported(ctypes.byref(p)), "bla_window_forward")
-    o = _out(out, q, (B, H, L, d))
-    lse = torch.empty((B, H, L), dtype=torch.float32, device=dev) if want_lse else None
-    ck = torch.empty(ring, dtype=dt, device=dev) if want_cache else None
-    cv = torch.empty(ring, dtype=dt, device=dev) if want_cache else None
-    ws = _room(workspace, lib().bla_window_workspace_size(ctypes.byref(p)), dev)
-    _call(lib().bla_window_forward, "bla_window_forward", dev, ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(lengths),
-          _ptr(pos), _ptr(cache_k), _ptr(cache_v), _ptr(o), _ptr(lse), _ptr(ck), _ptr(cv), _ptr(ws), ws.numel())
+    o = _result(out, q, (B, H, L, d))
+    lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device) if want_lse else None
+    ck = torch.empty(ring, dtype=dt, device=q.device) if want_cache else None
+    cv = torch.empty(ring, dtype=dt, device=q.device) if want_cache else None
+    keep, ws, n = _room(workspace, need, q)
+    _call(lib().bla_window_forward, "bla_window_forward", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths),
+          _ptr(pos), _ptr(cache_k), _ptr(cache_v), o.data_ptr(), _ptr(lse), _ptr(ck), _ptr(cv), ws, n)
     return o, lse, ck, cv
 
 
@@ -536,21 +553,21 @@ def window_step(q, k, v, window: int, sinks: int, cache_k, cache_v, pos=None, t0
     """bla_window_step: one decode token per row, q [B,H,d], k and v [B,H_kv,d]; the rings cache_k / cache_v
     [B,H_kv,sinks+window,d] take its key and value in place.  A row with a negative pos is idle (zeros)."""
     B, H, d = q.shape
-    Hkv, dt, dev = k.shape[1], q.dtype, q.device
-    p = _window_params(q, k, window, sinks, t0, scale)
+    Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
+    p, need = _window_plan("bla_window_step_workspace_size", "bla_window_step", B, H, Hkv, 1, d, int(window), int(sinks),
+                           int(t0), 0.0 if scale is None else float(scale), dt)
     _check_on(q, (B, H, d), dt, "q", dev)
     _check_on(k, (B, Hkv, d), dt, "k", dev)
     _check_on(v, (B, Hkv, d), dt, "v", dev)
-    ring = (B, Hkv, int(sinks) + int(window), d)
+    ring = (B, Hkv, sinks + window, d)
     _check_on(cache_k, ring, dt, "cache_k", dev)
     _check_on(cache_v, ring, dt, "cache_v", dev)
     if pos is not None:
         _check_on(pos, (B,), torch.int64, "pos", dev)
-    _window_check(lib().bla_window_supported(ctypes.byref(p)), "bla_window_step")
-    o = _out(out, q, (B, H, d))
-    ws = _room(workspace, lib().bla_window_step_workspace_size(ctypes.byref(p)), dev)
-    _call(lib().bla_window_step, "bla_window_step", dev, ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(pos),
-          _ptr(cache_k), _ptr(cache_v), _ptr(o), _ptr(ws), ws.numel())
+    o = _result(out, q, (B, H, d))
+    keep, ws, n = _room(workspace, need, q)
+    _call(lib().bla_window_step, "bla_window_step", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(pos),
+          cache_k.data_ptr(), cache_v.data_ptr(), o.data_ptr(), ws, n)
     return o
 
 
@@ -558,35 +575,40 @@ def window_backward(q, k, v, o, lse, dO, window: int, sinks: int = 0, scale: flo
                     workspace=None):
     """bla_window_backward: (dq, dk, dv) of window_forward without rings from its outputs o and lse and dO = dLoss/dO."""
     B, H, L, d = q.shape
-    Hkv, dt, dev = k.shape[1], q.dtype, q.device
-    p = _window_params(q, k, window, sinks, 0, scale)
+    Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
+    p, need = _window_plan("bla_window_backward_workspace_size", "bla_window_backward", B, H, Hkv, L, d, int(window),
+                           int(sinks), 0, 0.0 if scale is None else float(scale), dt)
     for name, t, h in (("q", q, H), ("k", k, Hkv), ("v", v, Hkv), ("o", o, H), ("dO", dO, H)):
         _check_on(t, (B, h, L, d), dt, name, dev)
     _check_on(lse, (B, H, L), torch.float32, "lse", dev)
     if lengths is not None:
         _check_on(lengths, (B,), torch.int32, "lengths", dev)
-    _window_check(lib().bla_window_supported(ctypes.byref(p)), "bla_window_backward")
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
-    ws = _room(workspace, lib().bla_window_backward_workspace_size(ctypes.byref(p)), dev)
-    _call(lib().bla_window_backward, "bla_window_backward", dev, ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(o),
-          _ptr(lse), _ptr(dO), _ptr(lengths), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws.numel())
+    keep, ws, n = _room(workspace, need, q)
+    _call(lib().bla_window_backward, "bla_window_backward", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+          lse.data_ptr(), dO.data_ptr(), _ptr(lengths), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws, n)
     return dq, dk, dv
 
 
+@functools.lru_cache(maxsize=256)
+def _conv_plan(what, B, H, L, d, K, silu, dtype):
+    p = ctypes.byref(ConvParams(B, H, L, d, K, silu, _io(dtype, "x")))
+    _shape_status(lib().bla_conv_supported(p), what)
+    return p, lib().bla_conv_backward_workspace_size(p)
+
+
 def _conv_check(x, w, bias, silu, what):
-    """The checks that the convolution's calls share; returns its parameters."""
-    H, d = x.shape[1], x.shape[-1]
+    """The checks that the convolution's calls share: (parameters, bytes of the backward's workspace, taps)."""
+    H, d, dev = x.shape[1], x.shape[-1], x.get_device()
     if w.dim() != 3:
         raise ValueError(f"w: expected [H, d, taps], got {tuple(w.shape)}")
-    K, dev = w.shape[2], x.device
-    p = ConvParams(x.shape[0], H, x.shape[2] if x.dim() == 4 else 1, d, K, int(silu), _io(x, "x"))
+    K = w.shape[2]
+    p, need = _conv_plan(what, x.shape[0], H, x.shape[2] if x.dim() == 4 else 1, d, K, int(silu), x.dtype)
+    _check_on(x, x.shape, x.dtype, "x", dev)
     _check_on(w, (H, d, K), torch.float32, "w", dev)
     if bias is not None:
         _check_on(bias, (H, d), torch.float32, "bias", dev)
-    st = lib().bla_conv_supported(ctypes.byref(p))
-    if st != 0:
-        raise BlaError(st, f"{what} (shape check)")
-    return p, K
+    return p, need, K
 
 
 def conv_forward(x, w, bias=None, silu: bool = True, state=None, lengths=None, want_state: bool = True, out=None):
@@ -594,17 +616,16 @@ def conv_forward(x, w, bias=None, silu: bool = True, state=None, lengths=None, w
     bias [H,d] (float32), then SiLU if silu.  state [B,H,taps-1,d] float32: the tokens before the call (None = zeros).
     lengths (int32 [B]): tokens of each row.  Returns (y, state after the call or None)."""
     B, H, L, d = x.shape
-    dev = x.device
-    _check_on(x, (B, H, L, d), x.dtype, "x", dev)
-    p, K = _conv_check(x, w, bias, silu, "bla_conv_forward")
+    dev = x.get_device()
+    p, _, K = _conv_check(x, w, bias, silu, "bla_conv_forward")
     if state is not None:
         _check_on(state, (B, H, K - 1, d), torch.float32, "state", dev)
     if lengths is not None:
         _check_on(lengths, (B,), torch.int32, "lengths", dev)
-    y = _out(out, x, (B, H, L, d))
-    so = torch.empty((B, H, K - 1, d), dtype=torch.float32, device=dev) if want_state else None
-    _call(lib().bla_conv_forward, "bla_conv_forward", dev, ctypes.byref(p), _ptr(x), _ptr(w), _ptr(bias), _ptr(lengths),
-          _ptr(state), _ptr(y), _ptr(so))
+    y = _result(out, x, (B, H, L, d))
+    so = torch.empty((B, H, K - 1, d), dtype=torch.float32, device=x.device) if want_state else None
+    _call(lib().bla_conv_forward, "bla_conv_forward", dev, p, x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(lengths),
+          _ptr(state), y.data_ptr(), _ptr(so))
     return y, so
 
 
@@ -612,15 +633,16 @@ def conv_step(x, w, state, bias=None, silu: bool = True, state_out=None, out=Non
     """bla_conv_step: one token per row, x [B,H,d].  The state [B,H,taps-1,d] is updated in place, or left alone where
     state_out receives it."""
     B, H, d = x.shape
-    dev = x.device
-    _check_on(x, (B, H, d), x.dtype, "x", dev)
-    p, K = _conv_check(x, w, bias, silu, "bla_conv_step")
-    state_out = state if state_out is None else state_out
+    dev = x.get_device()
+    p, _, K = _conv_check(x, w, bias, silu, "bla_conv_step")
     _check_on(state, (B, H, K - 1, d), torch.float32, "state", dev)
-    _check_on(state_out, (B, H, K - 1, d), torch.float32, "state_out", dev)
-    y = _out(out, x, (B, H, d))
-    _call(lib().bla_conv_step, "bla_conv_step", dev, ctypes.byref(p), _ptr(x), _ptr(w), _ptr(bias), _ptr(state), _ptr(y),
-          _ptr(state_out))
+    if state_out is None:
+        state_out = state
+    else:
+        _check_on(state_out, (B, H, K - 1, d), torch.float32, "state_out", dev)
+    y = _result(out, x, (B, H, d))
+    _call(lib().bla_conv_step, "bla_conv_step", dev, p, x.data_ptr(), w.data_ptr(), _ptr(bias), state.data_ptr(),
+          y.data_ptr(), state_out.data_ptr())
     return y
 
 
@@ -630,42 +652,46 @@ def conv_backward(x, w, dy, bias=None, silu: bool = True, state=None, dstate=Non
     zero).  Returns (dx, dw, dbias, dLoss/d(state before the call) or None); dbias is that of a zero bias where bias is
     None."""
     B, H, L, d = x.shape
-    dev = x.device
-    _check_on(x, (B, H, L, d), x.dtype, "x", dev)
+    dev = x.get_device()
+    p, need, K = _conv_check(x, w, bias, silu, "bla_conv_backward")
     _check_on(dy, (B, H, L, d), x.dtype, "dy", dev)
-    p, K = _conv_check(x, w, bias, silu, "bla_conv_backward")
     for name, t in (("state", state), ("dstate", dstate)):
         if t is not None:
             _check_on(t, (B, H, K - 1, d), torch.float32, name, dev)
     if lengths is not None:
         _check_on(lengths, (B,), torch.int32, "lengths", dev)
     dx, dw = torch.empty_like(x), torch.empty_like(w)
-    db = torch.empty((H, d), dtype=torch.float32, device=dev)
-    ds = torch.empty((B, H, K - 1, d), dtype=torch.float32, device=dev) if want_state_grad else None
-    ws = _room(workspace, lib().bla_conv_backward_workspace_size(ctypes.byref(p)), dev)
-    _call(lib().bla_conv_backward, "bla_conv_backward", dev, ctypes.byref(p), _ptr(x), _ptr(w), _ptr(bias), _ptr(dy),
-          _ptr(lengths), _ptr(state), _ptr(dstate), _ptr(dx), _ptr(dw), _ptr(db), _ptr(ds), _ptr(ws), ws.numel())
+    db = torch.empty((H, d), dtype=torch.float32, device=x.device)
+    ds = torch.empty((B, H, K - 1, d), dtype=torch.float32, device=x.device) if want_state_grad else None
+    keep, ws, n = _room(workspace, need, x)
+    _call(lib().bla_conv_backward, "bla_conv_backward", dev, p, x.data_ptr(), w.data_ptr(), _ptr(bias), dy.data_ptr(),
+          _ptr(lengths), _ptr(state), _ptr(dstate), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), _ptr(ds), ws, n)
     return dx, dw, db, ds
 
 
-def _ssm_check(x, dt, A, Bm, Cm, D, what):
-    """The checks that the scan's calls share; returns its parameters and the shape of a state."""
+@functools.lru_cache(maxsize=256)
+def _ssm_plan(size, what, B, H, G, L, d, N, dtype):
+    p = ctypes.byref(SsmParams(B, H, G, L, d, N, _io(dtype, "x")))
+    _shape_status(lib().bla_ssm_supported(p), what)
+    return p, getattr(lib(), size)(p) if size else 0
+
+
+def _ssm_check(x, dt, A, Bm, Cm, D, size, what):
+    """The checks that the scan's calls share: (parameters, workspace bytes, shape of a state)."""
     tok = x.shape[2:-1]
-    B, H, d = x.shape[0], x.shape[1], x.shape[-1]
+    B, H, d, io, dev = x.shape[0], x.shape[1], x.shape[-1], x.dtype, x.get_device()
     if Bm.dim() != x.dim():
         raise ValueError(f"Bm: expected {x.dim()} dimensions, got {tuple(Bm.shape)}")
-    G, N, dev = Bm.shape[1], Bm.shape[-1], x.device
-    p = SsmParams(B, H, G, tok[0] if tok else 1, d, N, _io(x, "x"))
-    _check_on(Bm, (B, G, *tok, N), x.dtype, "Bm", dev)
-    _check_on(Cm, (B, G, *tok, N), x.dtype, "Cm", dev)
+    G, N = Bm.shape[1], Bm.shape[-1]
+    p, need = _ssm_plan(size, what, B, H, G, tok[0] if tok else 1, d, N, io)
+    _check_on(x, x.shape, io, "x", dev)
+    _check_on(Bm, (B, G, *tok, N), io, "Bm", dev)
+    _check_on(Cm, (B, G, *tok, N), io, "Cm", dev)
     _check_on(dt, (B, H, *tok), torch.float32, "dt", dev)
     _check_on(A, (H,), torch.float32, "A", dev)
     if D is not None:
         _check_on(D, (H,), torch.float32, "D", dev)
-    st = lib().bla_ssm_supported(ctypes.byref(p))
-    if st != 0:
-        raise BlaError(st, f"{what} (shape check)")
-    return p, (B, H, N, d)
+    return p, need, (B, H, N, d)
 
 
 def ssm_forward(x, dt, A, Bm, Cm, D=None, state=None, lengths=None, want_state: bool = True, workspace=None, out=None):
@@ -675,18 +701,17 @@ def ssm_forward(x, dt, A, Bm, Cm, D=None, state=None, lengths=None, want_state: 
     [B,H,N,d] float32 before the call (None = zero), lengths (int32 [B]): tokens of each row.  Returns (y, state after
     the call or None)."""
     B, H, L, d = x.shape
-    dev = x.device
-    _check_on(x, (B, H, L, d), x.dtype, "x", dev)
-    p, shape = _ssm_check(x, dt, A, Bm, Cm, D, "bla_ssm_forward")
+    dev = x.get_device()
+    p, need, shape = _ssm_check(x, dt, A, Bm, Cm, D, "bla_ssm_workspace_size", "bla_ssm_forward")
     if state is not None:
         _check_on(state, shape, torch.float32, "state", dev)
     if lengths is not None:
         _check_on(lengths, (B,), torch.int32, "lengths", dev)
-    y = _out(out, x, (B, H, L, d))
-    so = torch.empty(shape, dtype=torch.float32, device=dev) if want_state else None
-    ws = _room(workspace, lib().bla_ssm_workspace_size(ctypes.byref(p)), dev)
-    _call(lib().bla_ssm_forward, "bla_ssm_forward", dev, ctypes.byref(p), _ptr(x), _ptr(dt), _ptr(A), _ptr(Bm), _ptr(Cm),
-          _ptr(D), _ptr(lengths), _ptr(state), _ptr(y), _ptr(so), _ptr(ws), ws.numel())
+    y = _result(out, x, (B, H, L, d))
+    so = torch.empty(shape, dtype=torch.float32, device=x.device) if want_state else None
+    keep, ws, n = _room(workspace, need, x)
+    _call(lib().bla_ssm_forward, "bla_ssm_forward", dev, p, x.data_ptr(), dt.data_ptr(), A.data_ptr(), Bm.data_ptr(),
+          Cm.data_ptr(), _ptr(D), _ptr(lengths), _ptr(state), y.data_ptr(), _ptr(so), ws, n)
     return y, so
 
 
@@ -694,15 +719,16 @@ def ssm_step(x, dt, A, Bm, Cm, state, D=None, state_out=None, out=None):
     """bla_ssm_step: one token per row, x [B,H,d], dt [B,H], Bm and Cm [B,G,N].  The state [B,H,N,d] is updated in place, or
     left alone where state_out receives it."""
     B, H, d = x.shape
-    dev = x.device
-    _check_on(x, (B, H, d), x.dtype, "x", dev)
-    p, shape = _ssm_check(x, dt, A, Bm, Cm, D, "bla_ssm_step")
-    state_out = state if state_out is None else state_out
+    dev = x.get_device()
+    p, _, shape = _ssm_check(x, dt, A, Bm, Cm, D, None, "bla_ssm_step")
     _check_on(state, shape, torch.float32, "state", dev)
-    _check_on(state_out, shape, torch.float32, "state_out", dev)
-    y = _out(out, x, (B, H, d))
-    _call(lib().bla_ssm_step, "bla_ssm_step", dev, ctypes.byref(p), _ptr(x), _ptr(dt), _ptr(A), _ptr(Bm), _ptr(Cm), _ptr(D),
-          _ptr(state), _ptr(y), _ptr(state_out))
+    if state_out is None:
+        state_out = state
+    else:
+        _check_on(state_out, shape, torch.float32, "state_out", dev)
+    y = _result(out, x, (B, H, d))
+    _call(lib().bla_ssm_step, "bla_ssm_step", dev, p, x.data_ptr(), dt.data_ptr(), A.data_ptr(), Bm.data_ptr(),
+          Cm.data_ptr(), _ptr(D), state.data_ptr(), y.data_ptr(), state_out.data_ptr())
     return y
 
 
@@ -712,10 +738,9 @@ def ssm_backward(x, dt, A, Bm, Cm, dy, D=None, state=None, dstate=None, lengths=
     zero).  Returns (dx, ddt, dA, dBm, dCm, dD, dLoss/d(state before the call) or None); dD is that of a zero D where D is
     None."""
     B, H, L, d = x.shape
-    dev = x.device
-    _check_on(x, (B, H, L, d), x.dtype, "x", dev)
+    dev = x.get_device()
+    p, need, shape = _ssm_check(x, dt, A, Bm, Cm, D, "bla_ssm_backward_workspace_size", "bla_ssm_backward")
     _check_on(dy, (B, H, L, d), x.dtype, "dy", dev)
-    p, shape = _ssm_check(x, dt, A, Bm, Cm, D, "bla_ssm_backward")
     for name, t in (("state", state), ("dstate", dstate)):
         if t is not None:
             _check_on(t, shape, torch.float32, name, dev)
@@ -723,9 +748,9 @@ def ssm_backward(x, dt, A, Bm, Cm, dy, D=None, state=None, dstate=None, lengths=
         _check_on(lengths, (B,), torch.int32, "lengths", dev)
     dx, ddt, dA = torch.empty_like(x), torch.empty_like(dt), torch.empty_like(A)
     dB, dC, dD = torch.empty_like(Bm), torch.empty_like(Cm), torch.empty_like(A)
-    ds = torch.empty(shape, dtype=torch.float32, device=dev) if want_state_grad else None
-    ws = _room(workspace, lib().bla_ssm_backward_workspace_size(ctypes.byref(p)), dev)
-    _call(lib().bla_ssm_backward, "bla_ssm_backward", dev, ctypes.byref(p), _ptr(x), _ptr(dt), _ptr(A), _ptr(Bm), _ptr(Cm),
-          _ptr(D), _ptr(dy), _ptr(lengths), _ptr(state), _ptr(dstate), _ptr(dx), _ptr(ddt), _ptr(dA), _ptr(dB), _ptr(dC),
-          _ptr(dD), _ptr(ds), _ptr(ws), ws.numel())
+    ds = torch.empty(shape, dtype=torch.float32, device=x.device) if want_state_grad else None
+    keep, ws, n = _room(workspace, need, x)
+    _call(lib().bla_ssm_backward, "bla_ssm_backward", dev, p, x.data_ptr(), dt.data_ptr(), A.data_ptr(), Bm.data_ptr(),
+          Cm.data_ptr(), _ptr(D), dy.data_ptr(), _ptr(lengths), _ptr(state), _ptr(dstate), dx.data_ptr(), ddt.data_ptr(),
+          dA.data_ptr(), dB.data_ptr(), dC.data_ptr(), dD.data_ptr(), _ptr(ds), ws, n)
     return dx, ddt, dA, dB, dC, dD, ds
