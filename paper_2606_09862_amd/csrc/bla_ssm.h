@@ -51,17 +51,20 @@ struct SsmBwdArgs {
     long long walk_units, walk_per, units, per;
 };
 
-// Eight products of a float32 weight and an operand value, as an operand of a contraction whose float32 results keep the weight's
-// precision: in bf16 as a sum of two roundings (2^-17 relative; two products), in float32 as it is.
+// Eight products of a float32 weight and an operand value, as an operand of a contraction whose float32 results keep float32's
+// precision: in bf16 as a sum of three roundings (2^-26 relative at most; two would leave 2^-17, which the results of a long sum show), in
+// float32 as it is.
 template <typename T> struct Split;
 template <> struct Split<bf16> {
-    bf16x8 hi, lo;
+    bf16x8 hi, mid, lo;
     __device__ __forceinline__ void set(floatx8 v)
     {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             hi[e] = (bf16)v[e];
-            lo[e] = (bf16)(v[e] - (float)hi[e]);
+            const float x = v[e] - (float)hi[e];
+            mid[e] = (bf16)x;
+            lo[e] = (bf16)(x - (float)mid[e]);
         }
     }
 };
@@ -69,7 +72,10 @@ template <> struct Split<float> {
     floatx8 hi;
     __device__ __forceinline__ void set(floatx8 v) { hi = v; }
 };
-__device__ __forceinline__ floatx4 mma_split(bf16x8 a, const Split<bf16>& b, floatx4 c) { return mma(a, b.hi, mma(a, b.lo, c)); }
+__device__ __forceinline__ floatx4 mma_split(bf16x8 a, const Split<bf16>& b, floatx4 c)
+{
+    return mma(a, b.hi, mma(a, b.mid, mma(a, b.lo, c)));
+}
 __device__ __forceinline__ floatx4 mma_split(floatx8 a, const Split<float>& b, floatx4 c) { return mma(a, b.hi, c); }
 __device__ __forceinline__ floatx8 to_f8(bf16x8 x)
 {

@@ -12,7 +12,7 @@
 //   ddt_t = p_t + A da_t,   dA = sum_t dt_t da_t,   dD = sum_t x_t . dy_t.
 // Two walks over the chunks leave h and g of every chunk in the workspace; then the chunks are independent.  ddt, dA, dD and the
 // state's gradient are float32 results and take no operand rounding: their products of bf16 inputs are exact,
-// and h and g enter them as sums of two bf16 (2^-17 relative).  dx, dB, dC take weights in the operand type.
+// and h and g enter them as sums of three bf16 (Split).  dx, dB, dC take weights in the operand type.
 #include "bla_ssm.h"
 
 namespace bla {
@@ -140,7 +140,7 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
     constexpr int TN = NP / 16, TD = D / 16, SH = NP * LD1;
     __shared__ __attribute__((aligned(16))) T s1[64 * LD1];             // x, then dy
     __shared__ __attribute__((aligned(16))) T s2[64 * LD2];             // B, then C
-    __shared__ __attribute__((aligned(16))) T sH[(two ? 2 : 1) * SH];   // h, then g: rounded, and what that leaves
+    __shared__ __attribute__((aligned(16))) T sH[(two ? 3 : 1) * SH];   // h, then g: rounded, what that leaves, and what that leaves
     __shared__ __attribute__((aligned(16))) float sS[64], sSl[64], sDt[64];
     __shared__ float sE[64], sF[64], sDs[64], sP[64], sLate[64], sDot[4], sDD[4];
 
@@ -201,8 +201,9 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
                 T* to = sH + row * LD1 + dual_col<T>(row, k);
                 st4(to, v);
                 if constexpr (two) {
-                    const floatx4 hi = to_f4(cvt4(v, T()));
-                    st4(to + SH, v - hi);
+                    v -= to_f4(cvt4(v, T()));
+                    st4(to + SH, v);
+                    st4(to + 2 * SH, v - to_f4(cvt4(v, T())));
                 }
             }
             return dot;
@@ -212,7 +213,10 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
             floatx4 o = zero4();
 #pragma unroll
             for (int kb = 0; kb < D / 32; ++kb) {
-                if constexpr (two) o = mma(ld_nat_dual(sH + SH, LD1, 16 * nt, kb, g, r), f[kb], o);
+                if constexpr (two) {
+                    o = mma(ld_nat_dual(sH + 2 * SH, LD1, 16 * nt, kb, g, r), f[kb], o);
+                    o = mma(ld_nat_dual(sH + SH, LD1, 16 * nt, kb, g, r), f[kb], o);
+                }
                 o = mma(ld_nat_dual(sH, LD1, 16 * nt, kb, g, r), f[kb], o);
             }
             return o;

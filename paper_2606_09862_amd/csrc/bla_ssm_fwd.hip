@@ -11,8 +11,8 @@ namespace {
 //   G^T = B C^T (rows u, columns t; tiles u <= t only), weighted by e^{s_t - s_u} dt_u: the operand of the second product;
 //   Y^T = h^T C^T scaled by e^{s_t}, plus X^T (weighted G)^T: h is published in LDS in the operand type;
 //   h^T <- e^{s_c} h^T + X^T (w B)^T with w_u = e^{s_c - s_u} dt_u: the transposed fragments of X serve both products.
-// In bf16 the weighted G and the published h are rounded to 2^-9 relative, as y is; the weights of the state's update are kept to 2^-17
-// (Split), since the state is a float32 result and is carried on.
+// In bf16 the weighted G and the published h are rounded to 2^-9 relative, as y is; the weights of the state's update keep float32's
+// precision (Split), since the state is a float32 result and is carried on.
 // SUM: the segment's own state from zero and its decay, for the scan over the segments; no outputs.
 template <typename T, int D, int NP, bool SUM> struct SsmGeo {
     static constexpr int PE = 16 / (int)sizeof(T);
