@@ -72,11 +72,21 @@ template <> struct Split<float> {
     floatx8 hi;
     __device__ __forceinline__ void set(floatx8 v) { hi = v; }
 };
-__device__ __forceinline__ floatx4 mma_split(bf16x8 a, const Split<bf16>& b, floatx4 c)
+// c[i] += a[i] b for N tiles, term by term: consecutive products belong to different tiles and do not wait for each other.
+template <int N> __device__ __forceinline__ void mma_split(const bf16x8 (&a)[N], const Split<bf16>& b, floatx4 (&c)[N])
 {
-    return mma(a, b.hi, mma(a, b.mid, mma(a, b.lo, c)));
+#pragma unroll
+    for (int i = 0; i < N; ++i) c[i] = mma(a[i], b.lo, c[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) c[i] = mma(a[i], b.mid, c[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) c[i] = mma(a[i], b.hi, c[i]);
 }
-__device__ __forceinline__ floatx4 mma_split(floatx8 a, const Split<float>& b, floatx4 c) { return mma(a, b.hi, c); }
+template <int N> __device__ __forceinline__ void mma_split(const floatx8 (&a)[N], const Split<float>& b, floatx4 (&c)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) c[i] = mma(a[i], b.hi, c[i]);
+}
 __device__ __forceinline__ floatx8 to_f8(bf16x8 x)
 {
     floatx8 r;
@@ -102,24 +112,40 @@ __device__ __forceinline__ floatx8 ld_acc_dual(const float* M, int ld, int x0, i
     return ld_frag<float>(M + (x0 + r) * ld, 32 * kb, g);
 }
 
-// e^x of a float64 exponent to float32 precision: the part of x that float32 cannot hold goes in as a factor 1 + x_lo.
-__device__ __forceinline__ float exp_f64(double x)
+constexpr double kLog2e64 = 1.4426950408889634;
+
+// 2^y of a float64 exponent to float32 precision: the part of y that float32 cannot hold goes in as a factor 1 + y_lo ln 2.
+__device__ __forceinline__ float exp2_f64(double y)
 {
-    const double y = x * 1.4426950408889634;
     const float hi = (float)y;
     const float e = exp2_fast(hi);
     return __builtin_fmaf(e, (float)(y - (double)hi) * kLn2, e);
 }
 
-// Inclusive sum over the wave's lanes (lane = token).
-__device__ __forceinline__ double wave_scan(double x, int lane)
+// x of the lane that a data-parallel primitive names, zero where there is none.
+template <int CTRL, int ROWS> __device__ __forceinline__ double dpp_f64(double x)
 {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const double y = __shfl_up(x, off);
-        x += lane >= off ? y : 0.0;
-    }
+    const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), CTRL, ROWS, 0xf, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(x), CTRL, ROWS, 0xf, false);
+    return __hiloint2double(hi, lo);
+}
+
+// Inclusive sum over the wave's lanes (lane = token): within rows of 16 lanes, then the last lanes of rows 0 and 2 into rows 1 and 3, then
+// lane 31 into the upper half.  In registers; through LDS (six exchanges) it took 900 cycles.
+__device__ __forceinline__ double wave_scan(double x, int)
+{
+    x += dpp_f64<0x111, 0xf>(x);  // lane - 1
+    x += dpp_f64<0x112, 0xf>(x);
+    x += dpp_f64<0x114, 0xf>(x);
+    x += dpp_f64<0x118, 0xf>(x);
+    x += dpp_f64<0x142, 0xa>(x);  // lane 15 of the row before, into rows 1 and 3
+    x += dpp_f64<0x143, 0xc>(x);  // lane 31, into rows 2 and 3
     return x;
+}
+// The last lane's value in every lane.
+__device__ __forceinline__ double wave_last(double x)
+{
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), 63), __builtin_amdgcn_readlane(__double2loint(x), 63));
 }
 
 __device__ __forceinline__ int ssm_length(const int32_t* lengths, int b, int L) { return lengths ? min(max(lengths[b], 0), L) : L; }

@@ -18,9 +18,10 @@
 namespace bla {
 namespace {
 
-// States entering the chunks (forward: B, x) or gradients of the states leaving them (BACK: C, dy, chunks in reverse).  The columns d of a
-// state are independent, so a workgroup takes 32 of one head's.  As the state update of ssm_forward_kernel.
-template <typename T, int D, int NP, bool BACK> __global__ void __launch_bounds__(256) ssm_walk_kernel(SsmBwdArgs a)
+// States entering the chunks (from B, x), and in the second half of the grid the gradients of the states leaving them (`back`: from C, dy, chunks in
+// reverse): the two walks are independent, and either alone leaves half of the device idle.  The columns d of a
+// state are independent too, so a workgroup takes 32 of one head's.  As the state update of ssm_forward_kernel.
+template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_walk_kernel(SsmBwdArgs a)
 {
     typedef typename Frag<T>::type F;
     constexpr int DS = 32, PE = 16 / (int)sizeof(T), CHX = DS / PE, CHB = NP / PE;
@@ -31,7 +32,9 @@ template <typename T, int D, int NP, bool BACK> __global__ void __launch_bounds_
     __shared__ __attribute__((aligned(16))) float sW[2][64];
     __shared__ float sTot[2];
 
-    long long u = xcd_unit(blockIdx.x, a.walk_per);
+    const unsigned half = gridDim.x / 2;
+    const bool back = blockIdx.x >= half;
+    long long u = xcd_unit(back ? blockIdx.x - half : blockIdx.x, a.walk_per);
     if (u >= a.walk_units) return;
     const int d0 = (int)(u % (D / DS)) * DS;
     u /= D / DS;
@@ -39,12 +42,12 @@ template <typename T, int D, int NP, bool BACK> __global__ void __launch_bounds_
     const int bh = b * a.H + h, grp = h / (a.H / a.G);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
     const int len = ssm_length(a.lengths, b, a.L);
-    const T* x = (const T*)(BACK ? a.dy : a.x) + (size_t)bh * a.L * D + d0;
-    const T* Bm = (const T*)(BACK ? a.Cm : a.Bm) + ((size_t)b * a.G + grp) * a.L * a.N;
+    const T* x = (const T*)(back ? a.dy : a.x) + (size_t)bh * a.L * D + d0;
+    const T* Bm = (const T*)(back ? a.Cm : a.Bm) + ((size_t)b * a.G + grp) * a.L * a.N;
     const float* dt = a.dt + (size_t)bh * a.L;
-    const double A = a.A[h];
-    float* store = (BACK ? a.leave : a.enter) + (size_t)bh * a.nch * a.N * D + d0;
-    const float* from = BACK ? a.dstate_out : a.state_in;
+    const double A = a.A[h] * kLog2e64;  // exponents in units of 2
+    float* store = (back ? a.leave : a.enter) + (size_t)bh * a.nch * a.N * D + d0;
+    const float* from = back ? a.dstate_out : a.state_in;
 
     floatx4 hs[TNW][TD];
 #pragma unroll
@@ -82,8 +85,8 @@ template <typename T, int D, int NP, bool BACK> __global__ void __launch_bounds_
         if (wave == 0) dtr = lane < n ? dt[64 * c + lane] : 0.f;
     };
     // the last chunk in the order of the walk is needed only for the gradient of the state before the call
-    const int steps = BACK ? a.nch : a.nch - 1;
-    auto chunk = [&](int i) { return BACK ? a.nch - 1 - i : i; };
+    const int steps = back ? a.nch : a.nch - 1;
+    auto chunk = [&](int i) { return back ? a.nch - 1 - i : i; };
     if (steps > 0) load(chunk(0));
     for (int i = 0; i < steps; ++i) {
         const int buf = i & 1;
@@ -98,9 +101,9 @@ template <typename T, int D, int NP, bool BACK> __global__ void __launch_bounds_
             *(intx4*)(sB[buf] + row * LB + dual_col<T>(row, ch * PE)) = br[k];
         }
         if (wave == 0) {
-            const double s = wave_scan((double)dtr * A, lane), tot = __shfl(s, 63);
-            sW[buf][lane] = BACK ? exp_f64(s) : exp_f64(tot - s) * dtr;
-            if (lane == 0) sTot[buf] = exp_f64(tot);
+            const double s = wave_scan((double)dtr * A, lane), tot = wave_last(s);
+            sW[buf][lane] = back ? exp2_f64(s) : exp2_f64(tot - s) * dtr;
+            if (lane == 0) sTot[buf] = exp2_f64(tot);
         }
         __syncthreads();
         if (i + 1 < steps) load(chunk(i + 1));
@@ -115,18 +118,20 @@ template <typename T, int D, int NP, bool BACK> __global__ void __launch_bounds_
         }
         const float tot = sTot[buf];
 #pragma unroll
-        for (int d = 0; d < TD; ++d) {
-            const F xf[2] = {ld_red(sX[buf], LX, 16 * d, 0, g, r), ld_red(sX[buf], LX, 16 * d, 1, g, r)};
+        for (int nt = 0; nt < TNW; ++nt)
 #pragma unroll
-            for (int nt = 0; nt < TNW; ++nt) {
-                hs[nt][d] *= tot;
+            for (int d = 0; d < TD; ++d) hs[nt][d] *= tot;
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) hs[nt][d] = mma_split(xf[kb], wb[nt][kb], hs[nt][d]);
-            }
+        for (int kb = 0; kb < 2; ++kb) {
+            F xf[TD];
+#pragma unroll
+            for (int d = 0; d < TD; ++d) xf[d] = ld_red(sX[buf], LX, 16 * d, kb, g, r);
+#pragma unroll
+            for (int nt = 0; nt < TNW; ++nt) mma_split(xf, wb[nt][kb], hs[nt]);
         }
     }
-    if (!BACK) put(store + (size_t)(a.nch - 1) * a.N * D);
-    if (BACK && a.dstate_in) put(a.dstate_in + (size_t)bh * a.N * D + d0);
+    if (!back) put(store + (size_t)(a.nch - 1) * a.N * D);
+    if (back && a.dstate_in) put(a.dstate_in + (size_t)bh * a.N * D + d0);
 }
 
 // One chunk of a group's heads (or of a part of them).  Wave w owns 16 tokens, first as columns t (dC and the row sums of M), then as columns u
@@ -229,7 +234,7 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
             for (int e = 0; e < 4; ++e) {
                 float df = rows_are_t ? s[e] - st : st - s[e];
                 if (!two) df += rows_are_t ? sl[e] - stl : stl - sl[e];
-                out[e] = exp2_fast(df * kLog2e);
+                out[e] = exp2_fast(df);
             }
         };
 
@@ -239,12 +244,12 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
         stage_state(enter, nullptr);
         if (wave == 0) {
             const float d = lane < n ? a.dt[tok + lane] : 0.f;
-            const double s = wave_scan((double)d * A, lane), tot = __shfl(s, 63);
+            const double s = wave_scan((double)d * A * kLog2e64, lane), tot = wave_last(s);
             sS[lane] = (float)s;
             sSl[lane] = (float)(s - (double)(float)s);
             sDt[lane] = d;
-            sE[lane] = exp_f64(s);
-            sF[lane] = exp_f64(tot - s);
+            sE[lane] = exp2_f64(s);
+            sF[lane] = exp2_f64(tot - s);
         }
         F cf[NP / 32], yf[D / 32];
 #pragma unroll
@@ -364,12 +369,12 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
         if (lane == 0) sDD[wave] = diag;
         __syncthreads();
         if (wave == 0) {
-            const double ds = sDs[lane], below = wave_scan(ds, lane), all = __shfl(below, 63);
-            const double late_all = __shfl(wave_scan((double)sLate[lane], lane), 63);
+            const double ds = sDs[lane], below = wave_scan(ds, lane), all = wave_last(below);
+            const double late_all = wave_last(wave_scan((double)sLate[lane], lane));
             const double end = late_all + (double)sE[63] * ((double)sDot[0] + sDot[1] + sDot[2] + sDot[3]);
             const double da = all - below + ds + end;
             if (64 * c + lane < a.L) a.ddt[tok + lane] = lane < n ? (float)((double)sP[lane] + A * da) : 0.f;
-            const double dA = __shfl(wave_scan((double)sDt[lane] * da, lane), 63);
+            const double dA = wave_last(wave_scan((double)sDt[lane] * da, lane));
             if (lane == 0) {
                 a.part_head[(bh * a.nch + c) * 2] = (float)dA;
                 a.part_head[(bh * a.nch + c) * 2 + 1] = sDD[0] + sDD[1] + sDD[2] + sDD[3];
@@ -441,9 +446,7 @@ __global__ void __launch_bounds__(256) ssm_bwd_head_kernel(SsmBwdArgs a)
 
 template <typename T, int D, int NP> hipError_t backward_n(const SsmBwdArgs& a, hipStream_t s)
 {
-    const dim3 walk((unsigned)(8 * a.walk_per));
-    hipLaunchKernelGGL((ssm_walk_kernel<T, D, NP, false>), walk, dim3(256), 0, s, a);
-    hipLaunchKernelGGL((ssm_walk_kernel<T, D, NP, true>), walk, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((ssm_walk_kernel<T, D, NP>), dim3((unsigned)(16 * a.walk_per)), dim3(256), 0, s, a);
     hipLaunchKernelGGL((ssm_bwd_kernel<T, D, NP>), dim3((unsigned)(8 * a.per)), dim3(256), 0, s, a);
     if (a.hsplit > 1) {
         const size_t n = (size_t)a.B * a.G * a.nch * 2 * 64 * (a.N / 4);

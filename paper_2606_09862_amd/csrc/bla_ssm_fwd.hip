@@ -30,8 +30,8 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
     __shared__ __attribute__((aligned(16))) T sX[64 * G::LX];
     __shared__ __attribute__((aligned(16))) T sB[64 * G::LB];
     __shared__ __attribute__((aligned(16))) T sH[SUM ? 8 : NP * G::LH];
-    __shared__ __attribute__((aligned(16))) float sS[64], sSl[64], sDt[64], sE[64], sW[64];
-    __shared__ float sTot;
+    __shared__ __attribute__((aligned(16))) float sS[2][64], sSl[2][64], sDt[2][64], sE[2][64], sW[2][64];
+    __shared__ float sTot[2];
 
     long long u = xcd_unit(blockIdx.x, a.per);
     if (u >= a.units) return;
@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
     const T* Cm = (const T*)a.Cm + ((size_t)b * a.G + grp) * a.L * a.N;
     T* y = SUM ? nullptr : (T*)a.y + (size_t)bh * a.L * D;
     const float* dt = a.dt + (size_t)bh * a.L;
-    const double A = a.A[h];
+    const double A = a.A[h] * kLog2e64;  // exponents in units of 2
     const float skip = a.Dm ? a.Dm[h] : 0.f;
     const int c0 = seg * a.cps, c1 = min(a.nch, c0 + a.cps);
     const int cend = min(c1, (len + 63) / 64);  // chunks past it are padding
@@ -66,9 +66,22 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
 
     intx4 xr[G::PX], br[G::PB];
     F cf[NP / 32], cn[NP / 32];
-    float dtr = 0.f;
     auto load = [&](int c) {
         const int n = min(64, len - 64 * c);
+        if (n == 64 && a.N == NP) {  // whole tiles lie in one piece: no arithmetic on the lanes
+            const T *xc = x + (size_t)(64 * c) * D, *bc = Bm + (size_t)(64 * c) * NP, *cc = Cm + (size_t)(64 * c) * NP;
+#pragma unroll
+            for (int i = 0; i < G::PX; ++i) xr[i] = *(const intx4*)(xc + (unsigned)((i * 256 + tid) * G::PE));
+#pragma unroll
+            for (int i = 0; i < G::PB; ++i) br[i] = *(const intx4*)(bc + (unsigned)((i * 256 + tid) * G::PE));
+            if (!SUM)
+#pragma unroll
+                for (int kb = 0; kb < NP / 32; ++kb) {
+                    const T* p = cc + (unsigned)((16 * wave + r) * NP + 32 * kb + 4 * g);
+                    cn[kb] = join(ld4<T>(p), ld4<T>(p + 16));
+                }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < G::PX; ++i) {
             const int row = (i * 256 + tid) / G::CHX, ch = (i * 256 + tid) % G::CHX;
@@ -87,12 +100,30 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
             for (int kb = 0; kb < NP / 32; ++kb)
                 cn[kb] = t < n ? ld_acc_row<T>(Cm + (size_t)(64 * c + t) * a.N, kb, g, a.N) : zero_frag<T>();
         }
-        if (wave == 0) dtr = lane < n ? dt[64 * c + lane] : 0.f;
+    };
+    double decay = 0.0;
+    float dtr = 0.f;
+    auto load_dt = [&](int c) { dtr = c < cend && lane < len - 64 * c ? dt[64 * c + lane] : 0.f; };
+    auto exponents = [&](int buf) {  // of the chunk whose dt is loaded
+        const double s = wave_scan((double)dtr * A, lane), tot = wave_last(s);
+        decay += tot;
+        if (!SUM) {
+            sS[buf][lane] = (float)s;
+            sSl[buf][lane] = (float)(s - (double)(float)s);
+            sDt[buf][lane] = dtr;
+            sE[buf][lane] = exp2_f64(s);
+        }
+        sW[buf][lane] = exp2_f64(tot - s) * dtr;
+        if (lane == 0) sTot[buf] = exp2_f64(tot);
     };
 
-    double decay = 0.0;
     if (c0 < cend) load(c0);
-    for (int c = c0; c < cend; ++c) {
+    if (wave == 0) {
+        load_dt(c0);
+        exponents(0);
+        load_dt(c0 + 1);
+    }
+    for (int c = c0, buf = 0; c < cend; ++c, buf ^= 1) {
 #pragma unroll
         for (int i = 0; i < G::PX; ++i) {
             const int row = (i * 256 + tid) / G::CHX, ch = (i * 256 + tid) % G::CHX;
@@ -102,16 +133,6 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
         for (int i = 0; i < G::PB; ++i) {
             const int row = (i * 256 + tid) / G::CHB, ch = (i * 256 + tid) % G::CHB;
             *(intx4*)(sB + row * G::LB + dual_col<T>(row, ch * G::PE)) = br[i];
-        }
-        if (wave == 0) {
-            const double s = wave_scan((double)dtr * A, lane), tot = __shfl(s, 63);
-            decay += tot;
-            sS[lane] = (float)s;
-            sSl[lane] = (float)(s - (double)(float)s);
-            sDt[lane] = dtr;
-            sE[lane] = exp_f64(s);
-            sW[lane] = exp_f64(tot - s) * dtr;
-            if (lane == 0) sTot = exp_f64(tot);
         }
         if (!SUM) {
 #pragma unroll
@@ -128,58 +149,89 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
         F pf[2] = {zero_frag<T>(), zero_frag<T>()};
         if (!SUM) {
             const int t = 16 * wave + r;
-            const float st = sS[t], stl = sSl[t];
-            floatx4 p[4];
+            const float st = sS[buf][t], stl = sSl[buf][t];
 #pragma unroll
-            for (int ut = 0; ut < 4; ++ut) {
-                p[ut] = zero4();
-                if (ut <= wave) {
+            for (int hf = 0; hf < 2; ++hf) {  // 32 tokens u
+                if (hf == 1 && wave < 2) continue;
+                floatx4 p[2] = {zero4(), zero4()};
 #pragma unroll
-                    for (int kb = 0; kb < NP / 32; ++kb) p[ut] = mma(ld_acc_dual(sB, G::LB, 16 * ut, kb, g, r), cf[kb], p[ut]);
-                    const floatx4 su = ld4f(sS + 16 * ut + 4 * g), du = ld4f(sDt + 16 * ut + 4 * g);
+                for (int kb = 0; kb < NP / 32; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        p[i] = mma(ld_acc_dual(sB, G::LB, 32 * hf + 16 * i, kb, g, r), cf[kb], p[i]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int u0 = 32 * hf + 16 * i + 4 * g;
+                    const floatx4 su = ld4f(sS[buf] + u0), du = ld4f(sDt[buf] + u0);
                     floatx4 sl = zero4();
-                    if (sizeof(T) == 4) sl = ld4f(sSl + 16 * ut + 4 * g);
+                    if (sizeof(T) == 4) sl = ld4f(sSl[buf] + u0);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         float df = st - su[e];
                         if (sizeof(T) == 4) df += stl - sl[e];
-                        const float w = exp2_fast(df * kLog2e) * du[e] * p[ut][e];
-                        p[ut][e] = 16 * ut + 4 * g + e <= t ? w : 0.f;
+                        p[i][e] *= exp2_fast(df) * du[e];
                     }
+                    if (2 * hf + i >= wave)  // the tile on the diagonal, or the one past it
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) p[i][e] = u0 + e <= t ? p[i][e] : 0.f;
                 }
+                pf[hf] = frag_from_acc<T>(p[0], p[1]);
             }
-            pf[0] = frag_from_acc<T>(p[0], p[1]);
-            pf[1] = frag_from_acc<T>(p[2], p[3]);
         }
         Split<T> wb[G::TNW][2];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const floatx8 w = join(ld4f(sW + 32 * kb + 4 * g), ld4f(sW + 32 * kb + 16 + 4 * g));
+            const floatx8 w = join(ld4f(sW[buf] + 32 * kb + 4 * g), ld4f(sW[buf] + 32 * kb + 16 + 4 * g));
 #pragma unroll
             for (int nt = 0; nt < G::TNW; ++nt)
                 wb[nt][kb].set(w * to_f8(ld_red_dual(sB, G::LB, 16 * (G::TNW * wave + nt), kb, g, r)));
         }
-        const float es = sE[16 * wave + r], tot = sTot;
+        const float es = SUM ? 0.f : sE[buf][16 * wave + r], tot = sTot[buf];
 #pragma unroll
-        for (int d = 0; d < G::TD; ++d) {
-            const F xf[2] = {ld_red(sX, G::LX, 16 * d, 0, g, r), ld_red(sX, G::LX, 16 * d, 1, g, r)};
+        for (int nt = 0; nt < G::TNW; ++nt)
+#pragma unroll
+            for (int d = 0; d < G::TD; ++d) hs[nt][d] *= tot;
+        // the columns d in pairs of tiles, whose products alternate
+#pragma unroll
+        for (int d = 0; d < G::TD; d += 2) {
+            F xf[2][2];  // [kb][tile]
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) xf[kb][i] = ld_red(sX, G::LX, 16 * (d + i), kb, g, r);
             if (!SUM) {
-                floatx4 o = zero4();
+                floatx4 o[2] = {zero4(), zero4()};
 #pragma unroll
-                for (int kb = 0; kb < NP / 32; ++kb) o = mma(ld_red(sH, G::LH, 16 * d, kb, g, r), cf[kb], o);
-                o *= es;
-                o = mma(xf[0], pf[0], o);
-                if (wave >= 2) o = mma(xf[1], pf[1], o);
+                for (int kb = 0; kb < NP / 32; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) o[i] = mma(ld_red(sH, G::LH, 16 * (d + i), kb, g, r), cf[kb], o[i]);
                 const int t = 64 * c + 16 * wave + r;
-                const floatx4 xt = to_f4(ld4<T>(sX + (16 * wave + r) * G::LX + 16 * d + 4 * g));
-                if (t < a.L) st4(y + (size_t)t * D + 16 * d + 4 * g, t < len ? o + skip * xt : zero4());
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    o[i] = mma(xf[0][i], pf[0], o[i] * es);
+                    if (wave >= 2) o[i] = mma(xf[1][i], pf[1], o[i]);
+                    const floatx4 xt = to_f4(ld4<T>(sX + (16 * wave + r) * G::LX + 16 * (d + i) + 4 * g));
+                    o[i] += skip * xt;
+                    T* to = y + (size_t)(64 * c) * D + (unsigned)((16 * wave + r) * D + 16 * (d + i) + 4 * g);
+                    if (64 * c + 64 <= len)
+                        st4(to, o[i]);
+                    else if (t < a.L)
+                        st4(to, t < len ? o[i] : zero4());
+                }
             }
 #pragma unroll
-            for (int nt = 0; nt < G::TNW; ++nt) {
-                hs[nt][d] *= tot;
+            for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) hs[nt][d] = mma_split(xf[kb], wb[nt][kb], hs[nt][d]);
-            }
+                for (int nt = 0; nt < G::TNW; ++nt) {
+                    floatx4 hd[2] = {hs[nt][d], hs[nt][d + 1]};
+                    mma_split(xf[kb], wb[nt][kb], hd);
+                    hs[nt][d] = hd[0];
+                    hs[nt][d + 1] = hd[1];
+                }
+        }
+        if (wave == 0) {  // the wave with the fewest products
+            exponents(buf ^ 1);
+            load_dt(c + 2);
         }
         __syncthreads();
     }
@@ -199,7 +251,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
                 for (int d = 0; d < G::TD; ++d) st4f(to + (size_t)n * D + 16 * d + 4 * g, hs[nt][d]);
         }
     }
-    if (SUM && tid == 0) a.seg_decay[(size_t)seg * BH + bh] = exp_f64(decay);
+    if (SUM && tid == 0) a.seg_decay[(size_t)seg * BH + bh] = exp2_f64(decay);
 }
 
 // States entering segments 1 .. in place of the segments' own states: four elements of a head's state per lane.
@@ -233,7 +285,7 @@ template <typename T, int D, int PASSES> __global__ void __launch_bounds__(256) 
     const T* Bm = (const T*)a.Bm + ((size_t)b * a.G + grp) * a.N;
     const T* Cm = (const T*)a.Cm + ((size_t)b * a.G + grp) * a.N;
     const float dt = a.dt[bh];
-    const float keep = exp_f64((double)dt * (double)a.A[h]);
+    const float keep = exp2_f64((double)dt * (double)a.A[h] * kLog2e64);
     const floatx4 x = to_f4(ld4<T>((const T*)a.x + (size_t)bh * D + 4 * qd)), xd = dt * x;
     floatx4 y = zero4();
 #pragma unroll

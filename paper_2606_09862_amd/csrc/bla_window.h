@@ -68,7 +68,7 @@ hipError_t launch_window_step(int bf16_io, int D, const WindowStepArgs& a, hipSt
 hipError_t launch_window_backward(int bf16_io, int D, const WindowBwdArgs& a, hipStream_t s);
 int window_bwd_block(int D);  // queries (keys) per block of the query (key) pass
 
-// Join of nsplit parts of a softmax: o = sum_s e^{m_s - m} O_s / sum_s e^{m_s - m} l_s (m in the base-2 domain).
+// Join of nsplit (at most 64) parts of a softmax: o = sum_s e^{m_s - m} O_s / sum_s e^{m_s - m} l_s (m in the base-2 domain).
 struct JoinArgs {
     const float *part_o, *part_ml;
     void* o;

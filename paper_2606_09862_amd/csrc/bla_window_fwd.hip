@@ -235,32 +235,42 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
     }
 }
 
-// Four consecutive outputs of one row per lane.  Parts without a visible key have a sum of zero and are not read.
+// A wave joins a row: lane s holds the maximum and the sum of part s (at most 64 parts), then groups of D / 4 lanes take every
+// 64 / (D / 4)-th part's outputs, four columns to a lane, and are added up.  Parts without a visible key have a sum of zero and are not read.
+// (One thread to four columns of a row walked the parts one after the other: 26 us for 16 rows of 33 parts.)
 template <typename T, int D> __global__ void __launch_bounds__(256) window_join_kernel(JoinArgs a)
 {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long row = i / (D / 4);
-    const int c = 4 * (int)(i % (D / 4));
+    constexpr int LR = D / 4, PG = 64 / LR;
+    const long long row = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, c = 4 * (lane % LR), pg = lane / LR;
     if (row >= a.rows) return;
-    float m = kNoMax;
-    for (int s = 0; s < a.nsplit; ++s) {
-        const float* ml = a.part_ml + 2 * ((size_t)s * a.rows + row);
-        if (ml[1] != 0.f) m = fmaxf(m, ml[0]);
+    float m = kNoMax, l = 0.f;
+    if (lane < a.nsplit) {
+        const float* ml = a.part_ml + 2 * ((size_t)lane * a.rows + row);
+        l = ml[1];
+        m = l != 0.f ? ml[0] : kNoMax;
     }
-    float l = 0.f;
+    float top = m;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+    float w = l != 0.f ? exp2_fast(m - top) : 0.f;
+    l *= w;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
     floatx4 o = zero4();
-    for (int s = 0; s < a.nsplit; ++s) {
-        const size_t at = (size_t)s * a.rows + row;
-        const float ls = a.part_ml[2 * at + 1];
-        if (ls != 0.f) {
-            const float w = exp2_fast(a.part_ml[2 * at] - m);
-            l += w * ls;
-            o += w * ld4f(a.part_o + at * D + c);
-        }
+#pragma unroll 4
+    for (int s0 = 0; s0 < a.nsplit; s0 += PG) {
+        const int s = s0 + pg;
+        const float ws = __shfl(w, s & 63);
+        if (s < a.nsplit && ws != 0.f) o += ws * ld4f(a.part_o + ((size_t)s * a.rows + row) * D + c);
     }
+#pragma unroll
+    for (int off = 32; off >= LR; off >>= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off);
     const bool some = l != 0.f;
-    st4((T*)a.o + (size_t)row * D + c, some ? o * (1.f / l) : zero4());
-    if (a.lse && c == 0) a.lse[row] = some ? (m + __log2f(l)) * kLn2 : -INFINITY;
+    if (pg == 0) st4((T*)a.o + (size_t)row * D + c, some ? o * (1.f / l) : zero4());
+    if (a.lse && lane == 0) a.lse[row] = some ? (top + __log2f(l)) * kLn2 : -INFINITY;
 }
 
 // The rings after the call: slot s takes the newest token whose place it is, else what it held.
@@ -315,8 +325,7 @@ template <typename T, int D> hipError_t forward_d(int waves, const WindowArgs& a
 
 template <typename T, int D> hipError_t join_d(const JoinArgs& a, hipStream_t s)
 {
-    const long long n = a.rows * (D / 4);
-    hipLaunchKernelGGL((window_join_kernel<T, D>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((window_join_kernel<T, D>), dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
