@@ -137,7 +137,8 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
 // One chunk of a group's heads (or of a part of them).  Wave w owns 16 tokens, first as columns t (dC and the row sums of M), then as columns u
 // (dx, dB and the column sums), so that every product's second operand is an accumulator of the wave; dB and dC stay in registers
 // over the heads.
-template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_bwd_kernel(SsmBwdArgs a)
+template <typename T, int D, int NP>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_bwd_kernel(SsmBwdArgs a)
 {
     typedef typename Frag<T>::type F;
     constexpr bool two = sizeof(T) == 2;
@@ -182,27 +183,53 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
         const float skip = a.Dm ? a.Dm[h] : 0.f;
         const double A = a.A[h];
 
-        auto stage = [&](const T* p, T* to, int cols, int width, int ld) {  // 64 rows of `cols` columns, zeros past n and cols
-            const int ch = width / PE;
-            for (int i = tid; i < 64 * ch; i += 256) {
-                const int row = i / ch, k = (i % ch) * PE;
-                intx4 v = {0, 0, 0, 0};
-                if (row < n && k < cols) v = *(const intx4*)(p + (size_t)row * cols + k);
-                *(intx4*)(to + row * ld + dual_col<T>(row, k)) = v;
-            }
-        };
-        auto stage_state = [&](const float* p, const float* q) {  // and the product with the other state, if given
+        // A phase's tiles: 64 rows of D columns into s1, 64 of N into s2, a state into sH, and the product of two states if a second is
+        // given.  All loads are issued before the first store to LDS (tile by tile each waited for memory anew: 10000 cycles a phase
+        // instead of 4000).
+        auto stage = [&](const T* p1, const T* p2, const float* ps, const float* pq) {
+            constexpr int C1 = D / PE, C2 = NP / PE, P1 = 64 * C1 / 256, P2 = 64 * C2 / 256, PS = NP * D / 4 / 256;
+            intx4 r1[P1], r2[P2];
+            floatx4 rst[PS];
             float dot = 0.f;
-            for (int i = tid; i < NP * D / 4; i += 256) {
-                const int row = i / (D / 4), k = 4 * (i % (D / 4));
-                floatx4 v = zero4();
-                if (row < a.N) {
-                    v = ld4f(p + (size_t)row * D + k);
-                    if (q) {
-                        const floatx4 w = ld4f(q + (size_t)row * D + k);
-                        dot += v[0] * w[0] + v[1] * w[1] + v[2] * w[2] + v[3] * w[3];
-                    }
+#pragma unroll
+            for (int i = 0; i < P1; ++i) {
+                const int row = (i * 256 + tid) / C1, k = (i * 256 + tid) % C1 * PE;
+                r1[i] = *(const intx4*)(p1 + (size_t)min(row, n - 1) * D + k);
+            }
+#pragma unroll
+            for (int i = 0; i < P2; ++i) {
+                const int row = (i * 256 + tid) / C2, k = (i * 256 + tid) % C2 * PE;
+                r2[i] = *(const intx4*)(p2 + (size_t)min(row, n - 1) * a.N + min(k, a.N - PE));
+            }
+#pragma unroll
+            for (int i = 0; i < PS; ++i) {
+                const int row = (i * 256 + tid) / (D / 4), k = (i * 256 + tid) % (D / 4) * 4;
+                rst[i] = ld4f(ps + (size_t)min(row, a.N - 1) * D + k);
+            }
+            if (pq) {
+#pragma unroll
+                for (int i = 0; i < PS; ++i) {
+                    const int row = (i * 256 + tid) / (D / 4), k = (i * 256 + tid) % (D / 4) * 4;
+                    const floatx4 w = ld4f(pq + (size_t)min(row, a.N - 1) * D + k);
+                    const float x = rst[i][0] * w[0] + rst[i][1] * w[1] + rst[i][2] * w[2] + rst[i][3] * w[3];
+                    dot += row < a.N ? x : 0.f;
                 }
+            }
+            const intx4 zero = {0, 0, 0, 0};  // rows past n and columns past N
+#pragma unroll
+            for (int i = 0; i < P1; ++i) {
+                const int row = (i * 256 + tid) / C1, k = (i * 256 + tid) % C1 * PE;
+                *(intx4*)(s1 + row * LD1 + dual_col<T>(row, k)) = row < n ? r1[i] : zero;
+            }
+#pragma unroll
+            for (int i = 0; i < P2; ++i) {
+                const int row = (i * 256 + tid) / C2, k = (i * 256 + tid) % C2 * PE;
+                *(intx4*)(s2 + row * LD2 + dual_col<T>(row, k)) = row < n && k < a.N ? r2[i] : zero;
+            }
+#pragma unroll
+            for (int i = 0; i < PS; ++i) {
+                const int row = (i * 256 + tid) / (D / 4), k = (i * 256 + tid) % (D / 4) * 4;
+                floatx4 v = row < a.N ? rst[i] : zero4();
                 T* to = sH + row * LD1 + dual_col<T>(row, k);
                 st4(to, v);
                 if constexpr (two) {
@@ -239,11 +266,16 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
         };
 
         // ---- columns t
-        stage(x, s1, D, D, LD1);
-        stage(Bm, s2, a.N, NP, LD2);
-        stage_state(enter, nullptr);
+        float d = 0.f;
+        if (wave == 0 && lane < n) d = a.dt[tok + lane];
+        F cf[NP / 32], yf[D / 32];
+#pragma unroll
+        for (int kb = 0; kb < NP / 32; ++kb)
+            cf[kb] = me < n ? ld_acc_row<T>(Cm + (size_t)me * a.N, kb, g, a.N) : zero_frag<T>();
+#pragma unroll
+        for (int kb = 0; kb < D / 32; ++kb) yf[kb] = me < n ? ld_nat(dy + (size_t)me * D, kb, g) : zero_frag<T>();
+        stage(x, Bm, enter, nullptr);
         if (wave == 0) {
-            const float d = lane < n ? a.dt[tok + lane] : 0.f;
             const double s = wave_scan((double)d * A * kLog2e64, lane), tot = wave_last(s);
             sS[lane] = (float)s;
             sSl[lane] = (float)(s - (double)(float)s);
@@ -251,12 +283,6 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
             sE[lane] = exp2_f64(s);
             sF[lane] = exp2_f64(tot - s);
         }
-        F cf[NP / 32], yf[D / 32];
-#pragma unroll
-        for (int kb = 0; kb < NP / 32; ++kb)
-            cf[kb] = me < n ? ld_acc_row<T>(Cm + (size_t)me * a.N, kb, g, a.N) : zero_frag<T>();
-#pragma unroll
-        for (int kb = 0; kb < D / 32; ++kb) yf[kb] = me < n ? ld_nat(dy + (size_t)me * D, kb, g) : zero_frag<T>();
         __syncthreads();
         const float s_me = sS[me], sl_me = sSl[me], dt_me = sDt[me], e_me = sE[me], f_me = sF[me];
         float rs = 0.f;
@@ -297,18 +323,16 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
         __syncthreads();
 
         // ---- columns u
-        stage(dy, s1, D, D, LD1);
-        stage(Cm, s2, a.N, NP, LD2);
-        float dot = stage_state(leave, enter);
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) dot += __shfl_xor(dot, off);
-        if (lane == 0) sDot[wave] = dot;
         F bf[NP / 32], xf[D / 32];
 #pragma unroll
         for (int kb = 0; kb < NP / 32; ++kb)
             bf[kb] = me < n ? ld_acc_row<T>(Bm + (size_t)me * a.N, kb, g, a.N) : zero_frag<T>();
 #pragma unroll
         for (int kb = 0; kb < D / 32; ++kb) xf[kb] = me < n ? ld_nat(x + (size_t)me * D, kb, g) : zero_frag<T>();
+        float dot = stage(dy, Cm, leave, enter);
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) dot += __shfl_xor(dot, off);
+        if (lane == 0) sDot[wave] = dot;
         __syncthreads();
         float pu = 0.f, late = 0.f, diag = 0.f;
         {

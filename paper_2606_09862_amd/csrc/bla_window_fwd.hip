@@ -258,11 +258,18 @@ template <typename T, int D> __global__ void __launch_bounds__(256) window_join_
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
     floatx4 o = zero4();
-#pragma unroll 4
-    for (int s0 = 0; s0 < a.nsplit; s0 += PG) {
-        const int s = s0 + pg;
-        const float ws = __shfl(w, s & 63);
-        if (s < a.nsplit && ws != 0.f) o += ws * ld4f(a.part_o + ((size_t)s * a.rows + row) * D + c);
+    for (int s0 = 0; s0 < a.nsplit; s0 += 8 * PG) {  // eight loads in flight; what a part without keys holds is dropped
+        floatx4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = ld4f(a.part_o + ((size_t)min(s0 + k * PG + pg, a.nsplit - 1) * a.rows + row) * D + c);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int s = s0 + k * PG + pg;
+            float ws = __shfl(w, s & 63);  // lanes past nsplit hold a weight of zero
+            ws = s < 64 ? ws : 0.f;
+            o += ws * (ws != 0.f ? v[k] : zero4());
+        }
     }
 #pragma unroll
     for (int off = 32; off >= LR; off >>= 1)
