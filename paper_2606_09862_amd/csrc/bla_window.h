@@ -49,8 +49,8 @@ struct WindowBwdArgs {
     float scale;
     float* delta;                   // [B, H, L]: sum of dO o
     int nqb, nkb;                   // query and key blocks of a sequence
-    int nsb, ssplit;                // key blocks that hold sinks, parts of the queries that see them
-    float* part;                    // [ssplit][B Hkv][nsb * keys per block][2][D]
+    int ns, ssplit;                 // sinks of a sequence, parts of the queries that see them from beyond their windows
+    float *near, *part;             // float32 dk and dv of the sinks: [B Hkv][ns][2][D], [ssplit][B Hkv][ns][2][D]
     long long q_units, q_per, k_units, k_per;
 };
 

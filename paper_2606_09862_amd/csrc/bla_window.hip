@@ -73,12 +73,11 @@ StepPlan step_plan(const bla_window_params* p)
     return s;
 }
 
-// Backward: the keys of the blocks that hold sinks are seen by every later query; their queries go in parts of about
-// what a plain block sees.
+// Backward: the sinks' queries beyond their windows in as many parts as fill the device with waves, a block of 32 queries or more to each.
 struct BackwardPlan {
-    int nqb, nkb, nsb, ssplit;
+    int nqb, nkb, ns, ssplit;
     long long q_units, k_units;
-    size_t off_part, total;
+    size_t off_near, off_part, total;
 };
 BackwardPlan backward_plan(const bla_window_params* p)
 {
@@ -87,15 +86,17 @@ BackwardPlan backward_plan(const bla_window_params* p)
     const int nk = window_bwd_block(p->d);
     b.nqb = (p->L + nk - 1) / nk;
     b.nkb = (p->L + nk - 1) / nk;
-    const int sinks = p->sinks < p->L ? p->sinks : p->L;
-    b.nsb = (sinks + nk - 1) / nk;
-    const long long plain = (long long)p->window + nk < 256 ? 256 : (long long)p->window + nk;
-    long long n = (p->L + plain - 1) / plain;
+    b.ns = p->sinks < p->L ? p->sinks : p->L;
+    const long long wgs = bk * ((b.ns + 15) / 16), items = p->H_kv > 0 ? (long long)(p->H / p->H_kv) * ((p->L + 31) / 32) : 1;
+    long long n = wgs > 0 ? (2 * kFill + wgs - 1) / wgs : 1;
+    if (n > items / 4) n = items / 4;
     b.ssplit = (int)(n < 1 ? 1 : n > kMaxParts ? kMaxParts : n);
     b.q_units = bh * b.nqb;
-    b.k_units = bk * ((long long)b.nsb * b.ssplit + b.nkb - b.nsb);
-    b.off_part = seq_align((size_t)bh * p->L * 4);
-    b.total = b.off_part + seq_align((size_t)b.ssplit * bk * b.nsb * nk * 2 * p->d * 4);
+    b.k_units = bk * b.nkb;
+    const size_t one = seq_align((size_t)bk * b.ns * 2 * p->d * 4);
+    b.off_near = seq_align((size_t)bh * p->L * 4);
+    b.off_part = b.off_near + one;
+    b.total = b.off_part + seq_align((size_t)b.ssplit * bk * b.ns * 2 * p->d * 4);
     return b;
 }
 
@@ -236,8 +237,9 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
     WindowBwdArgs a = {};
     a.q = q, a.k = k, a.v = v, a.o = o, a.dO = dO, a.lse = lse, a.dq = dq, a.dk = dk, a.dv = dv, a.lengths = lengths;
     a.B = p->B, a.H = p->H, a.Hkv = p->H_kv, a.L = p->L, a.W = p->window, a.S = p->sinks, a.scale = scale_of(p);
-    a.delta = (float*)workspace, a.part = (float*)((char*)workspace + b.off_part);
-    a.nqb = b.nqb, a.nkb = b.nkb, a.nsb = b.nsb, a.ssplit = b.ssplit;
+    a.delta = (float*)workspace, a.near = (float*)((char*)workspace + b.off_near);
+    a.part = (float*)((char*)workspace + b.off_part);
+    a.nqb = b.nqb, a.nkb = b.nkb, a.ns = b.ns, a.ssplit = b.ssplit;
     a.q_units = b.q_units, a.q_per = (b.q_units + 7) / 8, a.k_units = b.k_units, a.k_per = (b.k_units + 7) / 8;
     return launch_window_backward(bf16, p->d, a, (hipStream_t)stream) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }

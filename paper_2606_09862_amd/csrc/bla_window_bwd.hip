@@ -3,8 +3,8 @@
 // With P = exp(scale q k - lse) on the visible pairs and delta_i = sum_c dO_ic o_ic:
 //   dS = P (dO v^T - delta),   dq = scale dS k,   dk = scale dS^T q,   dv = P^T dO.
 // Two passes recompute P from lse, one per query block (dq, and delta for the other) and one per key block (dk, dv, summed over the
-// heads that share the key head and over the queries that see the block), so that every gradient has one
-// owner and a fixed order of sums, without atomics.  P and dS are rounded to the operand type before their second
+// heads that share the key head and over the queries whose windows reach the block; the sinks' other queries have a kernel of
+// their own), so that every gradient has a fixed order of sums, without atomics.  P and dS are rounded to the operand type before their second
 // products (2^-9 relative in bf16, as the results are); sums and row terms are float32.
 #include "bla_window.h"
 
@@ -176,9 +176,8 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
 
 // Key pass.  Wave w owns 16 KT keys: their K and V are operands in registers for the whole walk, and S = Q K^T and
 // dP = dO V^T (accumulator rows: queries) give P and dS as operands of dV^T = dO^T P and dK^T = Q^T dS.  The walk goes over the
-// heads of the group and the 64-query tiles that see the block.  Keys that are sinks are seen by every later
-// query, so the blocks that hold some are split over the queries into parts of about a plain block's work, whose
-// float32 results window_bwd_sum_kernel adds up in order.
+// heads of the group and the 64-query tiles whose windows hold keys of the block.  Later queries see sinks as well: those pairs
+// are window_bwd_sink_kernel's, and the sinks' gradients go out in float32 for window_bwd_sum_kernel to add up.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
 {
@@ -191,12 +190,9 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
     long long u = xcd_unit(blockIdx.x, a.k_per);
     if (u >= a.k_units) return;
     const int grp = a.H / a.Hkv;
-    const int jobs = a.nsb * a.ssplit + a.nkb - a.nsb;  // of one key head
-    const int job = (int)(u % jobs);
-    u /= jobs;
+    const int nb = (int)(u % a.nkb);
+    u /= a.nkb;
     const int hk = (int)(u % a.Hkv), b = (int)(u / a.Hkv);
-    const bool sink = job < a.nsb * a.ssplit;
-    const int nb = sink ? job / a.ssplit : job - a.nsb * a.ssplit + a.nsb, part = sink ? job % a.ssplit : 0;
     const int n0 = nb * G::NB;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
     const int len = a.lengths ? min(max(a.lengths[b], 0), a.L) : a.L;
@@ -204,14 +200,8 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
     const int ch = tid % G::CH, lrow = tid / G::CH;
 
     // 64-query tiles of the walk, from query n0 on
-    const int qend = sink ? len : (int)min((long long)len, (long long)n0 + G::NB - 1 + a.W);
-    int tb = 0, te = qend > n0 ? (qend - n0 + 63) / 64 : 0;
-    if (sink) {
-        const int each = (te + a.ssplit - 1) / a.ssplit;
-        tb = part * each;
-        te = min(te, tb + each);
-    }
-    const int nt = max(0, te - tb);
+    const int qend = (int)min((long long)len, (long long)n0 + G::NB - 1 + a.W);
+    const int nt = qend > n0 ? (qend - n0 + 63) / 64 : 0;
 
     const int k0 = n0 + 16 * KT * wave, kend = k0 + 16 * KT - 1;  // the wave's keys
     F kf[KT][D / 32], vf[KT][D / 32];
@@ -221,7 +211,7 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
         const int j = k0 + 16 * kt + r;
         const size_t at = (kvrow + min(j, a.L - 1)) * D;
         const bool in = j < len;
-        span[kt] = in ? (unsigned)(j < a.S ? len - j : min(len - j, a.W)) : 0u;
+        span[kt] = in ? (unsigned)min(len - j, a.W) : 0u;
 #pragma unroll
         for (int kb = 0; kb < D / 32; ++kb) {
             kf[kt][kb] = in ? ld_nat((const T*)a.k + at, kb, g) : zero_frag<T>();
@@ -240,7 +230,7 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
     const T *qp = (const T*)a.q + ch * G::PE, *dp_ = (const T*)a.dO + ch * G::PE;
     auto load = [&](int hg, int t) {  // queries past the row's last repeat it: the masks hide them
         const size_t row0 = ((size_t)b * a.H + hk * grp + hg) * a.L;
-        const int q0 = n0 + 64 * (tb + t);
+        const int q0 = n0 + 64 * t;
 #pragma unroll
         for (int ps = 0; ps < G::NP; ++ps) {
             const size_t at = (row0 + min(q0 + ps * G::RPP + lrow, len - 1)) * D;
@@ -273,8 +263,8 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
                 load(hg + 1, 0);
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-                const int q0 = n0 + 64 * (tb + t) + 32 * hf, q1 = q0 + 31;
-                if (q0 >= len || k0 > q1 || (k0 >= a.S && q0 - kend >= a.W)) continue;
+                const int q0 = n0 + 64 * t + 32 * hf, q1 = q0 + 31;
+                if (q0 >= len || k0 > q1 || q0 - kend >= a.W) continue;
                 floatx4 s[KT][2], dp[KT][2];
 #pragma unroll
                 for (int qt = 0; qt < 2; ++qt) {
@@ -303,7 +293,7 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
                             dp[kt][qt][e] = s[kt][qt][e] * (dp[kt][qt][e] - delta[e]);
                         }
                 }
-                if (kend > q0 || q1 >= len || (q1 - k0 >= a.W && kend >= a.S)) {  // some pair is not visible
+                if (kend > q0 || q1 >= len || q1 - k0 >= a.W) {  // some pair is not visible
 #pragma unroll
                     for (int kt = 0; kt < KT; ++kt) {
                         const int q = q0 + 4 * g - (k0 + 16 * kt + r);
@@ -335,8 +325,8 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
         const int key = k0 + 16 * kt + r;
-        if (sink) {
-            float* to = a.part + ((((size_t)part * a.B + b) * a.Hkv + hk) * a.nsb * G::NB + key) * 2 * D;
+        if (key < a.S && key < a.L) {
+            float* to = a.near + (((size_t)b * a.Hkv + hk) * a.ns + key) * 2 * D;
 #pragma unroll
             for (int dt = 0; dt < D / 16; ++dt) {
                 st4f(to + 16 * dt + 4 * g, dk[kt][dt]);
@@ -353,19 +343,116 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
     }
 }
 
-// dk and dv of the keys of the blocks with sinks: the parts, added in order.
-template <typename T, int D> __global__ void __launch_bounds__(256) window_bwd_sum_kernel(WindowBwdArgs a, int block)
+// The pairs of sinks and the queries that see them from beyond their windows.  A wave takes 16 sinks and every so-maniest 32 queries of every head of
+// the group, on its own: rows of Q and dO come from memory as operands of S and dP, and through LDS that only the wave touches
+// as the transposed operands of dV^T and dK^T.  The four waves are added up in LDS, a workgroup writes one part.  Bound: the bytes of Q
+// and dO.  (128 x 4096 tokens at d = 64, window 511, 4 sinks: 31 us for 117 MB.  In the key kernel these queries took a fifth of the
+// workgroups for one wave's work each: 251 us with them, 204 without.)
+template <typename T, int D> __global__ void __launch_bounds__(256) window_bwd_sink_kernel(WindowBwdArgs a)
 {
-    const int keys = a.nsb * block;
+    typedef typename Frag<T>::type F;
+    constexpr int LD = dual_ld<T>(D), LO = D + 4;
+    constexpr size_t QB = sizeof(T) * 4 * 2 * 32 * LD, OB = sizeof(float) * 4 * 16 * LO;
+    __shared__ __attribute__((aligned(16))) char raw[QB > OB ? QB : OB];
+    unsigned u = blockIdx.x;
+    const int part = (int)(u % (unsigned)a.ssplit);
+    u /= (unsigned)a.ssplit;
+    const int nst = (a.ns + 15) / 16, st = (int)(u % (unsigned)nst);
+    u /= (unsigned)nst;
+    const int hk = (int)(u % (unsigned)a.Hkv), b = (int)(u / (unsigned)a.Hkv);
+    const int grp = a.H / a.Hkv;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
+    const int len = a.lengths ? min(max(a.lengths[b], 0), a.L) : a.L;
+    const int j = 16 * st + r;                                                // the lane's sink
+    const long long first = (long long)16 * st + a.W;                        // the first query past a window that holds one
+    const int q_first = (int)min(first, (long long)len), blocks = (len - q_first + 31) / 32;
+
+    F kf[D / 32], vf[D / 32];
+    {
+        const size_t at = (((size_t)b * a.Hkv + hk) * a.L + min(j, a.L - 1)) * D;
+        const bool in = j < a.ns && j < len;
+#pragma unroll
+        for (int kb = 0; kb < D / 32; ++kb) {
+            kf[kb] = in ? ld_nat((const T*)a.k + at, kb, g) : zero_frag<T>();
+            vf[kb] = in ? ld_nat((const T*)a.v + at, kb, g) : zero_frag<T>();
+        }
+    }
+    // the lane's sink is seen from beyond its window by the queries from j + W on
+    const int q_sink = j < a.ns && j < len ? (int)min((long long)j + a.W, (long long)len) : len;
+    floatx4 dk[D / 16], dv[D / 16];
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) dk[dt] = dv[dt] = zero4();
+    const float sc = a.scale * kLog2e;
+    T *sQ = (T*)raw + wave * 2 * 32 * LD, *sD = sQ + 32 * LD;
+
+    for (long long it = part * 4 + wave; it < (long long)grp * blocks; it += a.ssplit * 4) {
+        const int hg = (int)(it / blocks), q0 = q_first + 32 * (int)(it % blocks);
+        const size_t row0 = ((size_t)b * a.H + hk * grp + hg) * a.L;
+        floatx4 s[2], dp[2];
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt) {
+            const size_t at = (row0 + min(q0 + 16 * qt + r, len - 1)) * D;
+            s[qt] = dp[qt] = zero4();
+#pragma unroll
+            for (int kb = 0; kb < D / 32; ++kb) {
+                const F qf = ld_nat((const T*)a.q + at, kb, g), df = ld_nat((const T*)a.dO + at, kb, g);
+                *(F*)(sQ + (16 * qt + r) * LD + 32 * kb + 8 * g) = qf;
+                *(F*)(sD + (16 * qt + r) * LD + 32 * kb + 8 * g) = df;
+                s[qt] = mma(qf, kf[kb], s[qt]);
+                dp[qt] = mma(df, vf[kb], dp[qt]);
+            }
+        }
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int q = q0 + 16 * qt + 4 * g + e;
+                const size_t at = row0 + min(q, len - 1);
+                const float p = exp2_fast(__builtin_fmaf(s[qt][e], sc, -a.lse[at] * kLog2e));
+                const bool seen = (q >= q_sink) & (q < len);
+                s[qt][e] = seen ? p : 0.f;
+                dp[qt][e] = seen ? p * (dp[qt][e] - a.delta[at]) : 0.f;
+            }
+        const F pf = frag_from_acc<T>(s[0], s[1]), sf = frag_from_acc<T>(dp[0], dp[1]);
+        // the wave's own stores above, read by its other lanes (LDS serves a wave in order)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+            dv[dt] = mma(ld_red_dual(sD, LD, 16 * dt, 0, g, r), pf, dv[dt]);
+            dk[dt] = mma(ld_red_dual(sQ, LD, 16 * dt, 0, g, r), sf, dk[dt]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    float* sO = (float*)raw;
+    for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) st4f(sO + (wave * 16 + r) * LO + 16 * dt + 4 * g, which ? dv[dt] : dk[dt]);
+        __syncthreads();
+        for (int i = tid; i < 16 * (D / 4); i += 256) {
+            const int key = i / (D / 4), c = 4 * (i % (D / 4));
+            if (16 * st + key >= a.ns) continue;
+            floatx4 x = ld4f(sO + key * LO + c);
+#pragma unroll
+            for (int w = 1; w < 4; ++w) x += ld4f(sO + (w * 16 + key) * LO + c);
+            st4f(a.part + (((((size_t)part * a.B + b) * a.Hkv + hk) * a.ns + 16 * st + key) * 2 + which) * D + c, x);
+        }
+    }
+}
+
+// dk and dv of the sinks: the key kernel's and the parts, added in order.
+template <typename T, int D> __global__ void __launch_bounds__(256) window_bwd_sum_kernel(WindowBwdArgs a)
+{
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     const int c = 4 * (int)(i % (2 * D / 4));
-    const long long row = i / (2 * D / 4);  // (b, hk, key)
-    if (row >= (long long)a.B * a.Hkv * keys) return;
-    const int key = (int)(row % keys);
-    if (key >= a.L) return;
-    floatx4 x = zero4();
-    for (int s = 0; s < a.ssplit; ++s) x += ld4f(a.part + ((size_t)s * a.B * a.Hkv * keys + row) * 2 * D + c);
-    const size_t at = ((size_t)(row / keys) * a.L + key) * D;
+    const long long row = i / (2 * D / 4), rows = (long long)a.B * a.Hkv * a.ns;  // (b, hk, key)
+    if (row >= rows) return;
+    floatx4 x = ld4f(a.near + row * 2 * D + c);
+#pragma unroll 8
+    for (int s = 0; s < a.ssplit; ++s) x += ld4f(a.part + ((size_t)s * rows + row) * 2 * D + c);
+    const size_t at = ((size_t)(row / a.ns) * a.L + row % a.ns) * D;
     if (c < D)
         st4((T*)a.dk + at + c, x * a.scale);
     else
@@ -377,9 +464,12 @@ template <typename T, int D> hipError_t backward_d(const WindowBwdArgs& a, hipSt
     typedef BwdGeo<T, D> G;
     hipLaunchKernelGGL((window_bwd_q_kernel<T, D>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
     hipLaunchKernelGGL((window_bwd_k_kernel<T, D>), dim3((unsigned)(8 * a.k_per)), dim3(G::NT), 0, s, a);
-    if (a.nsb > 0) {
-        const long long n = (long long)a.B * a.Hkv * a.nsb * G::NB * (2 * D / 4);
-        hipLaunchKernelGGL((window_bwd_sum_kernel<T, D>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a, G::NB);
+    if (a.ns > 0) {
+        const int tiles = (a.ns + 15) / 16;
+        hipLaunchKernelGGL((window_bwd_sink_kernel<T, D>), dim3((unsigned)((long long)a.B * a.Hkv * tiles * a.ssplit)), dim3(256), 0,
+                           s, a);
+        const long long n = (long long)a.B * a.Hkv * a.ns * (2 * D / 4);
+        hipLaunchKernelGGL((window_bwd_sum_kernel<T, D>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
     }
     return hipGetLastError();
 }
