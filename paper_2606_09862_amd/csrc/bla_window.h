@@ -63,7 +63,6 @@ __device__ __forceinline__ int row_tokens(const int32_t* lengths, const int64_t*
 }
 
 hipError_t launch_window_forward(int bf16_io, int D, int waves, const WindowArgs& a, hipStream_t s);
-hipError_t launch_window_ring(int bf16_io, int D, const WindowArgs& a, hipStream_t s);
 hipError_t launch_window_step(int bf16_io, int D, const WindowStepArgs& a, hipStream_t s);
 hipError_t launch_window_backward(int bf16_io, int D, const WindowBwdArgs& a, hipStream_t s);
 int window_bwd_block(int D);  // queries (keys) per block of the query (key) pass

@@ -23,14 +23,14 @@ bla_status check(const bla_window_params* p, bool step)
     if ((long long)p->window + p->sinks > (1ll << 30) || p->L > (1 << 30)) return BLA_ERR_UNSUPPORTED;
     const long long L = step ? 1 : p->L, slots = (long long)p->window + p->sinks;
     if ((double)p->B * p->H * ((L + 63) / 64) > (double)kMaxGrid / kMaxParts) return BLA_ERR_UNSUPPORTED;
-    if ((double)p->B * p->H_kv * slots * p->d > 256.0 * 4 * kMaxGrid) return BLA_ERR_UNSUPPORTED;
+    if ((double)p->B * p->H_kv * slots * p->d > 256.0 * kMaxGrid) return BLA_ERR_UNSUPPORTED;
     return BLA_OK;
 }
 
 float scale_of(const bla_window_params* p) { return p->scale == 0.f ? 1.f / sqrtf((float)p->d) : p->scale; }
 
-// Forward: 128 queries to a workgroup (each fragment of keys serves two query tiles), 64 where that fills the device better;
-// the keys of a block in parts of at least four tiles where the blocks alone do not fill it.
+// Forward: 128 queries to a workgroup (fewer reads of keys), 64 where that fills the device better;
+// the keys of a block in parts of at least two tiles where the blocks alone do not fill it.
 struct ForwardPlan {
     int waves, nqb, nsplit;
     long long units;
@@ -48,7 +48,7 @@ ForwardPlan forward_plan(const bla_window_params* p, bool cached)
     const long long tiles = (keys + kWinKeys - 1) / kWinKeys;
     long long n = 1;
     if (blocks > 0 && blocks < kFill) n = (kFill + blocks - 1) / blocks;
-    if (n > tiles / 4) n = tiles / 4;
+    if (n > tiles / 2) n = tiles / 2;
     f.nsplit = (int)(n < 1 ? 1 : n > kMaxParts ? kMaxParts : n);
     f.units = blocks * f.nsplit;
     f.total = f.nsplit > 1 ? seq_align((size_t)f.nsplit * bh * p->L * (p->d + 2) * 4) : 0;
@@ -147,12 +147,11 @@ bla_status bla_window_forward(const bla_window_params* p, const void* q, const v
     a.part_o = (float*)workspace;
     a.part_ml = f.nsplit > 1 ? a.part_o + (size_t)f.nsplit * rows * p->d : nullptr;
     hipStream_t s = (hipStream_t)stream;
-    if (p->L > 0 && launch_window_forward(bf16, p->d, f.waves, a, s) != hipSuccess) return BLA_ERR_HIP;
+    if ((p->L > 0 || cache_k_out) && launch_window_forward(bf16, p->d, f.waves, a, s) != hipSuccess) return BLA_ERR_HIP;
     if (p->L > 0 && f.nsplit > 1) {
         const JoinArgs j = {a.part_o, a.part_ml, o, lse, (long long)rows, f.nsplit};
         if (launch_window_join(bf16, p->d, j, s) != hipSuccess) return BLA_ERR_HIP;
     }
-    if (cache_k_out && launch_window_ring(bf16, p->d, a, s) != hipSuccess) return BLA_ERR_HIP;
     return BLA_OK;
 }
 

@@ -4,6 +4,41 @@
 namespace bla {
 namespace {
 
+// The rings after the call: slot s takes the newest token whose place it is, else what it held.  The forward kernel's workgroups past
+// its own do it, a piece of 16 bytes to a thread, so that it needs no launch.
+template <typename T, int D> __device__ __forceinline__ void window_ring(const WindowArgs& a, long long i)
+{
+    constexpr int PE = 16 / (int)sizeof(T), CH = D / PE;
+    const int slots = a.S + a.W;
+    const long long row = i / CH;
+    const int ch = (int)(i % CH);
+    if (row >= (long long)a.B * a.Hkv * slots) return;
+    const long long bh = row / slots;
+    const int slot = (int)(row % slots), b = (int)(bh / a.Hkv);
+    int64_t pos;
+    const int len = row_tokens(a.lengths, a.pos, a.t0, b, a.L, pos);
+    int64_t t = -1;  // the new token of the slot
+    if (len > 0) {
+        const int64_t last = pos + len - 1;
+        if (slot < a.S)
+            t = slot <= last ? slot - pos : -1;
+        else if (slot <= last)
+            t = last - (last - slot) % a.W - pos;
+    }
+    const size_t to = (size_t)row * D + ch * PE;
+    intx4 kx = {0, 0, 0, 0}, vx = {0, 0, 0, 0};
+    if (t >= 0) {
+        const size_t from = ((size_t)bh * a.L + t) * D + ch * PE;
+        kx = *(const intx4*)((const T*)a.k + from);
+        vx = *(const intx4*)((const T*)a.v + from);
+    } else if (a.ck) {
+        kx = *(const intx4*)((const T*)a.ck + to);
+        vx = *(const intx4*)((const T*)a.cv + to);
+    }
+    *(intx4*)((T*)a.ck_out + to) = kx;
+    *(intx4*)((T*)a.cv_out + to) = vx;
+}
+
 // One pass over a query block's keys with the running maximum and sum of the softmax.
 //
 // A workgroup of NW waves takes 16 NW queries of one head (wave w the 16 from 16 w on) and walks the keys that any of them
@@ -35,6 +70,10 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
     typedef typename Frag<T>::type F;
     __shared__ __attribute__((aligned(16))) T lds[2 * G::BUF];
 
+    if (blockIdx.x >= 8 * (unsigned)a.per) {
+        window_ring<T, D>(a, (long long)(blockIdx.x - 8 * (unsigned)a.per) * G::NT + threadIdx.x);
+        return;
+    }
     long long u = xcd_unit(blockIdx.x, a.per);
     if (u >= a.units) return;
     const int grp = a.H / a.Hkv;
@@ -280,44 +319,10 @@ template <typename T, int D> __global__ void __launch_bounds__(256) window_join_
     if (a.lse && lane == 0) a.lse[row] = some ? (top + __log2f(l)) * kLn2 : -INFINITY;
 }
 
-// The rings after the call: slot s takes the newest token whose place it is, else what it held.
-template <typename T, int D> __global__ void __launch_bounds__(256) window_ring_kernel(WindowArgs a)
-{
-    constexpr int PE = 16 / (int)sizeof(T), CH = D / PE;
-    const int slots = a.S + a.W;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long row = i / CH;
-    const int ch = (int)(i % CH);
-    if (row >= (long long)a.B * a.Hkv * slots) return;
-    const long long bh = row / slots;
-    const int slot = (int)(row % slots), b = (int)(bh / a.Hkv);
-    int64_t pos;
-    const int len = row_tokens(a.lengths, a.pos, a.t0, b, a.L, pos);
-    int64_t t = -1;  // the new token of the slot
-    if (len > 0) {
-        const int64_t last = pos + len - 1;
-        if (slot < a.S)
-            t = slot <= last ? slot - pos : -1;
-        else if (slot <= last)
-            t = last - (last - slot) % a.W - pos;
-    }
-    const size_t to = (size_t)row * D + ch * PE;
-    intx4 kx = {0, 0, 0, 0}, vx = {0, 0, 0, 0};
-    if (t >= 0) {
-        const size_t from = ((size_t)bh * a.L + t) * D + ch * PE;
-        kx = *(const intx4*)((const T*)a.k + from);
-        vx = *(const intx4*)((const T*)a.v + from);
-    } else if (a.ck) {
-        kx = *(const intx4*)((const T*)a.ck + to);
-        vx = *(const intx4*)((const T*)a.cv + to);
-    }
-    *(intx4*)((T*)a.ck_out + to) = kx;
-    *(intx4*)((T*)a.cv_out + to) = vx;
-}
-
 template <typename T, int D, bool RING> hipError_t forward_r(int waves, const WindowArgs& a, hipStream_t s)
 {
-    const dim3 grid((unsigned)(8 * a.per));
+    const long long pieces = a.ck_out ? (long long)a.B * a.Hkv * (a.S + a.W) * (D * (int)sizeof(T) / 16) : 0;
+    const dim3 grid((unsigned)(8 * a.per + (pieces + 64 * waves - 1) / (64 * waves)));
     if (waves == 8)
         hipLaunchKernelGGL((window_forward_kernel<T, D, 8, RING>), grid, dim3(512), 0, s, a);
     else
@@ -333,13 +338,6 @@ template <typename T, int D> hipError_t forward_d(int waves, const WindowArgs& a
 template <typename T, int D> hipError_t join_d(const JoinArgs& a, hipStream_t s)
 {
     hipLaunchKernelGGL((window_join_kernel<T, D>), dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, s, a);
-    return hipGetLastError();
-}
-
-template <typename T, int D> hipError_t ring_d(const WindowArgs& a, hipStream_t s)
-{
-    const long long n = (long long)a.B * a.Hkv * (a.S + a.W) * (D * (int)sizeof(T) / 16);
-    hipLaunchKernelGGL((window_ring_kernel<T, D>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -367,13 +365,6 @@ hipError_t launch_window_forward(int bf16_io, int D, int waves, const WindowArgs
 hipError_t launch_window_join(int bf16_io, int D, const JoinArgs& a, hipStream_t s)
 {
 #define BLA_CALL(T, DD) join_d<T, DD>(a, s)
-    BLA_BY_TYPE(BLA_CALL)
-#undef BLA_CALL
-}
-
-hipError_t launch_window_ring(int bf16_io, int D, const WindowArgs& a, hipStream_t s)
-{
-#define BLA_CALL(T, DD) ring_d<T, DD>(a, s)
     BLA_BY_TYPE(BLA_CALL)
 #undef BLA_CALL
 }
