@@ -144,8 +144,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
     constexpr bool two = sizeof(T) == 2;
     constexpr int PE = 16 / (int)sizeof(T), LD1 = dual_ld<T>(D), LD2 = dual_ld<T>(NP);
     constexpr int TN = NP / 16, TD = D / 16, SH = NP * LD1;
+    constexpr int C1 = D / PE, C2 = NP / PE, P1 = 64 * C1 / 256, P2 = 64 * C2 / 256, PS = NP * D / 4 / 256;
+    // States of up to 4096 elements: B and C stay in LDS for all heads, and h waits in registers for its product with g (bf16, d = N = 64: the
+    // kernel 98 -> 85 us).  Larger ones have neither the registers nor, at d = 128, the LDS: a workgroup per compute unit would go.
+    constexpr bool stay = PS <= 4;
     __shared__ __attribute__((aligned(16))) T s1[64 * LD1];             // x, then dy
-    __shared__ __attribute__((aligned(16))) T s2[64 * LD2];             // B, then C
+    __shared__ __attribute__((aligned(16))) T s2[(stay ? 2 : 1) * 64 * LD2];  // B, then C; or both
     __shared__ __attribute__((aligned(16))) T sH[(two ? 3 : 1) * SH];   // h, then g: rounded, what that leaves, and what that leaves
     __shared__ __attribute__((aligned(16))) float sS[64], sSl[64], sDt[64];
     __shared__ float sE[64], sF[64], sDs[64], sP[64], sLate[64], sDot[4], sDD[4];
@@ -169,6 +173,62 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
 #pragma unroll
     for (int i = 0; i < TN; ++i) dc[i] = db[i] = zero4();
 
+    // A phase's tiles: 64 rows of D columns for s1 and a state for sH.  All loads are issued before the first store to LDS (tile by tile
+    // each waited for memory anew: 10000 cycles a phase instead of 4000).
+    intx4 r1[P1];
+    floatx4 rst[PS], held[stay ? PS : 1];
+    const intx4 zero = {0, 0, 0, 0};  // rows past n and columns past N
+    auto fetch = [&](const T* p1, const float* ps) {
+#pragma unroll
+        for (int i = 0; i < P1; ++i) {
+            const int row = (i * 256 + tid) / C1, k = (i * 256 + tid) % C1 * PE;
+            r1[i] = *(const intx4*)(p1 + (unsigned)(min(row, n - 1) * D + k));
+        }
+#pragma unroll
+        for (int i = 0; i < PS; ++i) {
+            const int row = (i * 256 + tid) / (D / 4), k = (i * 256 + tid) % (D / 4) * 4;
+            rst[i] = ld4f(ps + (unsigned)(min(row, a.N - 1) * D + k));
+        }
+    };
+    auto place = [&] {
+#pragma unroll
+        for (int i = 0; i < P1; ++i) {
+            const int row = (i * 256 + tid) / C1, k = (i * 256 + tid) % C1 * PE;
+            *(intx4*)(s1 + row * LD1 + k) = row < n ? r1[i] : zero;
+        }
+#pragma unroll
+        for (int i = 0; i < PS; ++i) {
+            const int row = (i * 256 + tid) / (D / 4), k = (i * 256 + tid) % (D / 4) * 4;
+            floatx4 v = row < a.N ? rst[i] : zero4();
+            T* to = sH + row * LD1 + k;
+            st4(to, v);
+            if constexpr (two) {
+                v -= to_f4(cvt4(v, T()));
+                st4(to + SH, v);
+                st4(to + 2 * SH, v - to_f4(cvt4(v, T())));
+            }
+        }
+    };
+    auto rows_of = [&](const T* p2, T* to) {  // 64 rows of N columns
+        intx4 r2[P2];
+#pragma unroll
+        for (int i = 0; i < P2; ++i) {
+            const int row = (i * 256 + tid) / C2, k = (i * 256 + tid) % C2 * PE;
+            r2[i] = *(const intx4*)(p2 + (size_t)min(row, n - 1) * a.N + min(k, a.N - PE));
+        }
+#pragma unroll
+        for (int i = 0; i < P2; ++i) {
+            const int row = (i * 256 + tid) / C2, k = (i * 256 + tid) % C2 * PE;
+            *(intx4*)(to + row * LD2 + k) = row < n && k < a.N ? r2[i] : zero;
+        }
+    };
+    T *tB = s2, *tC = s2 + (stay ? 64 * LD2 : 0);
+    auto tokens = [&](const void* p, int h) { return (const T*)p + (((size_t)b * a.H + h) * a.L + 64 * c) * D; };
+    auto state = [&](const float* p, int h) { return p + (((size_t)b * a.H + h) * a.nch + c) * a.N * D; };
+    if (stay && n > 0 && h0 < h1) {
+        rows_of(Bm, tB);
+        rows_of(Cm, tC);
+    }
     for (int h = h0; h < h1; ++h) {
         const size_t bh = (size_t)b * a.H + h, tok = bh * a.L + 64 * c;
         const T *x = (const T*)a.x + tok * D, *dy = (const T*)a.dy + tok * D;
@@ -179,67 +239,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
             if (tid < 2) a.part_head[(bh * a.nch + c) * 2 + tid] = 0.f;
             continue;
         }
-        const float *enter = a.enter + (bh * a.nch + c) * a.N * D, *leave = a.leave + (bh * a.nch + c) * a.N * D;
         const float skip = a.Dm ? a.Dm[h] : 0.f;
         const double A = a.A[h];
 
-        // A phase's tiles: 64 rows of D columns into s1, 64 of N into s2, a state into sH, and the product of two states if a second is
-        // given.  All loads are issued before the first store to LDS (tile by tile each waited for memory anew: 10000 cycles a phase
-        // instead of 4000).
-        auto stage = [&](const T* p1, const T* p2, const float* ps, const float* pq) {
-            constexpr int C1 = D / PE, C2 = NP / PE, P1 = 64 * C1 / 256, P2 = 64 * C2 / 256, PS = NP * D / 4 / 256;
-            intx4 r1[P1], r2[P2];
-            floatx4 rst[PS];
-            float dot = 0.f;
-#pragma unroll
-            for (int i = 0; i < P1; ++i) {
-                const int row = (i * 256 + tid) / C1, k = (i * 256 + tid) % C1 * PE;
-                r1[i] = *(const intx4*)(p1 + (size_t)min(row, n - 1) * D + k);
-            }
-#pragma unroll
-            for (int i = 0; i < P2; ++i) {
-                const int row = (i * 256 + tid) / C2, k = (i * 256 + tid) % C2 * PE;
-                r2[i] = *(const intx4*)(p2 + (size_t)min(row, n - 1) * a.N + min(k, a.N - PE));
-            }
-#pragma unroll
-            for (int i = 0; i < PS; ++i) {
-                const int row = (i * 256 + tid) / (D / 4), k = (i * 256 + tid) % (D / 4) * 4;
-                rst[i] = ld4f(ps + (size_t)min(row, a.N - 1) * D + k);
-            }
-            if (pq) {
-#pragma unroll
-                for (int i = 0; i < PS; ++i) {
-                    const int row = (i * 256 + tid) / (D / 4), k = (i * 256 + tid) % (D / 4) * 4;
-                    const floatx4 w = ld4f(pq + (size_t)min(row, a.N - 1) * D + k);
-                    const float x = rst[i][0] * w[0] + rst[i][1] * w[1] + rst[i][2] * w[2] + rst[i][3] * w[3];
-                    dot += row < a.N ? x : 0.f;
-                }
-            }
-            const intx4 zero = {0, 0, 0, 0};  // rows past n and columns past N
-#pragma unroll
-            for (int i = 0; i < P1; ++i) {
-                const int row = (i * 256 + tid) / C1, k = (i * 256 + tid) % C1 * PE;
-                *(intx4*)(s1 + row * LD1 + dual_col<T>(row, k)) = row < n ? r1[i] : zero;
-            }
-#pragma unroll
-            for (int i = 0; i < P2; ++i) {
-                const int row = (i * 256 + tid) / C2, k = (i * 256 + tid) % C2 * PE;
-                *(intx4*)(s2 + row * LD2 + dual_col<T>(row, k)) = row < n && k < a.N ? r2[i] : zero;
-            }
-#pragma unroll
-            for (int i = 0; i < PS; ++i) {
-                const int row = (i * 256 + tid) / (D / 4), k = (i * 256 + tid) % (D / 4) * 4;
-                floatx4 v = row < a.N ? rst[i] : zero4();
-                T* to = sH + row * LD1 + dual_col<T>(row, k);
-                st4(to, v);
-                if constexpr (two) {
-                    v -= to_f4(cvt4(v, T()));
-                    st4(to + SH, v);
-                    st4(to + 2 * SH, v - to_f4(cvt4(v, T())));
-                }
-            }
-            return dot;
-        };
         // four rows n = 16 nt + 4g .. of the state times the lane's token
         auto mma_state = [&](int nt, const F(&f)[D / 32]) {
             floatx4 o = zero4();
@@ -271,10 +273,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
         F cf[NP / 32], yf[D / 32];
 #pragma unroll
         for (int kb = 0; kb < NP / 32; ++kb)
-            cf[kb] = me < n ? ld_acc_row<T>(Cm + (size_t)me * a.N, kb, g, a.N) : zero_frag<T>();
+            if (!stay) cf[kb] = me < n ? ld_acc_row<T>(Cm + (size_t)me * a.N, kb, g, a.N) : zero_frag<T>();
 #pragma unroll
         for (int kb = 0; kb < D / 32; ++kb) yf[kb] = me < n ? ld_nat(dy + (size_t)me * D, kb, g) : zero_frag<T>();
-        stage(x, Bm, enter, nullptr);
+        fetch(x, state(a.enter, h));
+        if (!stay) rows_of(Bm, tB);
+        place();
+        if constexpr (stay)
+#pragma unroll
+            for (int i = 0; i < PS; ++i) held[i] = rst[i];
         if (wave == 0) {
             const double s = wave_scan((double)d * A * kLog2e64, lane), tot = wave_last(s);
             sS[lane] = (float)s;
@@ -284,6 +291,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
             sF[lane] = exp2_f64(tot - s);
         }
         __syncthreads();
+        if (stay)
+#pragma unroll
+            for (int kb = 0; kb < NP / 32; ++kb) cf[kb] = ld_acc_dual(tC, LD2, 16 * wave, kb, g, r);
         const float s_me = sS[me], sl_me = sSl[me], dt_me = sDt[me], e_me = sE[me], f_me = sF[me];
         float rs = 0.f;
         {
@@ -294,7 +304,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                 if (ut <= wave) {
                     floatx4 k = zero4(), q = zero4(), l;
 #pragma unroll
-                    for (int kb = 0; kb < NP / 32; ++kb) k = mma(ld_acc_dual(s2, LD2, 16 * ut, kb, g, r), cf[kb], k);
+                    for (int kb = 0; kb < NP / 32; ++kb) k = mma(ld_acc_dual(tB, LD2, 16 * ut, kb, g, r), cf[kb], k);
 #pragma unroll
                     for (int kb = 0; kb < D / 32; ++kb) q = mma(ld_nat_dual(s1, LD1, 16 * ut, kb, g, r), yf[kb], q);
                     decay(s_me, sl_me, 16 * ut + 4 * g, l, false);
@@ -315,8 +325,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
 #pragma unroll
                 for (int e = 0; e < 4; ++e) rs += o[e] * (float)cf[nt >> 1][4 * (nt & 1) + e];
                 dc[nt] += o;
-                dc[nt] = mma(ld_red_dual(s2, LD2, 16 * nt, 0, g, r), pf[0], dc[nt]);
-                if (wave >= 2) dc[nt] = mma(ld_red_dual(s2, LD2, 16 * nt, 1, g, r), pf[1], dc[nt]);
+                dc[nt] = mma(ld_red_dual(tB, LD2, 16 * nt, 0, g, r), pf[0], dc[nt]);
+                if (wave >= 2) dc[nt] = mma(ld_red_dual(tB, LD2, 16 * nt, 1, g, r), pf[1], dc[nt]);
             }
         }
         rs = rows_sum(rs);
@@ -326,14 +336,29 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
         F bf[NP / 32], xf[D / 32];
 #pragma unroll
         for (int kb = 0; kb < NP / 32; ++kb)
-            bf[kb] = me < n ? ld_acc_row<T>(Bm + (size_t)me * a.N, kb, g, a.N) : zero_frag<T>();
+            if (!stay) bf[kb] = me < n ? ld_acc_row<T>(Bm + (size_t)me * a.N, kb, g, a.N) : zero_frag<T>();
 #pragma unroll
         for (int kb = 0; kb < D / 32; ++kb) xf[kb] = me < n ? ld_nat(x + (size_t)me * D, kb, g) : zero_frag<T>();
-        float dot = stage(dy, Cm, leave, enter);
+        fetch(dy, state(a.leave, h));
+        if (!stay) rows_of(Cm, tC);
+        place();
+        float dot = 0.f;  // <g, h>
+#pragma unroll
+        for (int i = 0; i < PS; ++i) {
+            const int row = (i * 256 + tid) / (D / 4), k = (i * 256 + tid) % (D / 4) * 4;
+            floatx4 w;
+            if constexpr (stay) w = held[i];
+            else w = ld4f(state(a.enter, h) + (unsigned)(min(row, a.N - 1) * D + k));
+            const float p = rst[i][0] * w[0] + rst[i][1] * w[1] + rst[i][2] * w[2] + rst[i][3] * w[3];
+            dot += row < a.N ? p : 0.f;
+        }
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) dot += __shfl_xor(dot, off);
         if (lane == 0) sDot[wave] = dot;
         __syncthreads();
+        if (stay)
+#pragma unroll
+            for (int kb = 0; kb < NP / 32; ++kb) bf[kb] = ld_acc_dual(tB, LD2, 16 * wave, kb, g, r);
         float pu = 0.f, late = 0.f, diag = 0.f;
         {
             floatx4 pk[4], pq[4];
@@ -343,7 +368,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                 if (tt >= wave) {
                     floatx4 k = zero4(), q = zero4(), l;
 #pragma unroll
-                    for (int kb = 0; kb < NP / 32; ++kb) k = mma(ld_acc_dual(s2, LD2, 16 * tt, kb, g, r), bf[kb], k);
+                    for (int kb = 0; kb < NP / 32; ++kb) k = mma(ld_acc_dual(tC, LD2, 16 * tt, kb, g, r), bf[kb], k);
 #pragma unroll
                     for (int kb = 0; kb < D / 32; ++kb) q = mma(ld_nat_dual(s1, LD1, 16 * tt, kb, g, r), xf[kb], q);
                     decay(s_me, sl_me, 16 * tt + 4 * g, l, true);
@@ -365,8 +390,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                 floatx4 o = mma_state(nt, xf) * f_me;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) late += o[e] * (float)bf[nt >> 1][4 * (nt & 1) + e];
-                if (wave < 2) o = mma(ld_red_dual(s2, LD2, 16 * nt, 0, g, r), qf[0], o);
-                o = mma(ld_red_dual(s2, LD2, 16 * nt, 1, g, r), qf[1], o);
+                if (wave < 2) o = mma(ld_red_dual(tC, LD2, 16 * nt, 0, g, r), qf[0], o);
+                o = mma(ld_red_dual(tC, LD2, 16 * nt, 1, g, r), qf[1], o);
                 db[nt] += dt_me * o;
             }
 #pragma unroll
