@@ -333,7 +333,7 @@ bla_status bla_layer_forward_timed(const bla_params* p, const double* T, const v
  * A non-finite value in a token of the sequence may reach the outputs of other queries that share a tile of keys with it.
  * Supported: float32 or bfloat16; d in {32, 64, 128}; H a multiple of H_kv; window >= 1, sinks >= 0, window + sinks <= 2^30; 1e-6 <=
  * |scale| <= 1e6.  Alignment, ownership, streams, workspaces and errors follow the conventions above; the outputs must not
- * overlap the inputs (BLA_ERR_INVALID_ARG).
+ * overlap the inputs or one another (BLA_ERR_INVALID_ARG).
  */
 typedef struct {
     int32_t B, H, H_kv, L; /* batch rows, query heads, key heads, tokens in this call       */
@@ -386,7 +386,7 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
  *   w: float32 [H, d, taps]   bias: float32 [H, d] (NULL = zero)
  *   state: float32 [B, H, taps - 1, d], the taps - 1 tokens before the call, oldest first (NULL = zeros)
  *   lengths: as for bla_window_forward; the state after the call is that after the row's last token.
- * Supported: float32 or bfloat16, 1 <= taps <= 8, d a multiple of 8.  Sums are float32.  Outputs must not overlap inputs;
+ * Supported: float32 or bfloat16, 1 <= taps <= 8, d a multiple of 8.  Sums are float32.  Outputs must not overlap inputs or one another;
  * bla_conv_step's state_out may be its state_in (updated in place).  Other conventions as above.
  */
 typedef struct {
@@ -429,7 +429,7 @@ bla_status bla_conv_backward(const bla_conv_params* p, const void* x, const floa
  * A is expected to be <= 0 with dt >= 0 (a decay); the formula is computed for any sign, and overflows where it does.
  * A non-finite value in a token may reach the other tokens of its 64-token chunk.
  * Supported: float32 or bfloat16; d in {32, 64, 128}; N a multiple of 8 up to 128; H a multiple of G.  The state and every sum are
- * float32, the sums of dt A float64.  Outputs must not overlap inputs; bla_ssm_step's state_out may be its state_in
+ * float32, the sums of dt A float64.  Outputs must not overlap inputs or one another; bla_ssm_step's state_out may be its state_in
  * (updated in place).  Other conventions as above.
  */
 typedef struct {

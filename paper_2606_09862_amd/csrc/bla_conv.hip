@@ -457,11 +457,9 @@ bla_status bla_conv_forward(const bla_conv_params* p, const void* x, const float
     for (const void* q : ptr)
         if (q && !is_aligned16(q)) return BLA_ERR_INVALID_ARG;
     if ((uintptr_t)lengths & 3) return BLA_ERR_INVALID_ARG;
-    const void* in[] = {x, w, bias, state_in};
-    const size_t nin[] = {n, nw, (size_t)p->H * p->d * 4, ns};
-    for (int i = 0; i < 4; ++i)
-        if (overlap(y, n, in[i], nin[i]) || overlap(state_out, ns, in[i], nin[i])) return BLA_ERR_INVALID_ARG;
-    if (overlap(y, n, state_out, ns)) return BLA_ERR_INVALID_ARG;
+    const Span in[] = {{x, n}, {w, nw}, {bias, (size_t)p->H * p->d * 4}, {state_in, ns}, {lengths, 4 * (size_t)p->B}};
+    const Span out[] = {{y, n}, {state_out, ns}};
+    if (clash(in, out)) return BLA_ERR_INVALID_ARG;
     const ConvArgs a = {x, w, bias, state_in, lengths, y, state_out, p->B, p->H, p->L, p->d, c.seg, c.nseg, p->silu,
                         (unsigned)c.threads};
     const dim3 grid((unsigned)((c.threads + 255) / 256));
@@ -489,12 +487,9 @@ bla_status bla_conv_step(const bla_conv_params* p, const void* x, const float* w
     const void* ptr[] = {x, w, bias, state_in, y, state_out};
     for (const void* q : ptr)
         if (q && !is_aligned16(q)) return BLA_ERR_INVALID_ARG;
-    const void* in[] = {x, w, bias};
-    const size_t nin[] = {n, nw, (size_t)p->H * p->d * 4};
-    for (int i = 0; i < 3; ++i)
-        if (overlap(y, n, in[i], nin[i]) || overlap(state_out, ns, in[i], nin[i])) return BLA_ERR_INVALID_ARG;
-    if (overlap(y, n, state_in, ns) || overlap(y, n, state_out, ns)) return BLA_ERR_INVALID_ARG;
-    if (state_in != state_out && overlap(state_in, ns, state_out, ns)) return BLA_ERR_INVALID_ARG;
+    const Span in[] = {{x, n}, {w, nw}, {bias, (size_t)p->H * p->d * 4}, {state_in == state_out ? nullptr : state_in, ns}};
+    const Span out[] = {{y, n}, {state_out, ns}};
+    if (clash(in, out)) return BLA_ERR_INVALID_ARG;
     const ConvArgs a = {x, w, bias, state_in, nullptr, y, state_out, p->B, p->H, 1, p->d, 1, 1, p->silu, (unsigned)c.threads};
     const dim3 grid((unsigned)((c.threads + 255) / 256));
     hipStream_t s = (hipStream_t)stream;
@@ -525,20 +520,13 @@ bla_status bla_conv_backward(const bla_conv_params* p, const void* x, const floa
     const size_t n = (size_t)p->B * p->H * p->L * p->d * elem_bytes(p->io_dtype);
     const size_t ns = (size_t)p->B * p->H * (p->taps - 1) * p->d * 4, nc = (size_t)p->H * p->d * 4, nw = nc * p->taps;
     if (!w || !dw || (p->L > 0 && (!x || !dy || !dx))) return BLA_ERR_INVALID_ARG;
-    const void* in[] = {x, w, bias, dy, state_in, dstate_out};
-    const size_t nin[] = {n, nw, nc, n, ns, ns};
-    void* out[] = {dx, dw, dbias, dstate_in};
-    const size_t nout[] = {n, nw, nc, ns};
-    for (const void* q : in)
+    const void* ptr[] = {x, w, bias, dy, state_in, dstate_out, dx, dw, dbias, dstate_in};
+    for (const void* q : ptr)
         if (q && !is_aligned16(q)) return BLA_ERR_INVALID_ARG;
     if ((uintptr_t)lengths & 3) return BLA_ERR_INVALID_ARG;
-    for (int i = 0; i < 4; ++i) {
-        if (out[i] && !is_aligned16(out[i])) return BLA_ERR_INVALID_ARG;
-        for (int j = 0; j < 6; ++j)
-            if (overlap(out[i], nout[i], in[j], nin[j])) return BLA_ERR_INVALID_ARG;
-        for (int j = 0; j < i; ++j)
-            if (overlap(out[i], nout[i], out[j], nout[j])) return BLA_ERR_INVALID_ARG;
-    }
+    const Span in[] = {{x, n}, {w, nw}, {bias, nc}, {dy, n}, {state_in, ns}, {dstate_out, ns}, {lengths, 4 * (size_t)p->B}};
+    const Span out[] = {{dx, n}, {dw, nw}, {dbias, nc}, {dstate_in, ns}};
+    if (clash(in, out)) return BLA_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < c.total || !is_aligned16(workspace)) return BLA_ERR_WORKSPACE;
     if (!tables_overwritten(workspace, c.total)) return BLA_ERR_HIP;
     const ConvBwdArgs a = {x, dy, w, bias, state_in, dstate_out, lengths, dx, dw, dbias, dstate_in, (float*)workspace,

@@ -83,6 +83,22 @@ inline bool overlap(const void* a, size_t n, const void* b, size_t m)
 {
     return a && b && (uintptr_t)a < (uintptr_t)b + m && (uintptr_t)b < (uintptr_t)a + n;
 }
+// A tensor of a call (null: not given).
+struct Span {
+    const void* p;
+    size_t n;  // bytes
+};
+// whether an output shares a byte with an input or with another output
+template <int I, int O> bool clash(const Span (&in)[I], const Span (&out)[O])
+{
+    for (int i = 0; i < O; ++i) {
+        for (const Span& x : in)
+            if (overlap(out[i].p, out[i].n, x.p, x.n)) return true;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return true;
+    }
+    return false;
+}
 
 constexpr long long kMaxGrid = 1ll << 30;  // most workgroups of a launch
 

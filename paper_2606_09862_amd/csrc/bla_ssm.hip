@@ -98,11 +98,9 @@ bla_status bla_ssm_forward(const bla_ssm_params* p, const void* x, const float* 
     for (const void* q : ptr)
         if (q && !is_aligned16(q)) return BLA_ERR_INVALID_ARG;
     if (!aligned4(dt) || !aligned4(A) || !aligned4(D) || !aligned4(lengths)) return BLA_ERR_INVALID_ARG;
-    const void* in[] = {x, Bm, Cm, dt, A, D, state_in};
-    const size_t nin[] = {z.x, z.bc, z.bc, z.dt, z.head, z.head, z.state};
-    for (int i = 0; i < 7; ++i)
-        if (overlap(y, z.x, in[i], nin[i]) || overlap(state_out, z.state, in[i], nin[i])) return BLA_ERR_INVALID_ARG;
-    if (overlap(y, z.x, state_out, z.state)) return BLA_ERR_INVALID_ARG;
+    const Span in[] = {{x, z.x}, {Bm, z.bc}, {Cm, z.bc}, {dt, z.dt}, {A, z.head}, {D, z.head}, {state_in, z.state}, {lengths, 4 * (size_t)p->B}};
+    const Span out[] = {{y, z.x}, {state_out, z.state}};
+    if (clash(in, out)) return BLA_ERR_INVALID_ARG;
     const ForwardPlan f = forward_plan(p);
     if (f.total > 0 && (!workspace || workspace_bytes < f.total || !is_aligned16(workspace))) return BLA_ERR_WORKSPACE;
     if (f.total > 0 && !tables_overwritten(workspace, f.total)) return BLA_ERR_HIP;
@@ -126,12 +124,9 @@ bla_status bla_ssm_step(const bla_ssm_params* p, const void* x, const float* dt,
     for (const void* q : ptr)
         if (!q || !is_aligned16(q)) return BLA_ERR_INVALID_ARG;
     if (!A || !dt || !aligned4(dt) || !aligned4(A) || !aligned4(D)) return BLA_ERR_INVALID_ARG;
-    const void* in[] = {x, Bm, Cm, dt, A, D};
-    const size_t nin[] = {z.x, z.bc, z.bc, z.dt, z.head, z.head};
-    for (int i = 0; i < 6; ++i)
-        if (overlap(y, z.x, in[i], nin[i]) || overlap(state_out, z.state, in[i], nin[i])) return BLA_ERR_INVALID_ARG;
-    if (overlap(y, z.x, state_in, z.state) || overlap(y, z.x, state_out, z.state)) return BLA_ERR_INVALID_ARG;
-    if (state_in != state_out && overlap(state_in, z.state, state_out, z.state)) return BLA_ERR_INVALID_ARG;
+    const Span in[] = {{x, z.x}, {Bm, z.bc}, {Cm, z.bc}, {dt, z.dt}, {A, z.head}, {D, z.head}, {state_in == state_out ? nullptr : state_in, z.state}};
+    const Span out[] = {{y, z.x}, {state_out, z.state}};
+    if (clash(in, out)) return BLA_ERR_INVALID_ARG;
     const SsmStepArgs a = {x, Bm, Cm, dt, A, D, state_in, y, state_out, p->B, p->H, p->G, p->N};
     return launch_ssm_step(p->io_dtype == BLA_BF16, p->d, a, (hipStream_t)stream) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }
@@ -151,21 +146,17 @@ bla_status bla_ssm_backward(const bla_ssm_params* p, const void* x, const float*
     if (p->H == 0) return BLA_OK;
     if (p->B == 0 || p->L == 0) return BLA_ERR_UNSUPPORTED;
     const Sizes z = sizes(p, p->L);
-    const void* in[] = {x, Bm, Cm, dy, state_in, dstate_out, dt, A, D};
-    const size_t nin[] = {z.x, z.bc, z.bc, z.x, z.state, z.state, z.dt, z.head, z.head};
-    void* out[] = {dx, dB, dC, dstate_in, ddt, dA, dD};
-    const size_t nout[] = {z.x, z.bc, z.bc, z.state, z.dt, z.head, z.head};
+    const Span in[] = {{x, z.x}, {Bm, z.bc}, {Cm, z.bc}, {dy, z.x}, {state_in, z.state}, {dstate_out, z.state}, {dt, z.dt}, {A, z.head},
+                       {D, z.head}, {lengths, 4 * (size_t)p->B}};
+    const Span out[] = {{dx, z.x}, {dB, z.bc}, {dC, z.bc}, {dstate_in, z.state}, {ddt, z.dt}, {dA, z.head}, {dD, z.head}};
     if (!x || !dt || !A || !Bm || !Cm || !dy || !dx || !ddt || !dA || !dB || !dC) return BLA_ERR_INVALID_ARG;
-    for (int i = 0; i < 9; ++i)
-        if (in[i] && (i < 6 ? !is_aligned16(in[i]) : !aligned4(in[i]))) return BLA_ERR_INVALID_ARG;
-    if (!aligned4(lengths)) return BLA_ERR_INVALID_ARG;
-    for (int i = 0; i < 7; ++i) {
-        if (out[i] && (i < 4 ? !is_aligned16(out[i]) : !aligned4(out[i]))) return BLA_ERR_INVALID_ARG;
-        for (int j = 0; j < 9; ++j)
-            if (overlap(out[i], nout[i], in[j], nin[j])) return BLA_ERR_INVALID_ARG;
-        for (int j = 0; j < i; ++j)
-            if (overlap(out[i], nout[i], out[j], nout[j])) return BLA_ERR_INVALID_ARG;
-    }
+    const void* wide[] = {x, Bm, Cm, dy, state_in, dstate_out, dx, dB, dC, dstate_in};
+    for (const void* q : wide)
+        if (!is_aligned16(q)) return BLA_ERR_INVALID_ARG;
+    const void* narrow[] = {dt, A, D, lengths, ddt, dA, dD};
+    for (const void* q : narrow)
+        if (!aligned4(q)) return BLA_ERR_INVALID_ARG;
+    if (clash(in, out)) return BLA_ERR_INVALID_ARG;
     const BackwardPlan b = backward_plan(p);
     if (!workspace || workspace_bytes < b.total || !is_aligned16(workspace)) return BLA_ERR_WORKSPACE;
     if (!tables_overwritten(workspace, b.total)) return BLA_ERR_HIP;

@@ -129,11 +129,10 @@ bla_status bla_window_forward(const bla_window_params* p, const void* q, const v
     for (const void* x : ptr)
         if (x && !is_aligned16(x)) return BLA_ERR_INVALID_ARG;
     if (!aligned(lengths, 4) || !aligned(pos, 8) || !aligned(lse, 4)) return BLA_ERR_INVALID_ARG;
-    const void* in[] = {q, k, v, cache_k_in, cache_v_in};
-    const size_t nin[] = {nq, nk, nk, nc, nc};
-    for (int i = 0; i < 5; ++i)
-        if (overlap(o, nq, in[i], nin[i]) || overlap(cache_k_out, nc, in[i], nin[i]) || overlap(cache_v_out, nc, in[i], nin[i]))
-            return BLA_ERR_INVALID_ARG;
+    const size_t nl = (size_t)p->B * p->H * p->L * 4, nb = (size_t)p->B;
+    const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {cache_k_in, nc}, {cache_v_in, nc}, {lengths, 4 * nb}, {pos, 8 * nb}};
+    const Span out[] = {{o, nq}, {lse, nl}, {cache_k_out, nc}, {cache_v_out, nc}};
+    if (clash(in, out)) return BLA_ERR_INVALID_ARG;
     const ForwardPlan f = forward_plan(p, cache_k_in != nullptr);
     if (f.total > 0 && (!workspace || workspace_bytes < f.total || !is_aligned16(workspace))) return BLA_ERR_WORKSPACE;
     if (f.total > 0 && !tables_overwritten(workspace, f.total)) return BLA_ERR_HIP;
@@ -173,13 +172,9 @@ bla_status bla_window_step(const bla_window_params* p, const void* q, const void
     for (const void* x : ptr)
         if (!x || !is_aligned16(x)) return BLA_ERR_INVALID_ARG;
     if (!aligned(pos, 8)) return BLA_ERR_INVALID_ARG;
-    if (overlap(cache_k, nc, cache_v, nc)) return BLA_ERR_INVALID_ARG;
-    void* out[] = {o, cache_k, cache_v};
-    const size_t nout[] = {nq, nc, nc};
-    for (int i = 0; i < 3; ++i)
-        if (overlap(out[i], nout[i], q, nq) || overlap(out[i], nout[i], k, nk) || overlap(out[i], nout[i], v, nk) ||
-            (i > 0 && overlap(out[i], nout[i], o, nq)))
-            return BLA_ERR_INVALID_ARG;
+    const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {pos, 8 * (size_t)p->B}};
+    const Span out[] = {{o, nq}, {cache_k, nc}, {cache_v, nc}};
+    if (clash(in, out)) return BLA_ERR_INVALID_ARG;
     const StepPlan sp = step_plan(p);
     if (sp.total > 0 && (!workspace || workspace_bytes < sp.total || !is_aligned16(workspace))) return BLA_ERR_WORKSPACE;
     if (sp.total > 0 && !tables_overwritten(workspace, sp.total)) return BLA_ERR_HIP;
@@ -215,20 +210,13 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
     if (p->B == 0 || p->H == 0 || p->L == 0) return BLA_OK;
     const int e = elem_bytes(p->io_dtype), bf16 = p->io_dtype == BLA_BF16;
     const size_t nq = (size_t)p->B * p->H * p->L * p->d * e, nk = (size_t)p->B * p->H_kv * p->L * p->d * e;
-    const void* in[] = {q, k, v, o, dO};
-    const size_t nin[] = {nq, nk, nk, nq, nq};
-    void* out[] = {dq, dk, dv};
-    const size_t nout[] = {nq, nk, nk};
-    for (const void* x : in)
+    const void* ptr[] = {q, k, v, o, dO, dq, dk, dv};
+    for (const void* x : ptr)
         if (!x || !is_aligned16(x)) return BLA_ERR_INVALID_ARG;
     if (!lse || !aligned(lse, 4) || !aligned(lengths, 4)) return BLA_ERR_INVALID_ARG;
-    for (int i = 0; i < 3; ++i) {
-        if (!out[i] || !is_aligned16(out[i])) return BLA_ERR_INVALID_ARG;
-        for (int j = 0; j < 5; ++j)
-            if (overlap(out[i], nout[i], in[j], nin[j])) return BLA_ERR_INVALID_ARG;
-        for (int j = 0; j < i; ++j)
-            if (overlap(out[i], nout[i], out[j], nout[j])) return BLA_ERR_INVALID_ARG;
-    }
+    const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {o, nq}, {dO, nq}, {lse, (size_t)p->B * p->H * p->L * 4}, {lengths, 4 * (size_t)p->B}};
+    const Span out[] = {{dq, nq}, {dk, nk}, {dv, nk}};
+    if (clash(in, out)) return BLA_ERR_INVALID_ARG;
     const BackwardPlan b = backward_plan(p);
     if (!workspace || workspace_bytes < b.total || !is_aligned16(workspace)) return BLA_ERR_WORKSPACE;
     if (!tables_overwritten(workspace, b.total)) return BLA_ERR_HIP;
