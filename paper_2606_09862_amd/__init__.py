@@ -1,4 +1,5 @@
-"""Blurry Window Attention forward operator (and its backward pass) on MI355X (gfx950).
+"""Blurry Window Attention forward operator (and its backward pass) on MI355X (gfx950), and the sequence operators beside it:
+window attention with sinks, the short causal convolution, the selective state space scan.
 
 A thin ctypes binding over ``libbla.so`` (the C ABI in ``include/bla.h``).  It
 only marshals arguments: every step of the operator runs in the library's HIP

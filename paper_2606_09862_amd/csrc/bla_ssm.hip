@@ -23,7 +23,7 @@ bla_status check(const bla_ssm_params* p, bool step)
 }
 
 // Segments of a sequence: enough for the workgroups to fill the device, each of at least four chunks (a segment costs the reading and
-// writing of a state besides).
+// writing of a state besides; 8 x 16 heads x 4096 tokens, d = 64, N = 128, bf16: 139 us, with half and twice as many workgroups more 151 and 148).
 struct ForwardPlan {
     int nch, cps, nseg;
     size_t off_decay, total;
