@@ -21,10 +21,10 @@ struct SsmArgs {
     const int32_t* lengths;
     void* y;
     float* state_out;               // or null
-    float* seg_state;               // [nseg - 1][B H][N][D]: segment summaries, then the states entering segments 1 ..
-    float* seg_decay;               // [nseg - 1][B H]
+    float* seg_state;               // [sub (nseg - 1)][B H][N][D]: summaries of the segments' parts, the last part's then the state entering the next segment
+    float* seg_decay;               // [sub (nseg - 1)][B H]
     int B, H, G, L, N;
-    int nch, cps, nseg;
+    int nch, cps, nseg, sub;        // chunks, chunks of a segment, segments, parts of a segment's summary
     long long units, per;
 };
 
@@ -67,10 +67,16 @@ template <> struct Split<bf16> {
             lo[e] = (bf16)(x - (float)mid[e]);
         }
     }
+    __device__ __forceinline__ void round(floatx8 v)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) hi[e] = (bf16)v[e];
+    }
 };
 template <> struct Split<float> {
     floatx8 hi;
     __device__ __forceinline__ void set(floatx8 v) { hi = v; }
+    __device__ __forceinline__ void round(floatx8 v) { hi = v; }
 };
 // c[i] += a[i] b for N tiles, term by term: consecutive products belong to different tiles and do not wait for each other.
 template <int N> __device__ __forceinline__ void mma_split(const bf16x8 (&a)[N], const Split<bf16>& b, floatx4 (&c)[N])

@@ -23,9 +23,11 @@ bla_status check(const bla_ssm_params* p, bool step)
 }
 
 // Segments of a sequence: enough for the workgroups to fill the device, each of at least four chunks (a segment costs the reading and
-// writing of a state besides; 8 x 16 heads x 4096 tokens, d = 64, N = 128, bf16: 139 us, with half and twice as many workgroups more 151 and 148).
+// writing of a state besides; 8 x 16 heads x 4096 tokens, d = 64, N = 128, bf16: 139 us, with half and twice as many workgroups more 151 and 148).  In bf16 the last segment, whose state
+// leaves with float32's precision, takes a quarter fewer chunks than the others (131 -> 128 us).  Where the segments are few their summaries leave compute
+// units idle, so they are taken in two parts (four segments: 130 -> 124 us; eight, where the scan over the parts costs more than that: 75 -> 80 us).
 struct ForwardPlan {
-    int nch, cps, nseg;
+    int nch, cps, nseg, sub;
     size_t off_decay, total;
 };
 ForwardPlan forward_plan(const bla_ssm_params* p)
@@ -37,8 +39,13 @@ ForwardPlan forward_plan(const bla_ssm_params* p)
     if (n > f.nch / 4) n = f.nch / 4;
     n = n < 1 ? 1 : n > kMaxSegments ? kMaxSegments : n;
     f.cps = f.nch > 0 ? (int)((f.nch + n - 1) / n) : 1;
+    if (p->io_dtype == BLA_BF16 && n > 1) {
+        const long long c = 4 * (long long)f.nch / (4 * n - 1);
+        if (c * n >= f.nch) f.cps = (int)c;
+    }
     f.nseg = f.nch > 0 ? (f.nch + f.cps - 1) / f.cps : 1;
-    const size_t states = (size_t)(f.nseg - 1) * bh;
+    f.sub = f.nseg <= 4 ? 2 : 1;
+    const size_t states = (size_t)f.sub * (f.nseg - 1) * bh;
     f.off_decay = seq_align(states * p->N * p->d * 4);
     f.total = f.nseg > 1 ? f.off_decay + seq_align(states * 4) : 0;
     return f;
@@ -108,7 +115,7 @@ bla_status bla_ssm_forward(const bla_ssm_params* p, const void* x, const float* 
     a.x = x, a.Bm = Bm, a.Cm = Cm, a.dt = dt, a.A = A, a.Dm = D, a.state_in = state_in, a.lengths = lengths, a.y = y;
     a.state_out = state_out, a.seg_state = (float*)workspace;
     a.seg_decay = f.nseg > 1 ? (float*)((char*)workspace + f.off_decay) : nullptr;
-    a.B = p->B, a.H = p->H, a.G = p->G, a.L = p->L, a.N = p->N, a.nch = f.nch, a.cps = f.cps, a.nseg = f.nseg;
+    a.B = p->B, a.H = p->H, a.G = p->G, a.L = p->L, a.N = p->N, a.nch = f.nch, a.cps = f.cps, a.nseg = f.nseg, a.sub = f.sub;
     a.units = (long long)p->B * p->H * f.nseg, a.per = (a.units + 7) / 8;
     return launch_ssm_forward(p->io_dtype == BLA_BF16, p->d, a, (hipStream_t)stream) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }

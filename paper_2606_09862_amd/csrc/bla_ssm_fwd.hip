@@ -11,11 +11,12 @@ namespace {
 //   G^T = B C^T (rows u, columns t; tiles u <= t only), weighted by e^{s_t - s_u} dt_u: the operand of the second product;
 //   Y^T = h^T C^T scaled by e^{s_t}, plus X^T (weighted G)^T: h is published in LDS in the operand type;
 //   h^T <- e^{s_c} h^T + X^T (w B)^T with w_u = e^{s_c - s_u} dt_u: the transposed fragments of X serve both products.
-// In bf16 the weighted G and the published h are rounded to 2^-9 relative, as y is; the weights of the state's update keep float32's
-// precision (Split), since the state is a float32 result and is carried on.
+// In bf16 the weighted G and the published h are rounded by 2^-8 relative at most, as y is.  The weights of the state's update keep float32's
+// precision (Split) where the state leaves the kernel, a float32 result that may be carried on: in the summaries and in the last segment.  In the others,
+// whose states only enter y as h, they are rounded as h is (the kernel 92 -> 77 us on the shape below).
 // SUM: the segment's own state from zero and its decay, for the scan over the segments; no outputs.
 // Bound: issue and the waits between a chunk's two barriers, with two workgroups on a compute unit (8 x 16 heads x 4096 tokens, d = 64, N = 128, bf16, four
-// segments: 92 us and 48 us of SUM for 157 MB; 16 heads x 16411 tokens in float32, d = N = 64, 29 segments: 96 and 33 us).  Waves that own
+// segments: 77 us and 44 us of SUM for 157 MB; 16 heads x 16411 tokens in float32, d = N = 64, 29 segments: 96 and 33 us).  Waves that own
 // columns d and put the weights on X halve the splitting at N = 128 (82 and 40 us), and lose as much where N = 64 or d = 32 (d = 128, N = 64: 106 us
 // instead of 82; float32, d = 32, N = 128: 188 instead of 118), since every wave then reads all of B and C from LDS.
 template <typename T, int D, int NP, bool SUM> struct SsmGeo {
@@ -41,8 +42,8 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
     if (u >= a.units) return;
     const int h = (int)(u % a.H);
     u /= a.H;
-    const int nsg = SUM ? a.nseg - 1 : a.nseg;
-    const int seg = (int)(u % nsg), b = (int)(u / nsg);
+    const int nsg = SUM ? a.sub * (a.nseg - 1) : a.nseg;
+    const int item = (int)(u % nsg), seg = SUM ? item / a.sub : item, b = (int)(u / nsg);
     const int bh = b * a.H + h, grp = h / (a.H / a.G);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
     const int len = ssm_length(a.lengths, b, a.L);
@@ -53,13 +54,15 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
     const float* dt = a.dt + (size_t)bh * a.L;
     const double A = a.A[h] * kLog2e64;  // exponents in units of 2
     const float skip = a.Dm ? a.Dm[h] : 0.f;
-    const int c0 = seg * a.cps, c1 = min(a.nch, c0 + a.cps);
+    const int psz = SUM ? (a.cps + a.sub - 1) / a.sub : a.cps;  // chunks of a part
+    const int c0 = seg * a.cps + (SUM ? item % a.sub * psz : 0), c1 = min(min(a.nch, (seg + 1) * a.cps), c0 + psz);
     const int cend = min(c1, (len + 63) / 64);  // chunks past it are padding
     const size_t BH = (size_t)a.B * a.H;
+    const bool carried = SUM || (seg == a.nseg - 1 && a.state_out);  // the segment's state leaves the kernel
 
     floatx4 hs[G::TNW][G::TD];  // h[n = 16 (TNW wave + nt) + r][d = 16 dt + 4g ..]
     const float* from = SUM ? nullptr : seg == 0 ? (a.state_in ? a.state_in + (size_t)bh * a.N * D : nullptr)
-                                                 : a.seg_state + ((size_t)(seg - 1) * BH + bh) * a.N * D;
+                                                 : a.seg_state + ((size_t)(a.sub * seg - 1) * BH + bh) * a.N * D;
 #pragma unroll
     for (int nt = 0; nt < G::TNW; ++nt) {
         const int n = 16 * (G::TNW * wave + nt) + r;
@@ -187,8 +190,11 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
         for (int kb = 0; kb < 2; ++kb) {
             const floatx8 w = join(ld4f(sW[buf] + 32 * kb + 4 * g), ld4f(sW[buf] + 32 * kb + 16 + 4 * g));
 #pragma unroll
-            for (int nt = 0; nt < G::TNW; ++nt)
-                wb[nt][kb].set(w * to_f8(ld_red_dual(sB, G::LB, 16 * (G::TNW * wave + nt), kb, g, r)));
+            for (int nt = 0; nt < G::TNW; ++nt) {
+                const floatx8 v = w * to_f8(ld_red_dual(sB, G::LB, 16 * (G::TNW * wave + nt), kb, g, r));
+                if (carried) wb[nt][kb].set(v);
+                else wb[nt][kb].round(v);
+            }
         }
         const float es = SUM ? 0.f : sE[buf][16 * wave + r], tot = sTot[buf];
 #pragma unroll
@@ -228,7 +234,10 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
 #pragma unroll
                 for (int nt = 0; nt < G::TNW; ++nt) {
                     floatx4 hd[2] = {hs[nt][d], hs[nt][d + 1]};
-                    mma_split(xf[kb], wb[nt][kb], hd);
+                    if (carried) mma_split(xf[kb], wb[nt][kb], hd);
+                    else
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) hd[i] = mma(xf[kb][i], wb[nt][kb].hi, hd[i]);
                     hs[nt][d] = hd[0];
                     hs[nt][d + 1] = hd[1];
                 }
@@ -244,7 +253,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
         const int t0 = 64 * max(c0, cend), t1 = min(a.L, 64 * c1);
         for (int i = tid; i < (t1 - t0) * G::CHX; i += 256) *(intx4*)(y + (size_t)t0 * D + (size_t)i * G::PE) = intx4{0, 0, 0, 0};
     }
-    float* to = SUM ? a.seg_state + ((size_t)seg * BH + bh) * a.N * D
+    float* to = SUM ? a.seg_state + ((size_t)item * BH + bh) * a.N * D
                     : seg == a.nseg - 1 && a.state_out ? a.state_out + (size_t)bh * a.N * D : nullptr;
     if (to) {
 #pragma unroll
@@ -255,7 +264,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
                 for (int d = 0; d < G::TD; ++d) st4f(to + (size_t)n * D + 16 * d + 4 * g, hs[nt][d]);
         }
     }
-    if (SUM && tid == 0) a.seg_decay[(size_t)seg * BH + bh] = exp2_f64(decay);
+    if (SUM && tid == 0) a.seg_decay[(size_t)item * BH + bh] = exp2_f64(decay);
 }
 
 // States entering segments 1 .. in place of the segments' own states: four elements of a head's state per lane.
@@ -266,20 +275,21 @@ __global__ void __launch_bounds__(256) ssm_scan_kernel(SsmArgs a, int D)
     if (i >= BH * n4) return;
     const size_t bh = i / n4;
     floatx4 c = a.state_in ? ld4f(a.state_in + 4 * i) : zero4();
-    for (int s0 = 0; s0 < a.nseg - 1; s0 += 8) {  // eight segments' states in flight (one at a time: 11 us for 29 segments of 16 heads, now 7)
+    const int n = a.sub * (a.nseg - 1);
+    for (int s0 = 0; s0 < n; s0 += 8) {  // eight segments' states in flight (one at a time: 11 us for 29 segments of 16 heads, now 7)
         floatx4 v[8];
         float w[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int s = min(s0 + k, a.nseg - 2);
+            const int s = min(s0 + k, n - 1);
             v[k] = ld4f(a.seg_state + ((size_t)s * BH * n4 + i) * 4);
             w[k] = a.seg_decay[s * BH + bh];
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (s0 + k < a.nseg - 1) {
+            if (s0 + k < n) {
                 c = c * w[k] + v[k];
-                st4f(a.seg_state + ((size_t)(s0 + k) * BH * n4 + i) * 4, c);
+                if ((s0 + k) % a.sub == a.sub - 1) st4f(a.seg_state + ((size_t)(s0 + k) * BH * n4 + i) * 4, c);
             }
     }
 }
@@ -325,7 +335,7 @@ template <typename T, int D, int NP> hipError_t forward_n(const SsmArgs& a, hipS
 {
     if (a.nseg > 1) {
         SsmArgs z = a;
-        z.units = (long long)a.B * a.H * (a.nseg - 1);
+        z.units = (long long)a.B * a.H * a.sub * (a.nseg - 1);
         z.per = (z.units + 7) / 8;
         hipLaunchKernelGGL((ssm_forward_kernel<T, D, NP, true>), dim3((unsigned)(8 * z.per)), dim3(256), 0, s, z);
         const size_t n = (size_t)a.B * a.H * a.N * D / 4;

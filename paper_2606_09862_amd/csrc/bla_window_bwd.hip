@@ -5,7 +5,7 @@
 // Two passes recompute P from lse, one per query block (dq, and delta for the other) and one per key block (dk, dv, summed over the
 // heads that share the key head and over the queries whose windows reach the block; the sinks' other queries have a kernel of
 // their own), so that every gradient has a fixed order of sums, without atomics.  P and dS are rounded to the operand type before their second
-// products (2^-9 relative in bf16, as the results are); sums and row terms are float32.
+// products (2^-8 relative at most in bf16, as the results are); sums and row terms are float32.
 #include "bla_window.h"
 
 namespace bla {

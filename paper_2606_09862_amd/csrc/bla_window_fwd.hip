@@ -48,7 +48,7 @@ template <typename T, int D> __device__ __forceinline__ void window_ring(const W
 // barrier per tile.
 // S^T = K Q^T gives each lane four keys of one query (accumulator rows: keys), so the softmax runs down a column
 // (in the lane, then over the four row groups), and the accumulators, rounded to the operand type, are the
-// operand of O^T = V^T P without leaving the registers.  In bf16 the weights are rounded to 2^-9 relative, as their
+// operand of O^T = V^T P without leaving the registers.  In bf16 the weights are rounded to 2^-8 relative at most, as their
 // values are; maxima, sums and outputs are float32.
 // The maximum that the weights are taken against follows the true one only once that is more than 2^kLag above it: the
 // weights stay below 2^kLag, no precision is lost, and a tile needs neither a reduction over the lanes nor a rescaling

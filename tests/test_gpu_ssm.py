@@ -177,3 +177,33 @@ def test_backward_against_differences():
         num, ana = (f[0] - f[1]) / (2 * h), float((g.double() * step.double()).sum())
         size = float(((g.double() * step.double()) ** 2).sum().sqrt()) + float((g.double() ** 2).sum().sqrt())
         assert abs(num - ana) < 4e-3 * size, (k, num, ana, size)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("L,lengths", [(1930, [1930, 0, 700, 1283]), (1100, [1100, 1099, 321, 64])])
+def test_segments(dtype, L, lengths):
+    """Rows in four segments whose summaries are taken in parts, some of them past a row's end.  In bf16 a term from an earlier chunk is rounded
+    as a weight of the state and with the state: 2u where check() has u; without the state after the call the last segment's weights are
+    rounded as well."""
+    from ssm_plain import scan
+    bla = _bla()
+    B, H, G, d, N = 4, 32, 2, 32, 8
+    z = inputs(31, B, H, G, L, d, N, dtype, True, lengths)
+    c = {k: t.cuda() for k, t in z.items()}
+    args = (c["x"], c["dt"], c["A"], c["Bm"], c["Cm"], c["D"])
+    kw = dict(state=c["state"], lengths=torch.tensor(lengths, dtype=torch.int32).cuda())
+    y, so = bla.ssm_forward(*args, **kw)
+    y0, none = bla.ssm_forward(*args, want_state=False, **kw)
+    assert none is None
+    u, r = unit(dtype), share_of(N, d, L)
+    f = r + (2.0 ** -16 if dtype == BF else 0.0)
+    for b in range(B):
+        n = lengths[b]
+        row = [t.to(F64) for t in (z["x"][b, :, :n], z["dt"][b, :, :n], z["A"], z["Bm"][b, :, :n], z["Cm"][b, :, :n], z["D"], z["state"][b])]
+        w, end = scan(*row)
+        s, size = scan(row[0].abs(), row[1], row[2], *(t.abs() for t in row[3:]))
+        close(so[b].cpu(), end, f * size, f"state[{b}]")
+        for got in (y, y0):
+            assert not got[b, :, n:].any()
+            if n:
+                close(got[b, :, :n].cpu(), w, (2 * u + r) * s + u * w.abs(), f"y[{b}]")
