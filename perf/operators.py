@@ -243,7 +243,7 @@ def _own(s):
                                             want_cache=c["cached"])
         return [o, lse] + ([ck, cv] if c["cached"] else [])
     if kind == "window_backward":
-        return list(bla.window_backward(s["q"], s["k"], s["v"], s["o"], s["lse"], s["dO"], c["window"], c["sinks"],
+        return list(bla.window_backward(s["q"], s["k"], s["v"], s["o"].contiguous(), s["lse"].contiguous(), s["dO"], c["window"], c["sinks"],
                                         lengths=s["lengths"]))
     if kind == "window_step":
         o = bla.window_step(s["q"], s["k"], s["v"], c["window"], c["sinks"], s["cache_k"], s["cache_v"], pos=s["pos"], out=s["o"])
