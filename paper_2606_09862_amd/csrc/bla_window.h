@@ -52,6 +52,7 @@ struct WindowBwdArgs {
     int ns, ssplit;                 // sinks of a sequence, parts of the queries that see them from beyond their windows
     float *near, *part;             // float32 dk and dv of the sinks: [B Hkv][ns][2][D], [ssplit][B Hkv][ns][2][D]
     long long q_units, q_per, k_units, k_per;
+    unsigned s_units;               // workgroups of the sinks' far queries
 };
 
 // Tokens of row b in this call, and the position of its first.

@@ -228,6 +228,7 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
     a.part = (float*)((char*)workspace + b.off_part);
     a.nqb = b.nqb, a.nkb = b.nkb, a.ns = b.ns, a.ssplit = b.ssplit;
     a.q_units = b.q_units, a.q_per = (b.q_units + 7) / 8, a.k_units = b.k_units, a.k_per = (b.k_units + 7) / 8;
+    a.s_units = (unsigned)((long long)p->B * p->H_kv * ((b.ns + 15) / 16) * b.ssplit);
     return launch_window_backward(bf16, p->d, a, (hipStream_t)stream) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }
 

@@ -3,8 +3,8 @@
 // With P = exp(scale q k - lse) on the visible pairs and delta_i = sum_c dO_ic o_ic:
 //   dS = P (dO v^T - delta),   dq = scale dS k,   dk = scale dS^T q,   dv = P^T dO.
 // Two passes recompute P from lse, one per query block (dq, and delta for the other) and one per key block (dk, dv, summed over the
-// heads that share the key head and over the queries whose windows reach the block; the sinks' other queries have a kernel of
-// their own), so that every gradient has a fixed order of sums, without atomics.  P and dS are rounded to the operand type before their second
+// heads that share the key head and over the queries whose windows reach the block; the sinks' other queries have
+// workgroups of their own), so that every gradient has a fixed order of sums, without atomics.  P and dS are rounded to the operand type before their second
 // products (2^-8 relative at most in bf16, as the results are); sums and row terms are float32.
 #include "bla_window.h"
 
@@ -175,11 +175,110 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
     }
 }
 
+// The pairs of sinks and the queries that see them from beyond their windows.  A wave takes 16 sinks and every so-maniest 32 queries of every head of
+// the group, on its own: rows of Q and dO come from memory as operands of S and dP, and through LDS that only the wave touches
+// as the transposed operands of dV^T and dK^T.  The four waves are added up in LDS, a workgroup writes one part.  Bound: the bytes of Q
+// and dO (128 x 4096 tokens at d = 64, window 511, 4 sinks: 117 MB).  As part of the key walk these queries took a fifth of the
+// workgroups for one wave's work each: 251 us with them, 204 without.
+template <typename T, int D> __device__ __forceinline__ void window_bwd_sinks(const WindowBwdArgs& a, unsigned u, char* raw)
+{
+    typedef typename Frag<T>::type F;
+    constexpr int LD = dual_ld<T>(D), LO = D + 4;
+    constexpr size_t QB = sizeof(T) * 4 * 2 * 32 * LD, OB = sizeof(float) * 4 * 16 * LO;
+    static_assert(QB <= sizeof(T) * 256 * BwdGeo<T, D>::LD && OB <= QB, "the key kernel's LDS");
+    const int part = (int)(u % (unsigned)a.ssplit);
+    u /= (unsigned)a.ssplit;
+    const int nst = (a.ns + 15) / 16, st = (int)(u % (unsigned)nst);
+    u /= (unsigned)nst;
+    const int hk = (int)(u % (unsigned)a.Hkv), b = (int)(u / (unsigned)a.Hkv);
+    const int grp = a.H / a.Hkv;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
+    const int len = a.lengths ? min(max(a.lengths[b], 0), a.L) : a.L;
+    const int j = 16 * st + r;                                                // the lane's sink
+    const long long first = (long long)16 * st + a.W;                        // the first query past a window that holds one
+    const int q_first = (int)min(first, (long long)len), blocks = (len - q_first + 31) / 32;
+
+    F kf[D / 32], vf[D / 32];
+    {
+        const size_t at = (((size_t)b * a.Hkv + hk) * a.L + min(j, a.L - 1)) * D;
+        const bool in = j < a.ns && j < len;
+#pragma unroll
+        for (int kb = 0; kb < D / 32; ++kb) {
+            kf[kb] = in ? ld_nat((const T*)a.k + at, kb, g) : zero_frag<T>();
+            vf[kb] = in ? ld_nat((const T*)a.v + at, kb, g) : zero_frag<T>();
+        }
+    }
+    // the lane's sink is seen from beyond its window by the queries from j + W on
+    const int q_sink = j < a.ns && j < len ? (int)min((long long)j + a.W, (long long)len) : len;
+    floatx4 dk[D / 16], dv[D / 16];
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) dk[dt] = dv[dt] = zero4();
+    const float sc = a.scale * kLog2e;
+    T *sQ = (T*)raw + wave * 2 * 32 * LD, *sD = sQ + 32 * LD;
+
+    for (long long it = part * 4 + wave; it < (long long)grp * blocks; it += a.ssplit * 4) {
+        const int hg = (int)(it / blocks), q0 = q_first + 32 * (int)(it % blocks);
+        const size_t row0 = ((size_t)b * a.H + hk * grp + hg) * a.L;
+        floatx4 s[2], dp[2];
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt) {
+            const size_t at = (row0 + min(q0 + 16 * qt + r, len - 1)) * D;
+            s[qt] = dp[qt] = zero4();
+#pragma unroll
+            for (int kb = 0; kb < D / 32; ++kb) {
+                const F qf = ld_nat((const T*)a.q + at, kb, g), df = ld_nat((const T*)a.dO + at, kb, g);
+                *(F*)(sQ + (16 * qt + r) * LD + 32 * kb + 8 * g) = qf;
+                *(F*)(sD + (16 * qt + r) * LD + 32 * kb + 8 * g) = df;
+                s[qt] = mma(qf, kf[kb], s[qt]);
+                dp[qt] = mma(df, vf[kb], dp[qt]);
+            }
+        }
+#pragma unroll
+        for (int qt = 0; qt < 2; ++qt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int q = q0 + 16 * qt + 4 * g + e;
+                const size_t at = row0 + min(q, len - 1);
+                const float p = exp2_fast(__builtin_fmaf(s[qt][e], sc, -a.lse[at] * kLog2e));
+                const bool seen = (q >= q_sink) & (q < len);
+                s[qt][e] = seen ? p : 0.f;
+                dp[qt][e] = seen ? p * (dp[qt][e] - a.delta[at]) : 0.f;
+            }
+        const F pf = frag_from_acc<T>(s[0], s[1]), sf = frag_from_acc<T>(dp[0], dp[1]);
+        // the wave's own stores above, read by its other lanes (LDS serves a wave in order)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+            dv[dt] = mma(ld_red_dual(sD, LD, 16 * dt, 0, g, r), pf, dv[dt]);
+            dk[dt] = mma(ld_red_dual(sQ, LD, 16 * dt, 0, g, r), sf, dk[dt]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    float* sO = (float*)raw;
+    for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) st4f(sO + (wave * 16 + r) * LO + 16 * dt + 4 * g, which ? dv[dt] : dk[dt]);
+        __syncthreads();
+        for (int i = tid; i < 16 * (D / 4); i += 256) {
+            const int key = i / (D / 4), c = 4 * (i % (D / 4));
+            if (16 * st + key >= a.ns) continue;
+            floatx4 x = ld4f(sO + key * LO + c);
+#pragma unroll
+            for (int w = 1; w < 4; ++w) x += ld4f(sO + (w * 16 + key) * LO + c);
+            st4f(a.part + (((((size_t)part * a.B + b) * a.Hkv + hk) * a.ns + 16 * st + key) * 2 + which) * D + c, x);
+        }
+    }
+}
+
 // Key pass.  Wave w owns 16 KT keys: their K and V are operands in registers for the whole walk, and S = Q K^T and
 // dP = dO V^T (accumulator rows: queries) give P and dS as operands of dV^T = dO^T P and dK^T = Q^T dS.  The walk goes over the
 // heads of the group and the 64-query tiles whose windows hold keys of the block.  Later queries see sinks as well: those pairs
-// are window_bwd_sink_kernel's, and the sinks' gradients go out in float32 for window_bwd_sum_kernel to add up.
-// Bound: issue (the query pass's shape: 203-215 us).
+// are window_bwd_sinks', and the sinks' gradients go out in float32 for window_bwd_sum_kernel to add up.
+// Bound: issue (the query pass's shape: 203-215 us of keys; with the sinks' workgroups 221-235, which took 31 us in a launch of their own and 340
+// us in all where they were spread among the keys').
 template <typename T, int D>
 __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
 {
@@ -189,6 +288,10 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
     __shared__ __attribute__((aligned(16))) T lds[2 * BUF];
     __shared__ __attribute__((aligned(16))) float sStat[2][2][64];
 
+    if (blockIdx.x >= 8 * a.k_per) {  // last: they fill the compute units that run out of keys
+        window_bwd_sinks<T, D>(a, blockIdx.x - (unsigned)(8 * a.k_per), (char*)lds);
+        return;
+    }
     long long u = xcd_unit(blockIdx.x, a.k_per);
     if (u >= a.k_units) return;
     const int grp = a.H / a.Hkv;
@@ -345,105 +448,6 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
     }
 }
 
-// The pairs of sinks and the queries that see them from beyond their windows.  A wave takes 16 sinks and every so-maniest 32 queries of every head of
-// the group, on its own: rows of Q and dO come from memory as operands of S and dP, and through LDS that only the wave touches
-// as the transposed operands of dV^T and dK^T.  The four waves are added up in LDS, a workgroup writes one part.  Bound: the bytes of Q
-// and dO.  (128 x 4096 tokens at d = 64, window 511, 4 sinks: 31 us for 117 MB.  In the key kernel these queries took a fifth of the
-// workgroups for one wave's work each: 251 us with them, 204 without.)
-template <typename T, int D> __global__ void __launch_bounds__(256) window_bwd_sink_kernel(WindowBwdArgs a)
-{
-    typedef typename Frag<T>::type F;
-    constexpr int LD = dual_ld<T>(D), LO = D + 4;
-    constexpr size_t QB = sizeof(T) * 4 * 2 * 32 * LD, OB = sizeof(float) * 4 * 16 * LO;
-    __shared__ __attribute__((aligned(16))) char raw[QB > OB ? QB : OB];
-    unsigned u = blockIdx.x;
-    const int part = (int)(u % (unsigned)a.ssplit);
-    u /= (unsigned)a.ssplit;
-    const int nst = (a.ns + 15) / 16, st = (int)(u % (unsigned)nst);
-    u /= (unsigned)nst;
-    const int hk = (int)(u % (unsigned)a.Hkv), b = (int)(u / (unsigned)a.Hkv);
-    const int grp = a.H / a.Hkv;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
-    const int len = a.lengths ? min(max(a.lengths[b], 0), a.L) : a.L;
-    const int j = 16 * st + r;                                                // the lane's sink
-    const long long first = (long long)16 * st + a.W;                        // the first query past a window that holds one
-    const int q_first = (int)min(first, (long long)len), blocks = (len - q_first + 31) / 32;
-
-    F kf[D / 32], vf[D / 32];
-    {
-        const size_t at = (((size_t)b * a.Hkv + hk) * a.L + min(j, a.L - 1)) * D;
-        const bool in = j < a.ns && j < len;
-#pragma unroll
-        for (int kb = 0; kb < D / 32; ++kb) {
-            kf[kb] = in ? ld_nat((const T*)a.k + at, kb, g) : zero_frag<T>();
-            vf[kb] = in ? ld_nat((const T*)a.v + at, kb, g) : zero_frag<T>();
-        }
-    }
-    // the lane's sink is seen from beyond its window by the queries from j + W on
-    const int q_sink = j < a.ns && j < len ? (int)min((long long)j + a.W, (long long)len) : len;
-    floatx4 dk[D / 16], dv[D / 16];
-#pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) dk[dt] = dv[dt] = zero4();
-    const float sc = a.scale * kLog2e;
-    T *sQ = (T*)raw + wave * 2 * 32 * LD, *sD = sQ + 32 * LD;
-
-    for (long long it = part * 4 + wave; it < (long long)grp * blocks; it += a.ssplit * 4) {
-        const int hg = (int)(it / blocks), q0 = q_first + 32 * (int)(it % blocks);
-        const size_t row0 = ((size_t)b * a.H + hk * grp + hg) * a.L;
-        floatx4 s[2], dp[2];
-#pragma unroll
-        for (int qt = 0; qt < 2; ++qt) {
-            const size_t at = (row0 + min(q0 + 16 * qt + r, len - 1)) * D;
-            s[qt] = dp[qt] = zero4();
-#pragma unroll
-            for (int kb = 0; kb < D / 32; ++kb) {
-                const F qf = ld_nat((const T*)a.q + at, kb, g), df = ld_nat((const T*)a.dO + at, kb, g);
-                *(F*)(sQ + (16 * qt + r) * LD + 32 * kb + 8 * g) = qf;
-                *(F*)(sD + (16 * qt + r) * LD + 32 * kb + 8 * g) = df;
-                s[qt] = mma(qf, kf[kb], s[qt]);
-                dp[qt] = mma(df, vf[kb], dp[qt]);
-            }
-        }
-#pragma unroll
-        for (int qt = 0; qt < 2; ++qt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int q = q0 + 16 * qt + 4 * g + e;
-                const size_t at = row0 + min(q, len - 1);
-                const float p = exp2_fast(__builtin_fmaf(s[qt][e], sc, -a.lse[at] * kLog2e));
-                const bool seen = (q >= q_sink) & (q < len);
-                s[qt][e] = seen ? p : 0.f;
-                dp[qt][e] = seen ? p * (dp[qt][e] - a.delta[at]) : 0.f;
-            }
-        const F pf = frag_from_acc<T>(s[0], s[1]), sf = frag_from_acc<T>(dp[0], dp[1]);
-        // the wave's own stores above, read by its other lanes (LDS serves a wave in order)
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) {
-            dv[dt] = mma(ld_red_dual(sD, LD, 16 * dt, 0, g, r), pf, dv[dt]);
-            dk[dt] = mma(ld_red_dual(sQ, LD, 16 * dt, 0, g, r), sf, dk[dt]);
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
-    float* sO = (float*)raw;
-    for (int which = 0; which < 2; ++which) {
-        __syncthreads();
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) st4f(sO + (wave * 16 + r) * LO + 16 * dt + 4 * g, which ? dv[dt] : dk[dt]);
-        __syncthreads();
-        for (int i = tid; i < 16 * (D / 4); i += 256) {
-            const int key = i / (D / 4), c = 4 * (i % (D / 4));
-            if (16 * st + key >= a.ns) continue;
-            floatx4 x = ld4f(sO + key * LO + c);
-#pragma unroll
-            for (int w = 1; w < 4; ++w) x += ld4f(sO + (w * 16 + key) * LO + c);
-            st4f(a.part + (((((size_t)part * a.B + b) * a.Hkv + hk) * a.ns + 16 * st + key) * 2 + which) * D + c, x);
-        }
-    }
-}
-
 // dk and dv of the sinks: the key kernel's and the parts, added in order.
 template <typename T, int D> __global__ void __launch_bounds__(256) window_bwd_sum_kernel(WindowBwdArgs a)
 {
@@ -465,11 +469,8 @@ template <typename T, int D> hipError_t backward_d(const WindowBwdArgs& a, hipSt
 {
     typedef BwdGeo<T, D> G;
     hipLaunchKernelGGL((window_bwd_q_kernel<T, D>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
-    hipLaunchKernelGGL((window_bwd_k_kernel<T, D>), dim3((unsigned)(8 * a.k_per)), dim3(G::NT), 0, s, a);
+    hipLaunchKernelGGL((window_bwd_k_kernel<T, D>), dim3((unsigned)(8 * a.k_per) + a.s_units), dim3(G::NT), 0, s, a);
     if (a.ns > 0) {
-        const int tiles = (a.ns + 15) / 16;
-        hipLaunchKernelGGL((window_bwd_sink_kernel<T, D>), dim3((unsigned)((long long)a.B * a.Hkv * tiles * a.ssplit)), dim3(256), 0,
-                           s, a);
         const long long n = (long long)a.B * a.Hkv * a.ns * (2 * D / 4);
         hipLaunchKernelGGL((window_bwd_sum_kernel<T, D>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
     }
