@@ -55,8 +55,8 @@ template <typename T, int D> __device__ __forceinline__ void window_ring(const W
 // unless some lane has found such a score.
 // Bound: issue.  A SIMD's vector and matrix instructions hardly overlap, and a score costs an exponential, a multiply-add and its part of
 // maximum, sum and conversion beside its products (8 x 16 heads x 4096 queries, four heads to a key head, d = 64, window 1024, bf16:
-// 190-210 us, 580-640 TFLOP/s of visible pairs; the first form, a wave to 16 queries of 4-wave groups with a reduction a tile, 337 us.  16 heads x 65536,
-// d = 128, window 255: 320-335 us for 1.08 GB, 3.3 TB/s; first form 893).
+// 190-220 us, 550-640 TFLOP/s of visible pairs; the first form, a wave to 16 queries of 4-wave groups with a reduction a tile, 337 us.  16 heads x 65536,
+// d = 128, window 255: 320-343 us for 1.08 GB, 3.3 TB/s; first form 893).
 template <typename T, int D, int NW> struct WinGeo {
     static constexpr int BQ = 16 * NW, NT = 64 * NW;
     static constexpr int LK = nat_ld<T>(D), LV = red_ld<T>(D);
