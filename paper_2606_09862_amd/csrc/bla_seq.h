@@ -47,7 +47,6 @@ template <typename T> __host__ __device__ constexpr int red_ld(int D) { return s
 // transposing reads one overlap in eight rows (the 8 x odd dwords that avoid it need a swizzle for the row reads and a sixth
 // more LDS, which costs a workgroup per compute unit).
 template <typename T> __host__ __device__ constexpr int dual_ld(int D) { return nat_ld<T>(D); }
-template <typename T> __device__ __forceinline__ int dual_col(int, int col) { return col; }
 // rows x0 .. x0+15 as a natural-order fragment
 template <typename T>
 __device__ __forceinline__ typename Frag<T>::type ld_nat_dual(const T* M, int ld, int x0, int kb, int g, int r)

@@ -99,7 +99,7 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
 #pragma unroll
         for (int k = 0; k < PB; ++k) {
             const int row = (k * 256 + tid) / CHB, ch = (k * 256 + tid) % CHB;
-            *(intx4*)(sB[buf] + row * LB + dual_col<T>(row, ch * PE)) = br[k];
+            *(intx4*)(sB[buf] + row * LB + ch * PE) = br[k];
         }
         if (wave == 0) {
             const double s = wave_scan((double)dtr * A, lane), tot = wave_last(s);
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                 o *= f_me;
                 if (wave < 2) o = mma(ld_red_dual(s1, LD1, 16 * d, 0, g, r), kf[0], o);
                 o = mma(ld_red_dual(s1, LD1, 16 * d, 1, g, r), kf[1], o);
-                const floatx4 yt = to_f4(ld4<T>(s1 + me * LD1 + dual_col<T>(me, 16 * d + 4 * g)));
+                const floatx4 yt = to_f4(ld4<T>(s1 + me * LD1 + 16 * d + 4 * g));
                 if (64 * c + me < a.L) st4((T*)a.dx + (tok + me) * D + 16 * d + 4 * g, me < n ? dt_me * o + skip * yt : zero4());
             }
         }

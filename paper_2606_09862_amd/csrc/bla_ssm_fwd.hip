@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
 #pragma unroll
         for (int i = 0; i < G::PB; ++i) {
             const int row = (i * 256 + tid) / G::CHB, ch = (i * 256 + tid) % G::CHB;
-            *(intx4*)(sB + row * G::LB + dual_col<T>(row, ch * G::PE)) = br[i];
+            *(intx4*)(sB + row * G::LB + ch * G::PE) = br[i];
         }
         if (!SUM) {
 #pragma unroll

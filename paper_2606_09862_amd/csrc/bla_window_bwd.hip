@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
 #pragma unroll
         for (int ps = 0; ps < G::NP; ++ps) {
             const int i = ps * G::RPP + lrow;
-            *(intx4*)(sK + i * G::LD + dual_col<T>(i, ch * G::PE)) = kr[ps];
+            *(intx4*)(sK + i * G::LD + ch * G::PE) = kr[ps];
             *(intx4*)(sV + i * G::LN + ch * G::PE) = vr[ps];
         }
         __syncthreads();
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
             float(*stat)[64] = sStat[buf];
 #pragma unroll
             for (int ps = 0; ps < G::NP; ++ps) {
-                    const int i = ps * G::RPP + lrow, at = i * G::LD + dual_col<T>(i, ch * G::PE);
+                    const int i = ps * G::RPP + lrow, at = i * G::LD + ch * G::PE;
                 *(intx4*)(sQ + at) = qr[ps];
                 *(intx4*)(sD + at) = dr[ps];
             }
