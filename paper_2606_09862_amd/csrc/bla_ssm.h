@@ -5,7 +5,9 @@
 // up to t and s_c its whole sum:
 //   y_t   = sum_{u <= t} e^{s_t - s_u} dt_u (C_t . B_u) x_u + e^{s_t} h_in^T C_t + D x_t
 //   h_out = e^{s_c} h_in + sum_u e^{s_c - s_u} dt_u B_u x_u^T
-// Only differences s_t - s_u of a chunk are exponentiated, so nothing overflows where A <= 0.  The sums s run in float64.
+// Only differences s_t - s_u of a chunk are exponentiated, so nothing overflows where A <= 0.  The sums s run in float64 and are
+// kept as two float32 each, so that a difference is as good behind a token that decays by far more than its neighbours (with the upper halves
+// alone y was off by nine times its bound in bf16 behind a token of dt A = -1e6).
 #pragma once
 
 #include "bla_seq.h"

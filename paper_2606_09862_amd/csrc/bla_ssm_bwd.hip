@@ -258,15 +258,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
             return o;
         };
         auto decay = [&](float st, float stl, int i, floatx4& out, bool rows_are_t) {  // e^{s_t - s_u} of four rows
-            const floatx4 s = ld4f(sS + i);
-            floatx4 sl = zero4();
-            if (!two) sl = ld4f(sSl + i);
+            const floatx4 s = ld4f(sS + i), sl = ld4f(sSl + i);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float df = rows_are_t ? s[e] - st : st - s[e];
-                if (!two) df += rows_are_t ? sl[e] - stl : stl - sl[e];
-                out[e] = exp2_fast(df);
-            }
+            for (int e = 0; e < 4; ++e) out[e] = exp2_fast(rows_are_t ? (s[e] - st) + (sl[e] - stl) : (st - s[e]) + (stl - sl[e]));
         };
 
         // ---- columns t

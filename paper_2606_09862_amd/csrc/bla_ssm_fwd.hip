@@ -169,15 +169,9 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int u0 = 32 * hf + 16 * i + 4 * g;
-                    const floatx4 su = ld4f(sS[buf] + u0), du = ld4f(sDt[buf] + u0);
-                    floatx4 sl = zero4();
-                    if (sizeof(T) == 4) sl = ld4f(sSl[buf] + u0);
+                    const floatx4 su = ld4f(sS[buf] + u0), sl = ld4f(sSl[buf] + u0), du = ld4f(sDt[buf] + u0);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float df = st - su[e];
-                        if (sizeof(T) == 4) df += stl - sl[e];
-                        p[i][e] *= exp2_fast(df) * du[e];
-                    }
+                    for (int e = 0; e < 4; ++e) p[i][e] *= exp2_fast((st - su[e]) + (stl - sl[e])) * du[e];
                     if (2 * hf + i >= wave)  // the tile on the diagonal, or the one past it
 #pragma unroll
                         for (int e = 0; e < 4; ++e) p[i][e] = u0 + e <= t ? p[i][e] : 0.f;
