@@ -69,16 +69,10 @@ template <> struct Split<bf16> {
             lo[e] = (bf16)(x - (float)mid[e]);
         }
     }
-    __device__ __forceinline__ void round(floatx8 v)
-    {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) hi[e] = (bf16)v[e];
-    }
 };
 template <> struct Split<float> {
     floatx8 hi;
     __device__ __forceinline__ void set(floatx8 v) { hi = v; }
-    __device__ __forceinline__ void round(floatx8 v) { hi = v; }
 };
 // c[i] += a[i] b for N tiles, term by term: consecutive products belong to different tiles and do not wait for each other.
 template <int N> __device__ __forceinline__ void mma_split(const bf16x8 (&a)[N], const Split<bf16>& b, floatx4 (&c)[N])

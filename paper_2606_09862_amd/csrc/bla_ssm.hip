@@ -23,9 +23,11 @@ bla_status check(const bla_ssm_params* p, bool step)
 }
 
 // Segments of a sequence: enough for the workgroups to fill the device, each of at least four chunks (a segment costs the reading and
-// writing of a state besides; 8 x 16 heads x 4096 tokens, d = 64, N = 128, bf16: 139 us, with half and twice as many workgroups more 151 and 148).  In bf16 the last segment, whose state
-// leaves with float32's precision, takes a quarter fewer chunks than the others (131 -> 128 us).  Where the segments are few their summaries leave compute
-// units idle, so they are taken in two parts (four segments: 130 -> 124 us; eight, where the scan over the parts costs more than that: 75 -> 80 us).
+// writing of a state besides; 8 x 16 heads x 4096 tokens, d = 64, N = 128, bf16: 134 us, with half and twice as many workgroups 151 and 145; 16 heads x 16411
+// tokens, d = N = 64, float32: 126, 142 and 145).  All but the last segment have a summary, so where the segments are few the summaries leave a half
+// to a quarter of the compute units idle, and are taken in two parts.  With more segments the scan over twice the parts costs more than that (4096 tokens, 16
+// heads, d = 64, N = 128, bf16, in one part and in two: 16 rows in two segments 234 and 221 us, 8 rows in four 131 and 124, 6 rows in six 124 and 130, 4 rows in
+// eight 78 and 83; float32 likewise, N = 64 in bf16 alike from six on).
 struct ForwardPlan {
     int nch, cps, nseg, sub;
     size_t off_decay, total;
@@ -39,10 +41,6 @@ ForwardPlan forward_plan(const bla_ssm_params* p)
     if (n > f.nch / 4) n = f.nch / 4;
     n = n < 1 ? 1 : n > kMaxSegments ? kMaxSegments : n;
     f.cps = f.nch > 0 ? (int)((f.nch + n - 1) / n) : 1;
-    if (p->io_dtype == BLA_BF16 && n > 1) {
-        const long long c = 4 * (long long)f.nch / (4 * n - 1);
-        if (c * n >= f.nch) f.cps = (int)c;
-    }
     f.nseg = f.nch > 0 ? (f.nch + f.cps - 1) / f.cps : 1;
     f.sub = f.nseg <= 4 ? 2 : 1;
     const size_t states = (size_t)f.sub * (f.nseg - 1) * bh;

@@ -12,11 +12,11 @@ namespace {
 //   Y^T = h^T C^T scaled by e^{s_t}, plus X^T (weighted G)^T: h is published in LDS in the operand type;
 //   h^T <- e^{s_c} h^T + X^T (w B)^T with w_u = e^{s_c - s_u} dt_u: the transposed fragments of X serve both products.
 // In bf16 the weighted G and the published h are rounded by 2^-8 relative at most, as y is.  The weights of the state's update keep float32's
-// precision (Split) where the state leaves the kernel, a float32 result that may be carried on: in the summaries and in the last segment.  In the others,
-// whose states only enter y as h, they are rounded as h is (the kernel 92 -> 77 us on the shape below).
+// precision (Split) in every segment: the state is a float32 result that is carried on, and y is the same whether it is asked for or not.
+// (Weights rounded once in the segments whose state only enters y: 77 us instead of 95 on the shape below.)
 // SUM: the segment's own state from zero and its decay, for the scan over the segments; no outputs.
 // Bound: issue and the waits between a chunk's two barriers, with two workgroups on a compute unit (8 x 16 heads x 4096 tokens, d = 64, N = 128, bf16, four
-// segments: 77 us and 44 us of SUM for 157 MB; 16 heads x 16411 tokens in float32, d = N = 64, 29 segments: 96 and 33 us).  Waves that own
+// segments: 95-102 us and 43-46 us of SUM for 157 MB; 16 heads x 16411 tokens in float32, d = N = 64, 29 segments: 96 and 33 us).  Waves that own
 // columns d and put the weights on X halve the splitting at N = 128 (82 and 40 us), and lose as much where N = 64 or d = 32 (d = 128, N = 64: 106 us
 // instead of 82; float32, d = 32, N = 128: 188 instead of 118), since every wave then reads all of B and C from LDS.
 template <typename T, int D, int NP, bool SUM> struct SsmGeo {
@@ -58,7 +58,6 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
     const int c0 = seg * a.cps + (SUM ? item % a.sub * psz : 0), c1 = min(min(a.nch, (seg + 1) * a.cps), c0 + psz);
     const int cend = min(c1, (len + 63) / 64);  // chunks past it are padding
     const size_t BH = (size_t)a.B * a.H;
-    const bool carried = SUM || (seg == a.nseg - 1 && a.state_out);  // the segment's state leaves the kernel
 
     floatx4 hs[G::TNW][G::TD];  // h[n = 16 (TNW wave + nt) + r][d = 16 dt + 4g ..]
     const float* from = SUM ? nullptr : seg == 0 ? (a.state_in ? a.state_in + (size_t)bh * a.N * D : nullptr)
@@ -184,11 +183,8 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
         for (int kb = 0; kb < 2; ++kb) {
             const floatx8 w = join(ld4f(sW[buf] + 32 * kb + 4 * g), ld4f(sW[buf] + 32 * kb + 16 + 4 * g));
 #pragma unroll
-            for (int nt = 0; nt < G::TNW; ++nt) {
-                const floatx8 v = w * to_f8(ld_red_dual(sB, G::LB, 16 * (G::TNW * wave + nt), kb, g, r));
-                if (carried) wb[nt][kb].set(v);
-                else wb[nt][kb].round(v);
-            }
+            for (int nt = 0; nt < G::TNW; ++nt)
+                wb[nt][kb].set(w * to_f8(ld_red_dual(sB, G::LB, 16 * (G::TNW * wave + nt), kb, g, r)));
         }
         const float es = SUM ? 0.f : sE[buf][16 * wave + r], tot = sTot[buf];
 #pragma unroll
@@ -228,10 +224,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
 #pragma unroll
                 for (int nt = 0; nt < G::TNW; ++nt) {
                     floatx4 hd[2] = {hs[nt][d], hs[nt][d + 1]};
-                    if (carried) mma_split(xf[kb], wb[nt][kb], hd);
-                    else
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) hd[i] = mma(xf[kb][i], wb[nt][kb].hi, hd[i]);
+                    mma_split(xf[kb], wb[nt][kb], hd);
                     hs[nt][d] = hd[0];
                     hs[nt][d + 1] = hd[1];
                 }
