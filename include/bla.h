@@ -426,7 +426,8 @@ bla_status bla_conv_backward(const bla_conv_params* p, const void* x, const floa
  *   dt: float32 [B, H, L]   A: float32 [H]   D: float32 [H] (NULL = zero)   state: float32 [B, H, N, d] (NULL = zero)
  *   lengths: as for bla_window_forward (padding is not read, y and the gradients are zero there, and the state after the call
  *   is that after the row's last token).
- * A is expected to be <= 0 with dt >= 0 (a decay); the formula is computed for any sign, and overflows where it does.
+ * A is expected to be <= 0 with dt >= 0 (a decay); the formula is computed for any sign, and overflows where it does.  A token's decay below
+ * 2^-16384 counts as 2^-16384 (zero in any type), also where dt A is past float32 or A is minus infinity; ddt and dA take a finite A.
  * A non-finite value in a token may reach the other tokens of its 64-token chunk.
  * Supported: float32 or bfloat16; d in {32, 64, 128}; N a multiple of 8 up to 128; H a multiple of G.  The state and every sum are
  * float32, the sums of dt A float64.  Outputs must not overlap inputs or one another; bla_ssm_step's state_out may be its state_in

@@ -116,6 +116,15 @@ __device__ __forceinline__ floatx8 ld_acc_dual(const float* M, int ld, int x0, i
 
 constexpr double kLog2e64 = 1.4426950408889634;
 
+// The exponent (in units of 2) of a token's decay, from the head's rate A log2 e.  Below -2^14 the decay is zero in any type, whatever the exponent, so it
+// counts as -2^14 there: a sum of exponents keeps its precision behind such a token, and stays finite where dt A does not.
+__device__ __forceinline__ double ssm_rate(float A) { return (double)(A < -__FLT_MAX__ ? -__FLT_MAX__ : A) * kLog2e64; }
+__device__ __forceinline__ double ssm_exponent(float dt, double rate)
+{
+    const double y = (double)dt * rate;
+    return y < -16384.0 ? -16384.0 : y;  // a NaN stays
+}
+
 // 2^y of a float64 exponent to float32 precision: the part of y that float32 cannot hold goes in as a factor 1 + y_lo ln 2.
 __device__ __forceinline__ float exp2_f64(double y)
 {

@@ -46,7 +46,7 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
     const T* x = (const T*)(back ? a.dy : a.x) + (size_t)bh * a.L * D + d0;
     const T* Bm = (const T*)(back ? a.Cm : a.Bm) + ((size_t)b * a.G + grp) * a.L * a.N;
     const float* dt = a.dt + (size_t)bh * a.L;
-    const double A = a.A[h] * kLog2e64;  // exponents in units of 2
+    const double rate = ssm_rate(a.A[h]);
     float* store = (back ? a.leave : a.enter) + (size_t)bh * a.nch * a.N * D + d0;
     const float* from = back ? a.dstate_out : a.state_in;
 
@@ -102,7 +102,7 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
             *(intx4*)(sB[buf] + row * LB + ch * PE) = br[k];
         }
         if (wave == 0) {
-            const double s = wave_scan((double)dtr * A, lane), tot = wave_last(s);
+            const double s = wave_scan(ssm_exponent(dtr, rate), lane), tot = wave_last(s);
             sW[buf][lane] = back ? exp2_f64(s) : exp2_f64(tot - s) * dtr;
             if (lane == 0) sTot[buf] = exp2_f64(tot);
         }
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
 #pragma unroll
             for (int i = 0; i < PS; ++i) held[i] = rst[i];
         if (wave == 0) {
-            const double s = wave_scan((double)d * A * kLog2e64, lane), tot = wave_last(s);
+            const double s = wave_scan(ssm_exponent(d, ssm_rate(a.A[h])), lane), tot = wave_last(s);
             sS[lane] = (float)s;
             sSl[lane] = (float)(s - (double)(float)s);
             sDt[lane] = d;

@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
     const T* Cm = (const T*)a.Cm + ((size_t)b * a.G + grp) * a.L * a.N;
     T* y = SUM ? nullptr : (T*)a.y + (size_t)bh * a.L * D;
     const float* dt = a.dt + (size_t)bh * a.L;
-    const double A = a.A[h] * kLog2e64;  // exponents in units of 2
+    const double rate = ssm_rate(a.A[h]);
     const float skip = a.Dm ? a.Dm[h] : 0.f;
     const int psz = SUM ? (a.cps + a.sub - 1) / a.sub : a.cps;  // chunks of a part
     const int c0 = seg * a.cps + (SUM ? item % a.sub * psz : 0), c1 = min(min(a.nch, (seg + 1) * a.cps), c0 + psz);
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
     float dtr = 0.f;
     auto load_dt = [&](int c) { dtr = c < cend && lane < len - 64 * c ? dt[64 * c + lane] : 0.f; };
     auto exponents = [&](int buf) {  // of the chunk whose dt is loaded
-        const double s = wave_scan((double)dtr * A, lane), tot = wave_last(s);
+        const double s = wave_scan(ssm_exponent(dtr, rate), lane), tot = wave_last(s);
         decay += tot;
         if (!SUM) {
             sS[buf][lane] = (float)s;
@@ -297,7 +297,7 @@ template <typename T, int D, int PASSES> __global__ void __launch_bounds__(256) 
     const T* Bm = (const T*)a.Bm + ((size_t)b * a.G + grp) * a.N;
     const T* Cm = (const T*)a.Cm + ((size_t)b * a.G + grp) * a.N;
     const float dt = a.dt[bh];
-    const float keep = exp2_f64((double)dt * (double)a.A[h] * kLog2e64);
+    const float keep = exp2_f64(ssm_exponent(dt, ssm_rate(a.A[h])));
     const floatx4 x = to_f4(ld4<T>((const T*)a.x + (size_t)bh * D + 4 * qd)), xd = dt * x;
     floatx4 y = zero4();
 #pragma unroll

@@ -37,3 +37,40 @@ def test_a_reset_early_in_a_chunk(dtype, d, N, far):
         z["dt"][:, :, t] = far / z["A"].abs()
         z["x"][:, ::2, t] = 0.0
     check(on_gpu(z))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("far", [1e12, 1e30])
+def test_a_reset_past_any_sum(dtype, far):
+    """Resets that no sum in float64 could hold beside the other tokens' exponents.  Their dt is as large, so they have no input."""
+    _say(f"scan with resets of {far} {dtype}")
+    z = inputs(82, 2, 4, 2, 150, 64, 32, dtype, True)
+    for t in (2, 64, 140):
+        z["dt"][:, :, t] = far / z["A"].abs()
+        z["x"][:, :, t] = 0.0
+    check(on_gpu(z))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rates_past_float32(dtype):
+    """Heads whose dt A leaves float32's range, and one of A = -inf: y is the token's own term, and the state that of the last token."""
+    bla = _bla()
+    _say(f"scan with A of -3e38 and -inf {dtype}")
+    B, H, G, L, d, N = 3, 4, 2, 150, 32, 16
+    lengths = [150, 65, 0]
+    z = inputs(83, B, H, G, L, d, N, dtype, True, lengths)
+    z["A"] = torch.tensor([-3e38, -torch.inf, -2.0, -1e36])
+    c = on_gpu(z)
+    args = (c["x"], c["dt"], c["A"], c["Bm"], c["Cm"], c["D"])
+    y, so = bla.ssm_forward(*args, state=c["state"], lengths=torch.tensor(lengths, dtype=torch.int32).cuda())
+    (w, end), (s, size), live = folded({**c, "A": c["A"].clamp_min(-3e38)}, lengths, False)
+    u, r = unit(dtype), share_of(N, d, L)
+    close(so.flatten(0, 1), end, (r + (2.0 ** -16 if dtype == BF else 0.0)) * size, "state")
+    close(y.flatten(0, 1), torch.where(live.repeat_interleave(H, 0)[..., None], w, 0.0), (u + r) * s + u * w.abs(), "y")
+    one = [c[k][:2, :, 0].contiguous() for k in ("x", "dt", "Bm", "Cm")]
+    state = c["state"][:2].clone()  # updated in place
+    got = bla.ssm_step(one[0], one[1], c["A"], one[2], one[3], state, c["D"])
+    first = {k: None if t is None else t[:2, :, :1] if k in ("x", "dt", "Bm", "Cm", "dy") else t[:2] if "state" in k else t for k, t in c.items()}
+    (w, end), (s, size), _ = folded({**first, "A": c["A"].clamp_min(-3e38)}, None, False)
+    close(state.flatten(0, 1), end, share_of(N, d, 1) * size, "state of a step")
+    close(got.flatten(0, 1)[:, None], w, share_of(N, d, 1) * s + u * w.abs(), "y of a step")
