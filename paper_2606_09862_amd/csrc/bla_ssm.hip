@@ -16,7 +16,7 @@ bla_status check(const bla_ssm_params* p, bool step)
     if (p->H > 0 && (p->G < 1 || p->H % p->G != 0)) return BLA_ERR_INVALID_ARG;
     if (p->d != 32 && p->d != 64 && p->d != 128) return BLA_ERR_UNSUPPORTED;
     if (p->N > 128 || p->N % 8 != 0) return BLA_ERR_UNSUPPORTED;
-    if (p->L > (1 << 30)) return BLA_ERR_UNSUPPORTED;
+    if (!step && p->L > (1 << 30)) return BLA_ERR_UNSUPPORTED;
     const long long nch = step ? 1 : (p->L + kSsmChunk - 1) / kSsmChunk;
     if ((double)p->B * p->H * (nch > 0 ? nch : 1) * (p->d / 32) > (double)kMaxGrid / kMaxSegments) return BLA_ERR_UNSUPPORTED;
     return BLA_OK;

@@ -20,7 +20,7 @@ bla_status check(const bla_window_params* p, bool step)
     if (p->d != 32 && p->d != 64 && p->d != 128) return BLA_ERR_UNSUPPORTED;
     // the kernels keep the running maximum in units of the raw products and place keys by 32-bit indices
     if (p->scale != 0.f && (fabsf(p->scale) < 1e-6f || fabsf(p->scale) > 1e6f)) return BLA_ERR_UNSUPPORTED;
-    if ((long long)p->window + p->sinks > (1ll << 30) || p->L > (1 << 30)) return BLA_ERR_UNSUPPORTED;
+    if ((long long)p->window + p->sinks > (1ll << 30) || (!step && p->L > (1 << 30))) return BLA_ERR_UNSUPPORTED;
     const long long L = step ? 1 : p->L, slots = (long long)p->window + p->sinks;
     if ((double)p->B * p->H * ((L + 63) / 64) > (double)kMaxGrid / kMaxParts) return BLA_ERR_UNSUPPORTED;
     if ((double)p->B * p->H_kv * slots * p->d > 256.0 * kMaxGrid) return BLA_ERR_UNSUPPORTED;
