@@ -411,6 +411,7 @@ bla_status conv_plan(const bla_conv_params* p, bool step, ConvPlan* c)
     if (bh > (1ull << 31) || (!step && p->L > (1 << 30))) return BLA_ERR_UNSUPPORTED;
     const int L = step ? 1 : p->L, pe = step ? 4 : kForwardChannels;
     auto threads = [&](int seg) { return bh * (L > seg ? (L + seg - 1) / seg : 1) * (p->d / pe); };
+    if ((double)bh * ((L + kLongSegment - 1) / kLongSegment) * (p->d / pe) > 1ull << 31) return BLA_ERR_UNSUPPORTED;  // the sums below stay in 64 bits
     c->seg = threads(kLongSegment) >= (1u << 16) ? kLongSegment : kShortSegment;
     c->nseg = L > c->seg ? (L + c->seg - 1) / c->seg : 1;
     c->threads = threads(c->seg);
@@ -428,9 +429,14 @@ bla_status conv_plan(const bla_conv_params* p, bool step, ConvPlan* c)
     const long long per = (long long)rows * c->bseg;
     c->nchunk = (int)(L > per ? (L + per - 1) / per : 1);
     c->blocks = blocks(c->bseg);
-    if (c->blocks >= (1ull << 31)) return BLA_ERR_UNSUPPORTED;
     c->total = seq_align((size_t)p->B * c->nchunk * p->H * p->d * (p->taps + 1) * 4);
     return BLA_OK;
+}
+
+// whether the backward pass's launches are ones
+bool backward_fits(const bla_conv_params* p, const ConvPlan& c)
+{
+    return launchable((double)c.blocks, 256) && launchable(ceil((double)p->H * p->d * (p->taps + 1) / 32), 256);
 }
 
 }  // namespace
@@ -506,7 +512,7 @@ bla_status bla_conv_step(const bla_conv_params* p, const void* x, const float* w
 size_t bla_conv_backward_workspace_size(const bla_conv_params* p)
 {
     ConvPlan c;
-    return conv_plan(p, false, &c) == BLA_OK ? c.total : 0;
+    return conv_plan(p, false, &c) == BLA_OK && backward_fits(p, c) ? c.total : 0;
 }
 
 bla_status bla_conv_backward(const bla_conv_params* p, const void* x, const float* w, const float* bias, const void* dy,
@@ -517,6 +523,7 @@ bla_status bla_conv_backward(const bla_conv_params* p, const void* x, const floa
     const bla_status st = conv_plan(p, false, &c);
     if (st != BLA_OK) return st;
     if (p->B == 0 || p->H == 0) return p->H == 0 ? BLA_OK : BLA_ERR_UNSUPPORTED;
+    if (!backward_fits(p, c)) return BLA_ERR_UNSUPPORTED;
     const size_t n = (size_t)p->B * p->H * p->L * p->d * elem_bytes(p->io_dtype);
     const size_t ns = (size_t)p->B * p->H * (p->taps - 1) * p->d * 4, nc = (size_t)p->H * p->d * 4, nw = nc * p->taps;
     if (!w || !dw || (p->L > 0 && (!x || !dy || !dx))) return BLA_ERR_INVALID_ARG;

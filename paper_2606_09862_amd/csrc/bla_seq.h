@@ -99,6 +99,8 @@ template <int I, int O> bool clash(const Span (&in)[I], const Span (&out)[O])
     return false;
 }
 
-constexpr long long kMaxGrid = 1ll << 30;  // most workgroups of a launch
+// A launch holds fewer than 2^32 threads.
+inline bool launchable(double workgroups, int threads) { return workgroups * threads < 4294967296.0; }
+constexpr double kMaxUnits = 1 << 24;  // units of work that a plan is made for (its arithmetic stays in 64 bits)
 
 }  // namespace bla

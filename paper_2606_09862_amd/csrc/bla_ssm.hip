@@ -18,7 +18,7 @@ bla_status check(const bla_ssm_params* p, bool step)
     if (p->N > 128 || p->N % 8 != 0) return BLA_ERR_UNSUPPORTED;
     if (!step && p->L > (1 << 30)) return BLA_ERR_UNSUPPORTED;
     const long long nch = step ? 1 : (p->L + kSsmChunk - 1) / kSsmChunk;
-    if ((double)p->B * p->H * (nch > 0 ? nch : 1) * (p->d / 32) > (double)kMaxGrid / kMaxSegments) return BLA_ERR_UNSUPPORTED;
+    if ((double)p->B * p->H * (nch > 0 ? nch : 1) * (p->d / 32) > kMaxUnits) return BLA_ERR_UNSUPPORTED;
     return BLA_OK;
 }
 
@@ -49,6 +49,12 @@ ForwardPlan forward_plan(const bla_ssm_params* p)
     return f;
 }
 
+bool fits(const bla_ssm_params* p, const ForwardPlan& f)
+{
+    const double bh = (double)p->B * p->H;
+    return launchable(8.0 * ceil(bh * f.nseg / 8), 256) && launchable(8.0 * ceil(bh * f.sub * (f.nseg - 1) / 8), 256);
+}
+
 struct BackwardPlan {
     int nch, hsplit;
     size_t off_leave, off_head, off_bc, total;
@@ -71,6 +77,12 @@ BackwardPlan backward_plan(const bla_ssm_params* p)
     return b;
 }
 
+bool fits(const bla_ssm_params* p, const BackwardPlan& b)
+{
+    return launchable(16.0 * ceil((double)p->B * p->H * (p->d / 32) / 8), 256) && launchable(8.0 * ceil((double)p->B * p->G * b.nch * b.hsplit / 8), 256) &&
+           launchable(p->H, 256);
+}
+
 struct Sizes {
     size_t x, bc, dt, head, state;
 };
@@ -86,9 +98,13 @@ bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
 extern "C" {
 
-bla_status bla_ssm_supported(const bla_ssm_params* p) { return check(p, false); }
+bla_status bla_ssm_supported(const bla_ssm_params* p)
+{
+    const bla_status st = check(p, false);
+    return st == BLA_OK && !fits(p, forward_plan(p)) ? BLA_ERR_UNSUPPORTED : st;
+}
 
-size_t bla_ssm_workspace_size(const bla_ssm_params* p) { return check(p, false) == BLA_OK ? forward_plan(p).total : 0; }
+size_t bla_ssm_workspace_size(const bla_ssm_params* p) { return bla_ssm_supported(p) == BLA_OK ? forward_plan(p).total : 0; }
 
 bla_status bla_ssm_forward(const bla_ssm_params* p, const void* x, const float* dt, const float* A, const void* Bm,
                            const void* Cm, const float* D, const int32_t* lengths, const float* state_in, void* y,
@@ -97,6 +113,8 @@ bla_status bla_ssm_forward(const bla_ssm_params* p, const void* x, const float* 
     const bla_status st = check(p, false);
     if (st != BLA_OK) return st;
     if (p->B == 0 || p->H == 0) return BLA_OK;
+    const ForwardPlan f = forward_plan(p);
+    if (!fits(p, f)) return BLA_ERR_UNSUPPORTED;
     const Sizes z = sizes(p, p->L);
     if (!A || (p->L > 0 && (!x || !dt || !Bm || !Cm || !y))) return BLA_ERR_INVALID_ARG;
     const void* ptr[] = {x, Bm, Cm, state_in, y, state_out};
@@ -106,7 +124,6 @@ bla_status bla_ssm_forward(const bla_ssm_params* p, const void* x, const float* 
     const Span in[] = {{x, z.x}, {Bm, z.bc}, {Cm, z.bc}, {dt, z.dt}, {A, z.head}, {D, z.head}, {state_in, z.state}, {lengths, 4 * (size_t)p->B}};
     const Span out[] = {{y, z.x}, {state_out, z.state}};
     if (clash(in, out)) return BLA_ERR_INVALID_ARG;
-    const ForwardPlan f = forward_plan(p);
     if (f.total > 0 && (!workspace || workspace_bytes < f.total || !is_aligned16(workspace))) return BLA_ERR_WORKSPACE;
     if (f.total > 0 && !tables_overwritten(workspace, f.total)) return BLA_ERR_HIP;
     SsmArgs a = {};
@@ -124,6 +141,7 @@ bla_status bla_ssm_step(const bla_ssm_params* p, const void* x, const float* dt,
     const bla_status st = check(p, true);
     if (st != BLA_OK) return st;
     if (p->B == 0 || p->H == 0) return BLA_OK;
+    if (!launchable((double)p->B * p->H, 256)) return BLA_ERR_UNSUPPORTED;
     const Sizes z = sizes(p, 1);
     const void* ptr[] = {x, Bm, Cm, state_in, y, state_out};
     for (const void* q : ptr)
@@ -138,7 +156,9 @@ bla_status bla_ssm_step(const bla_ssm_params* p, const void* x, const float* dt,
 
 size_t bla_ssm_backward_workspace_size(const bla_ssm_params* p)
 {
-    return check(p, false) == BLA_OK ? backward_plan(p).total : 0;
+    if (check(p, false) != BLA_OK) return 0;
+    const BackwardPlan b = backward_plan(p);
+    return fits(p, b) ? b.total : 0;
 }
 
 bla_status bla_ssm_backward(const bla_ssm_params* p, const void* x, const float* dt, const float* A, const void* Bm,
@@ -150,6 +170,8 @@ bla_status bla_ssm_backward(const bla_ssm_params* p, const void* x, const float*
     if (st != BLA_OK) return st;
     if (p->H == 0) return BLA_OK;
     if (p->B == 0 || p->L == 0) return BLA_ERR_UNSUPPORTED;
+    const BackwardPlan b = backward_plan(p);
+    if (!fits(p, b)) return BLA_ERR_UNSUPPORTED;
     const Sizes z = sizes(p, p->L);
     const Span in[] = {{x, z.x}, {Bm, z.bc}, {Cm, z.bc}, {dy, z.x}, {state_in, z.state}, {dstate_out, z.state}, {dt, z.dt}, {A, z.head},
                        {D, z.head}, {lengths, 4 * (size_t)p->B}};
@@ -162,7 +184,6 @@ bla_status bla_ssm_backward(const bla_ssm_params* p, const void* x, const float*
     for (const void* q : narrow)
         if (!aligned4(q)) return BLA_ERR_INVALID_ARG;
     if (clash(in, out)) return BLA_ERR_INVALID_ARG;
-    const BackwardPlan b = backward_plan(p);
     if (!workspace || workspace_bytes < b.total || !is_aligned16(workspace)) return BLA_ERR_WORKSPACE;
     if (!tables_overwritten(workspace, b.total)) return BLA_ERR_HIP;
     char* ws = (char*)workspace;

@@ -22,8 +22,8 @@ bla_status check(const bla_window_params* p, bool step)
     if (p->scale != 0.f && (fabsf(p->scale) < 1e-6f || fabsf(p->scale) > 1e6f)) return BLA_ERR_UNSUPPORTED;
     if ((long long)p->window + p->sinks > (1ll << 30) || (!step && p->L > (1 << 30))) return BLA_ERR_UNSUPPORTED;
     const long long L = step ? 1 : p->L, slots = (long long)p->window + p->sinks;
-    if ((double)p->B * p->H * ((L + 63) / 64) > (double)kMaxGrid / kMaxParts) return BLA_ERR_UNSUPPORTED;
-    if ((double)p->B * p->H_kv * slots * p->d > 256.0 * kMaxGrid) return BLA_ERR_UNSUPPORTED;
+    if ((double)p->B * p->H * ((L + 63) / 64) > kMaxUnits) return BLA_ERR_UNSUPPORTED;
+    if ((double)p->B * p->H_kv * slots * p->d > 256.0 * (1 << 30)) return BLA_ERR_UNSUPPORTED;
     return BLA_OK;
 }
 
@@ -55,6 +55,13 @@ ForwardPlan forward_plan(const bla_window_params* p, bool cached)
     return f;
 }
 
+// whether the forward kernel's launch is one, with the workgroups that write the rings after the call
+bool fits(const bla_window_params* p, const ForwardPlan& f, bool rings)
+{
+    const double pieces = (double)p->B * p->H_kv * ((double)p->window + p->sinks) * (p->d * elem_bytes(p->io_dtype) / 16);
+    return launchable(8.0 * ((f.units + 7) / 8) + (rings ? ceil(pieces / (64 * f.waves)) : 0.0), 64 * f.waves);
+}
+
 // Step: a key head's ring in parts of at least 128 slots where the key heads of all rows alone do not fill the device.
 struct StepPlan {
     int ngrp, nsplit;
@@ -72,11 +79,12 @@ StepPlan step_plan(const bla_window_params* p)
     s.total = s.nsplit > 1 ? seq_align((size_t)s.nsplit * p->B * p->H * (p->d + 2) * 4) : 0;
     return s;
 }
+bool fits(const bla_window_params* p, const StepPlan& s) { return launchable((double)p->B * p->H_kv * s.ngrp * s.nsplit, 256); }
 
 // Backward: the sinks' queries beyond their windows in as many parts as fill the device with waves, a block of 32 queries or more to each.
 struct BackwardPlan {
     int nqb, nkb, ns, ssplit;
-    long long q_units, k_units;
+    long long q_units, k_units, s_units;
     size_t off_near, off_part, total;
 };
 BackwardPlan backward_plan(const bla_window_params* p)
@@ -93,11 +101,18 @@ BackwardPlan backward_plan(const bla_window_params* p)
     b.ssplit = (int)(n < 1 ? 1 : n > kMaxParts ? kMaxParts : n);
     b.q_units = bh * b.nqb;
     b.k_units = bk * b.nkb;
+    b.s_units = bk * ((b.ns + 15) / 16) * b.ssplit;
     const size_t one = seq_align((size_t)bk * b.ns * 2 * p->d * 4);
     b.off_near = seq_align((size_t)bh * p->L * 4);
     b.off_part = b.off_near + one;
     b.total = b.off_part + seq_align((size_t)b.ssplit * bk * b.ns * 2 * p->d * 4);
     return b;
+}
+
+bool fits(const bla_window_params* p, const BackwardPlan& b)
+{
+    return launchable(8.0 * ((b.q_units + 7) / 8), 256) && launchable(8.0 * ((b.k_units + 7) / 8) + b.s_units, 256) &&
+           launchable((double)p->B * p->H_kv * b.ns * (2 * p->d / 4) / 256 + 1, 256);
 }
 
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -108,10 +123,14 @@ extern "C" {
 
 size_t bla_window_workspace_size(const bla_window_params* p)
 {
-    return check(p, false) == BLA_OK ? forward_plan(p, true).total : 0;
+    return bla_window_supported(p) == BLA_OK ? forward_plan(p, true).total : 0;
 }
 
-bla_status bla_window_supported(const bla_window_params* p) { return check(p, false); }
+bla_status bla_window_supported(const bla_window_params* p)
+{
+    const bla_status st = check(p, false);
+    return st == BLA_OK && !fits(p, forward_plan(p, true), false) ? BLA_ERR_UNSUPPORTED : st;
+}
 
 bla_status bla_window_forward(const bla_window_params* p, const void* q, const void* k, const void* v, const int32_t* lengths,
                               const int64_t* pos, const void* cache_k_in, const void* cache_v_in, void* o, float* lse,
@@ -120,6 +139,8 @@ bla_status bla_window_forward(const bla_window_params* p, const void* q, const v
     const bla_status st = check(p, false);
     if (st != BLA_OK) return st;
     if (p->B == 0 || p->H == 0) return BLA_OK;
+    const ForwardPlan f = forward_plan(p, cache_k_in != nullptr);
+    if (!fits(p, f, cache_k_out != nullptr)) return BLA_ERR_UNSUPPORTED;
     const int e = elem_bytes(p->io_dtype), bf16 = p->io_dtype == BLA_BF16;
     const size_t nq = (size_t)p->B * p->H * p->L * p->d * e, nk = (size_t)p->B * p->H_kv * p->L * p->d * e;
     const size_t nc = (size_t)p->B * p->H_kv * ((size_t)p->window + p->sinks) * p->d * e;
@@ -133,7 +154,6 @@ bla_status bla_window_forward(const bla_window_params* p, const void* q, const v
     const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {cache_k_in, nc}, {cache_v_in, nc}, {lengths, 4 * nb}, {pos, 8 * nb}};
     const Span out[] = {{o, nq}, {lse, nl}, {cache_k_out, nc}, {cache_v_out, nc}};
     if (clash(in, out)) return BLA_ERR_INVALID_ARG;
-    const ForwardPlan f = forward_plan(p, cache_k_in != nullptr);
     if (f.total > 0 && (!workspace || workspace_bytes < f.total || !is_aligned16(workspace))) return BLA_ERR_WORKSPACE;
     if (f.total > 0 && !tables_overwritten(workspace, f.total)) return BLA_ERR_HIP;
 
@@ -156,7 +176,9 @@ bla_status bla_window_forward(const bla_window_params* p, const void* q, const v
 
 size_t bla_window_step_workspace_size(const bla_window_params* p)
 {
-    return check(p, true) == BLA_OK ? step_plan(p).total : 0;
+    if (check(p, true) != BLA_OK) return 0;
+    const StepPlan s = step_plan(p);
+    return fits(p, s) ? s.total : 0;
 }
 
 bla_status bla_window_step(const bla_window_params* p, const void* q, const void* k, const void* v, const int64_t* pos,
@@ -165,6 +187,8 @@ bla_status bla_window_step(const bla_window_params* p, const void* q, const void
     const bla_status st = check(p, true);
     if (st != BLA_OK) return st;
     if (p->B == 0 || p->H == 0) return BLA_OK;
+    const StepPlan sp = step_plan(p);
+    if (!fits(p, sp)) return BLA_ERR_UNSUPPORTED;
     const int e = elem_bytes(p->io_dtype), bf16 = p->io_dtype == BLA_BF16;
     const size_t nq = (size_t)p->B * p->H * p->d * e, nk = (size_t)p->B * p->H_kv * p->d * e;
     const size_t nc = (size_t)p->B * p->H_kv * ((size_t)p->window + p->sinks) * p->d * e;
@@ -175,7 +199,6 @@ bla_status bla_window_step(const bla_window_params* p, const void* q, const void
     const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {pos, 8 * (size_t)p->B}};
     const Span out[] = {{o, nq}, {cache_k, nc}, {cache_v, nc}};
     if (clash(in, out)) return BLA_ERR_INVALID_ARG;
-    const StepPlan sp = step_plan(p);
     if (sp.total > 0 && (!workspace || workspace_bytes < sp.total || !is_aligned16(workspace))) return BLA_ERR_WORKSPACE;
     if (sp.total > 0 && !tables_overwritten(workspace, sp.total)) return BLA_ERR_HIP;
 
@@ -197,7 +220,9 @@ bla_status bla_window_step(const bla_window_params* p, const void* q, const void
 
 size_t bla_window_backward_workspace_size(const bla_window_params* p)
 {
-    return check(p, false) == BLA_OK ? backward_plan(p).total : 0;
+    if (check(p, false) != BLA_OK) return 0;
+    const BackwardPlan b = backward_plan(p);
+    return fits(p, b) ? b.total : 0;
 }
 
 bla_status bla_window_backward(const bla_window_params* p, const void* q, const void* k, const void* v, const void* o,
@@ -208,6 +233,8 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
     if (st != BLA_OK) return st;
     if (p->t0 != 0) return BLA_ERR_UNSUPPORTED;
     if (p->B == 0 || p->H == 0 || p->L == 0) return BLA_OK;
+    const BackwardPlan b = backward_plan(p);
+    if (!fits(p, b)) return BLA_ERR_UNSUPPORTED;
     const int e = elem_bytes(p->io_dtype), bf16 = p->io_dtype == BLA_BF16;
     const size_t nq = (size_t)p->B * p->H * p->L * p->d * e, nk = (size_t)p->B * p->H_kv * p->L * p->d * e;
     const void* ptr[] = {q, k, v, o, dO, dq, dk, dv};
@@ -217,7 +244,6 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
     const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {o, nq}, {dO, nq}, {lse, (size_t)p->B * p->H * p->L * 4}, {lengths, 4 * (size_t)p->B}};
     const Span out[] = {{dq, nq}, {dk, nk}, {dv, nk}};
     if (clash(in, out)) return BLA_ERR_INVALID_ARG;
-    const BackwardPlan b = backward_plan(p);
     if (!workspace || workspace_bytes < b.total || !is_aligned16(workspace)) return BLA_ERR_WORKSPACE;
     if (!tables_overwritten(workspace, b.total)) return BLA_ERR_HIP;
 
@@ -228,7 +254,7 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
     a.part = (float*)((char*)workspace + b.off_part);
     a.nqb = b.nqb, a.nkb = b.nkb, a.ns = b.ns, a.ssplit = b.ssplit;
     a.q_units = b.q_units, a.q_per = (b.q_units + 7) / 8, a.k_units = b.k_units, a.k_per = (b.k_units + 7) / 8;
-    a.s_units = (unsigned)((long long)p->B * p->H_kv * ((b.ns + 15) / 16) * b.ssplit);
+    a.s_units = (unsigned)b.s_units;
     return launch_window_backward(bf16, p->d, a, (hipStream_t)stream) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }
 
