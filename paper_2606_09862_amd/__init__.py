@@ -450,7 +450,8 @@ def layer_forward(x, w_qkv, w_o, T, H: int, M: int, S: int, t0: int = 0, scale: 
 # ---- window attention, the short convolution and the selective scan ----
 #
 # A decode step of these runs for a few microseconds on the device as well, so what depends on shapes alone (the
-# parameter block, whether the shape is supported, the workspace's size) is kept per shape.
+# parameter block, whether the shape is supported, the workspace's size) is kept per shape.  A position is no part of a shape: it goes into
+# a copy of the block.
 
 def _check_on(t, shape, dtype, name, dev):
     """A contiguous tensor of this shape and type on GPU number dev."""
@@ -505,11 +506,24 @@ def _shape_status(st, what):
 
 
 @functools.lru_cache(maxsize=256)
-def _window_plan(size, what, B, H, Hkv, L, d, window, sinks, t0, scale, dtype):
-    """(parameters by reference, workspace bytes by the library function `size`)."""
-    p = ctypes.byref(WindowParams(B, H, Hkv, L, d, window, sinks, _io(dtype, "q"), t0, scale))
-    _shape_status(lib().bla_window_supported(p), what)
-    return p, getattr(lib(), size)(p)
+def _window_plan(what, B, H, Hkv, L, d, window, sinks, scale, dtype):
+    """(parameters at t0 = 0, the same by reference, workspace bytes) of the library's call `what`."""
+    block = WindowParams(B, H, Hkv, L, d, window, sinks, _io(dtype, "q"), 0, scale)
+    p = ctypes.byref(block)
+    st = lib().bla_window_supported(p)
+    if what == "bla_window_forward" or st != 2:  # the launches of the other calls have limits of their own, which they check
+        _shape_status(st, what)
+    return block, p, getattr(lib(), what.replace("_forward", "") + "_workspace_size")(p)
+
+
+def _window_params(what, B, H, Hkv, L, d, window, sinks, t0, scale, dtype):
+    """(parameters by reference, workspace bytes)."""
+    block, p, need = _window_plan(what, B, H, Hkv, L, d, int(window), int(sinks), 0.0 if scale is None else float(scale), dtype)
+    if t0 != 0:
+        block = WindowParams.from_buffer_copy(block)
+        block.t0 = int(t0)
+        p = ctypes.byref(block)
+    return p, need
 
 
 def window_forward(q, k, v, window: int, sinks: int = 0, t0: int = 0, scale: float | None = None, lengths=None, pos=None,
@@ -524,8 +538,7 @@ def window_forward(q, k, v, window: int, sinks: int = 0, t0: int = 0, scale: flo
     """
     B, H, L, d = q.shape
     Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
-    p, need = _window_plan("bla_window_workspace_size", "bla_window_forward", B, H, Hkv, L, d, int(window), int(sinks),
-                           int(t0), 0.0 if scale is None else float(scale), dt)
+    p, need = _window_params("bla_window_forward", B, H, Hkv, L, d, window, sinks, t0, scale, dt)
     _check_on(q, (B, H, L, d), dt, "q", dev)
     _check_on(k, (B, Hkv, L, d), dt, "k", dev)
     _check_on(v, (B, Hkv, L, d), dt, "v", dev)
@@ -555,8 +568,7 @@ def window_step(q, k, v, window: int, sinks: int, cache_k, cache_v, pos=None, t0
     [B,H_kv,sinks+window,d] take its key and value in place.  A row with a negative pos is idle (zeros)."""
     B, H, d = q.shape
     Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
-    p, need = _window_plan("bla_window_step_workspace_size", "bla_window_step", B, H, Hkv, 1, d, int(window), int(sinks),
-                           int(t0), 0.0 if scale is None else float(scale), dt)
+    p, need = _window_params("bla_window_step", B, H, Hkv, 1, d, window, sinks, t0, scale, dt)
     _check_on(q, (B, H, d), dt, "q", dev)
     _check_on(k, (B, Hkv, d), dt, "k", dev)
     _check_on(v, (B, Hkv, d), dt, "v", dev)
@@ -577,8 +589,7 @@ def window_backward(q, k, v, o, lse, dO, window: int, sinks: int = 0, scale: flo
     """bla_window_backward: (dq, dk, dv) of window_forward without rings from its outputs o and lse and dO = dLoss/dO."""
     B, H, L, d = q.shape
     Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
-    p, need = _window_plan("bla_window_backward_workspace_size", "bla_window_backward", B, H, Hkv, L, d, int(window),
-                           int(sinks), 0, 0.0 if scale is None else float(scale), dt)
+    p, need = _window_params("bla_window_backward", B, H, Hkv, L, d, window, sinks, 0, scale, dt)
     for name, t, h in (("q", q, H), ("k", k, Hkv), ("v", v, Hkv), ("o", o, H), ("dO", dO, H)):
         _check_on(t, (B, h, L, d), dt, name, dev)
     _check_on(lse, (B, H, L), torch.float32, "lse", dev)
