@@ -505,9 +505,16 @@ def _shape_status(st, what):
         raise BlaError(st, f"{what} (shape check)")
 
 
+def _int32(what, *values):
+    """Refuses sizes past the parameter block's fields, which would take their lower bits."""
+    if not all(-(1 << 31) <= v < 1 << 31 for v in values):
+        raise BlaError(2, f"{what} (shape check)")
+
+
 @functools.lru_cache(maxsize=256)
 def _window_plan(what, B, H, Hkv, L, d, window, sinks, scale, dtype):
     """(parameters at t0 = 0, the same by reference, workspace bytes) of the library's call `what`."""
+    _int32(what, B, H, Hkv, L, d, window, sinks)
     block = WindowParams(B, H, Hkv, L, d, window, sinks, _io(dtype, "q"), 0, scale)
     p = ctypes.byref(block)
     st = lib().bla_window_supported(p)
@@ -520,6 +527,8 @@ def _window_params(what, B, H, Hkv, L, d, window, sinks, t0, scale, dtype):
     """(parameters by reference, workspace bytes)."""
     block, p, need = _window_plan(what, B, H, Hkv, L, d, int(window), int(sinks), 0.0 if scale is None else float(scale), dtype)
     if t0 != 0:
+        if not -(1 << 63) <= t0 < 1 << 63:
+            raise BlaError(1, what)
         block = WindowParams.from_buffer_copy(block)
         block.t0 = int(t0)
         p = ctypes.byref(block)
@@ -604,6 +613,7 @@ def window_backward(q, k, v, o, lse, dO, window: int, sinks: int = 0, scale: flo
 
 @functools.lru_cache(maxsize=256)
 def _conv_plan(what, B, H, L, d, K, silu, dtype):
+    _int32(what, B, H, L, d, K, silu)
     p = ctypes.byref(ConvParams(B, H, L, d, K, silu, _io(dtype, "x")))
     _shape_status(lib().bla_conv_supported(p), what)
     return p, lib().bla_conv_backward_workspace_size(p)
@@ -683,6 +693,7 @@ def conv_backward(x, w, dy, bias=None, silu: bool = True, state=None, dstate=Non
 
 @functools.lru_cache(maxsize=256)
 def _ssm_plan(size, what, B, H, G, L, d, N, dtype):
+    _int32(what, B, H, G, L, d, N)
     p = ctypes.byref(SsmParams(B, H, G, L, d, N, _io(dtype, "x")))
     _shape_status(lib().bla_ssm_supported(p), what)
     return p, getattr(lib(), size)(p) if size else 0
