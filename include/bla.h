@@ -333,7 +333,7 @@ bla_status bla_layer_forward_timed(const bla_params* p, const double* T, const v
  * A non-finite value in a token of the sequence may reach the outputs of other queries that share a tile of keys with it.
  * Supported: float32 or bfloat16; d in {32, 64, 128}; H a multiple of H_kv; window >= 1, sinks >= 0, window + sinks <= 2^30; 1e-6 <=
  * |scale| <= 1e6.  Alignment, ownership, streams, workspaces and errors follow the conventions above; the outputs must not
- * overlap the inputs or one another (BLA_ERR_INVALID_ARG).
+ * overlap the inputs or one another (BLA_ERR_INVALID_ARG).  H = 0 beside key heads is BLA_ERR_UNSUPPORTED where the call writes rings, dk or dv.
  */
 typedef struct {
     int32_t B, H, H_kv, L; /* batch rows, query heads, key heads, tokens in this call       */
@@ -457,7 +457,7 @@ bla_status bla_ssm_step(const bla_ssm_params* p, const void* x, const float* dt,
  * Gradients of bla_ssm_forward from its inputs, dy = dLoss/dy and dstate_out = dLoss/d(state after the call) (NULL = zero):
  * dx, dB, dC in the io dtype (dB and dC summed over the heads of a group), ddt [B, H, L], dA [H], dD [H] (NULL = not wanted) and
  * dstate_in [B, H, N, d] (NULL = not wanted) in float32.  The sums run in a fixed order (no atomics).  The workspace holds two
- * states of every 64 tokens and head.  B = 0 or L = 0 is BLA_ERR_UNSUPPORTED.
+ * states of every 64 tokens and head.  B = 0 or L = 0 is BLA_ERR_UNSUPPORTED, and so are groups without heads (dB and dC would be left unwritten).
  */
 size_t bla_ssm_backward_workspace_size(const bla_ssm_params* p);
 bla_status bla_ssm_backward(const bla_ssm_params* p, const void* x, const float* dt, const float* A, const void* Bm,

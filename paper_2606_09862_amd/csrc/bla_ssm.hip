@@ -168,8 +168,8 @@ bla_status bla_ssm_backward(const bla_ssm_params* p, const void* x, const float*
 {
     const bla_status st = check(p, false);
     if (st != BLA_OK) return st;
-    if (p->H == 0) return BLA_OK;
-    if (p->B == 0 || p->L == 0) return BLA_ERR_UNSUPPORTED;
+    if (p->H == 0 && (p->G == 0 || p->B == 0 || p->L == 0)) return BLA_OK;
+    if (p->H == 0 || p->B == 0 || p->L == 0) return BLA_ERR_UNSUPPORTED;
     const BackwardPlan b = backward_plan(p);
     if (!fits(p, b)) return BLA_ERR_UNSUPPORTED;
     const Sizes z = sizes(p, p->L);

@@ -29,6 +29,12 @@ bla_status check(const bla_window_params* p, bool step)
 
 float scale_of(const bla_window_params* p) { return p->scale == 0.f ? 1.f / sqrtf((float)p->d) : p->scale; }
 
+// A call without rows or query heads: done, unless key heads have outputs that nothing would write.
+bla_status empty(const bla_window_params* p, bool outputs)
+{
+    return outputs && p->B > 0 && p->H_kv > 0 ? BLA_ERR_UNSUPPORTED : BLA_OK;
+}
+
 // Forward: 128 queries to a workgroup (fewer reads of keys), 64 where that fills the device better;
 // the keys of a block in parts of at least two tiles where the blocks alone do not fill it.
 struct ForwardPlan {
@@ -138,7 +144,7 @@ bla_status bla_window_forward(const bla_window_params* p, const void* q, const v
 {
     const bla_status st = check(p, false);
     if (st != BLA_OK) return st;
-    if (p->B == 0 || p->H == 0) return BLA_OK;
+    if (p->B == 0 || p->H == 0) return empty(p, cache_k_out || cache_v_out);
     const ForwardPlan f = forward_plan(p, cache_k_in != nullptr);
     if (!fits(p, f, cache_k_out != nullptr)) return BLA_ERR_UNSUPPORTED;
     const int e = elem_bytes(p->io_dtype), bf16 = p->io_dtype == BLA_BF16;
@@ -186,7 +192,7 @@ bla_status bla_window_step(const bla_window_params* p, const void* q, const void
 {
     const bla_status st = check(p, true);
     if (st != BLA_OK) return st;
-    if (p->B == 0 || p->H == 0) return BLA_OK;
+    if (p->B == 0 || p->H == 0) return empty(p, true);
     const StepPlan sp = step_plan(p);
     if (!fits(p, sp)) return BLA_ERR_UNSUPPORTED;
     const int e = elem_bytes(p->io_dtype), bf16 = p->io_dtype == BLA_BF16;
@@ -232,7 +238,7 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
     const bla_status st = check(p, false);
     if (st != BLA_OK) return st;
     if (p->t0 != 0) return BLA_ERR_UNSUPPORTED;
-    if (p->B == 0 || p->H == 0 || p->L == 0) return BLA_OK;
+    if (p->B == 0 || p->H == 0 || p->L == 0) return empty(p, p->L > 0);
     const BackwardPlan b = backward_plan(p);
     if (!fits(p, b)) return BLA_ERR_UNSUPPORTED;
     const int e = elem_bytes(p->io_dtype), bf16 = p->io_dtype == BLA_BF16;

@@ -73,3 +73,19 @@ def test_ssm_launches(lib):  # noqa: F811
         p = ssm(B=B, H=16, G=1, L=64, d=32, N=8)
         assert call(lib.bla_ssm_backward, p, 17, drop=[0], tail=(WS, MUCH)) == want
         assert (sizes(lib, "bla_ssm_backward_workspace_size", p) > 0) == (want == INVALID)
+
+
+def test_no_query_heads(lib):  # noqa: F811
+    """H = 0 beside key heads or groups: refused where the call has outputs of theirs to write."""
+    tail = (WS, MUCH)
+    for heads, want in ((2, UNSUPPORTED), (0, OK)):
+        p, s = P(H=0, H_kv=heads), ssm(H=0, G=heads)
+        assert lib.bla_window_supported(ctypes.byref(p)) == lib.bla_ssm_supported(ctypes.byref(s)) == OK
+        assert call(lib.bla_window_forward, p, 11, tail=tail) == want
+        assert call(lib.bla_window_forward, p, 11, drop=[9, 10], tail=tail) == OK
+        assert call(lib.bla_window_step, p, 7, tail=tail) == want
+        assert call(lib.bla_window_backward, p, 10, tail=tail) == want
+        assert call(lib.bla_ssm_backward, s, 17, tail=tail) == want
+        assert call(lib.bla_ssm_forward, s, 10, tail=tail) == call(lib.bla_ssm_step, s, 9) == OK
+    for p, s in ((P(H=0, B=0), ssm(H=0, B=0)), (P(H=0, L=0), ssm(H=0, L=0))):
+        assert call(lib.bla_window_backward, p, 10, tail=tail) == call(lib.bla_ssm_backward, s, 17, tail=tail) == OK
