@@ -293,7 +293,8 @@ template <typename T, int D, int PASSES> __global__ void __launch_bounds__(256) 
     float* out = a.state_out + (size_t)bh * a.N * D;
     floatx4 s[PASSES];
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) s[p] = ld4f(in + (size_t)min(p * RPP + rg, a.N - 1) * D + 4 * qd);
+    for (int p = 0; p < PASSES; ++p)  // a lane reads the rows that it writes, no other: the state may be updated in place
+        s[p] = p * RPP + rg < a.N ? ld4f(in + (size_t)(p * RPP + rg) * D + 4 * qd) : zero4();
     const T* Bm = (const T*)a.Bm + ((size_t)b * a.G + grp) * a.N;
     const T* Cm = (const T*)a.Cm + ((size_t)b * a.G + grp) * a.N;
     const float dt = a.dt[bh];
