@@ -39,25 +39,10 @@ __device__ __forceinline__ floatx8 ld_red(const float* M, int ld, int x0, int kb
 // Row strides (elements) of LDS tiles of D columns.  A tile read by rows (ld_nat) is padded by 16 bytes: the sixteen
 // rows of a fragment start on different banks.  A tile read transposed is padded to 8 x odd dwords in bf16
 // (no conflicts in the transposing reads) and by four dwords in float32 (the four row groups of a
-// fragment read 16 banks apart).
+// fragment read 16 banks apart).  A tile read both ways takes the row reads' padding, which leaves the transposing reads of bf16 one overlap in eight
+// rows (the 8 x odd dwords that avoid it need a swizzle for the row reads and a sixth more LDS, which costs a workgroup per compute unit).
 template <typename T> __host__ __device__ constexpr int nat_ld(int D) { return D + 16 / (int)sizeof(T); }
 template <typename T> __host__ __device__ constexpr int red_ld(int D) { return sizeof(T) == 2 ? D + 16 : D + 4; }
-
-// A tile read both ways.  In bf16 rows padded by 16 bytes put the sixteen rows of a fragment on different banks and leave the
-// transposing reads one overlap in eight rows (the 8 x odd dwords that avoid it need a swizzle for the row reads and a sixth
-// more LDS, which costs a workgroup per compute unit).
-template <typename T> __host__ __device__ constexpr int dual_ld(int D) { return nat_ld<T>(D); }
-// rows x0 .. x0+15 as a natural-order fragment
-template <typename T>
-__device__ __forceinline__ typename Frag<T>::type ld_nat_dual(const T* M, int ld, int x0, int kb, int g, int r)
-{
-    return ld_nat(M + (x0 + r) * ld, kb, g);
-}
-template <typename T>
-__device__ __forceinline__ typename Frag<T>::type ld_red_dual(const T* M, int ld, int x0, int kb, int g, int r)
-{
-    return ld_red(M, ld, x0, kb, g, r);
-}
 
 // The largest of three, a NaN if one of them is (v_maximum3_f32; fmaxf would first quiet each operand, an instruction apiece).
 __device__ __forceinline__ float max3(float a, float b, float c)

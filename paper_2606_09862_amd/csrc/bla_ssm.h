@@ -104,12 +104,12 @@ template <typename T> __device__ __forceinline__ typename Frag<T>::type ld_acc_r
     const int k = 32 * kb + 4 * g;
     return join(k < N ? ld4<T>(row + k) : zero_half<T>(), k + 16 < N ? ld4<T>(row + k + 16) : zero_half<T>());
 }
-// The same of an LDS tile in the dual layout (row x0 + r, x0 a multiple of 16).
-__device__ __forceinline__ bf16x8 ld_acc_dual(const bf16* M, int ld, int x0, int kb, int g, int r)
+// The same of an LDS tile (row x0 + r, x0 a multiple of 16).
+__device__ __forceinline__ bf16x8 ld_acc(const bf16* M, int ld, int x0, int kb, int g, int r)
 {
     return ld_frag_2x8(M + (x0 + r) * ld, kb, g);
 }
-__device__ __forceinline__ floatx8 ld_acc_dual(const float* M, int ld, int x0, int kb, int g, int r)
+__device__ __forceinline__ floatx8 ld_acc(const float* M, int ld, int x0, int kb, int g, int r)
 {
     return ld_frag<float>(M + (x0 + r) * ld, 32 * kb, g);
 }
@@ -143,7 +143,7 @@ template <int CTRL, int ROWS> __device__ __forceinline__ double dpp_f64(double x
 
 // Inclusive sum over the wave's lanes (lane = token): within rows of 16 lanes, then the last lanes of rows 0 and 2 into rows 1 and 3, then
 // lane 31 into the upper half.  In registers; through LDS (six exchanges) it took 900 cycles.
-__device__ __forceinline__ double wave_scan(double x, int)
+__device__ __forceinline__ double wave_scan(double x)
 {
     x += dpp_f64<0x111, 0xf>(x);  // lane - 1
     x += dpp_f64<0x112, 0xf>(x);

@@ -27,7 +27,7 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
     typedef typename Frag<T>::type F;
     constexpr int DS = 32, PE = 16 / (int)sizeof(T), CHX = DS / PE, CHB = NP / PE;
     constexpr int NX = 64 * CHX, PB = 64 * CHB / 256, PX = (NX + 255) / 256;
-    constexpr int LX = red_ld<T>(DS), LB = dual_ld<T>(NP), TNW = NP / 64, TD = DS / 16;
+    constexpr int LX = red_ld<T>(DS), LB = nat_ld<T>(NP), TNW = NP / 64, TD = DS / 16;
     __shared__ __attribute__((aligned(16))) T sX[2][64 * LX];
     __shared__ __attribute__((aligned(16))) T sB[2][64 * LB];
     __shared__ __attribute__((aligned(16))) float sW[2][64];
@@ -102,7 +102,7 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
             *(intx4*)(sB[buf] + row * LB + ch * PE) = br[k];
         }
         if (wave == 0) {
-            const double s = wave_scan(ssm_exponent(dtr, rate), lane), tot = wave_last(s);
+            const double s = wave_scan(ssm_exponent(dtr, rate)), tot = wave_last(s);
             sW[buf][lane] = back ? exp2_f64(s) : exp2_f64(tot - s) * dtr;
             if (lane == 0) sTot[buf] = exp2_f64(tot);
         }
@@ -115,7 +115,7 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
             const floatx8 w = join(ld4f(sW[buf] + 32 * kb + 4 * g), ld4f(sW[buf] + 32 * kb + 16 + 4 * g));
 #pragma unroll
             for (int nt = 0; nt < TNW; ++nt)
-                wb[nt][kb].set(w * to_f8(ld_red_dual(sB[buf], LB, 16 * (TNW * wave + nt), kb, g, r)));
+                wb[nt][kb].set(w * to_f8(ld_red(sB[buf], LB, 16 * (TNW * wave + nt), kb, g, r)));
         }
         const float tot = sTot[buf];
 #pragma unroll
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
 {
     typedef typename Frag<T>::type F;
     constexpr bool two = sizeof(T) == 2;
-    constexpr int PE = 16 / (int)sizeof(T), LD1 = dual_ld<T>(D), LD2 = dual_ld<T>(NP);
+    constexpr int PE = 16 / (int)sizeof(T), LD1 = nat_ld<T>(D), LD2 = nat_ld<T>(NP);
     constexpr int TN = NP / 16, TD = D / 16, SH = NP * LD1;
     constexpr int C1 = D / PE, C2 = NP / PE, P1 = 64 * C1 / 256, P2 = 64 * C2 / 256, PS = NP * D / 4 / 256;
     // States of up to 4096 elements: B and C stay in LDS for all heads, and h waits in registers for its product with g (bf16, d = N = 64: the
@@ -250,10 +250,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
 #pragma unroll
             for (int kb = 0; kb < D / 32; ++kb) {
                 if constexpr (two) {
-                    o = mma(ld_nat_dual(sH + 2 * SH, LD1, 16 * nt, kb, g, r), f[kb], o);
-                    o = mma(ld_nat_dual(sH + SH, LD1, 16 * nt, kb, g, r), f[kb], o);
+                    o = mma(ld_nat(sH + 2 * SH + (16 * nt + r) * LD1, kb, g), f[kb], o);
+                    o = mma(ld_nat(sH + SH + (16 * nt + r) * LD1, kb, g), f[kb], o);
                 }
-                o = mma(ld_nat_dual(sH, LD1, 16 * nt, kb, g, r), f[kb], o);
+                o = mma(ld_nat(sH + (16 * nt + r) * LD1, kb, g), f[kb], o);
             }
             return o;
         };
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
 #pragma unroll
             for (int i = 0; i < PS; ++i) held[i] = rst[i];
         if (wave == 0) {
-            const double s = wave_scan(ssm_exponent(d, ssm_rate(a.A[h])), lane), tot = wave_last(s);
+            const double s = wave_scan(ssm_exponent(d, ssm_rate(a.A[h]))), tot = wave_last(s);
             sS[lane] = (float)s;
             sSl[lane] = (float)(s - (double)(float)s);
             sDt[lane] = d;
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
         __syncthreads();
         if (stay)
 #pragma unroll
-            for (int kb = 0; kb < NP / 32; ++kb) cf[kb] = ld_acc_dual(tC, LD2, 16 * wave, kb, g, r);
+            for (int kb = 0; kb < NP / 32; ++kb) cf[kb] = ld_acc(tC, LD2, 16 * wave, kb, g, r);
         const float s_me = sS[me], sl_me = sSl[me], dt_me = sDt[me], e_me = sE[me], f_me = sF[me];
         float rs = 0.f;
         {
@@ -300,9 +300,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                 if (ut <= wave) {
                     floatx4 k = zero4(), q = zero4(), l;
 #pragma unroll
-                    for (int kb = 0; kb < NP / 32; ++kb) k = mma(ld_acc_dual(tB, LD2, 16 * ut, kb, g, r), cf[kb], k);
+                    for (int kb = 0; kb < NP / 32; ++kb) k = mma(ld_acc(tB, LD2, 16 * ut, kb, g, r), cf[kb], k);
 #pragma unroll
-                    for (int kb = 0; kb < D / 32; ++kb) q = mma(ld_nat_dual(s1, LD1, 16 * ut, kb, g, r), yf[kb], q);
+                    for (int kb = 0; kb < D / 32; ++kb) q = mma(ld_nat(s1 + (16 * ut + r) * LD1, kb, g), yf[kb], q);
                     decay(s_me, sl_me, 16 * ut + 4 * g, l, false);
                     const floatx4 du = ld4f(sDt + 16 * ut + 4 * g);
 #pragma unroll
@@ -321,8 +321,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
 #pragma unroll
                 for (int e = 0; e < 4; ++e) rs += o[e] * (float)cf[nt >> 1][4 * (nt & 1) + e];
                 dc[nt] += o;
-                dc[nt] = mma(ld_red_dual(tB, LD2, 16 * nt, 0, g, r), pf[0], dc[nt]);
-                if (wave >= 2) dc[nt] = mma(ld_red_dual(tB, LD2, 16 * nt, 1, g, r), pf[1], dc[nt]);
+                dc[nt] = mma(ld_red(tB, LD2, 16 * nt, 0, g, r), pf[0], dc[nt]);
+                if (wave >= 2) dc[nt] = mma(ld_red(tB, LD2, 16 * nt, 1, g, r), pf[1], dc[nt]);
             }
         }
         rs = rows_sum(rs);
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
         __syncthreads();
         if (stay)
 #pragma unroll
-            for (int kb = 0; kb < NP / 32; ++kb) bf[kb] = ld_acc_dual(tB, LD2, 16 * wave, kb, g, r);
+            for (int kb = 0; kb < NP / 32; ++kb) bf[kb] = ld_acc(tB, LD2, 16 * wave, kb, g, r);
         float pu = 0.f, late = 0.f, diag = 0.f;
         {
             floatx4 pk[4], pq[4];
@@ -364,9 +364,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                 if (tt >= wave) {
                     floatx4 k = zero4(), q = zero4(), l;
 #pragma unroll
-                    for (int kb = 0; kb < NP / 32; ++kb) k = mma(ld_acc_dual(tC, LD2, 16 * tt, kb, g, r), bf[kb], k);
+                    for (int kb = 0; kb < NP / 32; ++kb) k = mma(ld_acc(tC, LD2, 16 * tt, kb, g, r), bf[kb], k);
 #pragma unroll
-                    for (int kb = 0; kb < D / 32; ++kb) q = mma(ld_nat_dual(s1, LD1, 16 * tt, kb, g, r), xf[kb], q);
+                    for (int kb = 0; kb < D / 32; ++kb) q = mma(ld_nat(s1 + (16 * tt + r) * LD1, kb, g), xf[kb], q);
                     decay(s_me, sl_me, 16 * tt + 4 * g, l, true);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -386,18 +386,18 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                 floatx4 o = mma_state(nt, xf) * f_me;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) late += o[e] * (float)bf[nt >> 1][4 * (nt & 1) + e];
-                if (wave < 2) o = mma(ld_red_dual(tC, LD2, 16 * nt, 0, g, r), qf[0], o);
-                o = mma(ld_red_dual(tC, LD2, 16 * nt, 1, g, r), qf[1], o);
+                if (wave < 2) o = mma(ld_red(tC, LD2, 16 * nt, 0, g, r), qf[0], o);
+                o = mma(ld_red(tC, LD2, 16 * nt, 1, g, r), qf[1], o);
                 db[nt] += dt_me * o;
             }
 #pragma unroll
             for (int d = 0; d < TD; ++d) {
                 floatx4 o = zero4();
 #pragma unroll
-                for (int kb = 0; kb < NP / 32; ++kb) o = mma(ld_red_dual(sH, LD1, 16 * d, kb, g, r), bf[kb], o);
+                for (int kb = 0; kb < NP / 32; ++kb) o = mma(ld_red(sH, LD1, 16 * d, kb, g, r), bf[kb], o);
                 o *= f_me;
-                if (wave < 2) o = mma(ld_red_dual(s1, LD1, 16 * d, 0, g, r), kf[0], o);
-                o = mma(ld_red_dual(s1, LD1, 16 * d, 1, g, r), kf[1], o);
+                if (wave < 2) o = mma(ld_red(s1, LD1, 16 * d, 0, g, r), kf[0], o);
+                o = mma(ld_red(s1, LD1, 16 * d, 1, g, r), kf[1], o);
                 const floatx4 yt = to_f4(ld4<T>(s1 + me * LD1 + 16 * d + 4 * g));
                 if (64 * c + me < a.L) st4((T*)a.dx + (tok + me) * D + 16 * d + 4 * g, me < n ? dt_me * o + skip * yt : zero4());
             }
@@ -414,12 +414,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
         if (lane == 0) sDD[wave] = diag;
         __syncthreads();
         if (wave == 0) {
-            const double ds = sDs[lane], below = wave_scan(ds, lane), all = wave_last(below);
-            const double late_all = wave_last(wave_scan((double)sLate[lane], lane));
+            const double ds = sDs[lane], below = wave_scan(ds), all = wave_last(below);
+            const double late_all = wave_last(wave_scan((double)sLate[lane]));
             const double end = late_all + (double)sE[63] * ((double)sDot[0] + sDot[1] + sDot[2] + sDot[3]);
             const double da = all - below + ds + end;
             if (64 * c + lane < a.L) a.ddt[tok + lane] = lane < n ? (float)((double)sP[lane] + A * da) : 0.f;
-            const double dA = wave_last(wave_scan((double)sDt[lane] * da, lane));
+            const double dA = wave_last(wave_scan((double)sDt[lane] * da));
             if (lane == 0) {
                 a.part_head[(bh * a.nch + c) * 2] = (float)dA;
                 a.part_head[(bh * a.nch + c) * 2 + 1] = sDD[0] + sDD[1] + sDD[2] + sDD[3];

@@ -19,18 +19,18 @@ namespace {
 // segments: 95-102 us and 43-46 us of SUM for 157 MB; 16 heads x 16411 tokens in float32, d = N = 64, 29 segments: 96 and 33 us).  Waves that own
 // columns d and put the weights on X halve the splitting at N = 128 (82 and 40 us), and lose as much where N = 64 or d = 32 (d = 128, N = 64: 106 us
 // instead of 82; float32, d = 32, N = 128: 188 instead of 118), since every wave then reads all of B and C from LDS.
-template <typename T, int D, int NP, bool SUM> struct SsmGeo {
+template <typename T, int D, int NP> struct SsmGeo {
     static constexpr int PE = 16 / (int)sizeof(T);
     static constexpr int CHX = D / PE, CHB = NP / PE;        // 16-byte pieces of a row
     static constexpr int PX = 64 * CHX / 256, PB = 64 * CHB / 256;
-    static constexpr int LX = red_ld<T>(D), LB = dual_ld<T>(NP), LH = red_ld<T>(D);
+    static constexpr int LX = red_ld<T>(D), LB = nat_ld<T>(NP), LH = red_ld<T>(D);
     static constexpr int TNW = NP / 64, TD = D / 16;
 };
 
 template <typename T, int D, int NP, bool SUM>
 __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
 {
-    typedef SsmGeo<T, D, NP, SUM> G;
+    typedef SsmGeo<T, D, NP> G;
     typedef typename Frag<T>::type F;
     __shared__ __attribute__((aligned(16))) T sX[64 * G::LX];
     __shared__ __attribute__((aligned(16))) T sB[64 * G::LB];
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
     float dtr = 0.f;
     auto load_dt = [&](int c) { dtr = c < cend && lane < len - 64 * c ? dt[64 * c + lane] : 0.f; };
     auto exponents = [&](int buf) {  // of the chunk whose dt is loaded
-        const double s = wave_scan(ssm_exponent(dtr, rate), lane), tot = wave_last(s);
+        const double s = wave_scan(ssm_exponent(dtr, rate)), tot = wave_last(s);
         decay += tot;
         if (!SUM) {
             sS[buf][lane] = (float)s;
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
                 for (int kb = 0; kb < NP / 32; ++kb)
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
-                        p[i] = mma(ld_acc_dual(sB, G::LB, 32 * hf + 16 * i, kb, g, r), cf[kb], p[i]);
+                        p[i] = mma(ld_acc(sB, G::LB, 32 * hf + 16 * i, kb, g, r), cf[kb], p[i]);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int u0 = 32 * hf + 16 * i + 4 * g;
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(256) ssm_forward_kernel(SsmArgs a)
             const floatx8 w = join(ld4f(sW[buf] + 32 * kb + 4 * g), ld4f(sW[buf] + 32 * kb + 16 + 4 * g));
 #pragma unroll
             for (int nt = 0; nt < G::TNW; ++nt)
-                wb[nt][kb].set(w * to_f8(ld_red_dual(sB, G::LB, 16 * (G::TNW * wave + nt), kb, g, r)));
+                wb[nt][kb].set(w * to_f8(ld_red(sB, G::LB, 16 * (G::TNW * wave + nt), kb, g, r)));
         }
         const float es = SUM ? 0.f : sE[buf][16 * wave + r], tot = sTot[buf];
 #pragma unroll

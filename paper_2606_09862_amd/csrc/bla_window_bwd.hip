@@ -19,7 +19,7 @@ template <typename T, int D> constexpr int bwd_tiles() { return D == 128 ? 1 : 2
 template <typename T, int D> struct BwdGeo {
     static constexpr int NT = 256, PE = 16 / (int)sizeof(T), CH = D / PE, RPP = NT / CH, NP = 64 / RPP;
     static constexpr int XT = bwd_tiles<T, D>(), NB = 64 * XT;
-    static constexpr int LD = dual_ld<T>(D), LN = nat_ld<T>(D);
+    static constexpr int LD = nat_ld<T>(D);
 };
 
 // Query pass: as the forward kernel, S^T and dP^T tiles (rows: keys) whose dS^T is the operand of dQ^T = K^T dS^T.
@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
 {
     typedef BwdGeo<T, D> G;
     typedef typename Frag<T>::type F;
-    constexpr int QT = G::XT, BUF = 64 * (G::LD + G::LN);
+    constexpr int QT = G::XT, BUF = 64 * 2 * G::LD;
     __shared__ __attribute__((aligned(16))) T lds[2 * BUF];
 
     long long u = xcd_unit(blockIdx.x, a.q_per);
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
         for (int ps = 0; ps < G::NP; ++ps) {
             const int i = ps * G::RPP + lrow;
             *(intx4*)(sK + i * G::LD + ch * G::PE) = kr[ps];
-            *(intx4*)(sV + i * G::LN + ch * G::PE) = vr[ps];
+            *(intx4*)(sV + i * G::LD + ch * G::PE) = vr[ps];
         }
         __syncthreads();
         if (t + 1 < ntile) load(t + 1);
@@ -120,8 +120,8 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
                 for (int qt = 0; qt < QT; ++qt) s[qt][kt] = dp[qt][kt] = zero4();
 #pragma unroll
                 for (int kb = 0; kb < D / 32; ++kb) {
-                    const F kf = ld_nat_dual(sK, G::LD, 32 * hf + 16 * kt, kb, g, r);
-                    const F vf = ld_nat(sV + (32 * hf + 16 * kt + r) * G::LN, kb, g);
+                    const F kf = ld_nat(sK + (32 * hf + 16 * kt + r) * G::LD, kb, g);
+                    const F vf = ld_nat(sV + (32 * hf + 16 * kt + r) * G::LD, kb, g);
 #pragma unroll
                     for (int qt = 0; qt < QT; ++qt) {
                         s[qt][kt] = mma(kf, qf[qt][kb], s[qt][kt]);
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
             for (int qt = 0; qt < QT; ++qt) sf[qt] = frag_from_acc<T>(s[qt][0], s[qt][1]);
 #pragma unroll
             for (int dt = 0; dt < D / 16; ++dt) {
-                const F kf = ld_red_dual(sK, G::LD, 16 * dt, hf, g, r);
+                const F kf = ld_red(sK, G::LD, 16 * dt, hf, g, r);
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt) acc[qt][dt] = mma(kf, sf[qt], acc[qt][dt]);
             }
@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
 template <typename T, int D> __device__ __forceinline__ void window_bwd_sinks(const WindowBwdArgs& a, unsigned u, char* raw)
 {
     typedef typename Frag<T>::type F;
-    constexpr int LD = dual_ld<T>(D), LO = D + 4;
+    constexpr int LD = nat_ld<T>(D), LO = D + 4;
     constexpr size_t QB = sizeof(T) * 4 * 2 * 32 * LD, OB = sizeof(float) * 4 * 16 * LO;
     static_assert(QB <= sizeof(T) * 256 * BwdGeo<T, D>::LD && OB <= QB, "the key kernel's LDS");
     const int part = (int)(u % (unsigned)a.ssplit);
@@ -250,8 +250,8 @@ template <typename T, int D> __device__ __forceinline__ void window_bwd_sinks(co
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) {
-            dv[dt] = mma(ld_red_dual(sD, LD, 16 * dt, 0, g, r), pf, dv[dt]);
-            dk[dt] = mma(ld_red_dual(sQ, LD, 16 * dt, 0, g, r), sf, dk[dt]);
+            dv[dt] = mma(ld_red(sD, LD, 16 * dt, 0, g, r), pf, dv[dt]);
+            dk[dt] = mma(ld_red(sQ, LD, 16 * dt, 0, g, r), sf, dk[dt]);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -377,8 +377,8 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
                     for (int kt = 0; kt < KT; ++kt) s[kt][qt] = dp[kt][qt] = zero4();
 #pragma unroll
                     for (int kb = 0; kb < D / 32; ++kb) {
-                        const F qf = ld_nat_dual(sQ, G::LD, 32 * hf + 16 * qt, kb, g, r);
-                        const F df = ld_nat_dual(sD, G::LD, 32 * hf + 16 * qt, kb, g, r);
+                        const F qf = ld_nat(sQ + (32 * hf + 16 * qt + r) * G::LD, kb, g);
+                        const F df = ld_nat(sD + (32 * hf + 16 * qt + r) * G::LD, kb, g);
 #pragma unroll
                         for (int kt = 0; kt < KT; ++kt) {
                             s[kt][qt] = mma(qf, kf[kt][kb], s[kt][qt]);
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
                 }
 #pragma unroll
                 for (int dt = 0; dt < D / 16; ++dt) {
-                    const F df = ld_red_dual(sD, G::LD, 16 * dt, hf, g, r), qf = ld_red_dual(sQ, G::LD, 16 * dt, hf, g, r);
+                    const F df = ld_red(sD, G::LD, 16 * dt, hf, g, r), qf = ld_red(sQ, G::LD, 16 * dt, hf, g, r);
 #pragma unroll
                     for (int kt = 0; kt < KT; ++kt) {
                         dv[kt][dt] = mma(df, pf[kt], dv[kt][dt]);
