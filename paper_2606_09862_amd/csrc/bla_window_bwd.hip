@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         s[qt][kt][e] = exp2_fast(__builtin_fmaf(s[qt][kt][e], sc, -lse2[qt])) * (dp[qt][kt][e] - delta[qt]);
-            if (i1 > c + a0 || (i0 <= c + aend - a.W && i1 >= sb)) {  // some pair is not visible
+            if (i1 > c + a0 || (i0 <= c + aend - a.W && i1 >= sb)) {  // some pair is not visible (selects without branches, as in the forward kernel)
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt) {
                     const int jhi = c + a0 + 16 * qt + r, jlo = jhi - (a.W - 1), j = i0 + 4 * g;
@@ -240,7 +240,7 @@ template <typename T, int D> __device__ __forceinline__ void window_bwd_sinks(co
                 const int q = q0 + 16 * qt + 4 * g + e;
                 const size_t at = row0 + min(q, len - 1);
                 const float p = exp2_fast(__builtin_fmaf(s[qt][e], sc, -a.lse[at] * kLog2e));
-                const bool seen = (q >= q_sink) & (q < len);
+                const bool seen = (q >= q_sink) & (q < len);  // no branch: see the forward kernel's masks
                 s[qt][e] = seen ? p : 0.f;
                 dp[qt][e] = seen ? p * (dp[qt][e] - a.delta[at]) : 0.f;
             }
@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(256) window_bwd_k_kernel(WindowBwdArgs a)
                             dp[kt][qt][e] = s[kt][qt][e] * (dp[kt][qt][e] - delta[e]);
                         }
                 }
-                if (kend > q0 || q1 >= len || q1 - k0 >= a.W) {  // some pair is not visible
+                if (kend > q0 || q1 >= len || q1 - k0 >= a.W) {  // some pair is not visible (selects without branches, as in the forward kernel)
 #pragma unroll
                     for (int kt = 0; kt < KT; ++kt) {
                         const int q = q0 + 4 * g - (k0 + 16 * kt + r);

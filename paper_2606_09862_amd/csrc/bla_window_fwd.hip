@@ -220,6 +220,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
 #pragma unroll
                 for (int kb = 0; kb < D / 32; ++kb) s[kt] = mma(ld_nat(sK + (32 * hf + 16 * kt + r) * G::LK, kb, g), qf[kb], s[kt]);
             }
+            // Masks are selects without branches (& and |, not && and ||, and every element assigned): a form that branched per lane around the
+            // products' results was compiled to code with wrong results.
             if (i1 > c + a0 || (i0 <= c + aend - a.W && i1 >= sb)) {  // some pair is not visible
                 const int j = i0 + 4 * g;
                 if (i0 >= sb) {
