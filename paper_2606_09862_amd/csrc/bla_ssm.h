@@ -47,7 +47,7 @@ struct SsmBwdArgs {
     float *ddt, *dA, *dD, *dstate_in;  // dD, dstate_in: or null
     float* enter;                   // [B H][nch][N][D]: the states entering the chunks
     float* leave;                   // [B H][nch][N][D]: the gradients of the states leaving them
-    float* part_head;               // [B H][nch][2]: a chunk's parts of dA and dD
+    double* part_head;              // [B H][nch][2]: a chunk's parts of dA and dD
     float* part_bc;                 // hsplit > 1: [hsplit][B][G][nch][2][64][N]
     int B, H, G, L, N, nch, hsplit;
     long long walk_units, walk_per, units, per;
@@ -152,6 +152,12 @@ __device__ __forceinline__ double wave_scan(double x)
     x += dpp_f64<0x142, 0xa>(x);  // lane 15 of the row before, into rows 1 and 3
     x += dpp_f64<0x143, 0xc>(x);  // lane 31, into rows 2 and 3
     return x;
+}
+// rows_sum (over the four row groups of a column) of float64 values
+__device__ __forceinline__ double rows_sum_f64(double x)
+{
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
 }
 // The last lane's value in every lane.
 __device__ __forceinline__ double wave_last(double x)

@@ -72,7 +72,7 @@ BackwardPlan backward_plan(const bla_ssm_params* p)
     b.hsplit = rep > 0 ? (int)((rep + (rep + n - 1) / n - 1) / ((rep + n - 1) / n)) : 1;  // parts of equal size, none empty
     b.off_leave = states;
     b.off_head = 2 * states;
-    b.off_bc = b.off_head + seq_align(bhc * 2 * 4);
+    b.off_bc = b.off_head + seq_align(bhc * 2 * 8);
     b.total = b.off_bc + (b.hsplit > 1 ? seq_align((size_t)b.hsplit * units * 2 * 64 * p->N * 4) : 0);
     return b;
 }
@@ -190,7 +190,7 @@ bla_status bla_ssm_backward(const bla_ssm_params* p, const void* x, const float*
     SsmBwdArgs a = {};
     a.x = x, a.Bm = Bm, a.Cm = Cm, a.dy = dy, a.dt = dt, a.A = A, a.Dm = D, a.state_in = state_in, a.dstate_out = dstate_out;
     a.lengths = lengths, a.dx = dx, a.dBm = dB, a.dCm = dC, a.ddt = ddt, a.dA = dA, a.dD = dD, a.dstate_in = dstate_in;
-    a.enter = (float*)ws, a.leave = (float*)(ws + b.off_leave), a.part_head = (float*)(ws + b.off_head);
+    a.enter = (float*)ws, a.leave = (float*)(ws + b.off_leave), a.part_head = (double*)(ws + b.off_head);
     a.part_bc = (float*)(ws + b.off_bc);
     a.B = p->B, a.H = p->H, a.G = p->G, a.L = p->L, a.N = p->N, a.nch = b.nch, a.hsplit = b.hsplit;
     a.walk_units = (long long)p->B * p->H * (p->d / 32), a.walk_per = (a.walk_units + 7) / 8;

@@ -12,7 +12,8 @@
 //   ddt_t = p_t + A da_t,   dA = sum_t dt_t da_t,   dD = sum_t x_t . dy_t.
 // Two walks over the chunks leave h and g of every chunk in the workspace; then the chunks are independent.  ddt, dA, dD and the
 // state's gradient are float32 results and take no operand rounding: their products of bf16 inputs are exact,
-// and h and g enter them as sums of three bf16 (Split).  dx, dB, dC take weights in the operand type.
+// and h and g enter them as sums of three bf16 (Split).  In da_t the M_t'u of u >= t are in the rows' sums and in the columns' and cancel, so both
+// sum the same float32 values in float64 (float32 sums left dA off by up to thirty times what a float32 recurrence leaves).  dx, dB, dC take weights in the operand type.
 #include "bla_ssm.h"
 
 namespace bla {
@@ -154,7 +155,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
     __shared__ __attribute__((aligned(16))) T s2[(stay ? 2 : 1) * 64 * LD2];  // B, then C; or both
     __shared__ __attribute__((aligned(16))) T sH[(two ? 3 : 1) * SH];   // h, then g: rounded, what that leaves, and what that leaves
     __shared__ __attribute__((aligned(16))) float sS[64], sSl[64], sDt[64];
-    __shared__ float sE[64], sF[64], sDs[64], sP[64], sLate[64], sDot[4], sDD[4];
+    __shared__ double sDs[64], sLate[64];
+    __shared__ float sE[64], sF[64], sP[64], sDot[4], sDD[4];
 
     long long u = xcd_unit(blockIdx.x, a.per);
     if (u >= a.units) return;
@@ -238,7 +240,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
             for (int i = tid; i < min(64, a.L - 64 * c) * (D / PE); i += 256)
                 *(intx4*)((T*)a.dx + tok * D + (size_t)i * PE) = intx4{0, 0, 0, 0};
             if (tid < min(64, a.L - 64 * c)) a.ddt[tok + tid] = 0.f;
-            if (tid < 2) a.part_head[(bh * a.nch + c) * 2 + tid] = 0.f;
+            if (tid < 2) a.part_head[(bh * a.nch + c) * 2 + tid] = 0.0;
             continue;
         }
         const float skip = a.Dm ? a.Dm[h] : 0.f;
@@ -291,8 +293,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
 #pragma unroll
             for (int kb = 0; kb < NP / 32; ++kb) cf[kb] = ld_acc(tC, LD2, 16 * wave, kb, g, r);
         const float s_me = sS[me], sl_me = sSl[me], dt_me = sDt[me], e_me = sE[me], f_me = sF[me];
-        float rs = 0.f;
+        double rs = 0.0;
         {
+            float rh = 0.f;
             floatx4 p[4];
 #pragma unroll
             for (int ut = 0; ut < 4; ++ut) {
@@ -307,10 +310,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                     const floatx4 du = ld4f(sDt + 16 * ut + 4 * g);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float w = l[e] * q[e] * du[e];
-                        w = 16 * ut + 4 * g + e <= me ? w : 0.f;
-                        p[ut][e] = w;
-                        rs += w * k[e];
+                        const float w = 16 * ut + 4 * g + e <= me ? l[e] * q[e] : 0.f;
+                        p[ut][e] = w * du[e];
+                        rs += (double)(w * k[e]) * (double)du[e];
                     }
                 }
             }
@@ -319,13 +321,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
             for (int nt = 0; nt < TN; ++nt) {
                 const floatx4 o = mma_state(nt, yf) * e_me;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) rs += o[e] * (float)cf[nt >> 1][4 * (nt & 1) + e];
+                for (int e = 0; e < 4; ++e) rh += o[e] * (float)cf[nt >> 1][4 * (nt & 1) + e];
                 dc[nt] += o;
                 dc[nt] = mma(ld_red(tB, LD2, 16 * nt, 0, g, r), pf[0], dc[nt]);
                 if (wave >= 2) dc[nt] = mma(ld_red(tB, LD2, 16 * nt, 1, g, r), pf[1], dc[nt]);
             }
+            rs = rows_sum_f64(rs) + (double)rows_sum(rh);
         }
-        rs = rows_sum(rs);
         __syncthreads();
 
         // ---- columns u
@@ -355,7 +357,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
         if (stay)
 #pragma unroll
             for (int kb = 0; kb < NP / 32; ++kb) bf[kb] = ld_acc(tB, LD2, 16 * wave, kb, g, r);
-        float pu = 0.f, late = 0.f, diag = 0.f;
+        double pu = 0.0;
+        float late = 0.f, diag = 0.f;
         {
             floatx4 pk[4], pq[4];
 #pragma unroll
@@ -375,7 +378,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                         diag += t == me ? q[e] : 0.f;
                         pk[tt][e] = t >= me ? w * k[e] : 0.f;
                         pq[tt][e] = t >= me ? w * q[e] : 0.f;
-                        pu += pq[tt][e] * k[e];
+                        pu += (double)(pq[tt][e] * k[e]);  // the value that the rows summed
                     }
                 }
             }
@@ -403,11 +406,11 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
             }
         }
         late = rows_sum(late);
-        pu = rows_sum(pu) + late;
+        pu = rows_sum_f64(pu) + (double)late;
         if (g == 0) {
-            sP[me] = pu;
-            sDs[me] = rs - dt_me * pu;
-            sLate[me] = dt_me * late;
+            sP[me] = (float)pu;
+            sDs[me] = rs - (double)dt_me * pu;
+            sLate[me] = (double)dt_me * (double)late;
         }
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) diag += __shfl_xor(diag, off);
@@ -415,14 +418,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
         __syncthreads();
         if (wave == 0) {
             const double ds = sDs[lane], below = wave_scan(ds), all = wave_last(below);
-            const double late_all = wave_last(wave_scan((double)sLate[lane]));
+            const double late_all = wave_last(wave_scan(sLate[lane]));
             const double end = late_all + (double)sE[63] * ((double)sDot[0] + sDot[1] + sDot[2] + sDot[3]);
             const double da = all - below + ds + end;
             if (64 * c + lane < a.L) a.ddt[tok + lane] = lane < n ? (float)((double)sP[lane] + A * da) : 0.f;
             const double dA = wave_last(wave_scan((double)sDt[lane] * da));
             if (lane == 0) {
-                a.part_head[(bh * a.nch + c) * 2] = (float)dA;
-                a.part_head[(bh * a.nch + c) * 2 + 1] = sDD[0] + sDD[1] + sDD[2] + sDD[3];
+                a.part_head[(bh * a.nch + c) * 2] = dA;
+                a.part_head[(bh * a.nch + c) * 2 + 1] = (double)sDD[0] + sDD[1] + sDD[2] + sDD[3];
             }
         }
     }
@@ -469,7 +472,7 @@ __global__ void __launch_bounds__(256) ssm_bwd_head_kernel(SsmBwdArgs a)
     const int h = blockIdx.x;
     double s[2] = {0.0, 0.0};
     for (int i = threadIdx.x; i < a.B * a.nch; i += 256) {
-        const float* p = a.part_head + (((size_t)(i / a.nch) * a.H + h) * a.nch + i % a.nch) * 2;
+        const double* p = a.part_head + (((size_t)(i / a.nch) * a.H + h) * a.nch + i % a.nch) * 2;
         s[0] += p[0];
         s[1] += p[1];
     }
