@@ -155,8 +155,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
     __shared__ __attribute__((aligned(16))) T s2[(stay ? 2 : 1) * 64 * LD2];  // B, then C; or both
     __shared__ __attribute__((aligned(16))) T sH[(two ? 3 : 1) * SH];   // h, then g: rounded, what that leaves, and what that leaves
     __shared__ __attribute__((aligned(16))) float sS[64], sSl[64], sDt[64];
-    __shared__ double sDs[64], sLate[64];
-    __shared__ float sE[64], sF[64], sP[64], sDot[4], sDD[4];
+    __shared__ double sDs[64], sLate[64], sDD[4];
+    __shared__ float sE[64], sF[64], sP[64], sDot[4];
 
     long long u = xcd_unit(blockIdx.x, a.per);
     if (u >= a.units) return;
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
 #pragma unroll
             for (int kb = 0; kb < NP / 32; ++kb) bf[kb] = ld_acc(tB, LD2, 16 * wave, kb, g, r);
         double pu = 0.0;
-        float late = 0.f, diag = 0.f;
+        float late = 0.f;
         {
             floatx4 pk[4], pq[4];
 #pragma unroll
@@ -375,7 +375,6 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                     for (int e = 0; e < 4; ++e) {
                         const int t = 16 * tt + 4 * g + e;
                         const float w = t >= me ? l[e] : 0.f;
-                        diag += t == me ? q[e] : 0.f;
                         pk[tt][e] = t >= me ? w * k[e] : 0.f;
                         pq[tt][e] = t >= me ? w * q[e] : 0.f;
                         pu += (double)(pq[tt][e] * k[e]);  // the value that the rows summed
@@ -405,6 +404,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
                 if (64 * c + me < a.L) st4((T*)a.dx + (tok + me) * D + 16 * d + 4 * g, me < n ? dt_me * o + skip * yt : zero4());
             }
         }
+        // x . dy of the token, a sum that goes on over all tokens of a head: products (exact in bf16) summed in float64
+        double xy = 0.0;
+#pragma unroll
+        for (int kb = 0; kb < D / 32; ++kb) {
+            const floatx8 a8 = to_f8(xf[kb]), b8 = to_f8(ld_nat(s1 + me * LD1, kb, g));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) xy += (double)(a8[e] * b8[e]);
+        }
         late = rows_sum(late);
         pu = rows_sum_f64(pu) + (double)late;
         if (g == 0) {
@@ -413,8 +420,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
             sLate[me] = (double)dt_me * (double)late;
         }
 #pragma unroll
-        for (int off = 32; off > 0; off >>= 1) diag += __shfl_xor(diag, off);
-        if (lane == 0) sDD[wave] = diag;
+        for (int off = 32; off > 0; off >>= 1) xy += __shfl_xor(xy, off);
+        if (lane == 0) sDD[wave] = xy;
         __syncthreads();
         if (wave == 0) {
             const double ds = sDs[lane], below = wave_scan(ds), all = wave_last(below);
@@ -425,7 +432,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_b
             const double dA = wave_last(wave_scan((double)sDt[lane] * da));
             if (lane == 0) {
                 a.part_head[(bh * a.nch + c) * 2] = dA;
-                a.part_head[(bh * a.nch + c) * 2 + 1] = (double)sDD[0] + sDD[1] + sDD[2] + sDD[3];
+                a.part_head[(bh * a.nch + c) * 2 + 1] = sDD[0] + sDD[1] + sDD[2] + sDD[3];
             }
         }
     }

@@ -48,3 +48,19 @@ def test_gradients_through_the_decays(dtype, B, H, G, L, d, N):
     for k in ("dA", "ddt"):
         own, plain, size = e[k]
         assert own <= 2 * more * plain + 2.0 ** -24 * size, (k, own / size, plain / size)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,H,G,L,d,N", [*SHAPES, (16, 1, 1, 2000, 64, 16)])
+def test_gradient_of_the_skip(dtype, B, H, G, L, d, N):
+    """dD sums the products of x and dy over all tokens, with signs that cancel: a rounding of each product in float32 (none in bf16, whose products are
+    exact), and of the result, is all that it may be off by."""
+    bla = _bla()
+    c = {k: None if t is None else t.cuda() for k, t in inputs(103, B, H, G, L, d, N, dtype, False).items()}
+    dD = bla.ssm_backward(c["x"], c["dt"], c["A"], c["Bm"], c["Cm"], c["dy"], c["D"])[5].to(F64)
+    terms = c["x"].to(F64) * c["dy"].to(F64)
+    want = terms.sum((0, 2, 3))
+    e = 2.0 ** -24
+    # random roundings of the products: five times their root sum of squares
+    bound = e * want.abs() + (5 * e * (terms ** 2).sum((0, 2, 3)).sqrt() if dtype == F32 else 1e-12 * terms.abs().sum((0, 2, 3)))
+    assert float(((dD - want).abs() / bound).max()) <= 1, ((dD - want).abs() / bound).tolist()
