@@ -6,6 +6,8 @@
 // heads that share the key head and over the queries whose windows reach the block; the sinks' other queries have
 // workgroups of their own), so that every gradient has a fixed order of sums, without atomics.  P and dS are rounded to the operand type before their second
 // products (2^-8 relative at most in bf16, as the results are); sums and row terms are float32.
+#include <algorithm>
+
 #include "bla_window.h"
 
 namespace bla {
@@ -24,7 +26,11 @@ template <typename T, int D> struct BwdGeo {
 
 // Query pass: as the forward kernel, S^T and dP^T tiles (rows: keys) whose dS^T is the operand of dQ^T = K^T dS^T.
 // Bound: issue, as the forward kernel (8 x 16 heads x 4096 queries, four heads to a key head, d = 64, window 511, bf16: 160-168 us).
-template <typename T, int D>
+//
+// EXACT: delta is formed from outputs that were rounded to bf16, which adds 2^-9 |dO| |o| or so to each dP - delta.  That is lost among dS's own
+// rounding where many keys share a row, and as large as it where few do.  The sum of the dS of a row is what delta is off by (the exact
+// ones sum to zero), so the row's dq is put right by that sum times sum_j P_j k_j, a third product, and delta goes on to the key pass without the error.
+template <typename T, int D, bool EXACT>
 __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
 {
     typedef BwdGeo<T, D> G;
@@ -87,14 +93,17 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
         }
         delta[qt] = rows_sum(x);
         lse2[qt] = a.lse[row0 + i] * kLog2e;
-        if (g == 0 && a0 + 16 * qt + r < nq) a.delta[row0 + i] = delta[qt];
+        if (!EXACT && g == 0 && a0 + 16 * qt + r < nq) a.delta[row0 + i] = delta[qt];
     }
     const float sc = a.scale * kLog2e;
-    floatx4 acc[QT][D / 16];
+    floatx4 acc[QT][D / 16], pk[EXACT ? QT : 1][D / 16];
+    float off[QT];
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt)
+    for (int qt = 0; qt < QT; ++qt) {
+        off[qt] = 0.f;
 #pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] = zero4();
+        for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] = pk[EXACT ? qt : 0][dt] = zero4();
+    }
 
     const int aend = min(a0 + 16 * QT, nq) - 1;
     load(0);
@@ -113,7 +122,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
         for (int hf = 0; hf < 2; ++hf) {
             const int i0 = t * 64 - ns + 32 * hf, i1 = i0 + 31;  // window keys (negative: sinks)
             if (i0 > c + aend || (i0 >= sb && i1 <= c + a0 - a.W)) continue;
-            floatx4 s[QT][2], dp[QT][2];
+            floatx4 s[QT][2], dp[QT][2];  // scores, then dS; dP, then P where it is wanted
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
 #pragma unroll
@@ -134,40 +143,63 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(WindowBwdArgs a)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s[qt][kt][e] = exp2_fast(__builtin_fmaf(s[qt][kt][e], sc, -lse2[qt])) * (dp[qt][kt][e] - delta[qt]);
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = exp2_fast(__builtin_fmaf(s[qt][kt][e], sc, -lse2[qt]));
+                        s[qt][kt][e] = p * (dp[qt][kt][e] - delta[qt]);
+                        dp[qt][kt][e] = p;
+                    }
             if (i1 > c + a0 || (i0 <= c + aend - a.W && i1 >= sb)) {  // some pair is not visible (selects without branches, as in the forward kernel)
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt) {
                     const int jhi = c + a0 + 16 * qt + r, jlo = jhi - (a.W - 1), j = i0 + 4 * g;
                     if (i0 >= sb) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            s[qt][e >> 2][e & 3] =
-                                (unsigned)(j + 16 * (e >> 2) + (e & 3) - jlo) < (unsigned)a.W ? s[qt][e >> 2][e & 3] : 0.f;
+                        for (int e = 0; e < 8; ++e) {
+                            const bool seen = (unsigned)(j + 16 * (e >> 2) + (e & 3) - jlo) < (unsigned)a.W;
+                            s[qt][e >> 2][e & 3] = seen ? s[qt][e >> 2][e & 3] : 0.f;
+                            if (EXACT) dp[qt][e >> 2][e & 3] = seen ? dp[qt][e >> 2][e & 3] : 0.f;
+                        }
                     } else {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             const int k = j + 16 * (e >> 2) + (e & 3);
-                            s[qt][e >> 2][e & 3] = (k <= jhi) & ((k >= jlo) | (k < sb)) ? s[qt][e >> 2][e & 3] : 0.f;
+                            const bool seen = (k <= jhi) & ((k >= jlo) | (k < sb));
+                            s[qt][e >> 2][e & 3] = seen ? s[qt][e >> 2][e & 3] : 0.f;
+                            if (EXACT) dp[qt][e >> 2][e & 3] = seen ? dp[qt][e >> 2][e & 3] : 0.f;
                         }
                     }
                 }
             }
-            F sf[QT];
+            F sf[QT], pf[QT];
 #pragma unroll
-            for (int qt = 0; qt < QT; ++qt) sf[qt] = frag_from_acc<T>(s[qt][0], s[qt][1]);
+            for (int qt = 0; qt < QT; ++qt) {
+                sf[qt] = frag_from_acc<T>(s[qt][0], s[qt][1]);
+                if (EXACT) {
+                    pf[qt] = frag_from_acc<T>(dp[qt][0], dp[qt][1]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) off[qt] += s[qt][e >> 2][e & 3];
+                }
+            }
 #pragma unroll
             for (int dt = 0; dt < D / 16; ++dt) {
                 const F kf = ld_red(sK, G::LD, 16 * dt, hf, g, r);
 #pragma unroll
-                for (int qt = 0; qt < QT; ++qt) acc[qt][dt] = mma(kf, sf[qt], acc[qt][dt]);
+                for (int qt = 0; qt < QT; ++qt) {
+                    acc[qt][dt] = mma(kf, sf[qt], acc[qt][dt]);
+                    if (EXACT) pk[qt][dt] = mma(kf, pf[qt], pk[qt][dt]);
+                }
             }
         }
     }
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         const int i = a0 + 16 * qt + r;
+        if (EXACT) {
+            off[qt] = rows_sum(off[qt]);
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] -= off[qt] * pk[qt][dt];
+            if (g == 0 && i < nq) a.delta[row0 + i] = delta[qt] + off[qt];
+        }
         if (i >= min(G::NB, a.L - q0)) continue;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt)
@@ -465,10 +497,19 @@ template <typename T, int D> __global__ void __launch_bounds__(256) window_bwd_s
         st4((T*)a.dv + at + c - D, x);
 }
 
+// Most keys of a row for which delta's error is taken out in the query pass (bf16).  Relative error of dq and dk with it and without, by keys of a row: 8 keys
+// 0.0023 and 0.0030-0.0034, 16 keys 0.0023 and 0.0027, 64 keys 0.0024 and 0.0026, 511 keys 0.0024 and 0.0025 (rounded results alone: 0.0017).  Time with it and
+// without, 8 x 16 heads x 4096 tokens on 4 key heads: d = 64, 8 keys 137 and 131 us, 64 keys 185 and 173; d = 32, 64 keys 112 and 100; d = 64, 515 keys 390 and
+// 340, which is why long windows go without.
+constexpr int kExactKeys = 64;
+
 template <typename T, int D> hipError_t backward_d(const WindowBwdArgs& a, hipStream_t s)
 {
     typedef BwdGeo<T, D> G;
-    hipLaunchKernelGGL((window_bwd_q_kernel<T, D>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
+    if (std::min((long long)a.W + a.S, (long long)a.L) <= kExactKeys)
+        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, sizeof(T) == 2>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
+    else
+        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, false>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
     hipLaunchKernelGGL((window_bwd_k_kernel<T, D>), dim3((unsigned)(8 * a.k_per) + a.s_units), dim3(G::NT), 0, s, a);
     if (a.ns > 0) {
         const long long n = (long long)a.B * a.Hkv * a.ns * (2 * D / 4);
