@@ -332,7 +332,7 @@ bla_status bla_layer_forward_timed(const bla_params* p, const double* T, const v
  *   2^62 has no tokens in this call (an idle row of a serving batch): zeros as for padding, and its ring stays.
  * A non-finite value in a token of the sequence may reach the outputs of other queries that share a tile of keys with it.
  * Supported: float32 or bfloat16; d in {32, 64, 128}; H a multiple of H_kv; window >= 1, sinks >= 0, window + sinks <= 2^30; 1e-6 <=
- * |scale| <= 1e6.  Alignment, ownership, streams, workspaces and errors follow the conventions above; the outputs must not
+ * |scale| <= 1e6; products <q, k> of less than 1e30.  Alignment, ownership, streams, workspaces and errors follow the conventions above; the outputs must not
  * overlap the inputs or one another (BLA_ERR_INVALID_ARG).  H = 0 beside key heads is BLA_ERR_UNSUPPORTED where the call writes rings, dk or dv.
  */
 typedef struct {
@@ -344,7 +344,7 @@ typedef struct {
     float scale;           /* softmax scale; 0 selects 1/sqrt(d)                            */
 } bla_window_params;
 
-/* BLA_OK if the shape in *p has kernels, else the error it would get. */
+/* BLA_OK if bla_window_forward takes the shape in *p, else the error it would get (the backward pass may have a lower limit: its workspace size is 0 then). */
 bla_status bla_window_supported(const bla_window_params* p);
 
 /* Bytes of device workspace bla_window_forward needs (0: none, or *p is not supported). */
@@ -396,7 +396,7 @@ typedef struct {
     int32_t io_dtype; /* bla_dtype of x, y, dx, dy */
 } bla_conv_params;
 
-/* BLA_OK if the shape in *p has kernels, else the error it would get. */
+/* BLA_OK if bla_conv_forward takes the shape in *p, else the error it would get (the backward pass may have a lower limit: its workspace size is 0 then). */
 bla_status bla_conv_supported(const bla_conv_params* p);
 
 /* state_out (NULL = not wanted) receives the state after the call. */
@@ -438,7 +438,7 @@ typedef struct {
     int32_t io_dtype; /* bla_dtype of x, Bm, Cm, y and their gradients */
 } bla_ssm_params;
 
-/* BLA_OK if the shape in *p has kernels, else the error it would get. */
+/* BLA_OK if bla_ssm_forward takes the shape in *p, else the error it would get (the backward pass may have a lower limit: its workspace size is 0 then). */
 bla_status bla_ssm_supported(const bla_ssm_params* p);
 
 /* Bytes of device workspace bla_ssm_forward needs (0: none, or *p is not supported). */

@@ -199,7 +199,8 @@ template <typename T, int K> __global__ void __launch_bounds__(256) conv_step_ke
 }
 
 // A thread takes four channels and a segment of `seg` tokens and walks seg + K - 1 of them, four rows loaded at a time (eight cost a third of
-// the waves: 55 us instead of 47 for 8 x 16 heads x 4096 tokens at d = 64, bf16, four taps; 201 MB, 4.3 TB/s): dz of the last K tokens in registers
+// the waves: 55 us instead of 47 for 8 x 16 heads x 4096 tokens at d = 64, bf16, four taps, the same inputs in every call; 51-54 us with inputs that change from
+// call to call, 201 MB, 3.9 TB/s): dz of the last K tokens in registers
 // gives dx of the token K - 1 back.  A workgroup holds cw channel threads by 256 / cw segments, adds their taps'
 // gradients up in LDS in order and writes one part; conv_taps_kernel adds the parts.
 template <typename T, int K> __global__ void __launch_bounds__(256) conv_backward_kernel(ConvBwdArgs a)

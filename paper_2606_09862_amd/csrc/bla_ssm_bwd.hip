@@ -22,7 +22,7 @@ namespace {
 // States entering the chunks (from B, x), and in the second half of the grid the gradients of the states leaving them (`back`: from C, dy, chunks in
 // reverse): the two walks are independent, and either alone leaves half of the device idle.  The columns d of a
 // state are independent too, so a workgroup takes 32 of one head's.  As the state update of ssm_forward_kernel.  Bound: the states' bytes (8 x 16
-// heads x 2048 tokens, d = N = 64, bf16: 49-54 us for 134 MB of states and 76 MB of reads, 4 TB/s; in two launches 80).
+// heads x 2048 tokens, d = N = 64, bf16: 49-61 us for 134 MB of states and 76 MB of reads, 3.5-4.3 TB/s; in two launches 80).
 template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_walk_kernel(SsmBwdArgs a)
 {
     typedef typename Frag<T>::type F;
@@ -138,8 +138,9 @@ template <typename T, int D, int NP> __global__ void __launch_bounds__(256) ssm_
 
 // One chunk of a group's heads (or of a part of them).  Wave w owns 16 tokens, first as columns t (dC and the row sums of M), then as columns u
 // (dx, dB and the column sums), so that every product's second operand is an accumulator of the wave; dB and dC stay in registers
-// over the heads.  Bound: issue and the waits between its phases (8 x 16 heads x 2048 tokens in two groups, d = N = 64, bf16: 82-84 us for 250 MB, two
-// states of 64 tokens among them; loads a phase ahead cost spills and gained nothing).
+// over the heads.  Bound: the waits between its phases, for memory and at barriers (8 x 16 heads x 2048 tokens in two groups, d = N = 64, bf16: 85-92 us for 250
+// MB, two states of 64 tokens among them: more than half of the waves' cycles are waits, the matrix pipes are busy 12 % and vector instructions issue in 39 %;
+// loads a phase ahead cost spills and gained nothing).
 template <typename T, int D, int NP>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 && NP == 64 ? 2 : 1) ssm_bwd_kernel(SsmBwdArgs a)
 {

@@ -15,7 +15,8 @@ namespace {
 // precision (Split) in every segment: the state is a float32 result that is carried on, and y is the same whether it is asked for or not.
 // (Weights rounded once in the segments whose state only enters y: 77 us instead of 95 on the shape below.)
 // SUM: the segment's own state from zero and its decay, for the scan over the segments; no outputs.
-// Bound: issue and the waits between a chunk's two barriers, with two workgroups on a compute unit (8 x 16 heads x 4096 tokens, d = 64, N = 128, bf16, four
+// Bound: the waits between a chunk's two barriers at two waves to a SIMD (in both forms the matrix pipes are busy 17-19 % of the cycles and vector
+// instructions issue in 40 %; two workgroups on a compute unit, 8 x 16 heads x 4096 tokens, d = 64, N = 128, bf16, four
 // segments: 95-102 us and 43-46 us of SUM for 157 MB; 16 heads x 16411 tokens in float32, d = N = 64, 29 segments: 96 and 33 us).  Waves that own
 // columns d and put the weights on X halve the splitting at N = 128 (82 and 40 us), and lose as much where N = 64 or d = 32 (d = 128, N = 64: 106 us
 // instead of 82; float32, d = 32, N = 128: 188 instead of 118), since every wave then reads all of B and C from LDS.

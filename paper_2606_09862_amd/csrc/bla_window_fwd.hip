@@ -53,8 +53,10 @@ template <typename T, int D> __device__ __forceinline__ void window_ring(const W
 // The maximum that the weights are taken against follows the true one only once that is more than 2^kLag above it: the
 // weights stay below 2^kLag, no precision is lost, and a tile needs neither a reduction over the lanes nor a rescaling
 // unless some lane has found such a score.
-// Bound: issue.  A SIMD's vector and matrix instructions hardly overlap, and a score costs an exponential, a multiply-add and its part of
-// maximum, sum and conversion beside its products (8 x 16 heads x 4096 queries, four heads to a key head, d = 64, window 1024, bf16:
+// Bound: issue.  A SIMD's vector and matrix instructions hardly overlap.  Of 32 keys a lane has eight scores: 30 vector instructions for exponentials, sums and
+// conversion and 5 for the maximum, then 24 or 40 more if some pair is masked and 32 (d = 64) or 48 (d = 128) if the maximum moves; a tile costs 23 or 46 for
+// the next one's addresses, and a workgroup some 300 before its first tile and after its last.  That is 9.6 a visible pair at d = 64 and window 1024, and 19.6 at
+// d = 128 and window 255, where a lane has 64 visible pairs in all and a third of its tiles are masked (8 x 16 heads x 4096 queries, four heads to a key head, d = 64, window 1024, bf16:
 // 190-220 us, 550-640 TFLOP/s of visible pairs; the first form, a wave to 16 queries of 4-wave groups with a reduction a tile, 337 us.  16 heads x 65536,
 // d = 128, window 255: 320-343 us for 1.08 GB, 3.3 TB/s; first form 893).
 template <typename T, int D, int NW> struct WinGeo {
