@@ -497,10 +497,10 @@ template <typename T, int D> __global__ void __launch_bounds__(256) window_bwd_s
         st4((T*)a.dv + at + c - D, x);
 }
 
-// Most keys of a row for which delta's error is taken out in the query pass (bf16).  Relative error of dq and dk with it and without, by keys of a row: 8 keys
-// 0.0023 and 0.0030-0.0034, 16 keys 0.0023 and 0.0027, 64 keys 0.0024 and 0.0026, 511 keys 0.0024 and 0.0025 (rounded results alone: 0.0017).  Time with it and
-// without, 8 x 16 heads x 4096 tokens on 4 key heads: d = 64, 8 keys 137 and 131 us, 64 keys 185 and 173; d = 32, 64 keys 112 and 100; d = 64, 515 keys 390 and
-// 340, which is why long windows go without.
+// Most keys of a row for which delta's error is taken out in the query pass (bf16).  Relative error of dq without it (dk a little less), at d = 64: sequences of
+// 16 tokens 0.0032, 8 keys a row 0.0030, 16 keys 0.0028, 64 keys 0.0026, 511 keys 0.0025; with it 0.0024 everywhere (dS and dq rounded; dq alone: 0.0017).
+// Time without it and with it, 8 x 16 heads x 4096 tokens on 4 key heads: d = 64, 8 keys 131 and 137 us, 64 keys 173 and 185; d = 32, 64 keys 100 and 112; d =
+// 64, 515 keys 340 and 390, which is why long windows go without.
 constexpr int kExactKeys = 64;
 
 template <typename T, int D> hipError_t backward_d(const WindowBwdArgs& a, hipStream_t s)
