@@ -379,6 +379,68 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
                                void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Window attention with a learned bias: the scores carry a bias of the query head and of the distance's bucket,
+ *     z_pj = scale <q_p, k_j> + bias[h][bucket(p - j)],   bucket(n) = the number of edges at or below n,
+ * so bucket 0 holds the distances below edges[0], bucket u those from edges[u - 1] to edges[u] - 1, the last those from the last edge on.
+ *   bias: device float32 [H, buckets]   edges: HOST int32 [buckets - 1], ascending (equal ones leave a bucket without a distance), >= 0
+ * edges is read before the call returns.  Everything else is window attention's: parameters, rings, lengths, pos, workspaces
+ * (bla_window_workspace_size, bla_window_step_workspace_size), errors and limits.  bucket counts above 64 and edges above 2^29 are
+ * BLA_ERR_UNSUPPORTED.  A bias below -1e30 counts as minus infinity: its pairs have no weight.  A query that is left without a key gives zeros
+ * (lse: minus infinity; gradients: zeros).  Larger biases than 1e30 and NaN are not supported.
+ */
+bla_status bla_bias_forward(const bla_window_params* p, int32_t buckets, const int32_t* edges, const void* q, const void* k,
+                            const void* v, const float* bias, const int32_t* lengths, const int64_t* pos,
+                            const void* cache_k_in, const void* cache_v_in, void* o, float* lse, void* cache_k_out,
+                            void* cache_v_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token for every row: the rings take its key and value in place. */
+bla_status bla_bias_step(const bla_window_params* p, int32_t buckets, const int32_t* edges, const void* q, const void* k,
+                         const void* v, const float* bias, const int64_t* pos, void* cache_k, void* cache_v, void* o,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of bla_bias_forward without rings and with t0 = 0, as bla_window_backward's, and dbias [H, buckets] float32: the sum over
+ * all pairs of a bucket of dLoss/dz.  Its sums run in a fixed order (no atomics between waves) over terms that are not rounded.
+ * B = 0 or L = 0 is BLA_ERR_UNSUPPORTED (dbias would be left unwritten).
+ */
+size_t bla_bias_backward_workspace_size(const bla_window_params* p, int32_t buckets);
+bla_status bla_bias_backward(const bla_window_params* p, int32_t buckets, const int32_t* edges, const void* q, const void* k,
+                             const void* v, const float* bias, const void* o, const float* lse, const void* dO,
+                             const int32_t* lengths, void* dq, void* dk, void* dv, float* dbias, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
+ * Window attention behind a prefix that rows share: every query sees all tokens of its row's prefix, and of its own row's tokens those that
+ * window attention shows it.  The rows b with the same b / (B / G) share one of G prefixes:
+ *   prefix_k, prefix_v: [G, H_kv, P, d] in the io dtype (not read where P = 0)
+ *   prefix_lengths (device int32 [G], NULL = P): a prefix has its first prefix_lengths[g] tokens only (clamped to 0 .. P).
+ * w describes the rows' own tokens, their rings, lengths and positions, as for window attention: position 0 is the row's first token behind the
+ * prefix.  Supported: what window attention takes; P <= 2^30.
+ */
+typedef struct {
+    bla_window_params w;
+    int32_t P, G; /* tokens of a prefix, prefixes (B is a multiple of G) */
+} bla_prefix_params;
+
+/* BLA_OK if bla_prefix_forward takes the shape in *p, else the error it would get. */
+bla_status bla_prefix_supported(const bla_prefix_params* p);
+
+/* Bytes of device workspace bla_prefix_forward needs (0: none, or *p is not supported). */
+size_t bla_prefix_workspace_size(const bla_prefix_params* p);
+
+/* L tokens of every row, as bla_window_forward. */
+bla_status bla_prefix_forward(const bla_prefix_params* p, const void* q, const void* k, const void* v, const void* prefix_k,
+                              const void* prefix_v, const int32_t* prefix_lengths, const int32_t* lengths, const int64_t* pos,
+                              const void* cache_k_in, const void* cache_v_in, void* o, float* lse, void* cache_k_out,
+                              void* cache_v_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One token for every row, as bla_window_step (p->w.L is ignored): the prefix is read once for all rows and heads that share it. */
+size_t bla_prefix_step_workspace_size(const bla_prefix_params* p);
+bla_status bla_prefix_step(const bla_prefix_params* p, const void* q, const void* k, const void* v, const void* prefix_k,
+                           const void* prefix_v, const int32_t* prefix_lengths, const int64_t* pos, void* cache_k,
+                           void* cache_v, void* o, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The short causal convolution of each channel, as the paper's models apply it to queries, keys and values ahead of the
  * operator:
  *     z_t = bias + sum_{j < taps} w[j] x_{t - taps + 1 + j},   y_t = z_t (silu = 0) or z_t sigmoid(z_t) (silu = 1).

@@ -44,6 +44,11 @@ class WindowParams(ctypes.Structure):
                 ("io_dtype", ctypes.c_int32), ("t0", ctypes.c_int64), ("scale", ctypes.c_float)]
 
 
+class PrefixParams(ctypes.Structure):
+    """Mirror of ``bla_prefix_params``."""
+    _fields_ = [("w", WindowParams), ("P", ctypes.c_int32), ("G", ctypes.c_int32)]
+
+
 class ConvParams(ctypes.Structure):
     """Mirror of ``bla_conv_params``."""
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32), ("d", ctypes.c_int32),
@@ -116,6 +121,23 @@ def lib():
         L.bla_window_step.argtypes = [W] + [_vp] * 8 + [ctypes.c_size_t, _vp]
         L.bla_window_backward.argtypes = [W] + [_vp] * 11 + [ctypes.c_size_t, _vp]
         for name in ("bla_window_supported", "bla_window_forward", "bla_window_step", "bla_window_backward"):
+            getattr(L, name).restype = ctypes.c_int
+        i32, ip = ctypes.c_int32, ctypes.POINTER(ctypes.c_int32)
+        L.bla_bias_forward.argtypes = [W, i32, ip] + [_vp] * 13 + [ctypes.c_size_t, _vp]
+        L.bla_bias_step.argtypes = [W, i32, ip] + [_vp] * 9 + [ctypes.c_size_t, _vp]
+        L.bla_bias_backward.argtypes = [W, i32, ip] + [_vp] * 13 + [ctypes.c_size_t, _vp]
+        L.bla_bias_backward_workspace_size.argtypes = [W, i32]
+        L.bla_bias_backward_workspace_size.restype = ctypes.c_size_t
+        for name in ("bla_bias_forward", "bla_bias_step", "bla_bias_backward"):
+            getattr(L, name).restype = ctypes.c_int
+        X = ctypes.POINTER(PrefixParams)
+        for name in ("bla_prefix_workspace_size", "bla_prefix_step_workspace_size"):
+            getattr(L, name).argtypes = [X]
+            getattr(L, name).restype = ctypes.c_size_t
+        L.bla_prefix_supported.argtypes = [X]
+        L.bla_prefix_forward.argtypes = [X] + [_vp] * 15 + [ctypes.c_size_t, _vp]
+        L.bla_prefix_step.argtypes = [X] + [_vp] * 11 + [ctypes.c_size_t, _vp]
+        for name in ("bla_prefix_supported", "bla_prefix_forward", "bla_prefix_step"):
             getattr(L, name).restype = ctypes.c_int
         C = ctypes.POINTER(ConvParams)
         L.bla_conv_backward_workspace_size.argtypes = [C]
@@ -609,6 +631,201 @@ def window_backward(q, k, v, o, lse, dO, window: int, sinks: int = 0, scale: flo
     _call(lib().bla_window_backward, "bla_window_backward", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
           lse.data_ptr(), dO.data_ptr(), _ptr(lengths), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws, n)
     return dq, dk, dv
+
+
+# ---- window attention with a learned bias ----
+
+def bias_edges(buckets: int, max_distance: int) -> tuple:
+    """The edges of the usual buckets of a causal relative position bias: half of the buckets hold one distance each, the bounds of the
+    others are in geometric progression up to max_distance, the last holds what is beyond.  Bucket half + e begins at the smallest whole n with
+    (n / half)^m >= (max_distance / half)^e, m = buckets - half, found in whole numbers."""
+    half = int(buckets) // 2
+    m, far = int(buckets) - half, int(max_distance)
+    if half < 1 or far < half:
+        raise ValueError(f"bias_edges: expected buckets >= 2 and max_distance >= buckets // 2, got {buckets} and {max_distance}")
+    edges = list(range(1, half + 1))
+    for e in range(1, m):
+        lo, hi, want = half, far, half ** m * far ** e
+        while lo < hi:
+            n = (lo + hi) // 2
+            if n ** m * half ** e >= want:
+                hi = n
+            else:
+                lo = n + 1
+        edges.append(lo)
+    return tuple(edges)
+
+
+@functools.lru_cache(maxsize=256)
+def _edge_array(edges):
+    _int32("edges", *edges)
+    return (ctypes.c_int32 * max(len(edges), 1))(*edges)
+
+
+def _bias_check(bias, edges, H, dev):
+    """(buckets, the edges' host array)."""
+    edges = tuple(edges)
+    _check_on(bias, (H, len(edges) + 1), torch.float32, "bias", dev)
+    return len(edges) + 1, _edge_array(edges)
+
+
+def bias_forward(q, k, v, bias, edges, window: int, sinks: int = 0, t0: int = 0, scale: float | None = None, lengths=None, pos=None,
+                 cache_k=None, cache_v=None, want_lse: bool = False, want_cache: bool = False, workspace=None, out=None):
+    """bla_bias_forward: window_forward whose scores carry bias[h][bucket(p - j)].
+
+    bias [H, len(edges) + 1] float32; edges: whole numbers on the host, ascending; a distance's bucket is the number of edges at or below it
+    (bias_edges gives the usual ones).  The rest, and what returns, as for window_forward.
+    """
+    B, H, L, d = q.shape
+    Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
+    p, need = _window_params("bla_window_forward", B, H, Hkv, L, d, window, sinks, t0, scale, dt)
+    _check_on(q, (B, H, L, d), dt, "q", dev)
+    _check_on(k, (B, Hkv, L, d), dt, "k", dev)
+    _check_on(v, (B, Hkv, L, d), dt, "v", dev)
+    n, e = _bias_check(bias, edges, H, dev)
+    ring = _past_check(B, Hkv, d, window, sinks, dt, dev, cache_k, cache_v, lengths, pos)
+    o = _result(out, q, (B, H, L, d))
+    lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device) if want_lse else None
+    ck = torch.empty(ring, dtype=dt, device=q.device) if want_cache else None
+    cv = torch.empty(ring, dtype=dt, device=q.device) if want_cache else None
+    keep, ws, m = _room(workspace, need, q)
+    _call(lib().bla_bias_forward, "bla_bias_forward", dev, p, n, e, q.data_ptr(), k.data_ptr(), v.data_ptr(), bias.data_ptr(), _ptr(lengths),
+          _ptr(pos), _ptr(cache_k), _ptr(cache_v), o.data_ptr(), _ptr(lse), _ptr(ck), _ptr(cv), ws, m)
+    return o, lse, ck, cv
+
+
+def _past_check(B, Hkv, d, window, sinks, dt, dev, cache_k, cache_v, lengths, pos):
+    """The checks of a prompt's rings, lengths and positions: the rings' shape."""
+    ring = (B, Hkv, sinks + window, d)
+    if (cache_k is None) != (cache_v is None):
+        raise ValueError("cache_k and cache_v: both or neither")
+    if cache_k is not None:
+        _check_on(cache_k, ring, dt, "cache_k", dev)
+        _check_on(cache_v, ring, dt, "cache_v", dev)
+    if lengths is not None:
+        _check_on(lengths, (B,), torch.int32, "lengths", dev)
+    if pos is not None:
+        _check_on(pos, (B,), torch.int64, "pos", dev)
+    return ring
+
+
+def _step_check(q, k, v, window, sinks, cache_k, cache_v, pos):
+    """The checks of a single token's tensors and rings."""
+    B, H, d = q.shape
+    Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
+    _check_on(q, (B, H, d), dt, "q", dev)
+    _check_on(k, (B, Hkv, d), dt, "k", dev)
+    _check_on(v, (B, Hkv, d), dt, "v", dev)
+    _check_on(cache_k, (B, Hkv, sinks + window, d), dt, "cache_k", dev)
+    _check_on(cache_v, (B, Hkv, sinks + window, d), dt, "cache_v", dev)
+    if pos is not None:
+        _check_on(pos, (B,), torch.int64, "pos", dev)
+
+
+def bias_step(q, k, v, bias, edges, window: int, sinks: int, cache_k, cache_v, pos=None, t0: int = 0, scale: float | None = None,
+              workspace=None, out=None):
+    """bla_bias_step: window_step whose scores carry the bias of bias_forward."""
+    B, H, d = q.shape
+    Hkv, dev = k.shape[1], q.get_device()
+    p, need = _window_params("bla_window_step", B, H, Hkv, 1, d, window, sinks, t0, scale, q.dtype)
+    _step_check(q, k, v, window, sinks, cache_k, cache_v, pos)
+    n, e = _bias_check(bias, edges, H, dev)
+    o = _result(out, q, (B, H, d))
+    keep, ws, m = _room(workspace, need, q)
+    _call(lib().bla_bias_step, "bla_bias_step", dev, p, n, e, q.data_ptr(), k.data_ptr(), v.data_ptr(), bias.data_ptr(), _ptr(pos),
+          cache_k.data_ptr(), cache_v.data_ptr(), o.data_ptr(), ws, m)
+    return o
+
+
+def bias_backward(q, k, v, o, lse, dO, bias, edges, window: int, sinks: int = 0, scale: float | None = None, lengths=None, workspace=None):
+    """bla_bias_backward: (dq, dk, dv, dbias) of bias_forward without rings from its outputs o and lse and dO = dLoss/dO; dbias is float32."""
+    B, H, L, d = q.shape
+    Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
+    p, _ = _window_params("bla_window_backward", B, H, Hkv, L, d, window, sinks, 0, scale, dt)
+    for name, t, h in (("q", q, H), ("k", k, Hkv), ("v", v, Hkv), ("o", o, H), ("dO", dO, H)):
+        _check_on(t, (B, h, L, d), dt, name, dev)
+    _check_on(lse, (B, H, L), torch.float32, "lse", dev)
+    n, e = _bias_check(bias, edges, H, dev)
+    if lengths is not None:
+        _check_on(lengths, (B,), torch.int32, "lengths", dev)
+    dq, dk, dv, db = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v), torch.empty_like(bias)
+    keep, ws, m = _room(workspace, lib().bla_bias_backward_workspace_size(p, n), q)
+    _call(lib().bla_bias_backward, "bla_bias_backward", dev, p, n, e, q.data_ptr(), k.data_ptr(), v.data_ptr(), bias.data_ptr(), o.data_ptr(),
+          lse.data_ptr(), dO.data_ptr(), _ptr(lengths), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), db.data_ptr(), ws, m)
+    return dq, dk, dv, db
+
+
+# ---- window attention behind a shared prefix ----
+
+@functools.lru_cache(maxsize=256)
+def _prefix_plan(what, B, H, Hkv, L, d, window, sinks, scale, dtype, P, G):
+    _int32(what, B, H, Hkv, L, d, window, sinks, P, G)
+    block = PrefixParams(WindowParams(B, H, Hkv, L, d, window, sinks, _io(dtype, "q"), 0, scale), P, G)
+    p = ctypes.byref(block)
+    st = lib().bla_prefix_supported(p)
+    if what == "bla_prefix_forward" or st != 2:  # the step's launch has a limit of its own, which it checks
+        _shape_status(st, what)
+    return block, p, getattr(lib(), what.replace("_forward", "") + "_workspace_size")(p)
+
+
+def _prefix_check(what, q, k, prefix_k, prefix_v, prefix_lengths, L, window, sinks, t0, scale):
+    """(parameters by reference, workspace bytes)."""
+    B, H, d = q.shape[0], q.shape[1], q.shape[-1]
+    Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
+    if prefix_k.dim() != 4:
+        raise ValueError(f"prefix_k: expected [G, H_kv, P, d], got {tuple(prefix_k.shape)}")
+    G, P = prefix_k.shape[0], prefix_k.shape[2]
+    _check_on(prefix_k, (G, Hkv, P, d), dt, "prefix_k", dev)
+    _check_on(prefix_v, (G, Hkv, P, d), dt, "prefix_v", dev)
+    if prefix_lengths is not None:
+        _check_on(prefix_lengths, (G,), torch.int32, "prefix_lengths", dev)
+    block, p, need = _prefix_plan(what, B, H, Hkv, L, d, int(window), int(sinks), 0.0 if scale is None else float(scale), dt, P, G)
+    if t0 != 0:
+        if not -(1 << 63) <= t0 < 1 << 63:
+            raise BlaError(1, what)
+        block = PrefixParams.from_buffer_copy(block)
+        block.w.t0 = int(t0)
+        p = ctypes.byref(block)
+    return p, need
+
+
+def prefix_forward(q, k, v, prefix_k, prefix_v, window: int, sinks: int = 0, t0: int = 0, scale: float | None = None, lengths=None, pos=None,
+                   prefix_lengths=None, cache_k=None, cache_v=None, want_lse: bool = False, want_cache: bool = False, workspace=None, out=None):
+    """bla_prefix_forward: window_forward whose queries also see every token of a prefix that rows share.
+
+    prefix_k, prefix_v [G,H_kv,P,d]: rows b with the same b // (B // G) share one; prefix_lengths (int32 [G]): its tokens (None: all P).
+    The rest, and what returns, as for window_forward: the window, the rings and positions are those of the row's own tokens.
+    """
+    B, H, L, d = q.shape
+    Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
+    p, need = _prefix_check("bla_prefix_forward", q, k, prefix_k, prefix_v, prefix_lengths, L, window, sinks, t0, scale)
+    _check_on(q, (B, H, L, d), dt, "q", dev)
+    _check_on(k, (B, Hkv, L, d), dt, "k", dev)
+    _check_on(v, (B, Hkv, L, d), dt, "v", dev)
+    ring = _past_check(B, Hkv, d, window, sinks, dt, dev, cache_k, cache_v, lengths, pos)
+    o = _result(out, q, (B, H, L, d))
+    lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device) if want_lse else None
+    ck = torch.empty(ring, dtype=dt, device=q.device) if want_cache else None
+    cv = torch.empty(ring, dtype=dt, device=q.device) if want_cache else None
+    keep, ws, n = _room(workspace, need, q)
+    _call(lib().bla_prefix_forward, "bla_prefix_forward", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), prefix_k.data_ptr(),
+          prefix_v.data_ptr(), _ptr(prefix_lengths), _ptr(lengths), _ptr(pos), _ptr(cache_k), _ptr(cache_v), o.data_ptr(), _ptr(lse), _ptr(ck),
+          _ptr(cv), ws, n)
+    return o, lse, ck, cv
+
+
+def prefix_step(q, k, v, prefix_k, prefix_v, window: int, sinks: int, cache_k, cache_v, pos=None, t0: int = 0, scale: float | None = None,
+                prefix_lengths=None, workspace=None, out=None):
+    """bla_prefix_step: window_step behind the prefix of prefix_forward, which is read once for all the rows that share it."""
+    B, H, d = q.shape
+    dev = q.get_device()
+    p, need = _prefix_check("bla_prefix_step", q, k, prefix_k, prefix_v, prefix_lengths, 1, window, sinks, t0, scale)
+    _step_check(q, k, v, window, sinks, cache_k, cache_v, pos)
+    o = _result(out, q, (B, H, d))
+    keep, ws, n = _room(workspace, need, q)
+    _call(lib().bla_prefix_step, "bla_prefix_step", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), prefix_k.data_ptr(), prefix_v.data_ptr(),
+          _ptr(prefix_lengths), _ptr(pos), cache_k.data_ptr(), cache_v.data_ptr(), o.data_ptr(), ws, n)
+    return o
 
 
 @functools.lru_cache(maxsize=256)

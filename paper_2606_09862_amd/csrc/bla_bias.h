@@ -1,0 +1,51 @@
+// A learned bias of each head and bucket of distance: what the kernels that add it share.
+//
+// Bucket n of a distance is the number of edges at or below it: bucket u holds the distances edges[u - 1] .. edges[u] - 1.  There are at most 64
+// buckets, so a wave holds them in two registers, an edge and a bias to each lane: a distance that is the same in every lane finds its
+// bucket with a comparison and a count of the lanes.
+#pragma once
+
+#include "bla_seq.h"
+
+namespace bla {
+
+constexpr int kMaxBuckets = 64;
+constexpr int kNear = 256;           // distances that have a table in LDS
+constexpr float kBiasNone = -1e30f;  // a bias below it counts as minus infinity (its pairs have no weight)
+
+struct BiasSpec {
+    const float* bias;  // [H, buckets]
+    int buckets;
+    int32_t edges[kMaxBuckets - 1];
+};
+
+// The buckets of one head in a wave.
+struct BiasLanes {
+    int edge;    // of lane u: the first distance of bucket u + 1
+    float bias;  // of lane u: that of bucket u, in the base-2 domain
+
+    __device__ __forceinline__ void set_edges(const BiasSpec& a, int lane)
+    {
+        edge = lane < a.buckets - 1 ? a.edges[lane] : INT32_MAX;
+    }
+    __device__ __forceinline__ void set_head(const BiasSpec& a, int h, int lane)
+    {
+        const float x = lane < a.buckets ? a.bias[(size_t)h * a.buckets + lane] : 0.f;
+        bias = x < kBiasNone ? -INFINITY : x * kLog2e;
+    }
+    // the bucket of a distance that is the same in every lane
+    __device__ __forceinline__ int bucket(int n) const { return __popcll(__ballot(edge <= n)); }
+    // u: the same in every lane
+    __device__ __forceinline__ float of(int u) const { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(bias), u)); }
+    __device__ __forceinline__ int first(int u) const { return __builtin_amdgcn_readlane(edge, u - 1); }
+    // the lane's own distance (every lane of the wave calls)
+    __device__ __forceinline__ int bucket_of_lane(const BiasSpec& a, int n) const
+    {
+        int u = 0;
+        for (int i = 1; i < a.buckets; ++i) u += first(i) <= n ? 1 : 0;
+        return u;
+    }
+    __device__ __forceinline__ float of_lane(int u) const { return __shfl(bias, u); }
+};
+
+}  // namespace bla

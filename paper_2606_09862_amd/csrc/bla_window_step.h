@@ -1,0 +1,265 @@
+// One decode token per row of window attention: the kernel of bla_window_step, of bla_bias_step and of the rings of bla_prefix_step.
+#pragma once
+
+#include "bla_window_fwd.h"
+
+namespace bla {
+
+struct BiasStepArgs : WindowStepArgs {
+    BiasSpec spec;
+};
+// The prefix's parts stand ahead of the rings' in part_o and part_ml.
+struct PrefixStepArgs : WindowStepArgs {
+    const void *pk, *pv;       // [G, Hkv, P, D]
+    const int32_t* plen;       // [G] or null
+    int P, G;
+    int npart, nqb;            // parts of the prefix, blocks of the queries that share it
+    long long units, per;      // workgroups of the prefix, per XCD
+    float *pre_o, *pre_ml;     // the prefix's parts
+};
+template <int EXT> struct ExtStepArgs { typedef WindowStepArgs type; };
+template <> struct ExtStepArgs<kBias> { typedef BiasStepArgs type; };
+template <> struct ExtStepArgs<kPrefix> { typedef PrefixStepArgs type; };
+
+// A workgroup of four waves takes up to 16 query heads of one key head and a part of the ring: the heads are the
+// columns of S^T = K Q^T, so a key is read once for all of them.  Wave w walks blocks of 32 slots, four blocks apart, with a
+// running maximum and sum of its own; K fragments come straight from memory (a lane's 16 bytes of a row), V rows go through
+// a tile of LDS that only the wave touches, to be read transposed.  The waves' results are joined through LDS, the
+// parts' by window_join_kernel.  The token's own key and value are taken from k and v wherever its slot is met, so no
+// workgroup reads the slot that one of them writes.  Bound: the ring's bytes (512 rows, four key heads of 1028 slots, d = 64, bf16: 76-81 us
+// for 408 MB, 5.2 TB/s); of one row, latency (4 key heads of 4100 slots, d = 128: 6 us in 33 parts and 5 us for their join, which
+// took 26 us with a thread to four columns of a row).
+template <typename T, int D> struct StepGeo {
+    static constexpr int LV = red_ld<T>(D), LO = D + 4;
+    static constexpr size_t VB = sizeof(T) * 4 * 32 * LV, OB = sizeof(float) * 4 * 16 * LO;
+    static constexpr size_t LDS = VB > OB ? VB : OB;
+};
+
+// EXT = kBias: the heads have biases of their own, so a lane, whose query head is r, takes them from a table in LDS; the 32 slots of a block are
+// as many distances in a row, but where they hold sinks or the ring's seam.  EXT = kPrefix: the results are parts, to be joined with the prefix's.
+template <typename T, int D, int EXT>
+__device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>::type& a, unsigned u, char* raw, float (&sml)[2][4][16])
+{
+    typedef typename Frag<T>::type F;
+    constexpr int PE = 16 / (int)sizeof(T), CH = D / PE, LV = red_ld<T>(D);
+    constexpr int NV = 32 * CH / 64;  // 16-byte pieces of V of a lane
+    constexpr int LO = D + 4;
+    __shared__ float sB[EXT == kBias ? kMaxBuckets * 16 : 1];
+    const bool whole = EXT != kPrefix && a.nsplit == 1;
+
+    const int part = (int)(u % (unsigned)a.nsplit);
+    u /= (unsigned)a.nsplit;
+    const int gi = (int)(u % (unsigned)a.ngrp);
+    u /= (unsigned)a.ngrp;
+    const int hk = (int)(u % (unsigned)a.Hkv), b = (int)(u / (unsigned)a.Hkv);
+    const int grp = a.H / a.Hkv, h0 = hk * grp + 16 * gi, nh = min(16, grp - 16 * gi);
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
+    const size_t qrow = (size_t)b * a.H + h0, rows = (size_t)a.B * a.H;
+
+    int64_t pos;
+    if (row_tokens(nullptr, a.pos, a.t0, b, 1, pos) == 0) {  // a row without a token
+        for (int i = tid; i < nh * D; i += 256)
+            if (whole) ((T*)a.o)[qrow * D + i] = (T)0.f;
+        if (!whole && tid < nh) {
+            const size_t at = (size_t)part * rows + qrow + tid;
+            a.part_ml[2 * at] = kNoMax;
+            a.part_ml[2 * at + 1] = 0.f;
+        }
+        return;
+    }
+    const int slots = a.S + a.W;
+    const int n = (int)min(pos + 1, (int64_t)slots);
+    const int mine = pos < a.S ? (int)pos : a.S + (int)((pos - a.S) % a.W);  // the token's slot
+    const size_t bh = (size_t)b * a.Hkv + hk;
+    const T *kn = (const T*)a.k + bh * D, *vn = (const T*)a.v + bh * D;
+    T *ck = (T*)a.ck + bh * slots * D, *cv = (T*)a.cv + bh * slots * D;
+    if (part == 0 && gi == 0 && tid < 2 * CH) {
+        const int ch = tid % CH;
+        if (tid < CH)
+            *(intx4*)(ck + (size_t)mine * D + ch * PE) = *(const intx4*)(kn + ch * PE);
+        else
+            *(intx4*)(cv + (size_t)mine * D + ch * PE) = *(const intx4*)(vn + ch * PE);
+    }
+
+    const int nblk = (n + 31) / 32, each = (nblk + a.nsplit - 1) / a.nsplit;
+    const int bb = part * each, be = min(nblk, bb + each);
+
+    F qf[D / 32];
+    {
+        const T* q = (const T*)a.q + (qrow + min(r, nh - 1)) * D;
+        const float sgn = a.scale < 0.f ? -1.f : 1.f;
+#pragma unroll
+        for (int kb = 0; kb < D / 32; ++kb) {
+            qf[kb] = ld_nat(q, kb, g);
+            if (a.scale < 0.f)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) qf[kb][e] = (T)(sgn * (float)qf[kb][e]);
+        }
+    }
+    const float sc = fabsf(a.scale) * kLog2e;
+
+    BiasLanes lanes = {};
+    int pm = -1;                            // the token's slot of the ring, counted from its first
+    if constexpr (EXT == kBias) {
+        lanes.set_edges(a.spec, lane);
+        for (int i = tid; i < a.spec.buckets * 16; i += 256) {
+            const float x = a.spec.bias[(size_t)(h0 + min(i & 15, nh - 1)) * a.spec.buckets + (i >> 4)];
+            sB[i] = x < kBiasNone ? -INFINITY : x * kLog2e;
+        }
+        if (pos >= a.S) pm = mine - a.S;
+        __syncthreads();
+    }
+    const float sx = EXT == kBias ? 1.f : sc;  // what takes a score to the base-2 domain
+
+    T* sV = (T*)raw + wave * 32 * LV;
+    F kf[2][D / 32];
+    intx4 vr[NV];
+    auto load = [&](int blk) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const int i = min(32 * blk + 16 * kt + r, n - 1);
+            const T* row = i == mine ? kn : ck + (size_t)i * D;
+#pragma unroll
+            for (int kb = 0; kb < D / 32; ++kb) kf[kt][kb] = ld_nat(row, kb, g);
+        }
+#pragma unroll
+        for (int x = 0; x < NV; ++x) {
+            const int i = min(32 * blk + (x * 64 + lane) / CH, n - 1);
+            const T* row = i == mine ? vn : cv + (size_t)i * D;
+            vr[x] = *(const intx4*)(row + ((x * 64 + lane) % CH) * PE);
+        }
+    };
+
+    floatx4 acc[D / 16];
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) acc[dt] = zero4();
+    float mx = kNoMax, sum = 0.f;
+    int blk = bb + wave;
+    if (blk < be) load(blk);
+    for (; blk < be; blk += 4) {
+#pragma unroll
+        for (int x = 0; x < NV; ++x)
+            *(intx4*)(sV + ((x * 64 + lane) / CH) * LV + ((x * 64 + lane) % CH) * PE) = vr[x];
+        floatx4 s[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            s[kt] = zero4();
+#pragma unroll
+            for (int kb = 0; kb < D / 32; ++kb) s[kt] = mma(kf[kt][kb], qf[kb], s[kt]);
+        }
+        if (blk + 4 < be) load(blk + 4);
+        if constexpr (EXT == kBias) {
+            const int i0 = 32 * blk, i1 = i0 + 31;
+            int ulo = 0, uhi = a.spec.buckets - 1;
+            if (i1 < a.S) {  // distances past 2^30 are in the last bucket
+                ulo = lanes.bucket((int)min(pos - i1, (int64_t)1 << 30));
+                uhi = lanes.bucket((int)min(pos - i0, (int64_t)1 << 30));
+            } else if (i0 >= a.S && (i1 - a.S <= pm || i0 - a.S > pm)) {
+                const int wrap = i0 - a.S > pm ? a.W : 0;
+                ulo = lanes.bucket(pm - (i1 - a.S) + wrap);
+                uhi = lanes.bucket(pm - (i0 - a.S) + wrap);
+            }
+            float bv[8];
+            const float b0 = sB[ulo * 16 + r];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) bv[e] = b0;
+            if (ulo != uhi) {
+                int d[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int i = i0 + 16 * (e >> 2) + 4 * g + (e & 3), x = pm - (i - a.S);
+                    d[e] = i < a.S ? (int)min(pos - i, (int64_t)1 << 30) : x + (x < 0 ? a.W : 0);
+                }
+                for (int w = ulo + 1; w <= uhi; ++w) {
+                    const int edge = lanes.first(w);
+                    const float x = sB[w * 16 + r];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) bv[e] = d[e] >= edge ? x : bv[e];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = __builtin_fmaf(s[e >> 2][e & 3], sc, bv[e]);
+        }
+        if (32 * blk + 32 > n) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[kt][e] = 32 * blk + 16 * kt + 4 * g + e < n ? s[kt][e] : -INFINITY;
+        }
+        float m = kNoMax;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) m = fmaxf(m, fmaxf(fmaxf(s[kt][0], s[kt][1]), fmaxf(s[kt][2], s[kt][3])));
+        m = fmaxf(mx, rows_max(m));
+        const float al = exp2_fast((mx - m) * sx), nm = -m * sx;
+        mx = m;
+        sum *= al;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[kt][e] = exp2_fast(__builtin_fmaf(s[kt][e], sx, nm));
+                sum += s[kt][e];
+            }
+        const F pf = frag_from_acc<T>(s[0], s[1]);
+        // the wave's own stores above, read by its other lanes (LDS serves a wave in order)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+            acc[dt] *= al;
+            acc[dt] = mma(ld_red(sV, LV, 16 * dt, 0, g, r), pf, acc[dt]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    sum = rows_sum(sum);
+
+    __syncthreads();
+    float* sO = (float*)raw;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) st4f(sO + (wave * 16 + r) * LO + 16 * dt + 4 * g, acc[dt]);
+    if (g == 0) {
+        sml[0][wave][r] = mx * sx;
+        sml[1][wave][r] = sum;
+    }
+    __syncthreads();
+    for (int i = tid; i < nh * (D / 4); i += 256) {
+        const int hq = i / (D / 4), c = 4 * (i % (D / 4));
+        float m = kNoMax * sx;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, sml[0][w][hq]);
+        float l = 0.f;
+        floatx4 o = zero4();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = exp2_fast(sml[0][w][hq] - m);
+            l += f * sml[1][w][hq];
+            o += f * ld4f(sO + (w * 16 + hq) * LO + c);
+        }
+        if (whole) {
+            st4((T*)a.o + (qrow + hq) * D + c, EXT != kBias || l > 0.f ? o * (1.f / l) : zero4());
+        } else {
+            const size_t at = (size_t)part * rows + qrow + hq;
+            st4f(a.part_o + at * D + c, o);
+            if (c == 0) {
+                a.part_ml[2 * at] = m;
+                a.part_ml[2 * at + 1] = l;
+            }
+        }
+    }
+}
+
+template <typename T, int D, int EXT> __global__ void __launch_bounds__(256) window_step_kernel(typename ExtStepArgs<EXT>::type a)
+{
+    __shared__ __attribute__((aligned(16))) char raw[StepGeo<T, D>::LDS];
+    __shared__ float sml[2][4][16];
+    window_step_part<T, D, EXT>(a, blockIdx.x, raw, sml);
+}
+
+template <typename T, int D, int EXT> hipError_t step_d(const typename ExtStepArgs<EXT>::type& a, hipStream_t s)
+{
+    hipLaunchKernelGGL((window_step_kernel<T, D, EXT>), dim3((unsigned)((long long)a.B * a.Hkv * a.ngrp * a.nsplit)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace bla
