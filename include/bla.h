@@ -441,6 +441,61 @@ bla_status bla_prefix_step(const bla_prefix_params* p, const void* q, const void
                            void* cache_v, void* o, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention over a cache of bounded size, which gives up the tokens that least weight has gone to.  A key head keeps up to `slots` tokens, in any order;
+ * a token's score is the sum of the softmax weights that it has got, over the queries since it came and over the query heads of its key head.
+ * A row at position pos (tokens before the call) has min(pos, slots) tokens, in the first slots.
+ *   cache_k, cache_v: [B, H_kv, slots, d] in the io dtype   score: float32 [B, H_kv, slots]   at: int64 [B, H_kv, slots], the tokens' positions
+ * The newest `recent` tokens are never given up.  Scores are compared as numbers (NaN above all of them); of equal ones the lowest entry goes
+ * first into what stays, and is the first to be replaced by bla_evict_step.
+ *   q, o: [B, H, L, d]   k, v: [B, H_kv, L, d]   lengths, pos: as for bla_window_forward, idle rows included (their caches stay as they are).
+ * Slots that no token has reached are never read as tokens.  Supported: shapes and types of window attention; 1 <= slots <= 2^24, 0 <= recent < slots.
+ */
+typedef struct {
+    int32_t B, H, H_kv, L; /* batch rows, query heads, key heads, tokens in this call */
+    int32_t d;             /* head width */
+    int32_t slots, recent; /* tokens of a cache, newest tokens that stay */
+    int32_t io_dtype;      /* bla_dtype of q, k, v, o and the caches */
+    int64_t t0;            /* position of token 0 of every row (pos = NULL) */
+    float scale;           /* softmax scale; 0 selects 1/sqrt(d) */
+} bla_evict_params;
+
+/* BLA_OK if bla_evict_forward takes the shape in *p, else the error it would get. */
+bla_status bla_evict_supported(const bla_evict_params* p);
+
+/* Bytes of device workspace bla_evict_forward needs (0: *p is not supported). */
+size_t bla_evict_workspace_size(const bla_evict_params* p);
+
+/*
+ * L tokens of every row: each query sees all tokens of the cache and the call's up to its own.  cache_k, cache_v and score_in: all or none (NULL: nothing
+ * before token 0 exists); they stay as they are.  lse as for bla_window_forward.  score_out [B, H_kv, slots + L] receives the scores of the cache's tokens
+ * (entries 0 .. slots - 1) and of the call's (slots + t) after it, zeros where there is none.  The sums run in a fixed order.
+ */
+bla_status bla_evict_forward(const bla_evict_params* p, const void* q, const void* k, const void* v, const int32_t* lengths,
+                             const int64_t* pos, const void* cache_k, const void* cache_v, const float* score_in, void* o,
+                             float* lse, float* score_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The cache after L tokens: of its tokens and the call's the newest `recent` stay and of the others those with the largest scores [B, H_kv, slots + L], slots
+ * in all, in the order of their entries; their scores and positions go with them.  Slots without a token: zeros, at = -1.  cache_k_in, cache_v_in and
+ * at_in: all or none.  p->H and p->scale are not used.
+ */
+size_t bla_evict_select_workspace_size(const bla_evict_params* p);
+bla_status bla_evict_select(const bla_evict_params* p, const void* k, const void* v, const float* score, const int32_t* lengths,
+                            const int64_t* pos, const void* cache_k_in, const void* cache_v_in, const int64_t* at_in,
+                            void* cache_k_out, void* cache_v_out, float* score_out, int64_t* at_out, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * One token for every row (p->L is ignored): it takes slot pos while the cache is not full, then the slot with the least score among those with at < pos - recent,
+ * with a score of zero; it sees the cache with itself in it, and all weights are added to the scores.  cache_k and cache_v are updated in place;
+ * score_out may be score_in, at_out may be at_in (updated in place).
+ */
+size_t bla_evict_step_workspace_size(const bla_evict_params* p);
+bla_status bla_evict_step(const bla_evict_params* p, const void* q, const void* k, const void* v, const int64_t* pos, void* cache_k,
+                          void* cache_v, const float* score_in, const int64_t* at_in, void* o, float* score_out, int64_t* at_out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The short causal convolution of each channel, as the paper's models apply it to queries, keys and values ahead of the
  * operator:
  *     z_t = bias + sum_{j < taps} w[j] x_{t - taps + 1 + j},   y_t = z_t (silu = 0) or z_t sigmoid(z_t) (silu = 1).

@@ -49,6 +49,13 @@ class PrefixParams(ctypes.Structure):
     _fields_ = [("w", WindowParams), ("P", ctypes.c_int32), ("G", ctypes.c_int32)]
 
 
+class EvictParams(ctypes.Structure):
+    """Mirror of ``bla_evict_params``."""
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("L", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("slots", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("t0", ctypes.c_int64), ("scale", ctypes.c_float)]
+
+
 class ConvParams(ctypes.Structure):
     """Mirror of ``bla_conv_params``."""
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32), ("d", ctypes.c_int32),
@@ -138,6 +145,16 @@ def lib():
         L.bla_prefix_forward.argtypes = [X] + [_vp] * 15 + [ctypes.c_size_t, _vp]
         L.bla_prefix_step.argtypes = [X] + [_vp] * 11 + [ctypes.c_size_t, _vp]
         for name in ("bla_prefix_supported", "bla_prefix_forward", "bla_prefix_step"):
+            getattr(L, name).restype = ctypes.c_int
+        E = ctypes.POINTER(EvictParams)
+        for name in ("bla_evict_workspace_size", "bla_evict_select_workspace_size", "bla_evict_step_workspace_size"):
+            getattr(L, name).argtypes = [E]
+            getattr(L, name).restype = ctypes.c_size_t
+        L.bla_evict_supported.argtypes = [E]
+        L.bla_evict_forward.argtypes = [E] + [_vp] * 12 + [ctypes.c_size_t, _vp]
+        L.bla_evict_select.argtypes = [E] + [_vp] * 13 + [ctypes.c_size_t, _vp]
+        L.bla_evict_step.argtypes = [E] + [_vp] * 12 + [ctypes.c_size_t, _vp]
+        for name in ("bla_evict_supported", "bla_evict_forward", "bla_evict_select", "bla_evict_step"):
             getattr(L, name).restype = ctypes.c_int
         C = ctypes.POINTER(ConvParams)
         L.bla_conv_backward_workspace_size.argtypes = [C]
@@ -826,6 +843,123 @@ def prefix_step(q, k, v, prefix_k, prefix_v, window: int, sinks: int, cache_k, c
     _call(lib().bla_prefix_step, "bla_prefix_step", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), prefix_k.data_ptr(), prefix_v.data_ptr(),
           _ptr(prefix_lengths), _ptr(pos), cache_k.data_ptr(), cache_v.data_ptr(), o.data_ptr(), ws, n)
     return o
+
+
+# ---- attention over a cache of bounded size ----
+
+@functools.lru_cache(maxsize=256)
+def _evict_plan(what, B, H, Hkv, L, d, slots, recent, scale, dtype):
+    _int32(what, B, H, Hkv, L, d, slots, recent)
+    block = EvictParams(B, H, Hkv, L, d, slots, recent, _io(dtype, "k"), 0, scale)
+    p = ctypes.byref(block)
+    st = lib().bla_evict_supported(p)
+    if what == "bla_evict_forward" or st != 2:  # the launches of the other calls have limits of their own, which they check
+        _shape_status(st, what)
+    return block, p, getattr(lib(), what.replace("_forward", "") + "_workspace_size")(p)
+
+
+def _evict_params(what, B, H, Hkv, L, d, slots, recent, t0, scale, dtype):
+    """(parameters by reference, workspace bytes)."""
+    block, p, need = _evict_plan(what, B, H, Hkv, L, d, int(slots), int(recent), 0.0 if scale is None else float(scale), dtype)
+    if t0 != 0:
+        if not -(1 << 63) <= t0 < 1 << 63:
+            raise BlaError(1, what)
+        block = EvictParams.from_buffer_copy(block)
+        block.t0 = int(t0)
+        p = ctypes.byref(block)
+    return p, need
+
+
+def _evict_cache(cache_k, cache_v, other, name, dtype, B, Hkv, slots, d, dt, dev):
+    """The checks of a cache, which comes with its scores or positions or not at all."""
+    given = [x is not None for x in (cache_k, cache_v, other)]
+    if any(given) and not all(given):
+        raise ValueError(f"cache_k, cache_v and {name}: all or none")
+    if cache_k is not None:
+        _check_on(cache_k, (B, Hkv, slots, d), dt, "cache_k", dev)
+        _check_on(cache_v, (B, Hkv, slots, d), dt, "cache_v", dev)
+        _check_on(other, (B, Hkv, slots), dtype, name, dev)
+
+
+def evict_forward(q, k, v, slots: int, cache_k=None, cache_v=None, score=None, t0: int = 0, scale: float | None = None, lengths=None, pos=None,
+                  want_lse: bool = False, workspace=None, out=None):
+    """bla_evict_forward: attention of L tokens over a cache of up to `slots` tokens and themselves, and the weight that each token gets.
+
+    q [B,H,L,d], k and v [B,H_kv,L,d]; cache_k / cache_v [B,H_kv,slots,d] with score [B,H_kv,slots] float32 (all or none): a row at position
+    pos (int64 [B], or t0) has min(pos, slots) tokens there.  lengths (int32 [B]): tokens of each row.  Returns (o, lse or None, scores after the call
+    [B,H_kv,slots+L]: the cache's entries, then the call's); evict_select makes the cache after the call of them.
+    """
+    B, H, L, d = q.shape
+    Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
+    p, need = _evict_params("bla_evict_forward", B, H, Hkv, L, d, slots, 0, t0, scale, dt)
+    _check_on(q, (B, H, L, d), dt, "q", dev)
+    _check_on(k, (B, Hkv, L, d), dt, "k", dev)
+    _check_on(v, (B, Hkv, L, d), dt, "v", dev)
+    _evict_cache(cache_k, cache_v, score, "score", torch.float32, B, Hkv, slots, d, dt, dev)
+    if lengths is not None:
+        _check_on(lengths, (B,), torch.int32, "lengths", dev)
+    if pos is not None:
+        _check_on(pos, (B,), torch.int64, "pos", dev)
+    o = _result(out, q, (B, H, L, d))
+    lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device) if want_lse else None
+    after = torch.empty((B, Hkv, slots + L), dtype=torch.float32, device=q.device)
+    keep, ws, n = _room(workspace, need, q)
+    _call(lib().bla_evict_forward, "bla_evict_forward", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), _ptr(pos), _ptr(cache_k),
+          _ptr(cache_v), _ptr(score), o.data_ptr(), _ptr(lse), after.data_ptr(), ws, n)
+    return o, lse, after
+
+
+def evict_select(k, v, score, slots: int, recent: int = 0, cache_k=None, cache_v=None, at=None, t0: int = 0, lengths=None, pos=None,
+                 workspace=None):
+    """bla_evict_select: the cache after L tokens: of the cache's tokens and the call's k, v [B,H_kv,L,d] the newest `recent` stay, and of the others those
+    with the largest score [B,H_kv,slots+L] (of equal ones the lowest entries), `slots` in all, in the order of their entries.
+
+    cache_k / cache_v [B,H_kv,slots,d] and at [B,H_kv,slots] int64 (the tokens' positions): all or none.  Returns (cache_k, cache_v, score, at)
+    after the call, new tensors; slots without a token hold zeros and a position of -1.
+    """
+    B, Hkv, L, d = k.shape
+    dt, dev = k.dtype, k.get_device()
+    p, need = _evict_params("bla_evict_select", B, Hkv, Hkv, L, d, slots, recent, t0, None, dt)
+    _check_on(k, (B, Hkv, L, d), dt, "k", dev)
+    _check_on(v, (B, Hkv, L, d), dt, "v", dev)
+    _check_on(score, (B, Hkv, slots + L), torch.float32, "score", dev)
+    _evict_cache(cache_k, cache_v, at, "at", torch.int64, B, Hkv, slots, d, dt, dev)
+    if lengths is not None:
+        _check_on(lengths, (B,), torch.int32, "lengths", dev)
+    if pos is not None:
+        _check_on(pos, (B,), torch.int64, "pos", dev)
+    ck, cv = (torch.empty((B, Hkv, slots, d), dtype=dt, device=k.device) for _ in range(2))
+    kept = torch.empty((B, Hkv, slots), dtype=torch.float32, device=k.device)
+    where = torch.empty((B, Hkv, slots), dtype=torch.int64, device=k.device)
+    keep, ws, n = _room(workspace, need, k)
+    _call(lib().bla_evict_select, "bla_evict_select", dev, p, k.data_ptr(), v.data_ptr(), score.data_ptr(), _ptr(lengths), _ptr(pos), _ptr(cache_k),
+          _ptr(cache_v), _ptr(at), ck.data_ptr(), cv.data_ptr(), kept.data_ptr(), where.data_ptr(), ws, n)
+    return ck, cv, kept, where
+
+
+def evict_step(q, k, v, cache_k, cache_v, score, at, recent: int = 0, pos=None, t0: int = 0, scale: float | None = None, workspace=None,
+               out=None, score_out=None, at_out=None):
+    """bla_evict_step: one decode token per row, q [B,H,d], k and v [B,H_kv,d], over a cache [B,H_kv,slots,d] that takes it in place: in slot pos while it is not
+    full, then in that of the least score among the tokens older than the newest `recent`.  score [B,H_kv,slots] float32 and at [B,H_kv,slots] int64 are updated in place,
+    or written to score_out and at_out.  A row with a negative pos is idle (zeros).  Returns (o, score after the call, at after the call)."""
+    B, H, d = q.shape
+    Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
+    if cache_k.dim() != 4:
+        raise ValueError(f"cache_k: expected [B, H_kv, slots, d], got {tuple(cache_k.shape)}")
+    slots = cache_k.shape[2]
+    p, need = _evict_params("bla_evict_step", B, H, Hkv, 1, d, slots, recent, t0, scale, dt)
+    _step_check(q, k, v, slots, 0, cache_k, cache_v, pos)
+    _check_on(score, (B, Hkv, slots), torch.float32, "score", dev)
+    _check_on(at, (B, Hkv, slots), torch.int64, "at", dev)
+    for x, like, name in ((score_out, score, "score_out"), (at_out, at, "at_out")):
+        if x is not None:
+            _check_on(x, like.shape, like.dtype, name, dev)
+    score_out, at_out = score if score_out is None else score_out, at if at_out is None else at_out
+    o = _result(out, q, (B, H, d))
+    keep, ws, n = _room(workspace, need, q)
+    _call(lib().bla_evict_step, "bla_evict_step", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(pos), cache_k.data_ptr(), cache_v.data_ptr(),
+          score.data_ptr(), at.data_ptr(), o.data_ptr(), score_out.data_ptr(), at_out.data_ptr(), ws, n)
+    return o, score_out, at_out
 
 
 @functools.lru_cache(maxsize=256)

@@ -1,0 +1,43 @@
+// Attention over a cache of bounded size that gives up its tokens of least weight: kernel arguments.
+#pragma once
+
+#include "bla_window_step.h"
+
+namespace bla {
+
+// The weight that each token gets from the queries of a call.
+struct EvictSumArgs {
+    const void *q, *k, *ck;    // [B, H, L, D], [B, Hkv, L, D], [B, Hkv, slots, D] or null
+    const float* lse;          // [B, H, L]
+    const int32_t* lengths;
+    const int64_t* pos;
+    int64_t t0;
+    int B, H, Hkv, L, slots;
+    float scale;
+    int ncb, nkb;              // key blocks of the cache, of cache and call together
+    long long units, per;
+    float* part;               // [B, H, slots + L]
+    const float* score_in;     // [B, Hkv, slots] or null
+    float* score_out;          // [B, Hkv, slots + L]
+};
+
+struct EvictSelectArgs {
+    const void *k, *v, *ck, *cv;
+    const float* score;        // [B, Hkv, slots + L]
+    const int64_t* at_in;      // [B, Hkv, slots] or null
+    const int32_t* lengths;
+    const int64_t* pos;
+    int64_t t0;
+    int B, Hkv, L, slots, recent;
+    int* index;                // [B, Hkv, slots]: the entry that a slot takes, or -1
+    void *ck_out, *cv_out;
+    float* score_out;
+    int64_t* at_out;
+};
+
+hipError_t launch_evict_sum(int bf16_io, int D, const EvictSumArgs& a, hipStream_t s);
+hipError_t launch_evict_select(int bf16_io, int D, const EvictSelectArgs& a, hipStream_t s);
+hipError_t launch_evict_step(int bf16_io, int D, const EvictStepArgs& a, hipStream_t s);
+constexpr int kEvictKeys = 128;  // keys of a workgroup of the sums
+
+}  // namespace bla

@@ -23,22 +23,6 @@ bla_status check_prefix(const bla_prefix_params* p, bool step)
     return BLA_OK;
 }
 
-// The forward plan of window attention, whose blocks have the prefix's keys as well.
-ForwardPlan prefix_plan(const bla_prefix_params* p, bool cached)
-{
-    ForwardPlan f = forward_plan(&p->w, cached);
-    const long long bh = (long long)p->w.B * p->w.H, blocks = bh * f.nqb;
-    long long keys = (long long)p->w.window - 1 + 16 * f.waves + p->w.sinks;
-    if (!cached && keys > p->w.L) keys = p->w.L;
-    const long long tiles = (keys + kWinKeys - 1) / kWinKeys + (p->P + kWinKeys - 1) / kWinKeys;
-    long long n = blocks > 0 && blocks < kFill ? (kFill + blocks - 1) / blocks : 1;
-    if (n > tiles / 2) n = tiles / 2;
-    f.nsplit = (int)(n < 1 ? 1 : n > kMaxParts ? kMaxParts : n);
-    f.units = blocks * f.nsplit;
-    f.total = f.nsplit > 1 ? seq_align((size_t)f.nsplit * bh * p->w.L * (p->w.d + 2) * 4) : 0;
-    return f;
-}
-
 // The step's: the prefix in parts of at least two tiles that fill the device with the blocks of its queries, beside the rings' parts.
 struct PrefixStepPlan : StepPlan {
     int npart, nqb;
@@ -81,12 +65,12 @@ extern "C" {
 bla_status bla_prefix_supported(const bla_prefix_params* p)
 {
     const bla_status st = check_prefix(p, false);
-    return st == BLA_OK && !fits(&p->w, prefix_plan(p, true), false) ? BLA_ERR_UNSUPPORTED : st;
+    return st == BLA_OK && !fits(&p->w, forward_plan(&p->w, true, p->P), false) ? BLA_ERR_UNSUPPORTED : st;
 }
 
 size_t bla_prefix_workspace_size(const bla_prefix_params* p)
 {
-    return bla_prefix_supported(p) == BLA_OK ? prefix_plan(p, true).total : 0;
+    return bla_prefix_supported(p) == BLA_OK ? forward_plan(&p->w, true, p->P).total : 0;
 }
 
 bla_status bla_prefix_forward(const bla_prefix_params* p, const void* q, const void* k, const void* v, const void* prefix_k,
@@ -98,7 +82,7 @@ bla_status bla_prefix_forward(const bla_prefix_params* p, const void* q, const v
     if (st != BLA_OK) return st;
     const bla_window_params* w = &p->w;
     if (w->B == 0 || w->H == 0) return empty(w, cache_k_out || cache_v_out);
-    const ForwardPlan f = prefix_plan(p, cache_k_in != nullptr);
+    const ForwardPlan f = forward_plan(w, cache_k_in != nullptr, p->P);
     if (!fits(w, f, cache_k_out != nullptr)) return BLA_ERR_UNSUPPORTED;
     if (w->L > 0 && (st = check_pointers(p, prefix_k, prefix_v, prefix_lengths)) != BLA_OK) return st;
     PrefixArgs a = {};

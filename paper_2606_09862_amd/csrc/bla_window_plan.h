@@ -36,13 +36,13 @@ inline bla_status empty(const bla_window_params* p, bool outputs)
 }
 
 // Forward: 128 queries to a workgroup (fewer reads of keys), 64 where that fills the device better;
-// the keys of a block in parts of at least two tiles where the blocks alone do not fill it.
+// the keys of a block, `front` tokens that every query sees among them, in parts of at least two tiles where the blocks alone do not fill it.
 struct ForwardPlan {
     int waves, nqb, nsplit;
     long long units;
     size_t total;
 };
-inline ForwardPlan forward_plan(const bla_window_params* p, bool cached)
+inline ForwardPlan forward_plan(const bla_window_params* p, bool cached, int front = 0)
 {
     ForwardPlan f;
     const long long bh = (long long)p->B * p->H;
@@ -51,7 +51,7 @@ inline ForwardPlan forward_plan(const bla_window_params* p, bool cached)
     const long long blocks = bh * f.nqb;
     long long keys = (long long)p->window - 1 + 16 * f.waves + p->sinks;
     if (!cached && keys > p->L) keys = p->L;
-    const long long tiles = (keys + kWinKeys - 1) / kWinKeys;
+    const long long tiles = (keys + kWinKeys - 1) / kWinKeys + (front + kWinKeys - 1) / kWinKeys;
     long long n = 1;
     if (blocks > 0 && blocks < kFill) n = (kFill + blocks - 1) / blocks;
     if (n > tiles / 2) n = tiles / 2;

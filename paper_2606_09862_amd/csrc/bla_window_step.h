@@ -17,9 +17,67 @@ struct PrefixStepArgs : WindowStepArgs {
     long long units, per;      // workgroups of the prefix, per XCD
     float *pre_o, *pre_ml;     // the prefix's parts
 };
+// Slots without order (W of them, S = 0); the scores in the base-2 domain go out for the sums of the weights.
+struct EvictStepArgs : WindowStepArgs {
+    const float* score_in;     // [B, Hkv, W]
+    float* score_out;
+    const int64_t* at_in;
+    int64_t* at_out;
+    int recent;
+    int* mine;                 // [B, Hkv]: the token's slot
+    float* z;                  // [B, H, pitch]
+    int pitch;
+    bool fused;                // a workgroup has all slots and heads of its key head: it forms the sums itself
+};
 template <int EXT> struct ExtStepArgs { typedef WindowStepArgs type; };
 template <> struct ExtStepArgs<kBias> { typedef BiasStepArgs type; };
 template <> struct ExtStepArgs<kPrefix> { typedef PrefixStepArgs type; };
+template <> struct ExtStepArgs<kEvict> { typedef EvictStepArgs type; };
+
+// A score's place in the order of scores: NaN above every number, the two zeros as one.
+__device__ __forceinline__ unsigned score_key(float x)
+{
+    if (x != x) return 0xfffffffeu;
+    const unsigned u = __float_as_uint(x == 0.f ? 0.f : x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// The slot that a token of a full cache takes: of those whose token is older than `old` the one with the least score, the lowest of several.  256 threads
+// call it with four words of LDS; every slot is one of slots whatever `at` holds.
+__device__ __forceinline__ int evict_slot(const float* score, const int64_t* at, int slots, int64_t old, uint64_t* lds)
+{
+    uint64_t best = ~0ull;
+    for (int i = threadIdx.x; i < slots; i += 256) {
+        const uint64_t key = (uint64_t)(at[i] < old ? score_key(score[i]) : 0xffffffffu) << 32 | (unsigned)i;
+        best = key < best ? key : best;
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        const uint64_t x = __shfl_xor((unsigned long long)best, off);
+        best = x < best ? x : best;
+    }
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = best;
+    __syncthreads();
+    best = lds[0];
+    for (int i = 1; i < 4; ++i) best = lds[i] < best ? lds[i] : best;
+    __syncthreads();  // the caller uses the words again
+    const unsigned slot = (unsigned)best;
+    return slot < (unsigned)slots ? (int)slot : 0;
+}
+
+// Slot i of a cache with n tokens after the call, of which the new one's weight is w as well.  Slots without a token stay as they are.
+__device__ __forceinline__ void evict_score_out(const EvictStepArgs& a, size_t bh, int i, int mine, int n, int64_t pos, float w)
+{
+    const size_t at = bh * a.W + i;
+    if (i < n)
+        a.score_out[at] = (i == mine ? 0.f : a.score_in[at]) + w;
+    else if (a.score_out != a.score_in)
+        a.score_out[at] = a.score_in[at];
+    if (i == mine)
+        a.at_out[at] = pos;
+    else if (a.at_out != a.at_in)
+        a.at_out[at] = a.at_in[at];
+}
 
 // A workgroup of four waves takes up to 16 query heads of one key head and a part of the ring: the heads are the
 // columns of S^T = K Q^T, so a key is read once for all of them.  Wave w walks blocks of 32 slots, four blocks apart, with a
@@ -37,6 +95,7 @@ template <typename T, int D> struct StepGeo {
 
 // EXT = kBias: the heads have biases of their own, so a lane, whose query head is r, takes them from a table in LDS; the 32 slots of a block are
 // as many distances in a row, but where they hold sinks or the ring's seam.  EXT = kPrefix: the results are parts, to be joined with the prefix's.
+// EXT = kEvict: the token's slot is found first, and the scores are kept until the softmax's sum is known.
 template <typename T, int D, int EXT>
 __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>::type& a, unsigned u, char* raw, float (&sml)[2][4][16])
 {
@@ -45,7 +104,9 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
     constexpr int NV = 32 * CH / 64;  // 16-byte pieces of V of a lane
     constexpr int LO = D + 4;
     __shared__ float sB[EXT == kBias ? kMaxBuckets * 16 : 1];
-    const bool whole = EXT != kPrefix && a.nsplit == 1;
+    __shared__ float sfin[EXT == kEvict ? 32 : 1];
+    bool whole = EXT != kPrefix && a.nsplit == 1;
+    if constexpr (EXT == kEvict) whole = a.fused;
 
     const int part = (int)(u % (unsigned)a.nsplit);
     u /= (unsigned)a.nsplit;
@@ -65,12 +126,22 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
             a.part_ml[2 * at] = kNoMax;
             a.part_ml[2 * at + 1] = 0.f;
         }
+        if constexpr (EXT == kEvict) {
+            const size_t bh = (size_t)b * a.Hkv + hk;
+            if (part == 0 && gi == 0 && tid == 0) a.mine[bh] = -1;
+            if (a.fused)
+                for (int i = tid; i < a.W; i += 256) evict_score_out(a, bh, i, -1, 0, pos, 0.f);
+        }
         return;
     }
     const int slots = a.S + a.W;
     const int n = (int)min(pos + 1, (int64_t)slots);
-    const int mine = pos < a.S ? (int)pos : a.S + (int)((pos - a.S) % a.W);  // the token's slot
     const size_t bh = (size_t)b * a.Hkv + hk;
+    int mine;  // the token's slot
+    if constexpr (EXT == kEvict)
+        mine = pos < slots ? (int)pos : evict_slot(a.score_in + bh * slots, a.at_in + bh * slots, slots, pos - a.recent, (uint64_t*)raw);
+    else
+        mine = pos < a.S ? (int)pos : a.S + (int)((pos - a.S) % a.W);
     const T *kn = (const T*)a.k + bh * D, *vn = (const T*)a.v + bh * D;
     T *ck = (T*)a.ck + bh * slots * D, *cv = (T*)a.cv + bh * slots * D;
     if (part == 0 && gi == 0 && tid < 2 * CH) {
@@ -186,6 +257,11 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[kt][e] = 32 * blk + 16 * kt + 4 * g + e < n ? s[kt][e] : -INFINITY;
         }
+        if constexpr (EXT == kEvict) {
+            if (r < nh)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) st4f(a.z + (qrow + r) * a.pitch + 32 * blk + 16 * kt + 4 * g, s[kt] * sc);
+        }
         float m = kNoMax;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) m = fmaxf(m, fmaxf(fmaxf(s[kt][0], s[kt][1]), fmaxf(s[kt][2], s[kt][3])));
@@ -236,6 +312,10 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
             l += f * sml[1][w][hq];
             o += f * ld4f(sO + (w * 16 + hq) * LO + c);
         }
+        if (EXT == kEvict && c == 0) {
+            sfin[hq] = m;
+            sfin[16 + hq] = 1.f / l;
+        }
         if (whole) {
             st4((T*)a.o + (qrow + hq) * D + c, EXT != kBias || l > 0.f ? o * (1.f / l) : zero4());
         } else {
@@ -245,6 +325,19 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
                 a.part_ml[2 * at] = m;
                 a.part_ml[2 * at + 1] = l;
             }
+        }
+    }
+    if constexpr (EXT == kEvict) {
+        if (!a.fused) {
+            if (part == 0 && gi == 0 && tid == 0) a.mine[bh] = mine;
+            return;
+        }
+        __syncthreads();  // sfin, and the scores that the waves have written
+        for (int i = tid; i < slots; i += 256) {
+            float w = 0.f;
+            if (i < n)
+                for (int h = 0; h < nh; ++h) w += exp2_fast(a.z[(qrow + h) * a.pitch + i] - sfin[h]) * sfin[16 + h];
+            evict_score_out(a, bh, i, mine, n, pos, w);
         }
     }
 }
