@@ -10,7 +10,8 @@
 namespace bla {
 
 constexpr int kMaxBuckets = 64;
-constexpr int kNear = 256;           // distances that have a table in LDS
+constexpr int kNear = 1024;          // distances that have a table in LDS
+constexpr int kPad = 64;             // places before them, for pairs of later keys in a tile that the masks hide
 constexpr float kBiasNone = -1e30f;  // a bias below it counts as minus infinity (its pairs have no weight)
 
 struct BiasSpec {
@@ -38,14 +39,27 @@ struct BiasLanes {
     // u: the same in every lane
     __device__ __forceinline__ float of(int u) const { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(bias), u)); }
     __device__ __forceinline__ int first(int u) const { return __builtin_amdgcn_readlane(edge, u - 1); }
-    // the lane's own distance (every lane of the wave calls)
-    __device__ __forceinline__ int bucket_of_lane(const BiasSpec& a, int n) const
+    // 64 distances from n0 on, the lane's n0 + lane: f(its bucket, that bucket's bias)
+    template <typename Fn> __device__ __forceinline__ void each(int n0, int lane, Fn f) const
     {
-        int u = 0;
-        for (int i = 1; i < a.buckets; ++i) u += first(i) <= n ? 1 : 0;
-        return u;
+        const int lo = bucket(n0), hi = bucket(n0 + 63);
+        int u = lo;
+        float x = of(lo);
+        for (int w = lo + 1; w <= hi; ++w) {
+            const bool in = n0 + lane >= first(w);
+            u = in ? w : u;
+            x = in ? of(w) : x;
+        }
+        f(u, x);
     }
-    __device__ __forceinline__ float of_lane(int u) const { return __shfl(bias, u); }
+    // The table of the near distances, as far as two of a tile's can have different buckets: each wave of the workgroup writes some of it.
+    __device__ __forceinline__ void table(const BiasSpec& a, float* near, int wave, int waves, int lane) const
+    {
+        const int last = a.buckets > 1 ? a.edges[a.buckets - 2] : 0;
+        if (wave == 0) near[lane] = of(0);
+        for (int c = wave; 64 * c < min(kNear, last + 64); c += waves)
+            each(64 * c, lane, [&](int, float x) { near[kPad + 64 * c + lane] = x; });
+    }
 };
 
 }  // namespace bla

@@ -9,7 +9,8 @@
 //
 // A bias (EXT = kBias) adds b to the exponent, as in the forward kernel, and its own gradient: the sum over pairs of dS by head and bucket.  The key pass
 // forms it, whose delta is exact (EXACT), from dS before its rounding.  Where the pairs of a wave share a bucket a lane adds its own to a
-// register; a wave has sums of its own for each bucket and key row, which go out once for each head and are added up by bias_bwd_sum_kernel in a fixed order.
+// register; elsewhere dS is summed along its diagonals, a distance to a lane, and then over the lanes of a bucket.  A wave's sums go out once for each head
+// and are added up by bias_bwd_sum_kernel in a fixed order.
 #pragma once
 
 #include <algorithm>
@@ -33,55 +34,123 @@ template <int EXT> __device__ __forceinline__ float lse_base2(float lse)
     return EXT == kBias && lse == -INFINITY ? 1e30f : lse * kLog2e;
 }
 
-// The wave's sums of dS: of each bucket, for each of the 16 key rows.
-struct BiasSums {
-    float* sums;  // [buckets][16]
-    float run;    // the lane's, of bucket cur
-    int cur;
+// The sum over the wave's lanes, the same in each.
+__device__ __forceinline__ float wave_sum(float x)
+{
+    x = rows_sum(x);
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xf, 0xf, false));  // the row rotated by 8, 4, 2 and 1 lanes
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x124, 0xf, 0xf, false));
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x122, 0xf, 0xf, false));
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x121, 0xf, 0xf, false));
+    return x;
+}
 
-    __device__ __forceinline__ void start(float* at, int buckets, int lane)
+// The lane's distance's bucket's terms up to and with the lane's own, x of a distance and u its bucket, which do not descend over the lanes: after it the last
+// lane of a bucket has the bucket's sum.  Steps of 1, 2, 4 and 8 lanes in a row of 16, then from row to row.
+template <int CTRL, int ROWS> __device__ __forceinline__ float bucket_step(float x, int u)
+{
+    const int v = __builtin_amdgcn_update_dpp(-1, u, CTRL, ROWS, 0xf, false);
+    const float y = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROWS, 0xf, false));
+    return x + (v == u ? y : 0.f);
+}
+__device__ __forceinline__ float bucket_sums(float x, int u)
+{
+    x = bucket_step<0x111, 0xf>(x, u);
+    x = bucket_step<0x112, 0xf>(x, u);
+    x = bucket_step<0x114, 0xf>(x, u);
+    x = bucket_step<0x118, 0xf>(x, u);
+    x = bucket_step<0x142, 0xa>(x, u);  // lane 15 of the rows 0 and 2 to the rows 1 and 3
+    return bucket_step<0x143, 0xc>(x, u);  // lane 31 to the rows 2 and 3
+}
+
+// The wave's sums of dS.
+struct BiasSums {
+    float* sums;      // of bucket u at u, in LDS
+    float sum = 0.f;  // lane u has more of bucket u's
+    float run = 0.f;  // the lane's terms of bucket cur, not yet in its sum
+    int cur = -1;
+
+    __device__ __forceinline__ void start(float* at, int lane)
     {
-        sums = at, run = 0.f, cur = -1;
-        for (int i = lane; i < buckets * 16; i += 64) sums[i] = 0.f;
+        sums = at;
+        sums[lane] = 0.f;
     }
-    __device__ __forceinline__ void add(int u, float x, int g, int r)  // x: a term of each lane
+    __device__ __forceinline__ void add(int u, float x, int lane)  // x: terms of bucket u in each lane
     {
-        x = rows_sum(x);
-        if (g == 0) sums[u * 16 + r] += x;
+        x = wave_sum(x);
+        sum += lane == u ? x : 0.f;
     }
-    __device__ __forceinline__ void one(int u, float x, int g, int r)  // all terms are bucket u's
+    __device__ __forceinline__ void one(int u, float x, int lane)  // the same, where bucket u comes several times in a row
     {
         if (u != cur) {
-            flush(g, r);
+            flush(lane);
             cur = u;
         }
         run += x;
     }
-    __device__ __forceinline__ void flush(int g, int r)
+    __device__ __forceinline__ void flush(int lane)
     {
-        if (cur >= 0) add(cur, run, g, r);
+        if (cur >= 0) add(cur, run, lane);
         run = 0.f, cur = -1;
     }
-    // the sums of a head go out, and the next one's start
-    __device__ __forceinline__ void out(float* to, int buckets, int lane, int g, int r)
+    __device__ __forceinline__ void several(int u, float x, int lane)  // the lane's bucket and term, as for bucket_sums
     {
-        flush(g, r);
+        x = bucket_sums(x, u);
+        const int next = __shfl_down(u, 1);
+        if (lane == 63 || next != u) sums[u] += x;
+    }
+    // the sums of a head go out, and the next one's start
+    __device__ __forceinline__ void out(float* to, int buckets, int lane)
+    {
+        flush(lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own stores, read by its other lanes
         __builtin_amdgcn_wave_barrier();
-        if (lane < buckets) {
-            float x = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float* p = sums + lane * 16 + ((i + lane) & 15);
-                x += *p;
-                *p = 0.f;
-            }
-            to[lane] = x;
-        }
+        if (lane < buckets) to[lane] = sum + sums[lane];
+        sums[lane] = sum = 0.f;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
 };
+
+// dS of 32 queries and C keys, x[kt][qt][e] of query 16 qt + 4 g + e and key 16 kt + r, summed along its diagonals: lane n gets those with query - key =
+// n - 32.  A row of LDS takes the two diagonals that are 32 apart, whose keys do not meet; two lanes read it, half of the keys each.
+template <int C> struct Shear {
+    static constexpr int PITCH = C + 4, SIZE = 32 * PITCH;
+};
+template <int KT> __device__ __forceinline__ void diagonals_put(const floatx4 (&x)[KT][2], float* lds, int g, int r)
+{
+    constexpr int PITCH = Shear<16 * KT>::PITCH;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            lds[((16 * (e >> 2) + 4 * g + (e & 3) - 16 * kt - r) & 31) * PITCH + 16 * kt + r] = x[kt][e >> 2][e & 3];
+}
+template <int KT> __device__ __forceinline__ float diagonals_sum(const float* lds, int lane)
+{
+    constexpr int C = 16 * KT, PITCH = Shear<C>::PITCH;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own stores, read by its other lanes
+    __builtin_amdgcn_wave_barrier();
+    const int d = lane & 31, h = lane >> 5, lim = 32 - d - h * (C / 2);  // the row's keys below lim are diagonal d's, the others d - 32's
+    const float* row = lds + d * PITCH + h * (C / 2);
+    float hi = 0.f, lo = 0.f;
+#pragma unroll
+    for (int i = 0; i < C / 2; i += 4) {
+        const floatx4 v = ld4f(row + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            hi += i + e < lim ? v[e] : 0.f;
+            lo += i + e < lim ? 0.f : v[e];
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const unsigned uh = __float_as_uint(hi), ul = __float_as_uint(lo);
+    const auto a = __builtin_amdgcn_permlane32_swap(uh, uh, false, false), b = __builtin_amdgcn_permlane32_swap(ul, ul, false, false);
+    hi = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    lo = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+    return h ? hi : lo;
+}
 
 // Tiles of 16 queries (query pass) or keys (key pass) that a wave owns: two where the registers hold them, so that each fragment read
 // from LDS serves two products.
@@ -100,14 +169,17 @@ template <typename T, int D> struct BwdGeo {
 // EXACT: delta is formed from outputs that were rounded to bf16, which adds 2^-9 |dO| |o| or so to each dP - delta.  That is lost among dS's own
 // rounding where many keys share a row, and as large as it where few do.  The sum of the dS of a row is what delta is off by (the exact
 // ones sum to zero), so the row's dq is put right by that sum times sum_j P_j k_j, a third product, and delta goes on to the key pass without the error.
-template <typename T, int D, bool EXACT, int EXT>
+//
+// EXACT = kDelta: delta alone is put right, for the key pass.
+constexpr int kRounded = 0, kDelta = 1, kExact = 2;
+template <typename T, int D, int EXACT, int EXT>
 __global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<EXT>::type a)
 {
     typedef BwdGeo<T, D> G;
     typedef typename Frag<T>::type F;
     constexpr int QT = G::XT, BUF = 64 * 2 * G::LD;
     __shared__ __attribute__((aligned(16))) T lds[2 * BUF];
-    __shared__ float near[EXT == kBias ? kNear : 1];
+    __shared__ float near[EXT == kBias ? kPad + kNear : 1];
 
     long long u = xcd_unit(blockIdx.x, a.q_per);
     if (u >= a.q_units) return;
@@ -171,16 +243,16 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<E
     if constexpr (EXT == kBias) {
         lanes.set_edges(a.spec, lane);
         lanes.set_head(a.spec, h, lane);
-        near[tid] = lanes.of_lane(lanes.bucket_of_lane(a.spec, tid));
+        lanes.table(a.spec, near, wave, 4, lane);
     }
     const int far = lo - ns;  // what a sink is further away than its index says
-    floatx4 acc[QT][D / 16], pk[EXACT ? QT : 1][D / 16];
+    floatx4 acc[QT][D / 16], pk[EXACT == kExact ? QT : 1][D / 16];
     float off[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         off[qt] = 0.f;
 #pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] = pk[EXACT ? qt : 0][dt] = zero4();
+        for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] = pk[EXACT == kExact ? qt : 0][dt] = zero4();
     }
 
     const int aend = min(a0 + 16 * QT, nq) - 1;
@@ -224,23 +296,23 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<E
                 if (ulo != uhi) {
 #pragma unroll
                     for (int qt = 0; qt < QT; ++qt) {
-                        int n[8];
                         float bv[8];
+                        const int n = c + a0 + 16 * qt + r - i0 - 4 * g;  // of the lane's first key
+                        if (dmax < kNear && (i0 >= 0 || i1 < 0)) {
+                            const float* from = near + kPad + n + (i0 < 0 ? far : 0);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const int j = i0 + 4 * g + 16 * (e >> 2) + (e & 3);
-                            n[e] = c + a0 + 16 * qt + r - j + (j < 0 ? far : 0);
-                            bv[e] = bu;
-                        }
-                        if (dmax < kNear) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) bv[e] = near[max(n[e], 0)];
+                            for (int e = 0; e < 8; ++e) bv[e] = from[-16 * (e >> 2) - (e & 3)];
                         } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) bv[e] = bu;
                             for (int w = ulo + 1; w <= uhi; ++w) {
                                 const int edge = lanes.first(w);
                                 const float x = lanes.of(w);
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) bv[e] = n[e] >= edge ? x : bv[e];
+                                for (int e = 0; e < 8; ++e) {
+                                    const int m = n - 16 * (e >> 2) - (e & 3), j = i0 + 4 * g + 16 * (e >> 2) + (e & 3);
+                                    bv[e] = m + (j < 0 ? far : 0) >= edge ? x : bv[e];
+                                }
                             }
                         }
 #pragma unroll
@@ -268,7 +340,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<E
                         for (int e = 0; e < 8; ++e) {
                             const bool seen = (unsigned)(j + 16 * (e >> 2) + (e & 3) - jlo) < (unsigned)a.W;
                             s[qt][e >> 2][e & 3] = seen ? s[qt][e >> 2][e & 3] : 0.f;
-                            if (EXACT) dp[qt][e >> 2][e & 3] = seen ? dp[qt][e >> 2][e & 3] : 0.f;
+                            if (EXACT == kExact) dp[qt][e >> 2][e & 3] = seen ? dp[qt][e >> 2][e & 3] : 0.f;
                         }
                     } else {
 #pragma unroll
@@ -276,7 +348,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<E
                             const int k = j + 16 * (e >> 2) + (e & 3);
                             const bool seen = (k <= jhi) & ((k >= jlo) | (k < sb));
                             s[qt][e >> 2][e & 3] = seen ? s[qt][e >> 2][e & 3] : 0.f;
-                            if (EXACT) dp[qt][e >> 2][e & 3] = seen ? dp[qt][e >> 2][e & 3] : 0.f;
+                            if (EXACT == kExact) dp[qt][e >> 2][e & 3] = seen ? dp[qt][e >> 2][e & 3] : 0.f;
                         }
                     }
                 }
@@ -285,8 +357,8 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<E
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
                 sf[qt] = frag_from_acc<T>(s[qt][0], s[qt][1]);
+                if (EXACT == kExact) pf[qt] = frag_from_acc<T>(dp[qt][0], dp[qt][1]);
                 if (EXACT) {
-                    pf[qt] = frag_from_acc<T>(dp[qt][0], dp[qt][1]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) off[qt] += s[qt][e >> 2][e & 3];
                 }
@@ -297,7 +369,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<E
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt) {
                     acc[qt][dt] = mma(kf, sf[qt], acc[qt][dt]);
-                    if (EXACT) pk[qt][dt] = mma(kf, pf[qt], pk[qt][dt]);
+                    if (EXACT == kExact) pk[qt][dt] = mma(kf, pf[qt], pk[qt][dt]);
                 }
             }
         }
@@ -307,8 +379,9 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<E
         const int i = a0 + 16 * qt + r;
         if (EXACT) {
             off[qt] = rows_sum(off[qt]);
+            if (EXACT == kExact)
 #pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] -= off[qt] * pk[qt][dt];
+                for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] -= off[qt] * pk[EXACT == kExact ? qt : 0][dt];
             if (g == 0 && i < nq) a.delta[row0 + i] = delta[qt] + off[qt];
         }
         if (i >= min(G::NB, a.L - q0)) continue;
@@ -366,7 +439,7 @@ __device__ __forceinline__ void window_bwd_sinks(const typename ExtBwdArgs<EXT>:
     float* to = nullptr;  // the wave's sums of dS, head by head
     if constexpr (EXT == kBias) {
         lanes.set_edges(a.spec, lane);
-        db.start(sums + wave * kMaxBuckets * 16, a.spec.buckets, lane);
+        db.start(sums + 64 * wave, lane);
         to = a.db_part + ((size_t)a.k_units + unit) * 4 * grp * a.spec.buckets + (size_t)wave * grp * a.spec.buckets;
         for (int i = lane; i < grp * a.spec.buckets; i += 64) to[i] = 0.f;  // heads that the wave does not meet
     }
@@ -376,7 +449,7 @@ __device__ __forceinline__ void window_bwd_sinks(const typename ExtBwdArgs<EXT>:
         const size_t row0 = ((size_t)b * a.H + hk * grp + hg) * a.L;
         if (EXT == kBias && hg != head) {
             if constexpr (EXT == kBias) {
-                if (head >= 0) db.out(to + (size_t)head * a.spec.buckets, a.spec.buckets, lane, g, r);
+                if (head >= 0) db.out(to + (size_t)head * a.spec.buckets, a.spec.buckets, lane);
                 lanes.set_head(a.spec, hk * grp + hg, lane);
             }
             head = hg;
@@ -428,7 +501,7 @@ __device__ __forceinline__ void window_bwd_sinks(const typename ExtBwdArgs<EXT>:
                 float x = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x += dp[e >> 2][e & 3];
-                db.one(ulo, x, g, r);
+                db.one(ulo, x, lane);
             } else {
                 for (int w = ulo; w <= uhi; ++w) {
                     const int from = w == ulo ? INT32_MIN : lanes.first(w), to_ = w == uhi ? INT32_MAX : lanes.first(w + 1);
@@ -438,7 +511,7 @@ __device__ __forceinline__ void window_bwd_sinks(const typename ExtBwdArgs<EXT>:
                         const int n = q0 + 16 * (e >> 2) + 4 * g + (e & 3) - j;
                         x += ((n >= from) & (n < to_)) ? dp[e >> 2][e & 3] : 0.f;
                     }
-                    db.add(w, x, g, r);
+                    db.add(w, x, lane);
                 }
             }
         }
@@ -455,7 +528,7 @@ __device__ __forceinline__ void window_bwd_sinks(const typename ExtBwdArgs<EXT>:
         __builtin_amdgcn_wave_barrier();
     }
     if constexpr (EXT == kBias)
-        if (head >= 0) db.out(to + (size_t)head * a.spec.buckets, a.spec.buckets, lane, g, r);
+        if (head >= 0) db.out(to + (size_t)head * a.spec.buckets, a.spec.buckets, lane);
     float* sO = (float*)raw;
     for (int which = 0; which < 2; ++which) {
         __syncthreads();
@@ -480,16 +553,17 @@ __device__ __forceinline__ void window_bwd_sinks(const typename ExtBwdArgs<EXT>:
 // Bound: issue (the query pass's shape: 203-215 us of keys; with the sinks' workgroups 221-235, which took 31 us in a launch of their own and 340
 // us in all where they were spread among the keys').
 template <typename T, int D, int EXT>
-__global__ void __launch_bounds__(256, EXT == kBias && sizeof(T) == 2 ? 2 : 1) window_bwd_k_kernel(typename ExtBwdArgs<EXT>::type a)
+__global__ void __launch_bounds__(256, EXT == kBias && sizeof(T) == 2 && D < 128 ? 2 : 1) window_bwd_k_kernel(typename ExtBwdArgs<EXT>::type a)
 {
     typedef BwdGeo<T, D> G;
     typedef typename Frag<T>::type F;
     constexpr int KT = G::XT, BUF = 64 * 2 * G::LD;
     __shared__ __attribute__((aligned(16))) T lds[2 * BUF];
     __shared__ __attribute__((aligned(16))) float sStat[2][2][64];
-    __shared__ float sums[EXT == kBias ? 4 * kMaxBuckets * 16 : 1];
-    __shared__ float near[2][EXT == kBias ? kNear : 1];           // of this head and of the last
-    __shared__ unsigned char nearu[EXT == kBias ? kNear : 1];     // their buckets
+    __shared__ __attribute__((aligned(16))) float shear[EXT == kBias ? 4 * Shear<16 * KT>::SIZE : 1];
+    __shared__ float near[2][EXT == kBias ? kPad + kNear : 1];           // of this head and of the last
+    __shared__ unsigned char nearu[EXT == kBias ? kPad + kNear : 1];     // their buckets
+    __shared__ float sums[EXT == kBias ? 4 * 64 : 1];
 
     if (blockIdx.x >= 8 * a.k_per) {  // last: they fill the compute units that run out of keys
         window_bwd_sinks<T, D, EXT>(a, blockIdx.x - (unsigned)(8 * a.k_per), (char*)lds, sums);
@@ -554,12 +628,11 @@ __global__ void __launch_bounds__(256, EXT == kBias && sizeof(T) == 2 ? 2 : 1) w
 
     BiasLanes lanes = {};
     BiasSums db;
-    int myu = 0;  // the bucket of distance tid
     if constexpr (EXT == kBias) {
         lanes.set_edges(a.spec, lane);
-        db.start(sums + wave * kMaxBuckets * 16, a.spec.buckets, lane);
-        myu = lanes.bucket_of_lane(a.spec, tid);
-        nearu[tid] = (unsigned char)myu;
+        db.start(sums + 64 * wave, lane);
+        if (wave == 0) nearu[lane] = 0;
+        for (int x = wave; x < kNear / 64; x += 4) lanes.each(64 * x, lane, [&](int w, float) { nearu[kPad + 64 * x + lane] = (unsigned char)w; });
     }
 
     if (nt > 0) load(0, 0);
@@ -567,7 +640,7 @@ __global__ void __launch_bounds__(256, EXT == kBias && sizeof(T) == 2 ? 2 : 1) w
     for (int hg = 0; hg < grp; ++hg) {
         if constexpr (EXT == kBias) {
             lanes.set_head(a.spec, hk * grp + hg, lane);
-            near[hg & 1][tid] = lanes.of_lane(myu);  // waves behind the others still read the last head's, those of the head before it are through
+            lanes.table(a.spec, near[hg & 1], wave, 4, lane);  // waves behind the others still read the last head's, those of the head before it are through
         }
         for (int t = 0; t < nt; ++t, buf ^= 1) {
             T *sQ = lds + buf * BUF, *sD = sQ + 64 * G::LD;
@@ -617,7 +690,7 @@ __global__ void __launch_bounds__(256, EXT == kBias && sizeof(T) == 2 ? 2 : 1) w
                             const int n = q0 + 4 * g - (k0 + 16 * kt + r);
                             if (dmax < kNear) {
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) bv[e] = near[hg & 1][max(n + 16 * (e >> 2) + (e & 3), 0)];
+                                for (int e = 0; e < 8; ++e) bv[e] = near[hg & 1][kPad + n + 16 * (e >> 2) + (e & 3)];
                             } else {
 #pragma unroll
                                 for (int e = 0; e < 8; ++e) bv[e] = bu;
@@ -665,33 +738,9 @@ __global__ void __launch_bounds__(256, EXT == kBias && sizeof(T) == 2 ? 2 : 1) w
                         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                             for (int e = 0; e < 8; ++e) x += dp[kt][e >> 2][e & 3];
-                        db.one(ulo, x, g, r);
-                    } else if (dmax < kNear) {
-                        db.flush(g, r);
-#pragma unroll
-                        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const int n = max(q0 + 4 * g - (k0 + 16 * kt + r) + 16 * (e >> 2) + (e & 3), 0);  // below zero: dS is zero
-                                float* at = db.sums + nearu[n] * 16 + r;
-                                for (int x = 0; x < 4; ++x) {  // one row group after the other: a fixed order (the barrier, of no cost, keeps them apart)
-                                    if (g == x) __hip_atomic_fetch_add(at, dp[kt][e >> 2][e & 3], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-                                    __builtin_amdgcn_wave_barrier();
-                                }
-                            }
+                        db.one(ulo, x, lane);
                     } else {
-                        for (int w = ulo; w <= uhi; ++w) {
-                            const int from = w == ulo ? INT32_MIN : lanes.first(w), to = w == uhi ? INT32_MAX : lanes.first(w + 1);
-                            float x = 0.f;
-#pragma unroll
-                            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const int n = q0 + 4 * g - (k0 + 16 * kt + r) + 16 * (e >> 2) + (e & 3);
-                                    x += ((n >= from) & (n < to)) ? dp[kt][e >> 2][e & 3] : 0.f;
-                                }
-                            db.add(w, x, g, r);
-                        }
+                        diagonals_put<KT>(dp, shear + wave * Shear<16 * KT>::SIZE, g, r);  // read below, when fewer registers are in use
                     }
                 }
                 F pf[KT], sf[KT];
@@ -709,10 +758,20 @@ __global__ void __launch_bounds__(256, EXT == kBias && sizeof(T) == 2 ? 2 : 1) w
                         dk[kt][dt] = mma(qf, sf[kt], dk[kt][dt]);
                     }
                 }
+                if constexpr (EXT == kBias) {
+                    if (ulo != uhi) {
+                        const float x = diagonals_sum<KT>(shear + wave * Shear<16 * KT>::SIZE, lane);
+                        const int n0 = q0 - k0 - 32;
+                        if (dmax < kNear)
+                            db.several(nearu[kPad + n0 + lane], x, lane);
+                        else
+                            lanes.each(n0, lane, [&](int w, float) { db.several(w, x, lane); });
+                    }
+                }
             }
         }
         if constexpr (EXT == kBias)
-            db.out(a.db_part + ((unit * 4 + wave) * grp + hg) * a.spec.buckets, a.spec.buckets, lane, g, r);
+            db.out(a.db_part + ((unit * 4 + wave) * grp + hg) * a.spec.buckets, a.spec.buckets, lane);
     }
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
@@ -761,10 +820,11 @@ constexpr int kExactKeys = 64;
 template <typename T, int D, int EXT> hipError_t backward_d(const typename ExtBwdArgs<EXT>::type& a, hipStream_t s)
 {
     typedef BwdGeo<T, D> G;
-    if (EXT == kBias || std::min((long long)a.W + a.S, (long long)a.L) <= kExactKeys)
-        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, sizeof(T) == 2, EXT>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
+    constexpr bool rounds = sizeof(T) == 2;  // the bias's gradient takes a delta that is not rounded
+    if (std::min((long long)a.W + a.S, (long long)a.L) <= kExactKeys)
+        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, rounds ? kExact : kRounded, EXT>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
     else
-        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, EXT == kBias && sizeof(T) == 2, EXT>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
+        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, rounds && EXT == kBias ? kDelta : kRounded, EXT>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
     hipLaunchKernelGGL((window_bwd_k_kernel<T, D, EXT>), dim3((unsigned)(8 * a.k_per) + a.s_units), dim3(G::NT), 0, s, a);
     if (a.ns > 0) {
         const long long n = (long long)a.B * a.Hkv * a.ns * (2 * D / 4);

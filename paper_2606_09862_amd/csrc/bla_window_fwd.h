@@ -94,7 +94,7 @@ template <typename T, int D, int NW> struct WinGeo {
 constexpr float kLag = 8.f;
 
 // A bias (EXT = kBias) takes the running maximum into the base-2 domain.  32 keys and 16 queries span 47 distances: where those share a bucket, which
-// they do nearly everywhere, the bias is one number beside the maximum in the exponent and costs nothing a pair; near the query it comes from a table in
+// they do nearly everywhere, the bias is one number beside the maximum in the exponent and costs nothing a pair; of near distances it comes from a table in
 // LDS, elsewhere from a selection at each edge.
 // A prefix (EXT = kPrefix) has tiles of its own ahead of the others.
 template <typename T, int D, int NW, bool RING, int EXT>
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
     typedef WinGeo<T, D, NW> G;
     typedef typename Frag<T>::type F;
     __shared__ __attribute__((aligned(16))) T lds[2 * G::BUF];
-    __shared__ float near[EXT == kBias ? kNear : 1];
+    __shared__ float near[EXT == kBias ? kPad + kNear : 1];
 
     if (blockIdx.x >= 8 * (unsigned)a.per) {
         window_ring<T, D>(a, (long long)(blockIdx.x - 8 * (unsigned)a.per) * G::NT + threadIdx.x);
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
     if constexpr (EXT == kBias) {
         lanes.set_edges(a.spec, lane);
         lanes.set_head(a.spec, h, lane);
-        if (wave < kNear / 64) near[tid] = lanes.of_lane(lanes.bucket_of_lane(a.spec, tid));
+        lanes.table(a.spec, near, wave, NW, lane);
         far = min(lo - s0 - ns, (int64_t)1 << 29);
     }
     const int ntile = ntp + (total + kWinKeys - 1) / kWinKeys;
@@ -309,23 +309,23 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
                 const int ulo = lanes.bucket(c + a0 - i1), uhi = lanes.bucket(dmax);
                 bu = lanes.of(ulo);
                 if (ulo != uhi) {
-                    int n[8];
                     float bv[8];
+                    const int n = jhi - i0 - 4 * g;  // of the lane's first key
+                    if (dmax < kNear && (i0 >= 0 || i1 < 0)) {
+                        const float* from = near + kPad + n + (i0 < 0 ? (int)far : 0);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int j = i0 + 4 * g + 16 * (e >> 2) + (e & 3);
-                        n[e] = jhi - j + (j < 0 ? (int)far : 0);
-                        bv[e] = bu;
-                    }
-                    if (dmax < kNear) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) bv[e] = near[max(n[e], 0)];
+                        for (int e = 0; e < 8; ++e) bv[e] = from[-16 * (e >> 2) - (e & 3)];
                     } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) bv[e] = bu;
                         for (int w = ulo + 1; w <= uhi; ++w) {
                             const int edge = lanes.first(w);
                             const float x = lanes.of(w);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) bv[e] = n[e] >= edge ? x : bv[e];
+                            for (int e = 0; e < 8; ++e) {
+                                const int j = i0 + 4 * g + 16 * (e >> 2) + (e & 3);
+                                bv[e] = jhi - j + (j < 0 ? (int)far : 0) >= edge ? x : bv[e];
+                            }
                         }
                     }
 #pragma unroll
