@@ -22,11 +22,10 @@ template <typename T, int D> __global__ void __launch_bounds__(256) evict_sum_ke
     __shared__ __attribute__((aligned(16))) T lds[2 * BUF];
     __shared__ __attribute__((aligned(16))) float sl[2][64];
 
-    long long u = xcd_unit(blockIdx.x, a.per);
+    const long long u = falling_unit(blockIdx.x, a.units);  // the first keys have most queries
     if (u >= a.units) return;
-    const int nb = (int)(u % a.nkb);
-    u /= a.nkb;
-    const int h = (int)(u % a.H), b = (int)(u / a.H), hk = h / (a.H / a.Hkv);
+    const long long bh = u % ((long long)a.B * a.H);
+    const int nb = (int)(u / ((long long)a.B * a.H)), h = (int)(bh % a.H), b = (int)(bh / a.H), hk = h / (a.H / a.Hkv);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
     int64_t pos;
     const int len = row_tokens(a.lengths, a.pos, a.t0, b, a.L, pos);

@@ -56,6 +56,16 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // unit (w mod 8) * per + w / 8 and each XCD walks `per` consecutive units, whose shared rows stay in its L2.
 __device__ __forceinline__ long long xcd_unit(unsigned w, long long per) { return (long long)(w & 7) * per + (w >> 3); }
 
+// Order of workgroups whose work falls from block to block (causal rows): all the `wide` sequences' first blocks, then their second and so on, so that the
+// device does not end with a few long ones.  Consecutive workgroups are of consecutive sequences: where these are a multiple of eight, a sequence's blocks
+// meet in one XCD's L2.  Every second 256 (a workgroup to each compute unit) is taken from behind, by the XCDs' eights, so that a compute unit that holds
+// two gets a long and a short one.  Returns the index of (block, sequence), sequences running faster.
+__device__ __forceinline__ long long falling_unit(unsigned w, long long units)
+{
+    const unsigned row = w & ~255u, col = w & 255u;
+    return (w & 256u) && row + 256 <= units ? (long long)row + (248u - (col & ~7u)) + (col & 7u) : w;
+}
+
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 

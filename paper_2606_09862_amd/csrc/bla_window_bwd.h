@@ -181,14 +181,26 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<E
     __shared__ __attribute__((aligned(16))) T lds[2 * BUF];
     __shared__ float near[EXT == kBias ? kPad + kNear : 1];
 
-    long long u = xcd_unit(blockIdx.x, a.q_per);
-    if (u >= a.q_units) return;
     const int grp = a.H / a.Hkv;
-    const int hg = (int)(u % grp);
-    u /= grp;
-    const int q0 = (int)(u % a.nqb) * G::NB;
-    u /= a.nqb;
-    const int hk = (int)(u % a.Hkv), b = (int)(u / a.Hkv);
+    int hg, q0, hk, b;
+    if constexpr (EXT == kPlain) {
+        long long u = xcd_unit(blockIdx.x, a.q_per);
+        if (u >= a.q_units) return;
+        hg = (int)(u % grp);
+        u /= grp;
+        q0 = (int)(u % a.nqb) * G::NB;
+        u /= a.nqb;
+        hk = (int)(u % a.Hkv), b = (int)(u / a.Hkv);
+    } else {  // windows as long as the rows: the last queries have most keys
+        long long u = falling_unit(blockIdx.x, a.q_units);
+        if (u >= a.q_units) return;
+        hk = (int)(u % a.Hkv);
+        u /= a.Hkv;
+        b = (int)(u % a.B);
+        u /= a.B;
+        hg = (int)(u % grp);
+        q0 = (a.nqb - 1 - (int)(u / grp)) * G::NB;
+    }
     const int h = hk * grp + hg;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
     const int len = a.lengths ? min(max(a.lengths[b], 0), a.L) : a.L;
@@ -569,13 +581,23 @@ __global__ void __launch_bounds__(256, EXT == kBias && sizeof(T) == 2 && D < 128
         window_bwd_sinks<T, D, EXT>(a, blockIdx.x - (unsigned)(8 * a.k_per), (char*)lds, sums);
         return;
     }
-    long long u = xcd_unit(blockIdx.x, a.k_per);
-    if (u >= a.k_units) return;
-    const size_t unit = (size_t)u;
     const int grp = a.H / a.Hkv;
-    const int nb = (int)(u % a.nkb);
-    u /= a.nkb;
-    const int hk = (int)(u % a.Hkv), b = (int)(u / a.Hkv);
+    int nb, hk, b;
+    if constexpr (EXT == kPlain) {
+        long long u = xcd_unit(blockIdx.x, a.k_per);
+        if (u >= a.k_units) return;
+        nb = (int)(u % a.nkb);
+        u /= a.nkb;
+        hk = (int)(u % a.Hkv), b = (int)(u / a.Hkv);
+    } else {  // the first keys have most queries
+        long long u = falling_unit(blockIdx.x, a.k_units);
+        if (u >= a.k_units) return;
+        hk = (int)(u % a.Hkv);
+        u /= a.Hkv;
+        b = (int)(u % a.B);
+        nb = (int)(u / a.B);
+    }
+    const size_t unit = ((size_t)b * a.Hkv + hk) * a.nkb + nb;
     const int n0 = nb * G::NB;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
     const int len = a.lengths ? min(max(a.lengths[b], 0), a.L) : a.L;

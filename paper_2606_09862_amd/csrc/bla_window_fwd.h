@@ -109,16 +109,30 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
         window_ring<T, D>(a, (long long)(blockIdx.x - 8 * (unsigned)a.per) * G::NT + threadIdx.x);
         return;
     }
-    long long u = xcd_unit(blockIdx.x, a.per);
-    if (u >= a.units) return;
     const int grp = a.H / a.Hkv;
-    const int hg = (int)(u % grp);
-    u /= grp;
-    const int part = (int)(u % a.nsplit);
-    u /= a.nsplit;
-    const int q0 = (int)(u % a.nqb) * G::BQ;
-    u /= a.nqb;
-    const int hk = (int)(u % a.Hkv), b = (int)(u / a.Hkv);
+    int hg, part, q0, hk, b;
+    if constexpr (EXT == kPlain) {
+        long long u = xcd_unit(blockIdx.x, a.per);
+        if (u >= a.units) return;
+        hg = (int)(u % grp);
+        u /= grp;
+        part = (int)(u % a.nsplit);
+        u /= a.nsplit;
+        q0 = (int)(u % a.nqb) * G::BQ;
+        u /= a.nqb;
+        hk = (int)(u % a.Hkv), b = (int)(u / a.Hkv);
+    } else {  // windows as long as the rows: the last queries have most keys
+        long long u = falling_unit(blockIdx.x, a.units);
+        if (u >= a.units) return;
+        hk = (int)(u % a.Hkv);
+        u /= a.Hkv;
+        b = (int)(u % a.B);
+        u /= a.B;
+        hg = (int)(u % grp);
+        u /= grp;
+        part = (int)(u % a.nsplit);
+        q0 = (a.nqb - 1 - (int)(u / a.nsplit)) * G::BQ;
+    }
     const int h = hk * grp + hg;
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
