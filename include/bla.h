@@ -479,11 +479,9 @@ bla_status bla_evict_forward(const bla_evict_params* p, const void* q, const voi
  * in all, in the order of their entries; their scores and positions go with them.  Slots without a token: zeros, at = -1.  cache_k_in, cache_v_in and
  * at_in: all or none.  p->H and p->scale are not used.
  */
-size_t bla_evict_select_workspace_size(const bla_evict_params* p);
 bla_status bla_evict_select(const bla_evict_params* p, const void* k, const void* v, const float* score, const int32_t* lengths,
                             const int64_t* pos, const void* cache_k_in, const void* cache_v_in, const int64_t* at_in,
-                            void* cache_k_out, void* cache_v_out, float* score_out, int64_t* at_out, void* workspace,
-                            size_t workspace_bytes, void* stream);
+                            void* cache_k_out, void* cache_v_out, float* score_out, int64_t* at_out, void* stream);
 
 /*
  * One token for every row (p->L is ignored): it takes slot pos while the cache is not full, then the slot with the least score among those with at < pos - recent,

@@ -147,12 +147,12 @@ def lib():
         for name in ("bla_prefix_supported", "bla_prefix_forward", "bla_prefix_step"):
             getattr(L, name).restype = ctypes.c_int
         E = ctypes.POINTER(EvictParams)
-        for name in ("bla_evict_workspace_size", "bla_evict_select_workspace_size", "bla_evict_step_workspace_size"):
+        for name in ("bla_evict_workspace_size", "bla_evict_step_workspace_size"):
             getattr(L, name).argtypes = [E]
             getattr(L, name).restype = ctypes.c_size_t
         L.bla_evict_supported.argtypes = [E]
         L.bla_evict_forward.argtypes = [E] + [_vp] * 12 + [ctypes.c_size_t, _vp]
-        L.bla_evict_select.argtypes = [E] + [_vp] * 13 + [ctypes.c_size_t, _vp]
+        L.bla_evict_select.argtypes = [E] + [_vp] * 12
         L.bla_evict_step.argtypes = [E] + [_vp] * 12 + [ctypes.c_size_t, _vp]
         for name in ("bla_evict_supported", "bla_evict_forward", "bla_evict_select", "bla_evict_step"):
             getattr(L, name).restype = ctypes.c_int
@@ -855,7 +855,7 @@ def _evict_plan(what, B, H, Hkv, L, d, slots, recent, scale, dtype):
     st = lib().bla_evict_supported(p)
     if what == "bla_evict_forward" or st != 2:  # the launches of the other calls have limits of their own, which they check
         _shape_status(st, what)
-    return block, p, getattr(lib(), what.replace("_forward", "") + "_workspace_size")(p)
+    return block, p, 0 if what == "bla_evict_select" else getattr(lib(), what.replace("_forward", "") + "_workspace_size")(p)
 
 
 def _evict_params(what, B, H, Hkv, L, d, slots, recent, t0, scale, dtype):
@@ -909,8 +909,7 @@ def evict_forward(q, k, v, slots: int, cache_k=None, cache_v=None, score=None, t
     return o, lse, after
 
 
-def evict_select(k, v, score, slots: int, recent: int = 0, cache_k=None, cache_v=None, at=None, t0: int = 0, lengths=None, pos=None,
-                 workspace=None):
+def evict_select(k, v, score, slots: int, recent: int = 0, cache_k=None, cache_v=None, at=None, t0: int = 0, lengths=None, pos=None):
     """bla_evict_select: the cache after L tokens: of the cache's tokens and the call's k, v [B,H_kv,L,d] the newest `recent` stay, and of the others those
     with the largest score [B,H_kv,slots+L] (of equal ones the lowest entries), `slots` in all, in the order of their entries.
 
@@ -919,7 +918,7 @@ def evict_select(k, v, score, slots: int, recent: int = 0, cache_k=None, cache_v
     """
     B, Hkv, L, d = k.shape
     dt, dev = k.dtype, k.get_device()
-    p, need = _evict_params("bla_evict_select", B, Hkv, Hkv, L, d, slots, recent, t0, None, dt)
+    p, _ = _evict_params("bla_evict_select", B, Hkv, Hkv, L, d, slots, recent, t0, None, dt)
     _check_on(k, (B, Hkv, L, d), dt, "k", dev)
     _check_on(v, (B, Hkv, L, d), dt, "v", dev)
     _check_on(score, (B, Hkv, slots + L), torch.float32, "score", dev)
@@ -928,12 +927,11 @@ def evict_select(k, v, score, slots: int, recent: int = 0, cache_k=None, cache_v
         _check_on(lengths, (B,), torch.int32, "lengths", dev)
     if pos is not None:
         _check_on(pos, (B,), torch.int64, "pos", dev)
-    ck, cv = (torch.empty((B, Hkv, slots, d), dtype=dt, device=k.device) for _ in range(2))
-    kept = torch.empty((B, Hkv, slots), dtype=torch.float32, device=k.device)
+    ck, cv = k.new_empty((B, Hkv, slots, d)), k.new_empty((B, Hkv, slots, d))
+    kept = score.new_empty((B, Hkv, slots))
     where = torch.empty((B, Hkv, slots), dtype=torch.int64, device=k.device)
-    keep, ws, n = _room(workspace, need, k)
     _call(lib().bla_evict_select, "bla_evict_select", dev, p, k.data_ptr(), v.data_ptr(), score.data_ptr(), _ptr(lengths), _ptr(pos), _ptr(cache_k),
-          _ptr(cache_v), _ptr(at), ck.data_ptr(), cv.data_ptr(), kept.data_ptr(), where.data_ptr(), ws, n)
+          _ptr(cache_v), _ptr(at), ck.data_ptr(), cv.data_ptr(), kept.data_ptr(), where.data_ptr())
     return ck, cv, kept, where
 
 

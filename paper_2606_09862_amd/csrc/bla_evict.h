@@ -29,15 +29,16 @@ struct EvictSelectArgs {
     const int64_t* pos;
     int64_t t0;
     int B, Hkv, L, slots, recent;
-    int* index;                // [B, Hkv, slots]: the entry that a slot takes, or -1
+    int slices, pieces;        // workgroups of a key head, pieces of 16 bytes of a key
     void *ck_out, *cv_out;
     float* score_out;
     int64_t* at_out;
 };
 
 hipError_t launch_evict_sum(int bf16_io, int D, const EvictSumArgs& a, hipStream_t s);
-hipError_t launch_evict_select(int bf16_io, int D, const EvictSelectArgs& a, hipStream_t s);
+hipError_t launch_evict_select(const EvictSelectArgs& a, hipStream_t s);
 hipError_t launch_evict_step(int bf16_io, int D, const EvictStepArgs& a, hipStream_t s);
-constexpr int kEvictKeys = 128;  // keys of a workgroup of the sums
+constexpr int kEvictKeys = 128;    // keys of a workgroup of the sums
+constexpr int kSliceSlots = 4096;  // most slots of a slice of the selection
 
 }  // namespace bla

@@ -57,8 +57,9 @@ bool fits(const bla_evict_params* p, const EvictPlan& e)
 }
 
 // Step: window attention's split; the sums are formed by the same workgroups where each has all slots and heads of its key head.
+constexpr long long kScoreLds = 32 * 1024;  // scores of a workgroup that stay in LDS (four such workgroups fill a compute unit's registers at d = 64)
 struct EvictStepPlan : StepPlan {
-    bool fused;
+    bool fused, in_lds;
     int pitch;
     size_t off_z, off_mine;
 };
@@ -71,22 +72,27 @@ EvictStepPlan evict_step_plan(const bla_evict_params* p)
     s.pitch = (p->slots + 31) & ~31;
     const size_t rows = (size_t)p->B * p->H;
     s.off_z = s.fused ? 0 : seq_align(s.nsplit * rows * (p->d + 2) * 4);
-    s.off_mine = s.off_z + seq_align(rows * s.pitch * 4);
+    s.in_lds = s.fused && p->H_kv > 0 && (long long)(p->H / p->H_kv) * s.pitch * 4 <= kScoreLds;
+    s.off_mine = s.off_z + (s.in_lds ? 0 : seq_align(rows * s.pitch * 4));
     s.total = s.off_mine + seq_align((size_t)p->B * p->H_kv * 4);
     return s;
 }
 bool fits(const bla_evict_params* p, const EvictStepPlan& s)
 {
-    return launchable((double)p->B * p->H_kv * s.ngrp * s.nsplit, 256) && launchable((double)p->B * p->H_kv * ((p->slots + 255) / 256), 256);
+    return launchable((double)p->B * p->H_kv * s.ngrp * s.nsplit, 256) &&
+           launchable((double)p->B * p->H_kv * ((p->slots + 255) / 256) + (double)p->B * p->H / 4 + 1, 256);
 }
 
-// Select: where each slot's token is.
-size_t select_total(const bla_evict_params* p) { return seq_align((size_t)p->B * p->H_kv * p->slots * 4); }
-bool select_fits(const bla_evict_params* p)
+// Select: a workgroup to a key head's slice of the slots, as many slices as fill the device (each finds what stays by itself).
+int select_slices(const bla_evict_params* p)
 {
-    return launchable((double)p->B * p->H_kv, 1024) &&
-           launchable((double)p->B * p->H_kv * p->slots * (p->d * elem_bytes(p->io_dtype) / 16) / 256 + 1, 256);
+    const long long bh = (long long)p->B * p->H_kv, least = (p->slots + kSliceSlots - 1) / kSliceSlots;
+    long long n = bh > 0 ? 256 / bh : 1;
+    const long long most = (p->slots + 63) / 64;
+    if (n > most) n = most;
+    return (int)(n < least ? least : n < 1 ? 1 : n);
 }
+bool select_fits(const bla_evict_params* p) { return launchable((double)p->B * p->H_kv * select_slices(p), 1024); }
 
 bool enough(const void* workspace, size_t bytes, size_t total) { return total == 0 || (workspace && bytes >= total && is_aligned16(workspace)); }
 
@@ -144,14 +150,9 @@ bla_status bla_evict_forward(const bla_evict_params* p, const void* q, const voi
     return launch_evict_sum(bf16, p->d, m, s) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }
 
-size_t bla_evict_select_workspace_size(const bla_evict_params* p)
-{
-    return check_evict(p, false) == BLA_OK && select_fits(p) ? select_total(p) : 0;
-}
-
 bla_status bla_evict_select(const bla_evict_params* p, const void* k, const void* v, const float* score, const int32_t* lengths,
                             const int64_t* pos, const void* cache_k_in, const void* cache_v_in, const int64_t* at_in, void* cache_k_out,
-                            void* cache_v_out, float* score_out, int64_t* at_out, void* workspace, size_t workspace_bytes, void* stream)
+                            void* cache_v_out, float* score_out, int64_t* at_out, void* stream)
 {
     const bla_status st = check_evict(p, false);
     if (st != BLA_OK) return st;
@@ -170,14 +171,12 @@ bla_status bla_evict_select(const bla_evict_params* p, const void* k, const void
                        {pos, 8 * (size_t)p->B}, {cache_k_in, n * row}, {cache_v_in, n * row}, {at_in, n * 8}};
     const Span out[] = {{cache_k_out, n * row}, {cache_v_out, n * row}, {score_out, n * 4}, {at_out, n * 8}};
     if (clash(in, out)) return BLA_ERR_INVALID_ARG;
-    const size_t total = select_total(p);
-    if (!enough(workspace, workspace_bytes, total)) return BLA_ERR_WORKSPACE;
-    if (!tables_overwritten(workspace, total)) return BLA_ERR_HIP;
     EvictSelectArgs a = {};
     a.k = k, a.v = v, a.ck = cache_k_in, a.cv = cache_v_in, a.score = score, a.at_in = at_in, a.lengths = lengths, a.pos = pos, a.t0 = p->t0;
-    a.B = p->B, a.Hkv = p->H_kv, a.L = p->L, a.slots = p->slots, a.recent = p->recent, a.index = (int*)workspace;
+    a.B = p->B, a.Hkv = p->H_kv, a.L = p->L, a.slots = p->slots, a.recent = p->recent, a.slices = select_slices(p);
+    a.pieces = (int)(row / 16);
     a.ck_out = cache_k_out, a.cv_out = cache_v_out, a.score_out = score_out, a.at_out = at_out;
-    return launch_evict_select(p->io_dtype == BLA_BF16, p->d, a, (hipStream_t)stream) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
+    return launch_evict_select(a, (hipStream_t)stream) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }
 
 size_t bla_evict_step_workspace_size(const bla_evict_params* p)
@@ -212,13 +211,10 @@ bla_status bla_evict_step(const bla_evict_params* p, const void* q, const void* 
     const size_t rows = (size_t)p->B * p->H;
     a.part_ml = a.part_o + (size_t)sp.nsplit * rows * p->d;
     a.score_in = score_in, a.score_out = score_out, a.at_in = at_in, a.at_out = at_out, a.recent = p->recent;
-    a.z = (float*)((char*)workspace + sp.off_z), a.pitch = sp.pitch, a.mine = (int*)((char*)workspace + sp.off_mine), a.fused = sp.fused;
+    a.z = (float*)((char*)workspace + sp.off_z), a.pitch = sp.pitch, a.mine = (int*)((char*)workspace + sp.off_mine), a.fused = sp.fused, a.in_lds = sp.in_lds;
     hipStream_t s = (hipStream_t)stream;
     const int bf16 = p->io_dtype == BLA_BF16;
-    if (launch_evict_step(bf16, p->d, a, s) != hipSuccess) return BLA_ERR_HIP;
-    if (sp.fused) return BLA_OK;
-    const JoinArgs j = {a.part_o, a.part_ml, o, nullptr, (long long)rows, sp.nsplit};
-    return launch_window_join(bf16, p->d, j, s) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
+    return launch_evict_step(bf16, p->d, a, s) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }
 
 }  // extern "C"

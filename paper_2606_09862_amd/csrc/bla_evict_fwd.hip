@@ -141,11 +141,38 @@ __global__ void __launch_bounds__(256) evict_sum_out_kernel(EvictSumArgs a)
     a.score_out[i] = x;
 }
 
-// Which entries stay.  A workgroup of 16 waves takes one key head of one row.  An entry's key is its score's place in the order of scores, the
+// Which entries stay, and their way to the cache.  A workgroup of 16 waves takes one key head of one row and moves a slice of the slots: several find the
+// same in parallel, which costs nothing where the key heads do not fill the device, and a second launch would cost more.  An entry's key is its score's place in the order of scores, the
 // largest of all for the newest `recent` tokens; three counts of its upper 11, next 11 and last 10 bits (by integer atomics in LDS, whose order does not
 // matter) find the key of the last entry that stays, of which the lowest entries fill the slots.  Then each wave walks a sixteenth of the entries
 // in order, first to count, then to number those that stay.
-// Bound: latency (32 key heads of 4096 entries for 1024 slots, with the launch that moves them: see bla_evict_select in the table of figures).
+// Bound: latency.
+__device__ __forceinline__ void move_slice(const EvictSelectArgs& a, size_t bh, int64_t pos, int s0, int s1, const int* index)
+{
+    const intx4 *ck = (const intx4*)a.ck + bh * a.slots * a.pieces, *cv = (const intx4*)a.cv + bh * a.slots * a.pieces;
+    const intx4 *k = (const intx4*)a.k + bh * a.L * a.pieces, *v = (const intx4*)a.v + bh * a.L * a.pieces;
+    const size_t to = bh * a.slots + s0;
+    const int shift = __builtin_ctz(a.pieces);  // 4, 8, 16 or 32
+    for (int i = threadIdx.x; i < (s1 - s0) << shift; i += 1024) {  // a piece of 16 bytes of a key and of a value to a thread
+        const int e = index[i >> shift], c = i & (a.pieces - 1);
+        intx4 kx = {0, 0, 0, 0}, vx = {0, 0, 0, 0};
+        if (e >= a.slots) {
+            kx = k[((size_t)(e - a.slots) << shift) + c];
+            vx = v[((size_t)(e - a.slots) << shift) + c];
+        } else if (e >= 0) {
+            kx = ck[((size_t)e << shift) + c];
+            vx = cv[((size_t)e << shift) + c];
+        }
+        ((intx4*)a.ck_out)[(to << shift) + i] = kx;
+        ((intx4*)a.cv_out)[(to << shift) + i] = vx;
+    }
+    for (int i = threadIdx.x; i < s1 - s0; i += 1024) {
+        const int e = index[i];
+        a.score_out[to + i] = e >= 0 ? a.score[bh * ((size_t)a.slots + a.L) + e] : 0.f;
+        a.at_out[to + i] = e >= a.slots ? pos + (e - a.slots) : e >= 0 ? a.at_in[bh * a.slots + e] : -1;
+    }
+}
+
 constexpr int kSelWaves = 16, kSelLds = 24 * 1024;  // entries whose keys are kept in LDS; those beyond are formed anew
 
 __global__ void __launch_bounds__(1024) evict_select_kernel(EvictSelectArgs a)
@@ -154,16 +181,20 @@ __global__ void __launch_bounds__(1024) evict_select_kernel(EvictSelectArgs a)
     __shared__ int hist[2048];
     __shared__ int wsum[2][kSelWaves];
     __shared__ int found[2];
-    const size_t bh = blockIdx.x;
+    __shared__ int index[kSliceSlots];  // the slice's entries
+    const size_t bh = blockIdx.x / a.slices;
+    const int slice = (int)(blockIdx.x % a.slices), each_slice = (a.slots + a.slices - 1) / a.slices;
+    const int s0 = slice * each_slice, s1 = min(a.slots, s0 + each_slice);
     const int b = (int)(bh / a.Hkv), tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    int* const index = a.index + bh * a.slots;
     int64_t pos;
     const int len = row_tokens(a.lengths, a.pos, a.t0, b, a.L, pos);
     const bool idle = pos < 0 || pos > kMaxPos;
     const int n = a.ck && !idle ? (int)min(pos, (int64_t)a.slots) : 0, total = n + len;
     if (idle || total <= a.slots) {  // everything stays
-        for (int i = tid; i < a.slots; i += 1024)
-            index[i] = idle ? (a.ck ? i : -1) : i < n ? i : i < total ? a.slots + i - n : -1;
+        for (int i = s0 + tid; i < s1; i += 1024)
+            index[i - s0] = idle ? (a.ck ? i : -1) : i < n ? i : i < total ? a.slots + i - n : -1;
+        __syncthreads();
+        move_slice(a, bh, pos, s0, s1, index);
         return;
     }
     const float* score = a.score + bh * ((size_t)a.slots + a.L);
@@ -228,50 +259,18 @@ __global__ void __launch_bounds__(1024) evict_select_kernel(EvictSelectArgs a)
         const unsigned long long eq = __ballot(in && x == prefix);
         const bool stay = in && (x > prefix || (x == prefix && same + __popcll(eq & below) < need));
         const unsigned long long kept = __ballot(stay);
-        if (stay) index[out + __popcll(kept & below)] = i + lane < n ? i + lane : a.slots + i + lane - n;
+        const int slot = out + __popcll(kept & below);
+        if (stay && slot >= s0 && slot < s1) index[slot - s0] = i + lane < n ? i + lane : a.slots + i + lane - n;
         same += __popcll(eq);
         out += __popcll(kept);
     }
-}
-
-// The tokens that stay, a piece of 16 bytes of a key and of a value to a thread.
-template <typename T, int D> __global__ void __launch_bounds__(256) evict_move_kernel(EvictSelectArgs a)
-{
-    constexpr int PE = 16 / (int)sizeof(T), CH = D / PE;
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, row = i / CH;
-    const int ch = (int)(i % CH);
-    if (row >= (size_t)a.B * a.Hkv * a.slots) return;
-    const size_t bh = row / a.slots;
-    const int e = a.index[row];
-    intx4 kx = {0, 0, 0, 0}, vx = {0, 0, 0, 0};
-    if (e >= a.slots) {
-        const size_t from = (bh * a.L + (e - a.slots)) * D + ch * PE;
-        kx = *(const intx4*)((const T*)a.k + from);
-        vx = *(const intx4*)((const T*)a.v + from);
-    } else if (e >= 0) {
-        const size_t from = (bh * a.slots + e) * D + ch * PE;
-        kx = *(const intx4*)((const T*)a.ck + from);
-        vx = *(const intx4*)((const T*)a.cv + from);
-    }
-    *(intx4*)((T*)a.ck_out + row * D + ch * PE) = kx;
-    *(intx4*)((T*)a.cv_out + row * D + ch * PE) = vx;
-    if (ch == 0) {
-        const int64_t pos = a.pos ? a.pos[bh / a.Hkv] : a.t0;
-        a.score_out[row] = e >= 0 ? a.score[bh * ((size_t)a.slots + a.L) + e] : 0.f;
-        a.at_out[row] = e >= a.slots ? pos + (e - a.slots) : e >= 0 ? a.at_in[bh * a.slots + e] : -1;
-    }
+    __syncthreads();
+    move_slice(a, bh, pos, s0, s1, index);
 }
 
 template <typename T, int D> hipError_t sum_d(const EvictSumArgs& a, hipStream_t s)
 {
     hipLaunchKernelGGL((evict_sum_kernel<T, D>), dim3((unsigned)(8 * a.per)), dim3(256), 0, s, a);
-    return hipGetLastError();
-}
-
-template <typename T, int D> hipError_t move_d(const EvictSelectArgs& a, hipStream_t s)
-{
-    const long long pieces = (long long)a.B * a.Hkv * a.slots * (D * (int)sizeof(T) / 16);
-    hipLaunchKernelGGL((evict_move_kernel<T, D>), dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -289,13 +288,10 @@ hipError_t launch_evict_sum(int bf16_io, int D, const EvictSumArgs& a, hipStream
     return hipGetLastError();
 }
 
-hipError_t launch_evict_select(int bf16_io, int D, const EvictSelectArgs& a, hipStream_t s)
+hipError_t launch_evict_select(const EvictSelectArgs& a, hipStream_t s)
 {
-    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)(a.B * a.Hkv)), dim3(1024), 0, s, a);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-#define BLA_CALL(T, DD) move_d<T, DD>(a, s)
-    BLA_BY_TYPE(BLA_CALL)
-#undef BLA_CALL
+    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)((long long)a.B * a.Hkv * a.slices)), dim3(1024), 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace bla

@@ -4,13 +4,19 @@
 namespace bla {
 namespace {
 
-// The sums of the weights where several workgroups share a key head's slots or heads: a workgroup takes 256 slots; the maxima and sums of
-// up to 64 heads at a time are joined from their parts (a wave to a head, a part to a lane), then each thread adds its slot's weights up, head by head.
-__global__ void __launch_bounds__(256) evict_finish_kernel(EvictStepArgs a)
+// What is left where several workgroups share a key head's slots or heads.  The first workgroups form the sums of the weights, 256 slots to each: the maxima
+// and sums of up to 64 heads at a time are joined from their parts (a wave to a head, a part to a lane), then each thread adds its slot's weights up,
+// head by head.  The others join the outputs, four rows to each.
+template <typename T, int D> __global__ void __launch_bounds__(256) evict_finish_kernel(EvictStepArgs a)
 {
     __shared__ float sm[64], sinv[64];
     const int blocks = (a.W + 255) / 256, grp = a.H / a.Hkv;
     const size_t bh = blockIdx.x / blocks;
+    if (bh >= (size_t)a.B * a.Hkv) {
+        const JoinArgs j = {a.part_o, a.part_ml, a.o, nullptr, (long long)a.B * a.H, a.nsplit};
+        join_rows<T, D>(j, (long long)blockIdx.x - (long long)a.B * a.Hkv * blocks);
+        return;
+    }
     const int i = (int)(blockIdx.x % blocks) * 256 + threadIdx.x;
     const int hk = (int)(bh % a.Hkv), b = (int)(bh / a.Hkv);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -43,17 +49,22 @@ __global__ void __launch_bounds__(256) evict_finish_kernel(EvictStepArgs a)
     if (i < a.W) evict_score_out(a, bh, i, mine, n, pos, w);
 }
 
+template <typename T, int D> hipError_t evict_d(const EvictStepArgs& a, hipStream_t s)
+{
+    const hipError_t e = step_d<T, D, kEvict>(a, s);
+    if (e != hipSuccess || a.fused) return e;
+    const long long sums = (long long)a.B * a.Hkv * ((a.W + 255) / 256), joins = ((long long)a.B * a.H + 3) / 4;
+    hipLaunchKernelGGL((evict_finish_kernel<T, D>), dim3((unsigned)(sums + joins)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_evict_step(int bf16_io, int D, const EvictStepArgs& a, hipStream_t s)
 {
-#define BLA_CALL(T, DD) step_d<T, DD, kEvict>(a, s)
-    const auto step = [&]() -> hipError_t { BLA_BY_TYPE(BLA_CALL) };
+#define BLA_CALL(T, DD) evict_d<T, DD>(a, s)
+    BLA_BY_TYPE(BLA_CALL)
 #undef BLA_CALL
-    const hipError_t e = step();
-    if (e != hipSuccess || a.fused) return e;
-    hipLaunchKernelGGL(evict_finish_kernel, dim3((unsigned)((long long)a.B * a.Hkv * ((a.W + 255) / 256))), dim3(256), 0, s, a);
-    return hipGetLastError();
 }
 
 }  // namespace bla

@@ -4,8 +4,7 @@
 
 namespace bla {
 hipError_t launch_prefix_forward(int bf16_io, int D, int waves, const PrefixArgs& a, hipStream_t s);
-hipError_t launch_prefix_step(int bf16_io, int D, const PrefixStepArgs& a, hipStream_t s);
-int prefix_step_block();  // queries of a workgroup
+hipError_t launch_prefix_step(int bf16_io, int D, const PrefixStepArgs& a, bool few, hipStream_t s);
 }  // namespace bla
 
 using namespace bla;
@@ -23,9 +22,12 @@ bla_status check_prefix(const bla_prefix_params* p, bool step)
     return BLA_OK;
 }
 
-// The step's: the prefix in parts of at least two tiles that fill the device with the blocks of its queries, beside the rings' parts.
+// The step's: the prefix in parts that fill the device with the blocks of its queries, of at least a tile for each group of waves, beside the rings' parts.  Few
+// queries go in blocks of 16, whose four waves take 32 tokens each.
+constexpr int kFewQueries = 32, kMaxPrefixParts = 192;
 struct PrefixStepPlan : StepPlan {
-    int npart, nqb;
+    bool few;
+    int npart, nqb, threads;
     long long units;
 };
 PrefixStepPlan prefix_step_plan(const bla_prefix_params* p)
@@ -35,19 +37,22 @@ PrefixStepPlan prefix_step_plan(const bla_prefix_params* p)
     const bla_window_params* w = &p->w;
     if (s.nsplit > kMaxParts / 4) s.nsplit = kMaxParts / 4;
     const long long rows = w->H_kv > 0 && p->G > 0 ? (long long)(w->B / p->G) * (w->H / w->H_kv) : 0;
-    s.nqb = (int)((rows + prefix_step_block() - 1) / prefix_step_block());
-    const long long blocks = (long long)p->G * w->H_kv * s.nqb, tiles = (p->P + kWinKeys - 1) / kWinKeys;
-    long long n = blocks > 0 ? (kFill + blocks - 1) / blocks : 1;
-    if (n > tiles / 2) n = tiles / 2;
-    if (n < 1) n = 1;
-    s.npart = p->P == 0 ? 0 : (int)(n > kMaxParts * 3 / 4 ? kMaxParts * 3 / 4 : n);
+    const PrefixShape shape = prefix_shape(w->io_dtype == BLA_BF16, w->d);
+    s.few = rows <= kFewQueries;
+    s.threads = s.few ? 256 : shape.threads;
+    const int block = s.few ? 16 : shape.block, least = s.few ? 128 : kWinKeys * shape.groups;
+    s.nqb = (int)((rows + block - 1) / block);
+    const long long blocks = (long long)p->G * w->H_kv * s.nqb, fill = s.few ? 2 * kFill : shape.fill;
+    long long n = blocks > 0 ? (fill + blocks - 1) / blocks : 1, most = (p->P + least - 1) / least;
+    if (n > most) n = most;
+    s.npart = (int)(n > kMaxPrefixParts ? kMaxPrefixParts : n);  // none where P = 0
     s.units = blocks * s.npart;
     s.total = seq_align((size_t)(s.npart + s.nsplit) * w->B * w->H * (w->d + 2) * 4);
     return s;
 }
 bool fits(const bla_prefix_params* p, const PrefixStepPlan& s)
 {
-    return launchable(8.0 * ((s.units + 7) / 8) + (double)p->w.B * p->w.H_kv * s.ngrp * s.nsplit, 256);
+    return launchable(8.0 * ((s.units + 7) / 8) + (double)p->w.B * p->w.H_kv * s.ngrp * s.nsplit, s.threads);
 }
 
 bla_status check_pointers(const bla_prefix_params* p, const void* prefix_k, const void* prefix_v, const int32_t* prefix_lengths)
@@ -124,7 +129,7 @@ bla_status bla_prefix_step(const bla_prefix_params* p, const void* q, const void
     a.pre_o = (float*)workspace, a.pre_ml = a.pre_o + (size_t)parts * rows * w->d;
     a.part_o = a.pre_o + (size_t)sp.npart * rows * w->d, a.part_ml = a.pre_ml + (size_t)sp.npart * rows * 2;
     hipStream_t s = (hipStream_t)stream;
-    if (launch_prefix_step(w->io_dtype == BLA_BF16, w->d, a, s) != hipSuccess) return BLA_ERR_HIP;
+    if (launch_prefix_step(w->io_dtype == BLA_BF16, w->d, a, sp.few, s) != hipSuccess) return BLA_ERR_HIP;
     const JoinArgs j = {a.pre_o, a.pre_ml, o, nullptr, (long long)rows, parts};
     return launch_window_join(w->io_dtype == BLA_BF16, w->d, j, s) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }

@@ -5,20 +5,26 @@ namespace bla {
 namespace {
 
 // The rows that share a prefix, with the query heads of a key head, are one matrix of queries: its products with the prefix are matrix products
-// without a mask.  A workgroup of four waves takes 64 QT queries (wave w the 16 QT from 16 QT w on) and a part of the prefix, in tiles of 64 tokens that pass
-// through two LDS buffers, one barrier per tile, as in window_forward_kernel; each fragment read from LDS serves QT products.  Its result is a part,
-// joined with the ring's parts by window_join_kernel.
+// without a mask.  A workgroup takes 64 QT queries and a part of the prefix, in tiles of 64 tokens that pass through two LDS buffers, one barrier per
+// tile, as in window_forward_kernel; each fragment read from LDS serves QT products.  KG groups of four waves take every KG-th tile, wave w of a group the
+// 16 QT queries from 16 QT w on, and are joined through LDS, so that a workgroup fills half a compute unit and leaves one part for as many waves.  The parts are
+// joined with the ring's by window_join_kernel.
+// Few queries (kFewQueries) leave most of such a workgroup idle: they go as the heads of a ring do, in window_step_part.
 template <typename T, int D> struct PrefixGeo {
-    static constexpr int NT = 256, PE = 16 / (int)sizeof(T), CH = D / PE, RPP = NT / CH, NP = (64 + RPP - 1) / RPP;
+    static constexpr int NT = 256, PE = 16 / (int)sizeof(T), CH = D / PE, RPP = NT / CH, NP = (64 + RPP - 1) / RPP;  // of a group
     static constexpr int QT = 2, NB = 64 * QT;
     static constexpr int LK = nat_ld<T>(D), LV = red_ld<T>(D), BUF = kWinKeys * (LK + LV);
+    static constexpr size_t ONE = sizeof(T) * 2 * BUF;  // LDS of a group
+    static constexpr int KG = ONE > 64 * 1024 && ONE <= 80 * 1024 ? 2 : 1, NW = 4 * KG;
+    static constexpr size_t TILES = KG * ONE, RING = StepGeo<T, D, NW>::LDS, LDS = TILES > RING ? TILES : RING;
+    static_assert(KG == 1 || sizeof(float) * 4 * 64 * QT * (D / 4 + 2) <= TILES, "the join's LDS");
 };
 
-template <typename T, int D> __device__ __forceinline__ void prefix_part(const PrefixStepArgs& a, long long u, T* lds)
+template <typename T, int D> __device__ __forceinline__ void prefix_part(const PrefixStepArgs& a, long long u, char* raw)
 {
     typedef PrefixGeo<T, D> G;
     typedef typename Frag<T>::type F;
-    constexpr int QT = G::QT;
+    constexpr int QT = G::QT, KG = G::KG;
     const int grp = a.H / a.Hkv, each_row = a.B / a.G;
     const int blk = (int)(u % a.nqb);
     u /= a.nqb;
@@ -26,7 +32,9 @@ template <typename T, int D> __device__ __forceinline__ void prefix_part(const P
     u /= a.npart;
     const int hk = (int)(u % a.Hkv), gi = (int)(u / a.Hkv);
     const int nq = each_row * grp, q0 = blk * G::NB;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
+    const int kg = KG > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0, tid = threadIdx.x & 255;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
+    T* const lds = (T*)raw + kg * 2 * G::BUF;
     const int np = a.plen ? min(max(a.plen[gi], 0), a.P) : a.P;
     const int ntile = (np + kWinKeys - 1) / kWinKeys, each = (ntile + a.npart - 1) / a.npart;
     const int tb = part * each, te = min(ntile, tb + each);
@@ -73,19 +81,21 @@ template <typename T, int D> __device__ __forceinline__ void prefix_part(const P
         for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] = zero4();
     }
 
-    if (tb < te) load(tb);
-    for (int t = tb; t < te; ++t) {
-        T *sK = lds + (t & 1) * G::BUF, *sV = sK + kWinKeys * G::LK;
+    if (tb + kg < te) load(tb + kg);
+    int buf = 0;
+    for (int t = tb + kg; t - kg < te; t += KG, buf ^= 1) {  // as many rounds in every group
+        T *sK = lds + buf * G::BUF, *sV = sK + kWinKeys * G::LK;
+        if (t < te)
 #pragma unroll
-        for (int ps = 0; ps < G::NP; ++ps) {
-            const int i = ps * G::RPP + lrow;
-            if (G::RPP > 64 && lrow >= kWinKeys) continue;
-            *(intx4*)(sK + i * G::LK + ch * G::PE) = kr[ps];
-            *(intx4*)(sV + i * G::LV + ch * G::PE) = vr[ps];
-        }
+            for (int ps = 0; ps < G::NP; ++ps) {
+                const int i = ps * G::RPP + lrow;
+                if (G::RPP > 64 && lrow >= kWinKeys) continue;
+                *(intx4*)(sK + i * G::LK + ch * G::PE) = kr[ps];
+                *(intx4*)(sV + i * G::LV + ch * G::PE) = vr[ps];
+            }
         __syncthreads();
-        if (t + 1 < te) load(t + 1);
-        if (a0 >= nq) continue;
+        if (t + KG < te) load(t + KG);
+        if (a0 >= nq || t >= te) continue;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
             const int left = np - t * kWinKeys - 32 * hf;
@@ -141,6 +151,31 @@ template <typename T, int D> __device__ __forceinline__ void prefix_part(const P
             }
         }
     }
+    if constexpr (KG > 1) {
+        float* const join = (float*)raw + (size_t)wave * 64 * QT * (D / 4 + 2);
+        __syncthreads();
+        if (kg == 1) {
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) {
+                float* x = join + qt * 64 * (D / 4 + 2);
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) st4f(x + (dt * 64 + lane) * 4, acc[qt][dt]);
+                x[64 * (D / 4) + lane] = mx[qt];
+                x[64 * (D / 4 + 1) + lane] = sum[qt];
+            }
+        }
+        __syncthreads();
+        if (kg == 1) return;
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+            const float* x = join + qt * 64 * (D / 4 + 2);
+            const float m1 = x[64 * (D / 4) + lane], m = fmaxf(mx[qt], m1), f0 = exp2_fast((mx[qt] - m) * sc), f1 = exp2_fast((m1 - m) * sc);
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] = acc[qt][dt] * f0 + ld4f(x + (dt * 64 + lane) * 4) * f1;
+            sum[qt] = sum[qt] * f0 + x[64 * (D / 4 + 1) + lane] * f1;
+            mx[qt] = m;
+        }
+    }
     const size_t rows = (size_t)a.B * a.H;
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
@@ -158,34 +193,55 @@ template <typename T, int D> __device__ __forceinline__ void prefix_part(const P
 }
 
 // The prefix's workgroups, then the rings' (which fill the compute units that run out of prefix): one launch.
-template <typename T, int D> __global__ void __launch_bounds__(256) prefix_step_kernel(PrefixStepArgs a)
+template <typename T, int D> __global__ void __launch_bounds__((64 * PrefixGeo<T, D>::NW)) prefix_step_kernel(PrefixStepArgs a)
 {
     typedef PrefixGeo<T, D> G;
-    constexpr size_t PB = sizeof(T) * 2 * G::BUF, LDS = PB > StepGeo<T, D>::LDS ? PB : StepGeo<T, D>::LDS;
-    __shared__ __attribute__((aligned(16))) char raw[LDS];
+    __shared__ __attribute__((aligned(16))) char raw[G::LDS];
+    __shared__ float sml[2][G::NW][16];
+    if (blockIdx.x < 8 * (unsigned)a.per) {
+        const long long u = xcd_unit(blockIdx.x, a.per);
+        if (u < a.units) prefix_part<T, D>(a, u, raw);
+        return;
+    }
+    window_step_part<T, D, kPrefix, G::NW>(a, blockIdx.x - 8 * (unsigned)a.per, raw, sml);
+}
+
+template <typename T, int D> __global__ void __launch_bounds__(256) prefix_few_kernel(PrefixStepArgs a)
+{
+    __shared__ __attribute__((aligned(16))) char raw[StepGeo<T, D>::LDS];
     __shared__ float sml[2][4][16];
     if (blockIdx.x < 8 * (unsigned)a.per) {
         const long long u = xcd_unit(blockIdx.x, a.per);
-        if (u < a.units) prefix_part<T, D>(a, u, (T*)raw);
+        if (u < a.units) window_step_part<T, D, kFew>(a, (unsigned)u, raw, sml);
         return;
     }
     window_step_part<T, D, kPrefix>(a, blockIdx.x - 8 * (unsigned)a.per, raw, sml);
 }
 
-template <typename T, int D> hipError_t prefix_d(const PrefixStepArgs& a, hipStream_t s)
+template <typename T, int D> hipError_t prefix_d(const PrefixStepArgs& a, bool few, hipStream_t s)
 {
-    const long long rings = (long long)a.B * a.Hkv * a.ngrp * a.nsplit;
-    hipLaunchKernelGGL((prefix_step_kernel<T, D>), dim3((unsigned)(8 * a.per + rings)), dim3(256), 0, s, a);
+    const dim3 grid((unsigned)(8 * a.per + (long long)a.B * a.Hkv * a.ngrp * a.nsplit));
+    if (few)
+        hipLaunchKernelGGL((prefix_few_kernel<T, D>), grid, dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((prefix_step_kernel<T, D>), grid, dim3(64 * PrefixGeo<T, D>::NW), 0, s, a);
     return hipGetLastError();
 }
 
+constexpr int FILL = 256;
+template <typename T, int D> PrefixShape shape_d() { return {PrefixGeo<T, D>::NB, PrefixGeo<T, D>::KG, 64 * PrefixGeo<T, D>::NW, FILL}; }
+
 }  // namespace
 
-int prefix_step_block() { return PrefixGeo<bf16, 64>::NB; }
-
-hipError_t launch_prefix_step(int bf16_io, int D, const PrefixStepArgs& a, hipStream_t s)
+PrefixShape prefix_shape(int bf16_io, int D)
 {
-#define BLA_CALL(T, DD) prefix_d<T, DD>(a, s)
+    if (bf16_io) return D == 32 ? shape_d<bf16, 32>() : D == 64 ? shape_d<bf16, 64>() : shape_d<bf16, 128>();
+    return D == 32 ? shape_d<float, 32>() : D == 64 ? shape_d<float, 64>() : shape_d<float, 128>();
+}
+
+hipError_t launch_prefix_step(int bf16_io, int D, const PrefixStepArgs& a, bool few, hipStream_t s)
+{
+#define BLA_CALL(T, DD) prefix_d<T, DD>(a, few, s)
     BLA_BY_TYPE(BLA_CALL)
 #undef BLA_CALL
 }

@@ -4,53 +4,67 @@
 namespace bla {
 namespace {
 
-// A wave joins a row: lane s holds the maximum and the sum of part s (at most 64 parts), then groups of D / 4 lanes take every
-// 64 / (D / 4)-th part's outputs, four columns to a lane, and are added up.  Parts without a visible key have a sum of zero and are not read.
-// (One thread to four columns of a row walked the parts one after the other: 26 us for 16 rows of 33 parts.)
-template <typename T, int D> __global__ void __launch_bounds__(256) window_join_kernel(JoinArgs a)
+template <typename T, int D> __global__ void __launch_bounds__(256) window_join_kernel(JoinArgs a) { join_rows<T, D>(a, blockIdx.x); }
+
+// More than 64 parts: a workgroup to a row.  A thread holds a part's maximum and sum, then groups of D / 4 threads take every so-maniest part's outputs,
+// four in flight, and are added up in order.
+constexpr int kWideParts = 256;
+template <typename T, int D> __global__ void __launch_bounds__(256) window_join_wide_kernel(JoinArgs a)
 {
-    constexpr int LR = D / 4, PG = 64 / LR;
-    const long long row = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63, c = 4 * (lane % LR), pg = lane / LR;
-    if (row >= a.rows) return;
+    constexpr int LR = D / 4, PG = 256 / LR;
+    __shared__ float w[kWideParts], red[2][4];
+    __shared__ __attribute__((aligned(16))) float so[PG][D];
+    const size_t row = blockIdx.x;
+    const int tid = threadIdx.x, wave = tid >> 6, c = 4 * (tid % LR), pg = tid / LR;
     float m = kNoMax, l = 0.f;
-    if (lane < a.nsplit) {
-        const float* ml = a.part_ml + 2 * ((size_t)lane * a.rows + row);
+    if (tid < a.nsplit) {
+        const float* ml = a.part_ml + 2 * ((size_t)tid * a.rows + row);
         l = ml[1];
         m = l != 0.f ? ml[0] : kNoMax;
     }
     float top = m;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-    float w = l != 0.f ? exp2_fast(m - top) : 0.f;
-    l *= w;
+    if ((tid & 63) == 0) red[0][wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    const float f = l != 0.f ? exp2_fast(m - top) : 0.f;
+    w[tid] = f;
+    l *= f;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
+    if ((tid & 63) == 0) red[1][wave] = l;
+    __syncthreads();
+    l = red[1][0] + red[1][1] + red[1][2] + red[1][3];
     floatx4 o = zero4();
-    for (int s0 = 0; s0 < a.nsplit; s0 += 8 * PG) {  // eight loads in flight; what a part without keys holds is dropped
-        floatx4 v[8];
+    for (int s0 = pg; s0 < a.nsplit; s0 += 4 * PG) {
+        floatx4 v[4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            v[k] = ld4f(a.part_o + ((size_t)min(s0 + k * PG + pg, a.nsplit - 1) * a.rows + row) * D + c);
+        for (int k = 0; k < 4; ++k) v[k] = ld4f(a.part_o + ((size_t)min(s0 + k * PG, a.nsplit - 1) * a.rows + row) * D + c);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int s = s0 + k * PG + pg;
-            float ws = __shfl(w, s & 63);  // lanes past nsplit hold a weight of zero
-            ws = s < 64 ? ws : 0.f;
-            o += ws * (ws != 0.f ? v[k] : zero4());
+        for (int k = 0; k < 4; ++k) {
+            const float x = s0 + k * PG < a.nsplit ? w[s0 + k * PG] : 0.f;
+            o += x * (x != 0.f ? v[k] : zero4());
         }
     }
-#pragma unroll
-    for (int off = 32; off >= LR; off >>= 1)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off);
+    st4f(&so[pg][c], o);
+    __syncthreads();
     const bool some = l != 0.f;
-    if (pg == 0) st4((T*)a.o + (size_t)row * D + c, some ? o * (1.f / l) : zero4());
-    if (a.lse && lane == 0) a.lse[row] = some ? (top + __log2f(l)) * kLn2 : -INFINITY;
+    if (pg == 0) {
+#pragma unroll
+        for (int k = 1; k < PG; ++k) o += ld4f(&so[k][c]);
+        st4((T*)a.o + row * D + c, some ? o * (1.f / l) : zero4());
+    }
+    if (a.lse && tid == 0) a.lse[row] = some ? (top + __log2f(l)) * kLn2 : -INFINITY;
 }
 
 template <typename T, int D> hipError_t join_d(const JoinArgs& a, hipStream_t s)
 {
+    if (a.nsplit > 64) {
+        if (a.nsplit > kWideParts) return hipErrorInvalidValue;
+        hipLaunchKernelGGL((window_join_wide_kernel<T, D>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL((window_join_kernel<T, D>), dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, s, a);
     return hipGetLastError();
 }

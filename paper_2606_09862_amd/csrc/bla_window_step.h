@@ -17,6 +17,11 @@ struct PrefixStepArgs : WindowStepArgs {
     long long units, per;      // workgroups of the prefix, per XCD
     float *pre_o, *pre_ml;     // the prefix's parts
 };
+// The prefix's workgroups where they take it in tiles: queries, groups of waves, threads, and how many fill the device.
+struct PrefixShape {
+    int block, groups, threads, fill;
+};
+PrefixShape prefix_shape(int bf16_io, int D);
 // Slots without order (W of them, S = 0); the scores in the base-2 domain go out for the sums of the weights.
 struct EvictStepArgs : WindowStepArgs {
     const float* score_in;     // [B, Hkv, W]
@@ -28,10 +33,12 @@ struct EvictStepArgs : WindowStepArgs {
     float* z;                  // [B, H, pitch]
     int pitch;
     bool fused;                // a workgroup has all slots and heads of its key head: it forms the sums itself
+    bool in_lds;               // ... and keeps the scores in LDS
 };
 template <int EXT> struct ExtStepArgs { typedef WindowStepArgs type; };
 template <> struct ExtStepArgs<kBias> { typedef BiasStepArgs type; };
 template <> struct ExtStepArgs<kPrefix> { typedef PrefixStepArgs type; };
+template <> struct ExtStepArgs<kFew> { typedef PrefixStepArgs type; };
 template <> struct ExtStepArgs<kEvict> { typedef EvictStepArgs type; };
 
 // A score's place in the order of scores: NaN above every number, the two zeros as one.
@@ -47,9 +54,19 @@ __device__ __forceinline__ unsigned score_key(float x)
 __device__ __forceinline__ int evict_slot(const float* score, const int64_t* at, int slots, int64_t old, uint64_t* lds)
 {
     uint64_t best = ~0ull;
-    for (int i = threadIdx.x; i < slots; i += 256) {
-        const uint64_t key = (uint64_t)(at[i] < old ? score_key(score[i]) : 0xffffffffu) << 32 | (unsigned)i;
-        best = key < best ? key : best;
+    for (int i0 = threadIdx.x; i0 < slots; i0 += 8 * 256) {  // eight loads in flight; a slot that comes twice changes nothing
+        float x[8];
+        int64_t p[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = min(i0 + 256 * k, slots - 1);
+            x[k] = score[i], p[k] = at[i];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint64_t key = (uint64_t)(p[k] < old ? score_key(x[k]) : 0xffffffffu) << 32 | (unsigned)min(i0 + 256 * k, slots - 1);
+            best = key < best ? key : best;
+        }
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
@@ -87,17 +104,18 @@ __device__ __forceinline__ void evict_score_out(const EvictStepArgs& a, size_t b
 // workgroup reads the slot that one of them writes.  Bound: the ring's bytes (512 rows, four key heads of 1028 slots, d = 64, bf16: 76-81 us
 // for 408 MB, 5.2 TB/s); of one row, latency (4 key heads of 4100 slots, d = 128: 6 us in 33 parts and 5 us for their join, which
 // took 26 us with a thread to four columns of a row).
-template <typename T, int D> struct StepGeo {
+template <typename T, int D, int NW = 4> struct StepGeo {
     static constexpr int LV = red_ld<T>(D), LO = D + 4;
-    static constexpr size_t VB = sizeof(T) * 4 * 32 * LV, OB = sizeof(float) * 4 * 16 * LO;
+    static constexpr size_t VB = sizeof(T) * NW * 32 * LV, OB = sizeof(float) * NW * 16 * LO;
     static constexpr size_t LDS = VB > OB ? VB : OB;
 };
 
 // EXT = kBias: the heads have biases of their own, so a lane, whose query head is r, takes them from a table in LDS; the 32 slots of a block are
 // as many distances in a row, but where they hold sinks or the ring's seam.  EXT = kPrefix: the results are parts, to be joined with the prefix's.
 // EXT = kEvict: the token's slot is found first, and the scores are kept until the softmax's sum is known.
-template <typename T, int D, int EXT>
-__device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>::type& a, unsigned u, char* raw, float (&sml)[2][4][16])
+// EXT = kFew: not the ring but a part of the prefix, for 16 of the few queries that share it (heads of one row or of several).
+template <typename T, int D, int EXT, int NW = 4>
+__device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>::type& a, unsigned u, char* raw, float (&sml)[2][NW][16])
 {
     typedef typename Frag<T>::type F;
     constexpr int PE = 16 / (int)sizeof(T), CH = D / PE, LV = red_ld<T>(D);
@@ -105,21 +123,37 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
     constexpr int LO = D + 4;
     __shared__ float sB[EXT == kBias ? kMaxBuckets * 16 : 1];
     __shared__ float sfin[EXT == kEvict ? 32 : 1];
-    bool whole = EXT != kPrefix && a.nsplit == 1;
+    extern __shared__ __attribute__((aligned(16))) float zlds[];  // kEvict: [heads][pitch]
+    constexpr int NT = 64 * NW;
+    bool whole = EXT != kPrefix && EXT != kFew && a.nsplit == 1;
     if constexpr (EXT == kEvict) whole = a.fused;
 
-    const int part = (int)(u % (unsigned)a.nsplit);
-    u /= (unsigned)a.nsplit;
-    const int gi = (int)(u % (unsigned)a.ngrp);
-    u /= (unsigned)a.ngrp;
-    const int hk = (int)(u % (unsigned)a.Hkv), b = (int)(u / (unsigned)a.Hkv);
-    const int grp = a.H / a.Hkv, h0 = hk * grp + 16 * gi, nh = min(16, grp - 16 * gi);
+    unsigned nsplit = a.nsplit, ngrp = a.ngrp;
+    if constexpr (EXT == kFew) nsplit = a.npart, ngrp = a.nqb;
+    const int part = (int)(u % nsplit);
+    u /= nsplit;
+    const int gi = (int)(u % ngrp);
+    u /= ngrp;
+    const int hk = (int)(u % (unsigned)a.Hkv), grp = a.H / a.Hkv;
+    int b = (int)(u / (unsigned)a.Hkv), queries = grp;  // kFew: the row is the prefix's first
+    if constexpr (EXT == kFew) {
+        queries *= a.B / a.G;
+        b *= a.B / a.G;
+    }
+    const int h0 = hk * grp + 16 * gi, nh = min(16, queries - 16 * gi);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, r = lane & 15;
     const size_t qrow = (size_t)b * a.H + h0, rows = (size_t)a.B * a.H;
+    const auto row_of = [&](int i) -> size_t {  // of the workgroup's query i
+        if constexpr (EXT == kFew) {
+            const int x = 16 * gi + i;
+            return (size_t)(b + x / grp) * a.H + hk * grp + x % grp;
+        }
+        return qrow + i;
+    };
 
     int64_t pos;
-    if (row_tokens(nullptr, a.pos, a.t0, b, 1, pos) == 0) {  // a row without a token
-        for (int i = tid; i < nh * D; i += 256)
+    if (EXT != kFew && row_tokens(nullptr, a.pos, a.t0, b, 1, pos) == 0) {  // a row without a token
+        for (int i = tid; i < nh * D; i += NT)
             if (whole) ((T*)a.o)[qrow * D + i] = (T)0.f;
         if (!whole && tid < nh) {
             const size_t at = (size_t)part * rows + qrow + tid;
@@ -130,21 +164,29 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
             const size_t bh = (size_t)b * a.Hkv + hk;
             if (part == 0 && gi == 0 && tid == 0) a.mine[bh] = -1;
             if (a.fused)
-                for (int i = tid; i < a.W; i += 256) evict_score_out(a, bh, i, -1, 0, pos, 0.f);
+                for (int i = tid; i < a.W; i += NT) evict_score_out(a, bh, i, -1, 0, pos, 0.f);
         }
         return;
     }
     const int slots = a.S + a.W;
-    const int n = (int)min(pos + 1, (int64_t)slots);
+    int n = (int)min(pos + 1, (int64_t)slots);
     const size_t bh = (size_t)b * a.Hkv + hk;
     int mine;  // the token's slot
-    if constexpr (EXT == kEvict)
+    if constexpr (EXT == kFew) {
+        const int gx = b / (a.B / a.G);
+        n = a.plen ? min(max(a.plen[gx], 0), a.P) : a.P;
+        mine = -1;
+    } else if constexpr (EXT == kEvict)
         mine = pos < slots ? (int)pos : evict_slot(a.score_in + bh * slots, a.at_in + bh * slots, slots, pos - a.recent, (uint64_t*)raw);
     else
         mine = pos < a.S ? (int)pos : a.S + (int)((pos - a.S) % a.W);
     const T *kn = (const T*)a.k + bh * D, *vn = (const T*)a.v + bh * D;
     T *ck = (T*)a.ck + bh * slots * D, *cv = (T*)a.cv + bh * slots * D;
-    if (part == 0 && gi == 0 && tid < 2 * CH) {
+    if constexpr (EXT == kFew) {
+        const size_t at = ((size_t)(b / (a.B / a.G)) * a.Hkv + hk) * a.P * D;
+        ck = (T*)a.pk + at, cv = (T*)a.pv + at;  // only read
+    }
+    if (EXT != kFew && part == 0 && gi == 0 && tid < 2 * CH) {
         const int ch = tid % CH;
         if (tid < CH)
             *(intx4*)(ck + (size_t)mine * D + ch * PE) = *(const intx4*)(kn + ch * PE);
@@ -152,12 +194,12 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
             *(intx4*)(cv + (size_t)mine * D + ch * PE) = *(const intx4*)(vn + ch * PE);
     }
 
-    const int nblk = (n + 31) / 32, each = (nblk + a.nsplit - 1) / a.nsplit;
+    const int nblk = (n + 31) / 32, each = (nblk + (int)nsplit - 1) / (int)nsplit;
     const int bb = part * each, be = min(nblk, bb + each);
 
     F qf[D / 32];
     {
-        const T* q = (const T*)a.q + (qrow + min(r, nh - 1)) * D;
+        const T* q = (const T*)a.q + row_of(min(r, nh - 1)) * D;
         const float sgn = a.scale < 0.f ? -1.f : 1.f;
 #pragma unroll
         for (int kb = 0; kb < D / 32; ++kb) {
@@ -173,7 +215,7 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
     int pm = -1;                            // the token's slot of the ring, counted from its first
     if constexpr (EXT == kBias) {
         lanes.set_edges(a.spec, lane);
-        for (int i = tid; i < a.spec.buckets * 16; i += 256) {
+        for (int i = tid; i < a.spec.buckets * 16; i += NT) {
             const float x = a.spec.bias[(size_t)(h0 + min(i & 15, nh - 1)) * a.spec.buckets + (i >> 4)];
             sB[i] = x < kBiasNone ? -INFINITY : x * kLog2e;
         }
@@ -207,7 +249,7 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
     float mx = kNoMax, sum = 0.f;
     int blk = bb + wave;
     if (blk < be) load(blk);
-    for (; blk < be; blk += 4) {
+    for (; blk < be; blk += NW) {
 #pragma unroll
         for (int x = 0; x < NV; ++x)
             *(intx4*)(sV + ((x * 64 + lane) / CH) * LV + ((x * 64 + lane) % CH) * PE) = vr[x];
@@ -218,7 +260,7 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
 #pragma unroll
             for (int kb = 0; kb < D / 32; ++kb) s[kt] = mma(kf[kt][kb], qf[kb], s[kt]);
         }
-        if (blk + 4 < be) load(blk + 4);
+        if (blk + NW < be) load(blk + NW);
         if constexpr (EXT == kBias) {
             const int i0 = 32 * blk, i1 = i0 + 31;
             int ulo = 0, uhi = a.spec.buckets - 1;
@@ -258,9 +300,15 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
                 for (int e = 0; e < 4; ++e) s[kt][e] = 32 * blk + 16 * kt + 4 * g + e < n ? s[kt][e] : -INFINITY;
         }
         if constexpr (EXT == kEvict) {
-            if (r < nh)
+            if (r < nh) {
+                if (a.in_lds) {
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt) st4f(a.z + (qrow + r) * a.pitch + 32 * blk + 16 * kt + 4 * g, s[kt] * sc);
+                    for (int kt = 0; kt < 2; ++kt) st4f(zlds + r * a.pitch + 32 * blk + 16 * kt + 4 * g, s[kt] * sc);
+                } else {
+#pragma unroll
+                    for (int kt = 0; kt < 2; ++kt) st4f(a.z + (qrow + r) * a.pitch + 32 * blk + 16 * kt + 4 * g, s[kt] * sc);
+                }
+            }
         }
         float m = kNoMax;
 #pragma unroll
@@ -299,15 +347,15 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
         sml[1][wave][r] = sum;
     }
     __syncthreads();
-    for (int i = tid; i < nh * (D / 4); i += 256) {
+    for (int i = tid; i < nh * (D / 4); i += NT) {
         const int hq = i / (D / 4), c = 4 * (i % (D / 4));
         float m = kNoMax * sx;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) m = fmaxf(m, sml[0][w][hq]);
+        for (int w = 0; w < NW; ++w) m = fmaxf(m, sml[0][w][hq]);
         float l = 0.f;
         floatx4 o = zero4();
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float f = exp2_fast(sml[0][w][hq] - m);
             l += f * sml[1][w][hq];
             o += f * ld4f(sO + (w * 16 + hq) * LO + c);
@@ -319,11 +367,17 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
         if (whole) {
             st4((T*)a.o + (qrow + hq) * D + c, EXT != kBias || l > 0.f ? o * (1.f / l) : zero4());
         } else {
-            const size_t at = (size_t)part * rows + qrow + hq;
-            st4f(a.part_o + at * D + c, o);
+            const size_t at = (size_t)part * rows + row_of(hq);
+            float *to = a.part_o, *ml = a.part_ml;
+            if constexpr (EXT == kFew) {
+                to = a.pre_o, ml = a.pre_ml;
+                int64_t at_row;
+                if (row_tokens(nullptr, a.pos, a.t0, b + (16 * gi + hq) / grp, 1, at_row) == 0) l = 0.f;
+            }
+            st4f(to + at * D + c, o);
             if (c == 0) {
-                a.part_ml[2 * at] = m;
-                a.part_ml[2 * at + 1] = l;
+                ml[2 * at] = m;
+                ml[2 * at + 1] = l;
             }
         }
     }
@@ -333,10 +387,14 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
             return;
         }
         __syncthreads();  // sfin, and the scores that the waves have written
-        for (int i = tid; i < slots; i += 256) {
+        for (int i = tid; i < slots; i += NT) {
             float w = 0.f;
-            if (i < n)
-                for (int h = 0; h < nh; ++h) w += exp2_fast(a.z[(qrow + h) * a.pitch + i] - sfin[h]) * sfin[16 + h];
+            if (i < n) {
+                if (a.in_lds)
+                    for (int h = 0; h < nh; ++h) w += exp2_fast(zlds[h * a.pitch + i] - sfin[h]) * sfin[16 + h];
+                else
+                    for (int h = 0; h < nh; ++h) w += exp2_fast(a.z[(qrow + h) * a.pitch + i] - sfin[h]) * sfin[16 + h];
+            }
             evict_score_out(a, bh, i, mine, n, pos, w);
         }
     }
@@ -351,7 +409,10 @@ template <typename T, int D, int EXT> __global__ void __launch_bounds__(256) win
 
 template <typename T, int D, int EXT> hipError_t step_d(const typename ExtStepArgs<EXT>::type& a, hipStream_t s)
 {
-    hipLaunchKernelGGL((window_step_kernel<T, D, EXT>), dim3((unsigned)((long long)a.B * a.Hkv * a.ngrp * a.nsplit)), dim3(256), 0, s, a);
+    size_t more = 0;
+    if constexpr (EXT == kEvict)
+        if (a.in_lds) more = sizeof(float) * (a.H / a.Hkv) * a.pitch;
+    hipLaunchKernelGGL((window_step_kernel<T, D, EXT>), dim3((unsigned)((long long)a.B * a.Hkv * a.ngrp * a.nsplit)), dim3(256), more, s, a);
     return hipGetLastError();
 }
 
