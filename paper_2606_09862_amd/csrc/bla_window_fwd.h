@@ -83,8 +83,8 @@ template <typename T, int D> __device__ __forceinline__ void window_ring(const W
 // d = 128 and window 255, where a lane has 64 visible pairs in all and a third of its tiles are masked (8 x 16 heads x 4096 queries, four heads to a key head, d = 64, window 1024, bf16:
 // 190-220 us, 550-640 TFLOP/s of visible pairs; the first form, a wave to 16 queries of 4-wave groups with a reduction a tile, 337 us.  16 heads x 65536,
 // d = 128, window 255: 320-343 us for 1.08 GB, 3.3 TB/s; first form 893).
-template <typename T, int D, int NW> struct WinGeo {
-    static constexpr int BQ = 16 * NW, NT = 64 * NW;
+template <typename T, int D, int NW, int QT> struct WinGeo {
+    static constexpr int BQ = 16 * QT * NW, NT = 64 * NW;
     static constexpr int LK = nat_ld<T>(D), LV = red_ld<T>(D);
     static constexpr int PE = 16 / (int)sizeof(T), CH = D / PE;  // 16-byte pieces of a row
     static constexpr int NPC = kWinKeys * CH;                    // pieces of a tile
@@ -97,10 +97,11 @@ constexpr float kLag = 8.f;
 // they do nearly everywhere, the bias is one number beside the maximum in the exponent and costs nothing a pair; of near distances it comes from a table in
 // LDS, elsewhere from a selection at each edge.
 // A prefix (EXT = kPrefix) has tiles of its own ahead of the others.
-template <typename T, int D, int NW, bool RING, int EXT>
+// QT tiles of 16 queries to a wave: with two each fragment read from LDS serves two products, and what a tile costs beside its pairs is shared.
+template <typename T, int D, int NW, int QT, bool RING, int EXT>
 __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) window_forward_kernel(typename ExtArgs<EXT>::type a)
 {
-    typedef WinGeo<T, D, NW> G;
+    typedef WinGeo<T, D, NW, QT> G;
     typedef typename Frag<T>::type F;
     __shared__ __attribute__((aligned(16))) T lds[2 * G::BUF];
     __shared__ float near[EXT == kBias ? kPad + kNear : 1];
@@ -141,7 +142,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
     const int nq = min(G::BQ, len - q0);
     const size_t row0 = ((size_t)b * a.H + h) * a.L + q0;  // the block's first row of q, o, lse
     T* const out = (T*)a.o + row0 * D;
-    const int a0 = 16 * wave;                              // the wave's first query in the block
+    const int a0 = 16 * QT * wave;                           // the wave's first query in the block
 
     if (nq <= 0) {  // padding: zeros
         const int rows = min(G::BQ, a.L - q0);
@@ -255,26 +256,31 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
     };
 
     // queries, sign of the scale folded in (exact), as the second operand of K Q^T
-    F qf[D / 32];
-    {
-        const T* qrow = (const T*)a.q + (row0 + min(a0 + r, nq - 1)) * D;
+    F qf[QT][D / 32];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        const T* qrow = (const T*)a.q + (row0 + min(a0 + 16 * qt + r, nq - 1)) * D;
 #pragma unroll
         for (int kb = 0; kb < D / 32; ++kb) {
-            qf[kb] = ld_nat(qrow, kb, g);
+            qf[qt][kb] = ld_nat(qrow, kb, g);
             if (a.scale < 0.f)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) qf[kb][e] = (T)(-(float)qf[kb][e]);
+                for (int e = 0; e < 8; ++e) qf[qt][kb][e] = (T)(-(float)qf[qt][kb][e]);
         }
     }
     const float sc = fabsf(a.scale) * kLog2e, lag = EXT == kBias ? kLag : kLag / sc;
 
-    floatx4 acc[D / 16];
-    float mx = kNoMax, sum = 0.f, limit = kNoMax;           // limit: mx + lag
+    floatx4 acc[QT][D / 16];
+    float mx[QT], sum[QT], limit[QT];                       // limit: mx + lag
 #pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) acc[dt] = zero4();
+    for (int qt = 0; qt < QT; ++qt) {
+        mx[qt] = limit[qt] = kNoMax, sum[qt] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] = zero4();
+    }
 
-    const int aend = min(a0 + 16, nq) - 1;  // the wave's last query
-    const int jhi = c + a0 + r, jlo = jhi - (a.W - 1);  // the lane's query sees the window keys jlo .. jhi, and those below sb up to jhi
+    const int aend = min(a0 + 16 * QT, nq) - 1;  // the wave's last query
+    const int jhi0 = c + a0 + r;  // with jhi = jhi0 + 16 qt and jlo = jhi - (W - 1) the lane's query sees the window keys jlo .. jhi, and those below sb up to jhi
     if (tb < te) load(tb);
     for (int t = tb; t < te; ++t) {
         T* buf = lds + (t & 1) * G::BUF;
@@ -290,104 +296,131 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
             const bool pre = EXT == kPrefix && t < ntp;
             const int left = np - t * kWinKeys - 32 * hf;                      // prefix tokens from here on
             if (pre ? left <= 0 : (i0 > c + aend || (i0 >= sb && i1 <= c + a0 - a.W))) continue;
-            floatx4 s[2];
+            floatx4 s[QT][2];
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
-                s[kt] = zero4();
 #pragma unroll
-                for (int kb = 0; kb < D / 32; ++kb) s[kt] = mma(ld_nat(sK + (32 * hf + 16 * kt + r) * G::LK, kb, g), qf[kb], s[kt]);
+                for (int qt = 0; qt < QT; ++qt) s[qt][kt] = zero4();
+#pragma unroll
+                for (int kb = 0; kb < D / 32; ++kb) {
+                    const F kf = ld_nat(sK + (32 * hf + 16 * kt + r) * G::LK, kb, g);
+#pragma unroll
+                    for (int qt = 0; qt < QT; ++qt) s[qt][kt] = mma(kf, qf[qt][kb], s[qt][kt]);
+                }
             }
             // Masks are selects without branches (& and |, not && and ||, and every element assigned): a form that branched per lane around the
             // products' results was compiled to code with wrong results.
             if (pre) {
                 if (left < 32)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = 4 * g + 16 * (e >> 2) + (e & 3) < left ? s[e >> 2][e & 3] : -INFINITY;
+                    for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            s[qt][e >> 2][e & 3] = 4 * g + 16 * (e >> 2) + (e & 3) < left ? s[qt][e >> 2][e & 3] : -INFINITY;
             } else if (i1 > c + a0 || (i0 <= c + aend - a.W && i1 >= sb)) {  // some pair is not visible
                 const int j = i0 + 4 * g;
-                if (i0 >= sb) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        s[e >> 2][e & 3] = (unsigned)(j + 16 * (e >> 2) + (e & 3) - jlo) < (unsigned)a.W ? s[e >> 2][e & 3] : -INFINITY;
-                } else {
+                for (int qt = 0; qt < QT; ++qt) {
+                    const int jhi = jhi0 + 16 * qt, jlo = jhi - (a.W - 1);
+                    if (i0 >= sb) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int k = j + 16 * (e >> 2) + (e & 3);
-                        s[e >> 2][e & 3] = (k <= jhi) & ((k >= jlo) | (k < sb)) ? s[e >> 2][e & 3] : -INFINITY;
+                        for (int e = 0; e < 8; ++e)
+                            s[qt][e >> 2][e & 3] = (unsigned)(j + 16 * (e >> 2) + (e & 3) - jlo) < (unsigned)a.W ? s[qt][e >> 2][e & 3] : -INFINITY;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int k = j + 16 * (e >> 2) + (e & 3);
+                            s[qt][e >> 2][e & 3] = (k <= jhi) & ((k >= jlo) | (k < sb)) ? s[qt][e >> 2][e & 3] : -INFINITY;
+                        }
                     }
                 }
             }
             float sx = sc, bu = 0.f;  // kBias: a score in the base-2 domain is s sx + bu
             if constexpr (EXT == kBias) {
-                const int dmax = c + a0 + 15 - i0 + (i0 < 0 ? (int)far : 0);
+                const int dmax = c + a0 + 16 * QT - 1 - i0 + (i0 < 0 ? (int)far : 0);
                 const int ulo = lanes.bucket(c + a0 - i1), uhi = lanes.bucket(dmax);
                 bu = lanes.of(ulo);
                 if (ulo != uhi) {
-                    float bv[8];
-                    const int n = jhi - i0 - 4 * g;  // of the lane's first key
-                    if (dmax < kNear && (i0 >= 0 || i1 < 0)) {
-                        const float* from = near + kPad + n + (i0 < 0 ? (int)far : 0);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) bv[e] = from[-16 * (e >> 2) - (e & 3)];
-                    } else {
+                    for (int qt = 0; qt < QT; ++qt) {
+                        float bv[8];
+                        const int jhi = jhi0 + 16 * qt, n = jhi - i0 - 4 * g;  // of the lane's first key
+                        if (dmax < kNear && (i0 >= 0 || i1 < 0)) {
+                            const float* from = near + kPad + n + (i0 < 0 ? (int)far : 0);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) bv[e] = bu;
-                        for (int w = ulo + 1; w <= uhi; ++w) {
-                            const int edge = lanes.first(w);
-                            const float x = lanes.of(w);
+                            for (int e = 0; e < 8; ++e) bv[e] = from[-16 * (e >> 2) - (e & 3)];
+                        } else {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const int j = i0 + 4 * g + 16 * (e >> 2) + (e & 3);
-                                bv[e] = jhi - j + (j < 0 ? (int)far : 0) >= edge ? x : bv[e];
+                            for (int e = 0; e < 8; ++e) bv[e] = bu;
+                            for (int w = ulo + 1; w <= uhi; ++w) {
+                                const int edge = lanes.first(w);
+                                const float x = lanes.of(w);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const int j = i0 + 4 * g + 16 * (e >> 2) + (e & 3);
+                                    bv[e] = jhi - j + (j < 0 ? (int)far : 0) >= edge ? x : bv[e];
+                                }
                             }
                         }
-                    }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = __builtin_fmaf(s[e >> 2][e & 3], sc, bv[e]);
+                        for (int e = 0; e < 8; ++e) s[qt][e >> 2][e & 3] = __builtin_fmaf(s[qt][e >> 2][e & 3], sc, bv[e]);
+                    }
                     sx = 1.f, bu = 0.f;
                 }
             }
-            float m = max3(max3(s[0][0], s[0][1], s[0][2]), max3(s[0][3], s[1][0], s[1][1]), max3(s[1][2], s[1][3], s[1][3]));
-            if constexpr (EXT == kBias) m = __builtin_fmaf(m, sx, bu);
-            if (__any(m > limit)) {
-                m = fmaxf(mx, rows_max(m));
-                const float al = exp2_fast(EXT == kBias ? mx - m : (mx - m) * sc);
-                sum *= al;
+            F pf[QT];
 #pragma unroll
-                for (int dt = 0; dt < D / 16; ++dt) acc[dt] *= al;
-                mx = m;
-                limit = m == kNoMax ? kNoMax : m + lag;
-            }
-            const float nm = EXT == kBias ? bu - mx : -mx * sc;
+            for (int qt = 0; qt < QT; ++qt) {
+                floatx4(&x)[2] = s[qt];
+                float m = max3(max3(x[0][0], x[0][1], x[0][2]), max3(x[0][3], x[1][0], x[1][1]), max3(x[1][2], x[1][3], x[1][3]));
+                if constexpr (EXT == kBias) m = __builtin_fmaf(m, sx, bu);
+                if (__any(m > limit[qt])) {
+                    m = fmaxf(mx[qt], rows_max(m));
+                    const float al = exp2_fast(EXT == kBias ? mx[qt] - m : (mx[qt] - m) * sc);
+                    sum[qt] *= al;
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[kt][e] = exp2_fast(__builtin_fmaf(s[kt][e], sx, nm));
-                    sum += s[kt][e];
+                    for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] *= al;
+                    mx[qt] = m;
+                    limit[qt] = m == kNoMax ? kNoMax : m + lag;
                 }
-            const F pf = frag_from_acc<T>(s[0], s[1]);
+                const float nm = EXT == kBias ? bu - mx[qt] : -mx[qt] * sc;
 #pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) acc[dt] = mma(ld_red(sV, G::LV, 16 * dt, hf, g, r), pf, acc[dt]);
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[kt][e] = exp2_fast(__builtin_fmaf(x[kt][e], sx, nm));
+                        sum[qt] += x[kt][e];
+                    }
+                pf[qt] = frag_from_acc<T>(x[0], x[1]);
+            }
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) {
+                const F vf = ld_red(sV, G::LV, 16 * dt, hf, g, r);
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt) acc[qt][dt] = mma(vf, pf[qt], acc[qt][dt]);
+            }
         }
     }
 
-    const int i = a0 + r;
-    const float l = rows_sum(sum), top = EXT == kBias ? mx : mx * sc;
-    if (i >= min(G::BQ, a.L - q0)) return;
-    const bool real = i < nq && (EXT != kBias || l > 0.f);  // a bias of minus infinity can leave a row without a key
-    if (a.nsplit == 1) {
-        const float inv = real ? 1.f / l : 0.f;
 #pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) st4(out + (size_t)i * D + 16 * dt + 4 * g, real ? acc[dt] * inv : zero4());
-        if (a.lse && g == 0) a.lse[row0 + i] = real ? (top + __log2f(l)) * kLn2 : -INFINITY;
-    } else {
-        const size_t at = (size_t)part * a.B * a.H * a.L + row0 + i;
+    for (int qt = 0; qt < QT; ++qt) {
+        const int i = a0 + 16 * qt + r;
+        const float l = rows_sum(sum[qt]), top = EXT == kBias ? mx[qt] : mx[qt] * sc;
+        if (i >= min(G::BQ, a.L - q0)) continue;
+        const bool real = i < nq && (EXT != kBias || l > 0.f);  // a bias of minus infinity can leave a row without a key
+        if (a.nsplit == 1) {
+            const float inv = real ? 1.f / l : 0.f;
 #pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) st4f(a.part_o + at * D + 16 * dt + 4 * g, acc[dt]);
-        if (g == 0) {
-            a.part_ml[2 * at] = real ? top : kNoMax;
-            a.part_ml[2 * at + 1] = real ? l : 0.f;
+            for (int dt = 0; dt < D / 16; ++dt) st4(out + (size_t)i * D + 16 * dt + 4 * g, real ? acc[qt][dt] * inv : zero4());
+            if (a.lse && g == 0) a.lse[row0 + i] = real ? (top + __log2f(l)) * kLn2 : -INFINITY;
+        } else {
+            const size_t at = (size_t)part * a.B * a.H * a.L + row0 + i;
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) st4f(a.part_o + at * D + 16 * dt + 4 * g, acc[qt][dt]);
+            if (g == 0) {
+                a.part_ml[2 * at] = real ? top : kNoMax;
+                a.part_ml[2 * at + 1] = real ? l : 0.f;
+            }
         }
     }
 }
@@ -438,14 +471,19 @@ template <typename T, int D> __device__ __forceinline__ void join_rows(const Joi
     if (a.lse && lane == 0) a.lse[row] = some ? (top + __log2f(l)) * kLn2 : -INFINITY;
 }
 
+// waves: of 16 queries in a workgroup, 4 or 8.
 template <typename T, int D, bool RING, int EXT> hipError_t forward_r(int waves, const typename ExtArgs<EXT>::type& a, hipStream_t s)
 {
+    constexpr bool two = EXT != kPlain && sizeof(T) == 2 && D <= 64;  // two tiles of queries to a wave
+    const int threads = waves == 8 && !two ? 512 : 256;
     const long long pieces = a.ck_out ? (long long)a.B * a.Hkv * (a.S + a.W) * (D * (int)sizeof(T) / 16) : 0;
-    const dim3 grid((unsigned)(8 * a.per + (pieces + 64 * waves - 1) / (64 * waves)));
-    if (waves == 8)
-        hipLaunchKernelGGL((window_forward_kernel<T, D, 8, RING, EXT>), grid, dim3(512), 0, s, a);
+    const dim3 grid((unsigned)(8 * a.per + (pieces + threads - 1) / threads));
+    if (waves != 8)
+        hipLaunchKernelGGL((window_forward_kernel<T, D, 4, 1, RING, EXT>), grid, dim3(threads), 0, s, a);
+    else if constexpr (two)
+        hipLaunchKernelGGL((window_forward_kernel<T, D, 4, 2, RING, EXT>), grid, dim3(threads), 0, s, a);
     else
-        hipLaunchKernelGGL((window_forward_kernel<T, D, 4, RING, EXT>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((window_forward_kernel<T, D, 8, 1, RING, EXT>), grid, dim3(threads), 0, s, a);
     return hipGetLastError();
 }
 
