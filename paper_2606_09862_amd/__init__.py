@@ -152,7 +152,7 @@ def lib():
             getattr(L, name).restype = ctypes.c_size_t
         L.bla_evict_supported.argtypes = [E]
         L.bla_evict_forward.argtypes = [E] + [_vp] * 12 + [ctypes.c_size_t, _vp]
-        L.bla_evict_select.argtypes = [E] + [_vp] * 12
+        L.bla_evict_select.argtypes = [E] + [_vp] * 13
         L.bla_evict_step.argtypes = [E] + [_vp] * 12 + [ctypes.c_size_t, _vp]
         for name in ("bla_evict_supported", "bla_evict_forward", "bla_evict_select", "bla_evict_step"):
             getattr(L, name).restype = ctypes.c_int
@@ -702,9 +702,8 @@ def bias_forward(q, k, v, bias, edges, window: int, sinks: int = 0, t0: int = 0,
     n, e = _bias_check(bias, edges, H, dev)
     ring = _past_check(B, Hkv, d, window, sinks, dt, dev, cache_k, cache_v, lengths, pos)
     o = _result(out, q, (B, H, L, d))
-    lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device) if want_lse else None
-    ck = torch.empty(ring, dtype=dt, device=q.device) if want_cache else None
-    cv = torch.empty(ring, dtype=dt, device=q.device) if want_cache else None
+    lse = q.new_empty((B, H, L), dtype=torch.float32) if want_lse else None
+    ck, cv = (q.new_empty(ring), q.new_empty(ring)) if want_cache else (None, None)
     keep, ws, m = _room(workspace, need, q)
     _call(lib().bla_bias_forward, "bla_bias_forward", dev, p, n, e, q.data_ptr(), k.data_ptr(), v.data_ptr(), bias.data_ptr(), _ptr(lengths),
           _ptr(pos), _ptr(cache_k), _ptr(cache_v), o.data_ptr(), _ptr(lse), _ptr(ck), _ptr(cv), ws, m)
@@ -821,9 +820,8 @@ def prefix_forward(q, k, v, prefix_k, prefix_v, window: int, sinks: int = 0, t0:
     _check_on(v, (B, Hkv, L, d), dt, "v", dev)
     ring = _past_check(B, Hkv, d, window, sinks, dt, dev, cache_k, cache_v, lengths, pos)
     o = _result(out, q, (B, H, L, d))
-    lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device) if want_lse else None
-    ck = torch.empty(ring, dtype=dt, device=q.device) if want_cache else None
-    cv = torch.empty(ring, dtype=dt, device=q.device) if want_cache else None
+    lse = q.new_empty((B, H, L), dtype=torch.float32) if want_lse else None
+    ck, cv = (q.new_empty(ring), q.new_empty(ring)) if want_cache else (None, None)
     keep, ws, n = _room(workspace, need, q)
     _call(lib().bla_prefix_forward, "bla_prefix_forward", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), prefix_k.data_ptr(),
           prefix_v.data_ptr(), _ptr(prefix_lengths), _ptr(lengths), _ptr(pos), _ptr(cache_k), _ptr(cache_v), o.data_ptr(), _ptr(lse), _ptr(ck),
@@ -901,8 +899,8 @@ def evict_forward(q, k, v, slots: int, cache_k=None, cache_v=None, score=None, t
     if pos is not None:
         _check_on(pos, (B,), torch.int64, "pos", dev)
     o = _result(out, q, (B, H, L, d))
-    lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device) if want_lse else None
-    after = torch.empty((B, Hkv, slots + L), dtype=torch.float32, device=q.device)
+    lse = q.new_empty((B, H, L), dtype=torch.float32) if want_lse else None
+    after = q.new_empty((B, Hkv, slots + L), dtype=torch.float32)
     keep, ws, n = _room(workspace, need, q)
     _call(lib().bla_evict_forward, "bla_evict_forward", dev, p, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(lengths), _ptr(pos), _ptr(cache_k),
           _ptr(cache_v), _ptr(score), o.data_ptr(), _ptr(lse), after.data_ptr(), ws, n)
@@ -929,7 +927,7 @@ def evict_select(k, v, score, slots: int, recent: int = 0, cache_k=None, cache_v
         _check_on(pos, (B,), torch.int64, "pos", dev)
     ck, cv = k.new_empty((B, Hkv, slots, d)), k.new_empty((B, Hkv, slots, d))
     kept = score.new_empty((B, Hkv, slots))
-    where = torch.empty((B, Hkv, slots), dtype=torch.int64, device=k.device)
+    where = k.new_empty((B, Hkv, slots), dtype=torch.int64)
     _call(lib().bla_evict_select, "bla_evict_select", dev, p, k.data_ptr(), v.data_ptr(), score.data_ptr(), _ptr(lengths), _ptr(pos), _ptr(cache_k),
           _ptr(cache_v), _ptr(at), ck.data_ptr(), cv.data_ptr(), kept.data_ptr(), where.data_ptr())
     return ck, cv, kept, where

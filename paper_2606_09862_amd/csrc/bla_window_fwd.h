@@ -474,7 +474,7 @@ template <typename T, int D> __device__ __forceinline__ void join_rows(const Joi
 // waves: of 16 queries in a workgroup, 4 or 8.
 template <typename T, int D, bool RING, int EXT> hipError_t forward_r(int waves, const typename ExtArgs<EXT>::type& a, hipStream_t s)
 {
-    constexpr bool two = EXT != kPlain && sizeof(T) == 2 && D <= 64;  // two tiles of queries to a wave
+    constexpr bool two = EXT != kPlain;
     const int threads = waves == 8 && !two ? 512 : 256;
     const long long pieces = a.ck_out ? (long long)a.B * a.Hkv * (a.S + a.W) * (D * (int)sizeof(T) / 16) : 0;
     const dim3 grid((unsigned)(8 * a.per + (pieces + threads - 1) / threads));
