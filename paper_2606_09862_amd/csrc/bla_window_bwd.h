@@ -173,7 +173,7 @@ template <typename T, int D> struct BwdGeo {
 // EXACT = kDelta: delta alone is put right, for the key pass.
 constexpr int kRounded = 0, kDelta = 1, kExact = 2;
 template <typename T, int D, int EXACT, int EXT>
-__global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<EXT>::type a)
+__global__ void __launch_bounds__(256, EXT == kBias && EXACT == kDelta && D == 64 ? 3 : 1) window_bwd_q_kernel(typename ExtBwdArgs<EXT>::type a)
 {
     typedef BwdGeo<T, D> G;
     typedef typename Frag<T>::type F;
