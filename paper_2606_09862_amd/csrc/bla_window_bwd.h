@@ -169,11 +169,8 @@ template <typename T, int D> struct BwdGeo {
 // EXACT: delta is formed from outputs that were rounded to bf16, which adds 2^-9 |dO| |o| or so to each dP - delta.  That is lost among dS's own
 // rounding where many keys share a row, and as large as it where few do.  The sum of the dS of a row is what delta is off by (the exact
 // ones sum to zero), so the row's dq is put right by that sum times sum_j P_j k_j, a third product, and delta goes on to the key pass without the error.
-//
-// EXACT = kDelta: delta alone is put right, for the key pass.
-constexpr int kRounded = 0, kDelta = 1, kExact = 2;
-template <typename T, int D, int EXACT, int EXT>
-__global__ void __launch_bounds__(256, EXT == kBias && EXACT == kDelta && D == 64 ? 3 : 1) window_bwd_q_kernel(typename ExtBwdArgs<EXT>::type a)
+template <typename T, int D, bool EXACT, int EXT>
+__global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<EXT>::type a)
 {
     typedef BwdGeo<T, D> G;
     typedef typename Frag<T>::type F;
@@ -258,13 +255,13 @@ __global__ void __launch_bounds__(256, EXT == kBias && EXACT == kDelta && D == 6
         lanes.table(a.spec, near, wave, 4, lane);
     }
     const int far = lo - ns;  // what a sink is further away than its index says
-    floatx4 acc[QT][D / 16], pk[EXACT == kExact ? QT : 1][D / 16];
+    floatx4 acc[QT][D / 16], pk[EXACT ? QT : 1][D / 16];
     float off[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         off[qt] = 0.f;
 #pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] = pk[EXACT == kExact ? qt : 0][dt] = zero4();
+        for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] = pk[EXACT ? qt : 0][dt] = zero4();
     }
 
     const int aend = min(a0 + 16 * QT, nq) - 1;
@@ -352,7 +349,7 @@ __global__ void __launch_bounds__(256, EXT == kBias && EXACT == kDelta && D == 6
                         for (int e = 0; e < 8; ++e) {
                             const bool seen = (unsigned)(j + 16 * (e >> 2) + (e & 3) - jlo) < (unsigned)a.W;
                             s[qt][e >> 2][e & 3] = seen ? s[qt][e >> 2][e & 3] : 0.f;
-                            if (EXACT == kExact) dp[qt][e >> 2][e & 3] = seen ? dp[qt][e >> 2][e & 3] : 0.f;
+                            if (EXACT) dp[qt][e >> 2][e & 3] = seen ? dp[qt][e >> 2][e & 3] : 0.f;
                         }
                     } else {
 #pragma unroll
@@ -360,7 +357,7 @@ __global__ void __launch_bounds__(256, EXT == kBias && EXACT == kDelta && D == 6
                             const int k = j + 16 * (e >> 2) + (e & 3);
                             const bool seen = (k <= jhi) & ((k >= jlo) | (k < sb));
                             s[qt][e >> 2][e & 3] = seen ? s[qt][e >> 2][e & 3] : 0.f;
-                            if (EXACT == kExact) dp[qt][e >> 2][e & 3] = seen ? dp[qt][e >> 2][e & 3] : 0.f;
+                            if (EXACT) dp[qt][e >> 2][e & 3] = seen ? dp[qt][e >> 2][e & 3] : 0.f;
                         }
                     }
                 }
@@ -369,8 +366,8 @@ __global__ void __launch_bounds__(256, EXT == kBias && EXACT == kDelta && D == 6
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
                 sf[qt] = frag_from_acc<T>(s[qt][0], s[qt][1]);
-                if (EXACT == kExact) pf[qt] = frag_from_acc<T>(dp[qt][0], dp[qt][1]);
                 if (EXACT) {
+                    pf[qt] = frag_from_acc<T>(dp[qt][0], dp[qt][1]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) off[qt] += s[qt][e >> 2][e & 3];
                 }
@@ -381,7 +378,7 @@ __global__ void __launch_bounds__(256, EXT == kBias && EXACT == kDelta && D == 6
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt) {
                     acc[qt][dt] = mma(kf, sf[qt], acc[qt][dt]);
-                    if (EXACT == kExact) pk[qt][dt] = mma(kf, pf[qt], pk[qt][dt]);
+                    if (EXACT) pk[qt][dt] = mma(kf, pf[qt], pk[qt][dt]);
                 }
             }
         }
@@ -391,9 +388,8 @@ __global__ void __launch_bounds__(256, EXT == kBias && EXACT == kDelta && D == 6
         const int i = a0 + 16 * qt + r;
         if (EXACT) {
             off[qt] = rows_sum(off[qt]);
-            if (EXACT == kExact)
 #pragma unroll
-                for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] -= off[qt] * pk[EXACT == kExact ? qt : 0][dt];
+            for (int dt = 0; dt < D / 16; ++dt) acc[qt][dt] -= off[qt] * pk[EXACT ? qt : 0][dt];
             if (g == 0 && i < nq) a.delta[row0 + i] = delta[qt] + off[qt];
         }
         if (i >= min(G::NB, a.L - q0)) continue;
@@ -842,11 +838,12 @@ constexpr int kExactKeys = 64;
 template <typename T, int D, int EXT> hipError_t backward_d(const typename ExtBwdArgs<EXT>::type& a, hipStream_t s)
 {
     typedef BwdGeo<T, D> G;
-    constexpr bool rounds = sizeof(T) == 2;  // the bias's gradient takes a delta that is not rounded
-    if (std::min((long long)a.W + a.S, (long long)a.L) <= kExactKeys)
-        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, rounds ? kExact : kRounded, EXT>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
+    // The bias's gradient is float32 and takes a delta that is not rounded.  (Putting only delta right for it in long rows, without the third product, took the
+    // query pass of bla_bias_backward from 188 to 146 us but left dq an error of 0.0026 where this has 0.0024 and one rounding of dq 0.0017.)
+    if (EXT == kBias || std::min((long long)a.W + a.S, (long long)a.L) <= kExactKeys)
+        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, sizeof(T) == 2, EXT>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
     else
-        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, rounds && EXT == kBias ? kDelta : kRounded, EXT>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
+        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, EXT == kBias && sizeof(T) == 2, EXT>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
     hipLaunchKernelGGL((window_bwd_k_kernel<T, D, EXT>), dim3((unsigned)(8 * a.k_per) + a.s_units), dim3(G::NT), 0, s, a);
     if (a.ns > 0) {
         const long long n = (long long)a.B * a.Hkv * a.ns * (2 * D / 4);
