@@ -7,7 +7,7 @@ namespace {
 template <typename T, int D> __global__ void __launch_bounds__(256) window_join_kernel(JoinArgs a) { join_rows<T, D>(a, blockIdx.x); }
 
 // More than 64 parts: a workgroup to a row.  A thread holds a part's maximum and sum, then groups of D / 4 threads take every so-maniest part's outputs,
-// four in flight, and are added up in order.
+// eight in flight, and are added up in order.
 constexpr int kWideParts = 256;
 template <typename T, int D> __global__ void __launch_bounds__(256) window_join_wide_kernel(JoinArgs a)
 {
@@ -37,12 +37,12 @@ template <typename T, int D> __global__ void __launch_bounds__(256) window_join_
     __syncthreads();
     l = red[1][0] + red[1][1] + red[1][2] + red[1][3];
     floatx4 o = zero4();
-    for (int s0 = pg; s0 < a.nsplit; s0 += 4 * PG) {
-        floatx4 v[4];
+    for (int s0 = pg; s0 < a.nsplit; s0 += 8 * PG) {
+        floatx4 v[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = ld4f(a.part_o + ((size_t)min(s0 + k * PG, a.nsplit - 1) * a.rows + row) * D + c);
+        for (int k = 0; k < 8; ++k) v[k] = ld4f(a.part_o + ((size_t)min(s0 + k * PG, a.nsplit - 1) * a.rows + row) * D + c);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 8; ++k) {
             const float x = s0 + k * PG < a.nsplit ? w[s0 + k * PG] : 0.f;
             o += x * (x != 0.f ? v[k] : zero4());
         }
