@@ -385,8 +385,8 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
  *   bias: device float32 [H, buckets]   edges: HOST int32 [buckets - 1], ascending (equal ones leave a bucket without a distance), >= 0
  * edges is read before the call returns.  Everything else is window attention's: parameters, rings, lengths, pos, workspaces
  * (bla_window_workspace_size, bla_window_step_workspace_size), errors and limits.  bucket counts above 64 and edges above 2^29 are
- * BLA_ERR_UNSUPPORTED.  A bias below -1e30 counts as minus infinity: its pairs have no weight.  A query that is left without a key gives zeros
- * (lse: minus infinity; gradients: zeros).  Larger biases than 1e30 and NaN are not supported.
+ * BLA_ERR_UNSUPPORTED.  A bias below -1e6 counts as minus infinity: its pairs have no weight, and its gradient is zero.  A query that is left without a
+ * key gives zeros (lse: minus infinity; gradients: zeros).  Biases above 1e6, NaN, and scores of 1e30 or more are not supported.
  */
 bla_status bla_bias_forward(const bla_window_params* p, int32_t buckets, const int32_t* edges, const void* q, const void* k,
                             const void* v, const float* bias, const int32_t* lengths, const int64_t* pos,
@@ -468,7 +468,8 @@ size_t bla_evict_workspace_size(const bla_evict_params* p);
 /*
  * L tokens of every row: each query sees all tokens of the cache and the call's up to its own.  cache_k, cache_v and score_in: all or none (NULL: nothing
  * before token 0 exists); they stay as they are.  lse as for bla_window_forward.  score_out [B, H_kv, slots + L] receives the scores of the cache's tokens
- * (entries 0 .. slots - 1) and of the call's (slots + t) after it, zeros where there is none.  The sums run in a fixed order.
+ * (entries 0 .. slots - 1) and of the call's (slots + t) after it, zeros where there is none; all of an idle row's go through.  The sums run in a
+ * fixed order.
  */
 bla_status bla_evict_forward(const bla_evict_params* p, const void* q, const void* k, const void* v, const int32_t* lengths,
                              const int64_t* pos, const void* cache_k, const void* cache_v, const float* score_in, void* o,

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 import os
 
 import torch
@@ -675,13 +676,13 @@ def bias_edges(buckets: int, max_distance: int) -> tuple:
 
 @functools.lru_cache(maxsize=256)
 def _edge_array(edges):
-    _int32("edges", *edges)
+    _int32("bla_bias", *edges)
     return (ctypes.c_int32 * max(len(edges), 1))(*edges)
 
 
 def _bias_check(bias, edges, H, dev):
     """(buckets, the edges' host array)."""
-    edges = tuple(edges)
+    edges = tuple(map(operator.index, edges))
     _check_on(bias, (H, len(edges) + 1), torch.float32, "bias", dev)
     return len(edges) + 1, _edge_array(edges)
 

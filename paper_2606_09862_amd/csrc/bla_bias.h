@@ -12,7 +12,9 @@ namespace bla {
 constexpr int kMaxBuckets = 64;
 constexpr int kNear = 1024;          // distances that have a table in LDS
 constexpr int kPad = 64;             // places before them, for pairs of later keys in a tile that the masks hide
-constexpr float kBiasNone = -1e30f;  // a bias below it counts as minus infinity (its pairs have no weight)
+// A bias below it counts as minus infinity: its pairs have no weight.  Past 2^20 or so a score's last bits are gone in float32, and the maximum that a kernel
+// forms from a tile's largest product would be off by more than its exponentials bear.
+constexpr float kBiasNone = -1e6f;
 
 struct BiasSpec {
     const float* bias;  // [H, buckets]

@@ -132,8 +132,9 @@ __global__ void __launch_bounds__(256) evict_sum_out_kernel(EvictSumArgs a)
     const int grp = a.H / a.Hkv, b = (int)(bh / a.Hkv), hk = (int)(bh % a.Hkv);
     int64_t pos;
     const int len = row_tokens(a.lengths, a.pos, a.t0, b, a.L, pos);
+    const bool idle = pos < 0 || pos > kMaxPos;  // such a row's cache stays as it is, its scores with it
     float x = 0.f;
-    if (e >= (size_t)a.slots || (a.ck && pos >= 0 && pos <= kMaxPos && (int64_t)e < pos)) {
+    if (e >= (size_t)a.slots || (a.ck && (idle || (int64_t)e < pos))) {
         if (len > 0 || e >= (size_t)a.slots)
             for (int h = 0; h < grp; ++h) x += a.part[((size_t)b * a.H + hk * grp + h) * n + e];
         if (e < (size_t)a.slots) x += a.score_in[bh * a.slots + e];

@@ -45,10 +45,10 @@ def row(q, k, v, first, window, sinks, scale, ring_k=None, ring_v=None, front_k=
     more = 0.0
     if bias is not None:
         bucket = bucket_of(gap.clamp(min=0), edges)
-        b = torch.where(bias < -1e30, -math.inf, bias.to(F64))[:, bucket]
+        b = torch.where(bias < -1e6, -math.inf, bias.to(F64))[:, bucket]  # such pairs have no weight
         z = z + b
         some = z[:, seen]
-        more = 4 * 2.0 ** -24 * float(bias[bias >= -1e30].abs().max() if (bias >= -1e30).any() else 0.0)
+        more = 4 * 2.0 ** -24 * float(bias[bias >= -1e6].abs().max() if (bias >= -1e6).any() else 0.0)
         more += 4 * 2.0 ** -24 * float(some[torch.isfinite(some)].abs().max() if torch.isfinite(some).any() else 0.0)
     z = z.masked_fill(~seen, -math.inf)
     top = z.amax(-1, keepdim=True)

@@ -105,6 +105,17 @@ def hidden(H, n, seed=3):
     return bias
 
 
+@pytest.mark.parametrize("hide", [-1.1e6, -1e10, -1e20, -3e38, -math.inf])
+def test_mask_values(hide):
+    """Far distances hidden by what programs use for it: the keys that come first in a row's walk have no weight, nothing overflows."""
+    bias = normal(4, 2, 16, dtype=F32)
+    bias[:, 12:] = hide
+    bias[1, 3] = hide
+    check_forward(1, 2, 1, 400, 64, 400, 0, BF, LOG, bias=bias)
+    check_forward(1, 2, 1, 2, 64, 3000, 0, BF, LOG, pos=[2500], cached=True, bias=bias)
+    check_backward(1, 2, 1, 200, 64, 200, 0, BF, LOG, bias=bias)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_hidden_distances(dtype):
     check_forward(2, 3, 3, 200, 64, 150, 3, dtype, LOG, bias=hidden(3, 16))

@@ -46,7 +46,7 @@ def check_forward(B, H, Hkv, L, d, slots, dtype, lengths=None, pos=None, cached=
     o, lse, after = bla.evict_forward(gq, gk, gv, slots, cache_k=gck, cache_v=gcv, score=gs, t0=t0, scale=scale, lengths=gl, pos=gp, want_lse=True)
     o2, none, after2 = bla.evict_forward(gq, gk, gv, slots, cache_k=gck, cache_v=gcv, score=gs, t0=t0, scale=scale, lengths=gl, pos=gp)
     torch.cuda.synchronize()
-    assert none is None and torch.equal(o, o2) and torch.equal(after, after2)
+    assert none is None and torch.equal(o, o2) and torch.equal(after.nan_to_num(-7.0), after2.nan_to_num(-7.0))
     o, lse, after = o.cpu(), lse.cpu(), after.cpu()
     sc = 1 / math.sqrt(d) if scale is None else scale
     u = unit(dtype)
@@ -55,7 +55,11 @@ def check_forward(B, H, Hkv, L, d, slots, dtype, lengths=None, pos=None, cached=
         n = 0 if p < 0 else L if lengths is None else min(max(lengths[b], 0), L)
         m = min(max(p, 0), slots) if cached else 0
         assert not o[b, :, n:].any() and torch.equal(lse[b, :, n:], torch.full_like(lse[b, :, n:], -math.inf))
-        assert not after[b, :, m:slots].any() and not after[b, :, slots + n:].any()
+        assert not after[b, :, slots + n:].any()
+        if p < 0 and cached:  # an idle row's scores go through
+            assert torch.equal(after[b, :, :slots].nan_to_num(-7.0), sc_in[b].nan_to_num(-7.0))
+            continue
+        assert not after[b, :, m:slots].any()
         if not n:
             assert m == 0 or torch.equal(after[b, :, :m], sc_in[b, :, :m])
             continue
@@ -272,6 +276,37 @@ def test_step_equal_and_special_scores():
         g = torch.Generator().manual_seed(len(pick))
         s = torch.tensor(pick)[torch.randint(0, len(pick), (4, 2, 50), generator=g)]
         check_step(4, 4, 2, 32, 50, 7, [50, 51, 70, 500], F32, score=s)
+
+
+@pytest.mark.parametrize("dtype,heads,slots", [(BF, 8, 1000), (F32, 8, 1024), (F32, 9, 1000)])
+def test_step_scores_in_lds(dtype, heads, slots):
+    """Wide heads whose scores fill what LDS has for them, and one head more than that: 512 rows, of which a few have tokens."""
+    bla = _bla()
+    B, d = 512, 128
+    _say(f"evict step 512x{heads}/1x128 slots {slots} {dtype}")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rand = lambda *s: torch.randn(*s, device="cuda", generator=g).to(dtype)  # noqa: E731
+    q, k, v, ck, cv = rand(B, heads, d), rand(B, 1, d), rand(B, 1, d), rand(B, 1, slots, d), rand(B, 1, slots, d)
+    score, at = torch.rand(B, 1, slots, device="cuda", generator=g), torch.arange(slots, device="cuda").expand(B, 1, slots).contiguous()
+    pos = torch.full((B,), -1, dtype=torch.int64)
+    some = {3: 10, 77: slots - 1, 300: slots, 511: slots + 5}
+    for b, p in some.items():
+        pos[b] = p
+    before = [x.cpu() for x in (ck, cv, score)]
+    o, score, at = bla.evict_step(q, k, v, ck, cv, score, at, 4, pos=pos.cuda())
+    u = unit(dtype)
+    for b, p in some.items():
+        old_k, old_v, old = (x[b] for x in before)
+        mine = p if p < slots else int(old[0, :min(slots, p - 4)].argmin())
+        n = min(p + 1, slots)
+        rest = torch.tensor([i for i in range(n) if i != mine])
+        ref = row(q[b, :, None].cpu(), k[b, :, None].cpu(), v[b, :, None].cpu(), 0, ENDLESS, 0, 1 / math.sqrt(d), front_k=old_k[:, rest], front_v=old_v[:, rest])
+        close(o[b, :, None].cpu(), ref["o"], (u + ref["r"]) * ref["spread"] + u * ref["o"].abs(), f"o[{b}]")
+        was = torch.cat([old[0, rest].to(F64), torch.zeros(1, dtype=F64)])[None]
+        got = torch.cat([score[b, 0, rest.cuda()], score[b, 0, mine:mine + 1]])[None].cpu()
+        close(got, was + ref["seen_by"], score_bound(ref, 1, heads, was), f"score[{b}]")
+        assert int(at[b, 0, mine]) == p
+    assert not o[torch.tensor([b for b in range(B) if b not in some])].any()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
