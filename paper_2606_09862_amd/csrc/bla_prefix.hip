@@ -4,7 +4,7 @@
 
 namespace bla {
 hipError_t launch_prefix_forward(int bf16_io, int D, int waves, const PrefixArgs& a, hipStream_t s);
-hipError_t launch_prefix_step(int bf16_io, int D, const PrefixStepArgs& a, bool few, hipStream_t s);
+hipError_t launch_prefix_step(int bf16_io, int D, const PrefixStepArgs& a, PrefixForm form, hipStream_t s);
 }  // namespace bla
 
 using namespace bla;
@@ -24,9 +24,9 @@ bla_status check_prefix(const bla_prefix_params* p, bool step)
 
 // The step's: the prefix in parts that fill the device with the blocks of its queries, of at least a tile for each group of waves, beside the rings' parts.  Few
 // queries go in blocks of 16, whose four waves take 32 tokens each.
-constexpr int kFewQueries = 32, kMaxPrefixParts = 192;
+constexpr int kFewQueries = 32, kMaxPrefixParts = 192, kShortBlocks = 48;
 struct PrefixStepPlan : StepPlan {
-    bool few;
+    bool few, both;  // both: no parts
     int npart, nqb, threads;
     long long units;
 };
@@ -39,6 +39,11 @@ PrefixStepPlan prefix_step_plan(const bla_prefix_params* p)
     const long long rows = w->H_kv > 0 && p->G > 0 ? (long long)(w->B / p->G) * (w->H / w->H_kv) : 0;
     const PrefixShape shape = prefix_shape(w->io_dtype == BLA_BF16, w->d);
     s.few = rows <= kFewQueries;
+    s.both = s.few && (p->P + 31) / 32 + ((long long)w->window + w->sinks + 31) / 32 <= kShortBlocks;
+    if (s.both) {
+        s.npart = s.nqb = 0, s.nsplit = 1, s.units = 0, s.threads = 512, s.total = 0;
+        return s;
+    }
     s.threads = s.few ? 256 : shape.threads;
     const int block = s.few ? 16 : shape.block, least = s.few ? 128 : kWinKeys * shape.groups;
     s.nqb = (int)((rows + block - 1) / block);
@@ -124,12 +129,13 @@ bla_status bla_prefix_step(const bla_prefix_params* p, const void* q, const void
     if ((st = step_args(a, w, sp, q, k, v, pos, cache_k, cache_v, o, extra, workspace, sp.total, workspace_bytes)) != BLA_OK) return st;
     a.pk = prefix_k, a.pv = prefix_v, a.plen = prefix_lengths, a.P = p->P, a.G = p->G;
     a.npart = sp.npart, a.nqb = sp.nqb, a.units = sp.units, a.per = (sp.units + 7) / 8;
+    hipStream_t s = (hipStream_t)stream;
+    if (sp.both) return launch_prefix_step(w->io_dtype == BLA_BF16, w->d, a, kFormBoth, s) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
     const size_t rows = (size_t)w->B * w->H;
     const int parts = sp.npart + sp.nsplit;
     a.pre_o = (float*)workspace, a.pre_ml = a.pre_o + (size_t)parts * rows * w->d;
     a.part_o = a.pre_o + (size_t)sp.npart * rows * w->d, a.part_ml = a.pre_ml + (size_t)sp.npart * rows * 2;
-    hipStream_t s = (hipStream_t)stream;
-    if (launch_prefix_step(w->io_dtype == BLA_BF16, w->d, a, sp.few, s) != hipSuccess) return BLA_ERR_HIP;
+    if (launch_prefix_step(w->io_dtype == BLA_BF16, w->d, a, sp.few ? kFormFew : kFormTiles, s) != hipSuccess) return BLA_ERR_HIP;
     const JoinArgs j = {a.pre_o, a.pre_ml, o, nullptr, (long long)rows, parts};
     return launch_window_join(w->io_dtype == BLA_BF16, w->d, j, s) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }

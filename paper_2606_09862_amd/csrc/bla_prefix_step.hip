@@ -9,7 +9,9 @@ namespace {
 // tile, as in window_forward_kernel; each fragment read from LDS serves QT products.  KG groups of four waves take every KG-th tile, wave w of a group the
 // 16 QT queries from 16 QT w on, and are joined through LDS, so that a workgroup fills half a compute unit and leaves one part for as many waves.  The parts are
 // joined with the ring's by window_join_kernel.
-// Few queries (kFewQueries) leave most of such a workgroup idle: they go as the heads of a ring do, in window_step_part.
+// Few queries (kFewQueries) leave most of such a workgroup idle: they go as the heads of a ring do, in window_step_part.  Where prefix and ring are short as well
+// (kShortBlocks), a workgroup of eight waves takes both for its key head's heads of one row: one launch, without parts, though each row reads the
+// prefix for itself (3 rows behind 777 tokens: 14.3 us a call with parts, XX without, most of it on the host).
 template <typename T, int D> struct PrefixGeo {
     static constexpr int NT = 256, PE = 16 / (int)sizeof(T), CH = D / PE, RPP = NT / CH, NP = (64 + RPP - 1) / RPP;  // of a group
     static constexpr int QT = 2, NB = 64 * QT;
@@ -218,10 +220,21 @@ template <typename T, int D> __global__ void __launch_bounds__(256) prefix_few_k
     window_step_part<T, D, kPrefix>(a, blockIdx.x - 8 * (unsigned)a.per, raw, sml);
 }
 
-template <typename T, int D> hipError_t prefix_d(const PrefixStepArgs& a, bool few, hipStream_t s)
+template <typename T, int D> __global__ void __launch_bounds__(512) prefix_both_kernel(PrefixStepArgs a)
 {
+    __shared__ __attribute__((aligned(16))) char raw[StepGeo<T, D, 8>::LDS];
+    __shared__ float sml[2][8][16];
+    window_step_part<T, D, kBoth, 8>(a, blockIdx.x, raw, sml);
+}
+
+template <typename T, int D> hipError_t prefix_d(const PrefixStepArgs& a, PrefixForm form, hipStream_t s)
+{
+    if (form == kFormBoth) {
+        hipLaunchKernelGGL((prefix_both_kernel<T, D>), dim3((unsigned)((long long)a.B * a.Hkv * a.ngrp)), dim3(512), 0, s, a);
+        return hipGetLastError();
+    }
     const dim3 grid((unsigned)(8 * a.per + (long long)a.B * a.Hkv * a.ngrp * a.nsplit));
-    if (few)
+    if (form == kFormFew)
         hipLaunchKernelGGL((prefix_few_kernel<T, D>), grid, dim3(256), 0, s, a);
     else
         hipLaunchKernelGGL((prefix_step_kernel<T, D>), grid, dim3(64 * PrefixGeo<T, D>::NW), 0, s, a);
@@ -239,9 +252,9 @@ PrefixShape prefix_shape(int bf16_io, int D)
     return D == 32 ? shape_d<float, 32>() : D == 64 ? shape_d<float, 64>() : shape_d<float, 128>();
 }
 
-hipError_t launch_prefix_step(int bf16_io, int D, const PrefixStepArgs& a, bool few, hipStream_t s)
+hipError_t launch_prefix_step(int bf16_io, int D, const PrefixStepArgs& a, PrefixForm form, hipStream_t s)
 {
-#define BLA_CALL(T, DD) prefix_d<T, DD>(a, few, s)
+#define BLA_CALL(T, DD) prefix_d<T, DD>(a, form, s)
     BLA_BY_TYPE(BLA_CALL)
 #undef BLA_CALL
 }

@@ -7,7 +7,7 @@
 
 namespace bla {
 
-constexpr int kPlain = 0, kBias = 1, kPrefix = 2, kEvict = 3, kFew = 4;  // what a call adds to window attention
+constexpr int kPlain = 0, kBias = 1, kPrefix = 2, kEvict = 3, kFew = 4, kBoth = 5;  // what a call adds to window attention
 
 struct BiasArgs : WindowArgs {
     BiasSpec spec;

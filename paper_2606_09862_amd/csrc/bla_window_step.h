@@ -22,6 +22,8 @@ struct PrefixShape {
     int block, groups, threads, fill;
 };
 PrefixShape prefix_shape(int bf16_io, int D);
+// How a step takes the prefix: in tiles, as a ring's heads do, or so together with the ring.
+enum PrefixForm { kFormTiles, kFormFew, kFormBoth };
 // Slots without order (W of them, S = 0); the scores in the base-2 domain go out for the sums of the weights.
 struct EvictStepArgs : WindowStepArgs {
     const float* score_in;     // [B, Hkv, W]
@@ -39,6 +41,7 @@ template <int EXT> struct ExtStepArgs { typedef WindowStepArgs type; };
 template <> struct ExtStepArgs<kBias> { typedef BiasStepArgs type; };
 template <> struct ExtStepArgs<kPrefix> { typedef PrefixStepArgs type; };
 template <> struct ExtStepArgs<kFew> { typedef PrefixStepArgs type; };
+template <> struct ExtStepArgs<kBoth> { typedef PrefixStepArgs type; };
 template <> struct ExtStepArgs<kEvict> { typedef EvictStepArgs type; };
 
 // A score's place in the order of scores: NaN above every number, the two zeros as one.
@@ -114,6 +117,7 @@ template <typename T, int D, int NW = 4> struct StepGeo {
 // as many distances in a row, but where they hold sinks or the ring's seam.  EXT = kPrefix: the results are parts, to be joined with the prefix's.
 // EXT = kEvict: the token's slot is found first, and the scores are kept until the softmax's sum is known.
 // EXT = kFew: not the ring but a part of the prefix, for 16 of the few queries that share it (heads of one row or of several).
+// EXT = kBoth: the blocks of the prefix, then the ring's, for the heads of one row.
 template <typename T, int D, int EXT, int NW = 4>
 __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>::type& a, unsigned u, char* raw, float (&sml)[2][NW][16])
 {
@@ -194,7 +198,16 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
             *(intx4*)(cv + (size_t)mine * D + ch * PE) = *(const intx4*)(vn + ch * PE);
     }
 
-    const int nblk = (n + 31) / 32, each = (nblk + (int)nsplit - 1) / (int)nsplit;
+    int np = 0, pblk = 0;  // kBoth: the prefix's tokens, and their blocks ahead of the ring's
+    const T *pk = nullptr, *pv = nullptr;
+    if constexpr (EXT == kBoth) {
+        const int gx = b / (a.B / a.G);
+        np = a.plen ? min(max(a.plen[gx], 0), a.P) : a.P;
+        pblk = (np + 31) / 32;
+        const size_t at = ((size_t)gx * a.Hkv + hk) * a.P * D;
+        pk = (const T*)a.pk + at, pv = (const T*)a.pv + at;
+    }
+    const int nblk = pblk + (n + 31) / 32, each = (nblk + (int)nsplit - 1) / (int)nsplit;
     const int bb = part * each, be = min(nblk, bb + each);
 
     F qf[D / 32];
@@ -228,17 +241,19 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
     F kf[2][D / 32];
     intx4 vr[NV];
     auto load = [&](int blk) {
+        const bool pre = EXT == kBoth && blk < pblk;
+        const int first = pre ? 32 * blk : 32 * (blk - pblk), last = (pre ? np : n) - 1;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
-            const int i = min(32 * blk + 16 * kt + r, n - 1);
-            const T* row = i == mine ? kn : ck + (size_t)i * D;
+            const int i = min(first + 16 * kt + r, last);
+            const T* row = pre ? pk + (size_t)i * D : i == mine ? kn : ck + (size_t)i * D;
 #pragma unroll
             for (int kb = 0; kb < D / 32; ++kb) kf[kt][kb] = ld_nat(row, kb, g);
         }
 #pragma unroll
         for (int x = 0; x < NV; ++x) {
-            const int i = min(32 * blk + (x * 64 + lane) / CH, n - 1);
-            const T* row = i == mine ? vn : cv + (size_t)i * D;
+            const int i = min(first + (x * 64 + lane) / CH, last);
+            const T* row = pre ? pv + (size_t)i * D : i == mine ? vn : cv + (size_t)i * D;
             vr[x] = *(const intx4*)(row + ((x * 64 + lane) % CH) * PE);
         }
     };
@@ -293,11 +308,12 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = __builtin_fmaf(s[e >> 2][e & 3], sc, bv[e]);
         }
-        if (32 * blk + 32 > n) {
+        const int left = EXT == kBoth && blk < pblk ? np - 32 * blk : n - 32 * (blk - pblk);  // tokens from here on
+        if (left < 32) {
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[kt][e] = 32 * blk + 16 * kt + 4 * g + e < n ? s[kt][e] : -INFINITY;
+                for (int e = 0; e < 4; ++e) s[kt][e] = 16 * kt + 4 * g + e < left ? s[kt][e] : -INFINITY;
         }
         if constexpr (EXT == kEvict) {
             if (r < nh) {

@@ -148,10 +148,12 @@ def test_prefix_refusals(lib):  # noqa: F811
     for out in (7, 8, 9):
         for i in (0, 1, 2, 3, 4, 5, 6):
             assert S(put=[(i, 0x9000000000), (out, 0x9000000000)]) == INVALID
-    need = lib.bla_prefix_step_workspace_size(ctypes.byref(prefix()))
-    assert need > 0 and S(tail=(WS, need - 1)) == S(tail=(None, 0)) == WORKSPACE
+    size = lambda **kw: lib.bla_prefix_step_workspace_size(ctypes.byref(prefix(**kw)))  # noqa: E731
+    need = size(P=3000)
+    assert need > 0 and S(prefix(P=3000), tail=(WS, need - 1)) == S(prefix(P=3000), tail=(None, 0)) == WORKSPACE
+    assert size() == size(P=0) == 0 and size(B=64) > 0        # few queries, a short prefix and ring: one launch without parts
     for L in (-1, 0, 7, (1 << 31) - 1):                       # the step ignores L
-        assert lib.bla_prefix_step_workspace_size(ctypes.byref(prefix(L=L))) == need and S(prefix(L=L), drop=[0]) == INVALID
+        assert size(P=3000, L=L) == need and S(prefix(L=L), drop=[0]) == INVALID
 
 
 @pytest.mark.parametrize("kw,expect", [
