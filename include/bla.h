@@ -384,7 +384,7 @@ bla_status bla_window_backward(const bla_window_params* p, const void* q, const 
  * so bucket 0 holds the distances below edges[0], bucket u those from edges[u - 1] to edges[u] - 1, the last those from the last edge on.
  *   bias: device float32 [H, buckets]   edges: HOST int32 [buckets - 1], ascending (equal ones leave a bucket without a distance), >= 0
  * edges is read before the call returns.  Everything else is window attention's: parameters, rings, lengths, pos, workspaces
- * (bla_window_workspace_size, bla_window_step_workspace_size), errors and limits.  bucket counts above 64 and edges above 2^29 are
+ * (bla_window_workspace_size, bla_bias_step_workspace_size), errors and limits.  bucket counts above 64 and edges above 2^29 are
  * BLA_ERR_UNSUPPORTED.  A bias below -1e6 counts as minus infinity: its pairs have no weight, and its gradient is zero.  A query that is left without a
  * key gives zeros (lse: minus infinity; gradients: zeros).  Biases above 1e6, NaN, and scores of 1e30 or more are not supported.
  */
@@ -394,6 +394,7 @@ bla_status bla_bias_forward(const bla_window_params* p, int32_t buckets, const i
                             void* cache_v_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* One token for every row: the rings take its key and value in place. */
+size_t bla_bias_step_workspace_size(const bla_window_params* p);
 bla_status bla_bias_step(const bla_window_params* p, int32_t buckets, const int32_t* edges, const void* q, const void* k,
                          const void* v, const float* bias, const int64_t* pos, void* cache_k, void* cache_v, void* o,
                          void* workspace, size_t workspace_bytes, void* stream);

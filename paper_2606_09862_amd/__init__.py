@@ -135,6 +135,8 @@ def lib():
         L.bla_bias_forward.argtypes = [W, i32, ip] + [_vp] * 13 + [ctypes.c_size_t, _vp]
         L.bla_bias_step.argtypes = [W, i32, ip] + [_vp] * 9 + [ctypes.c_size_t, _vp]
         L.bla_bias_backward.argtypes = [W, i32, ip] + [_vp] * 13 + [ctypes.c_size_t, _vp]
+        L.bla_bias_step_workspace_size.argtypes = [W]
+        L.bla_bias_step_workspace_size.restype = ctypes.c_size_t
         L.bla_bias_backward_workspace_size.argtypes = [W, i32]
         L.bla_bias_backward_workspace_size.restype = ctypes.c_size_t
         for name in ("bla_bias_forward", "bla_bias_step", "bla_bias_backward"):
@@ -745,7 +747,7 @@ def bias_step(q, k, v, bias, edges, window: int, sinks: int, cache_k, cache_v, p
     """bla_bias_step: window_step whose scores carry the bias of bias_forward."""
     B, H, d = q.shape
     Hkv, dev = k.shape[1], q.get_device()
-    p, need = _window_params("bla_window_step", B, H, Hkv, 1, d, window, sinks, t0, scale, q.dtype)
+    p, need = _window_params("bla_bias_step", B, H, Hkv, 1, d, window, sinks, t0, scale, q.dtype)
     _step_check(q, k, v, window, sinks, cache_k, cache_v, pos)
     n, e = _bias_check(bias, edges, H, dev)
     o = _result(out, q, (B, H, d))

@@ -5,7 +5,7 @@
 
 namespace bla {
 hipError_t launch_bias_forward(int bf16_io, int D, int waves, const BiasArgs& a, hipStream_t s);
-hipError_t launch_bias_step(int bf16_io, int D, const BiasStepArgs& a, hipStream_t s);
+hipError_t launch_bias_step(int bf16_io, int D, const BiasStepArgs& a, int waves, hipStream_t s);
 hipError_t launch_bias_backward(int bf16_io, int D, const BiasBwdArgs& a, hipStream_t s);
 }  // namespace bla
 
@@ -74,6 +74,13 @@ bla_status bla_bias_forward(const bla_window_params* p, int32_t buckets, const i
     return join_parts(p, p->L, f.nsplit, a.part_o, a.part_ml, o, lse, s);
 }
 
+size_t bla_bias_step_workspace_size(const bla_window_params* p)
+{
+    if (check(p, true) != BLA_OK) return 0;
+    const ShortStepPlan s = short_step_plan(p);
+    return fits(p, s) ? s.total : 0;
+}
+
 bla_status bla_bias_step(const bla_window_params* p, int32_t buckets, const int32_t* edges, const void* q, const void* k, const void* v,
                          const float* bias, const int64_t* pos, void* cache_k, void* cache_v, void* o, void* workspace,
                          size_t workspace_bytes, void* stream)
@@ -82,7 +89,7 @@ bla_status bla_bias_step(const bla_window_params* p, int32_t buckets, const int3
     if (st == BLA_OK) st = check_buckets(buckets, edges);
     if (st != BLA_OK) return st;
     if (p->B == 0 || p->H == 0) return empty(p, true);
-    const StepPlan sp = step_plan(p);
+    const ShortStepPlan sp = short_step_plan(p);
     if (!fits(p, sp)) return BLA_ERR_UNSUPPORTED;
     if (!bias || !aligned(bias, 4)) return BLA_ERR_INVALID_ARG;
     BiasStepArgs a = {};
@@ -90,7 +97,7 @@ bla_status bla_bias_step(const bla_window_params* p, int32_t buckets, const int3
     if ((st = step_args(a, p, sp, q, k, v, pos, cache_k, cache_v, o, extra, workspace, sp.total, workspace_bytes)) != BLA_OK) return st;
     set_spec(a.spec, bias, buckets, edges);
     hipStream_t s = (hipStream_t)stream;
-    if (launch_bias_step(p->io_dtype == BLA_BF16, p->d, a, s) != hipSuccess) return BLA_ERR_HIP;
+    if (launch_bias_step(p->io_dtype == BLA_BF16, p->d, a, sp.waves, s) != hipSuccess) return BLA_ERR_HIP;
     return join_parts(p, 1, sp.nsplit, a.part_o, a.part_ml, o, nullptr, s);
 }
 

@@ -3,9 +3,9 @@
 
 namespace bla {
 
-hipError_t launch_bias_step(int bf16_io, int D, const BiasStepArgs& a, hipStream_t s)
+hipError_t launch_bias_step(int bf16_io, int D, const BiasStepArgs& a, int waves, hipStream_t s)
 {
-#define BLA_CALL(T, DD) step_d<T, DD, kBias>(a, s)
+#define BLA_CALL(T, DD) step_d<T, DD, kBias>(a, waves, s)
     BLA_BY_TYPE(BLA_CALL)
 #undef BLA_CALL
 }

@@ -37,7 +37,10 @@ struct EvictSelectArgs {
 
 hipError_t launch_evict_sum(int bf16_io, int D, const EvictSumArgs& a, hipStream_t s);
 hipError_t launch_evict_select(const EvictSelectArgs& a, hipStream_t s);
-hipError_t launch_evict_step(int bf16_io, int D, const EvictStepArgs& a, hipStream_t s);
+hipError_t launch_evict_step(int bf16_io, int D, const EvictStepArgs& a, int waves, hipStream_t s);
+// Bytes of scores that a workgroup of the step keeps in LDS: four such workgroups fill a compute unit's registers at d = 64.  The tiles of eight waves take 133 KiB of
+// the 160 in float32 at d = 128.
+constexpr int score_lds(int waves, bool bf16_io, int D) { return waves == 8 && !bf16_io && D == 128 ? 16 * 1024 : 32 * 1024; }
 constexpr int kEvictKeys = 128;    // keys of a workgroup of the sums
 constexpr int kSliceSlots = 4096;  // most slots of a slice of the selection
 

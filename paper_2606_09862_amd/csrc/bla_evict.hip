@@ -57,8 +57,7 @@ bool fits(const bla_evict_params* p, const EvictPlan& e)
 }
 
 // Step: window attention's split; the sums are formed by the same workgroups where each has all slots and heads of its key head.
-constexpr long long kScoreLds = 32 * 1024;  // scores of a workgroup that stay in LDS (four such workgroups fill a compute unit's registers at d = 64)
-struct EvictStepPlan : StepPlan {
+struct EvictStepPlan : ShortStepPlan {
     bool fused, in_lds;
     int pitch;
     size_t off_z, off_mine;
@@ -67,19 +66,19 @@ EvictStepPlan evict_step_plan(const bla_evict_params* p)
 {
     EvictStepPlan s;
     const bla_window_params w = window_of(p, p->slots);
-    static_cast<StepPlan&>(s) = step_plan(&w);
+    static_cast<ShortStepPlan&>(s) = short_step_plan(&w);
     s.fused = s.nsplit == 1 && s.ngrp == 1;
     s.pitch = (p->slots + 31) & ~31;
     const size_t rows = (size_t)p->B * p->H;
     s.off_z = s.fused ? 0 : seq_align(s.nsplit * rows * (p->d + 2) * 4);
-    s.in_lds = s.fused && p->H_kv > 0 && (long long)(p->H / p->H_kv) * s.pitch * 4 <= kScoreLds;
+    s.in_lds = s.fused && p->H_kv > 0 && (long long)(p->H / p->H_kv) * s.pitch * 4 <= score_lds(s.waves, p->io_dtype == BLA_BF16, p->d);
     s.off_mine = s.off_z + (s.in_lds ? 0 : seq_align(rows * s.pitch * 4));
     s.total = s.off_mine + seq_align((size_t)p->B * p->H_kv * 4);
     return s;
 }
 bool fits(const bla_evict_params* p, const EvictStepPlan& s)
 {
-    return launchable((double)p->B * p->H_kv * s.ngrp * s.nsplit, 256) &&
+    return launchable((double)p->B * p->H_kv * s.ngrp * s.nsplit, 64 * s.waves) &&
            launchable((double)p->B * p->H_kv * ((p->slots + 255) / 256) + (double)p->B * p->H / 4 + 1, 256);
 }
 
@@ -214,7 +213,7 @@ bla_status bla_evict_step(const bla_evict_params* p, const void* q, const void* 
     a.z = (float*)((char*)workspace + sp.off_z), a.pitch = sp.pitch, a.mine = (int*)((char*)workspace + sp.off_mine), a.fused = sp.fused, a.in_lds = sp.in_lds;
     hipStream_t s = (hipStream_t)stream;
     const int bf16 = p->io_dtype == BLA_BF16;
-    return launch_evict_step(bf16, p->d, a, s) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
+    return launch_evict_step(bf16, p->d, a, sp.waves, s) == hipSuccess ? BLA_OK : BLA_ERR_HIP;
 }
 
 }  // extern "C"

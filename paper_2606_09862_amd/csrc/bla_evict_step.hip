@@ -49,9 +49,11 @@ template <typename T, int D> __global__ void __launch_bounds__(256) evict_finish
     if (i < a.W) evict_score_out(a, bh, i, mine, n, pos, w);
 }
 
-template <typename T, int D> hipError_t evict_d(const EvictStepArgs& a, hipStream_t s)
+template <typename T, int D> hipError_t evict_d(const EvictStepArgs& a, int waves, hipStream_t s)
 {
-    const hipError_t e = step_d<T, D, kEvict>(a, s);
+    static_assert(StepGeo<T, D, 4>::LDS + 2 * 4 * 16 * 4 + score_lds(4, sizeof(T) == 2, D) <= 160 * 1024, "the step's LDS");
+    static_assert(StepGeo<T, D, 8>::LDS + 2 * 8 * 16 * 4 + score_lds(8, sizeof(T) == 2, D) <= 160 * 1024, "the step's LDS");
+    const hipError_t e = step_d<T, D, kEvict>(a, waves, s);
     if (e != hipSuccess || a.fused) return e;
     const long long sums = (long long)a.B * a.Hkv * ((a.W + 255) / 256), joins = ((long long)a.B * a.H + 3) / 4;
     hipLaunchKernelGGL((evict_finish_kernel<T, D>), dim3((unsigned)(sums + joins)), dim3(256), 0, s, a);
@@ -60,9 +62,9 @@ template <typename T, int D> hipError_t evict_d(const EvictStepArgs& a, hipStrea
 
 }  // namespace
 
-hipError_t launch_evict_step(int bf16_io, int D, const EvictStepArgs& a, hipStream_t s)
+hipError_t launch_evict_step(int bf16_io, int D, const EvictStepArgs& a, int waves, hipStream_t s)
 {
-#define BLA_CALL(T, DD) evict_d<T, DD>(a, s)
+#define BLA_CALL(T, DD) evict_d<T, DD>(a, waves, s)
     BLA_BY_TYPE(BLA_CALL)
 #undef BLA_CALL
 }

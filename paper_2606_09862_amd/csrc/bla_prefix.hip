@@ -23,8 +23,11 @@ bla_status check_prefix(const bla_prefix_params* p, bool step)
 }
 
 // The step's: the prefix in parts that fill the device with the blocks of its queries, of at least a tile for each group of waves, beside the rings' parts.  Few
-// queries go in blocks of 16, whose four waves take 32 tokens each.
-constexpr int kFewQueries = 32, kMaxPrefixParts = 192, kShortBlocks = 48;
+// queries go in blocks of 16, whose four waves take 32 tokens each: against tiles, bf16 at d = 64 with 4 key heads, 16 queries behind each of 16 prefixes of 8192 tokens
+// 30.2 against 41.6 us, 32 queries 35.4 against 45.6, 64 queries 60.8 against 54.4; 32 queries behind one of 2048 7.4 against 9.0.  With a prefix and rings that are
+// short together they need no parts at all: 16 queries behind 512 tokens, rings of 128, 6.1 us in a graph against 6.9 with parts, 10.0 against 13.5 called; behind
+// 1024, rings of 512 (48 blocks), 10.1 against 7.0 and 10.8 against 14.4.
+constexpr int kFewQueries = 32, kMaxPrefixParts = 192;
 struct PrefixStepPlan : StepPlan {
     bool few, both;  // both: no parts
     int npart, nqb, threads;

@@ -85,7 +85,25 @@ inline StepPlan step_plan(const bla_window_params* p)
     s.total = s.nsplit > 1 ? seq_align((size_t)s.nsplit * p->B * p->H * (p->d + 2) * 4) : 0;
     return s;
 }
+// The step of the calls that add to window attention: a short ring's blocks of 32 slots go to the eight waves of one workgroup for each key head, in one launch, rather
+// than in parts that a second launch joins.  With a bias, 4 key heads, d = 64 bf16, one launch against parts: 1 row over 256 slots 7.8 against 9.7 us in a graph, 9.9
+// against 13.8 called; over 1024 10.4 against 9.8 and 10.9 against 14.4; over 1536 12.0 against 9.9 and 12.1 against 14.2.  Key heads that need two parts to fill the
+// device keep it busy by themselves: 36 rows over 2048 slots 17.6 against 22.4 us, but over 16384 of d = 128 231 against 226.
+constexpr int kShortBlocks = 32, kShortBlocksOfMany = 64;
+struct ShortStepPlan : StepPlan {
+    int waves;
+};
+inline ShortStepPlan short_step_plan(const bla_window_params* p)
+{
+    ShortStepPlan s;
+    static_cast<StepPlan&>(s) = step_plan(p);
+    s.waves = 4;
+    const bool many = 2ll * p->B * p->H_kv * s.ngrp > kFill;
+    if (s.nsplit > 1 && ((long long)p->window + p->sinks + 31) / 32 <= (many ? kShortBlocksOfMany : kShortBlocks)) s.nsplit = 1, s.total = 0, s.waves = 8;
+    return s;
+}
 inline bool fits(const bla_window_params* p, const StepPlan& s) { return launchable((double)p->B * p->H_kv * s.ngrp * s.nsplit, 256); }
+inline bool fits(const bla_window_params* p, const ShortStepPlan& s) { return launchable((double)p->B * p->H_kv * s.ngrp * s.nsplit, 64 * s.waves); }
 
 // Backward: the sinks' queries beyond their windows in as many parts as fill the device with waves, a block of 32 queries or more to each.
 struct BackwardPlan {

@@ -52,22 +52,22 @@ __device__ __forceinline__ unsigned score_key(float x)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// The slot that a token of a full cache takes: of those whose token is older than `old` the one with the least score, the lowest of several.  256 threads
-// call it with four words of LDS; every slot is one of slots whatever `at` holds.
-__device__ __forceinline__ int evict_slot(const float* score, const int64_t* at, int slots, int64_t old, uint64_t* lds)
+// The slot that a token of a full cache takes: of those whose token is older than `old` the one with the least score, the lowest of several.  The workgroup's NW
+// waves call it with as many words of LDS; every slot is one of slots whatever `at` holds.
+template <int NW> __device__ __forceinline__ int evict_slot(const float* score, const int64_t* at, int slots, int64_t old, uint64_t* lds)
 {
     uint64_t best = ~0ull;
-    for (int i0 = threadIdx.x; i0 < slots; i0 += 8 * 256) {  // eight loads in flight; a slot that comes twice changes nothing
+    for (int i0 = threadIdx.x; i0 < slots; i0 += 8 * 64 * NW) {  // eight loads in flight; a slot that comes twice changes nothing
         float x[8];
         int64_t p[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const int i = min(i0 + 256 * k, slots - 1);
+            const int i = min(i0 + 64 * NW * k, slots - 1);
             x[k] = score[i], p[k] = at[i];
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const uint64_t key = (uint64_t)(p[k] < old ? score_key(x[k]) : 0xffffffffu) << 32 | (unsigned)min(i0 + 256 * k, slots - 1);
+            const uint64_t key = (uint64_t)(p[k] < old ? score_key(x[k]) : 0xffffffffu) << 32 | (unsigned)min(i0 + 64 * NW * k, slots - 1);
             best = key < best ? key : best;
         }
     }
@@ -79,7 +79,7 @@ __device__ __forceinline__ int evict_slot(const float* score, const int64_t* at,
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = best;
     __syncthreads();
     best = lds[0];
-    for (int i = 1; i < 4; ++i) best = lds[i] < best ? lds[i] : best;
+    for (int i = 1; i < NW; ++i) best = lds[i] < best ? lds[i] : best;
     __syncthreads();  // the caller uses the words again
     const unsigned slot = (unsigned)best;
     return slot < (unsigned)slots ? (int)slot : 0;
@@ -181,7 +181,7 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
         n = a.plen ? min(max(a.plen[gx], 0), a.P) : a.P;
         mine = -1;
     } else if constexpr (EXT == kEvict)
-        mine = pos < slots ? (int)pos : evict_slot(a.score_in + bh * slots, a.at_in + bh * slots, slots, pos - a.recent, (uint64_t*)raw);
+        mine = pos < slots ? (int)pos : evict_slot<NW>(a.score_in + bh * slots, a.at_in + bh * slots, slots, pos - a.recent, (uint64_t*)raw);
     else
         mine = pos < a.S ? (int)pos : a.S + (int)((pos - a.S) % a.W);
     const T *kn = (const T*)a.k + bh * D, *vn = (const T*)a.v + bh * D;
@@ -416,19 +416,26 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
     }
 }
 
-template <typename T, int D, int EXT> __global__ void __launch_bounds__(256) window_step_kernel(typename ExtStepArgs<EXT>::type a)
+template <typename T, int D, int EXT, int NW> __global__ void __launch_bounds__(64 * NW) window_step_kernel(typename ExtStepArgs<EXT>::type a)
 {
-    __shared__ __attribute__((aligned(16))) char raw[StepGeo<T, D>::LDS];
-    __shared__ float sml[2][4][16];
-    window_step_part<T, D, EXT>(a, blockIdx.x, raw, sml);
+    __shared__ __attribute__((aligned(16))) char raw[StepGeo<T, D, NW>::LDS];
+    __shared__ float sml[2][NW][16];
+    window_step_part<T, D, EXT, NW>(a, blockIdx.x, raw, sml);
 }
 
-template <typename T, int D, int EXT> hipError_t step_d(const typename ExtStepArgs<EXT>::type& a, hipStream_t s)
+// waves: of a workgroup, 4, or 8 where the call adds to window attention.
+template <typename T, int D, int EXT> hipError_t step_d(const typename ExtStepArgs<EXT>::type& a, int waves, hipStream_t s)
 {
     size_t more = 0;
     if constexpr (EXT == kEvict)
         if (a.in_lds) more = sizeof(float) * (a.H / a.Hkv) * a.pitch;
-    hipLaunchKernelGGL((window_step_kernel<T, D, EXT>), dim3((unsigned)((long long)a.B * a.Hkv * a.ngrp * a.nsplit)), dim3(256), more, s, a);
+    const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.ngrp * a.nsplit));
+    if constexpr (EXT != kPlain)
+        if (waves == 8) {
+            hipLaunchKernelGGL((window_step_kernel<T, D, EXT, 8>), grid, dim3(512), more, s, a);
+            return hipGetLastError();
+        }
+    hipLaunchKernelGGL((window_step_kernel<T, D, EXT, 4>), grid, dim3(256), more, s, a);
     return hipGetLastError();
 }
 
