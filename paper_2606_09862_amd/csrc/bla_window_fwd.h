@@ -405,20 +405,20 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NW == 8 ? 4 : 1) wi
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         const int i = a0 + 16 * qt + r;
-        const float l = rows_sum(sum[qt]), top = EXT == kBias ? mx[qt] : mx[qt] * sc;
+        const float l = rows_sum(sum[qt]), unit = EXT == kBias ? 1.f : sc;  // mx's, in the base-2 domain
         if (i >= min(G::BQ, a.L - q0)) continue;
         const bool real = i < nq && (EXT != kBias || l > 0.f);  // a bias of minus infinity can leave a row without a key
         if (a.nsplit == 1) {
             const float inv = real ? 1.f / l : 0.f;
 #pragma unroll
             for (int dt = 0; dt < D / 16; ++dt) st4(out + (size_t)i * D + 16 * dt + 4 * g, real ? acc[qt][dt] * inv : zero4());
-            if (a.lse && g == 0) a.lse[row0 + i] = real ? (top + __log2f(l)) * kLn2 : -INFINITY;
+            if (a.lse && g == 0) a.lse[row0 + i] = real ? __builtin_fmaf(mx[qt], unit, __log2f(l)) * kLn2 : -INFINITY;
         } else {
             const size_t at = (size_t)part * a.B * a.H * a.L + row0 + i;
 #pragma unroll
             for (int dt = 0; dt < D / 16; ++dt) st4f(a.part_o + at * D + 16 * dt + 4 * g, acc[qt][dt]);
             if (g == 0) {
-                a.part_ml[2 * at] = real ? top : kNoMax;
+                a.part_ml[2 * at] = real ? mx[qt] * unit : kNoMax;
                 a.part_ml[2 * at + 1] = real ? l : 0.f;
             }
         }
