@@ -26,7 +26,7 @@ bla_status check_prefix(const bla_prefix_params* p, bool step)
 // queries go in blocks of 16, whose four waves take 32 tokens each: against tiles, bf16 at d = 64 with 4 key heads, 16 queries behind each of 16 prefixes of 8192 tokens
 // 30.2 against 41.6 us, 32 queries 35.4 against 45.6, 64 queries 60.8 against 54.4; 32 queries behind one of 2048 7.4 against 9.0.  With a prefix and rings that are
 // short together they need no parts at all: 16 queries behind 512 tokens, rings of 128, 6.1 us in a graph against 6.9 with parts, 10.0 against 13.5 called; behind
-// 1024, rings of 512 (48 blocks), 10.1 against 7.0 and 10.8 against 14.4.
+// 1024, rings of 512, 10.1 against 7.0 and 10.8 against 14.4.
 constexpr int kFewQueries = 32, kMaxPrefixParts = 192;
 struct PrefixStepPlan : StepPlan {
     bool few, both;  // both: no parts
@@ -42,7 +42,7 @@ PrefixStepPlan prefix_step_plan(const bla_prefix_params* p)
     const long long rows = w->H_kv > 0 && p->G > 0 ? (long long)(w->B / p->G) * (w->H / w->H_kv) : 0;
     const PrefixShape shape = prefix_shape(w->io_dtype == BLA_BF16, w->d);
     s.few = rows <= kFewQueries;
-    s.both = s.few && (p->P + 31) / 32 + ((long long)w->window + w->sinks + 31) / 32 <= kShortBlocks;
+    s.both = s.few && short_ring(w, (long long)p->P + w->window + w->sinks, false);
     if (s.both) {
         s.npart = s.nqb = 0, s.nsplit = 1, s.units = 0, s.threads = 512, s.total = 0;
         return s;

@@ -10,7 +10,7 @@ namespace {
 // 16 QT queries from 16 QT w on, and are joined through LDS, so that a workgroup fills half a compute unit and leaves one part for as many waves.  The parts are
 // joined with the ring's by window_join_kernel.
 // Few queries (kFewQueries) leave most of such a workgroup idle: they go as the heads of a ring do, in window_step_part.  Where prefix and ring are short as well
-// (kShortBlocks), a workgroup of eight waves takes both for its key head's heads of one row: one launch, without parts, though each row reads the
+// (short_ring), a workgroup of eight waves takes both for its key head's heads of one row: one launch, without parts, though each row reads the
 // prefix for itself (3 rows of float32 behind 777 tokens, d = 32: 14.3 us a call with parts, 9.5 without; the kernel takes 8.8).
 template <typename T, int D> struct PrefixGeo {
     static constexpr int NT = 256, PE = 16 / (int)sizeof(T), CH = D / PE, RPP = NT / CH, NP = (64 + RPP - 1) / RPP;  // of a group

@@ -86,10 +86,14 @@ inline StepPlan step_plan(const bla_window_params* p)
     return s;
 }
 // The step of the calls that add to window attention: a short ring's blocks of 32 slots go to the eight waves of one workgroup for each key head, in one launch, rather
-// than in parts that a second launch joins.  With a bias, 4 key heads, d = 64 bf16, one launch against parts: 1 row over 256 slots 7.8 against 9.7 us in a graph, 9.9
-// against 13.8 called; over 1024 10.4 against 9.8 and 10.9 against 14.4; over 1536 12.0 against 9.9 and 12.1 against 14.2.  Key heads that need two parts to fill the
-// device keep it busy by themselves: 36 rows over 2048 slots 17.6 against 22.4 us, but over 16384 of d = 128 231 against 226.
-constexpr int kShortBlocks = 32, kShortBlocksOfMany = 64;
+// than in parts that a second launch joins.  With a bias and 4 key heads, one launch against parts: 1 row, d = 64 bf16, 256 slots 7.8 against 9.7 us in a graph, 9.9
+// against 13.8 called; 1024 slots 10.4 against 9.8 and 10.9 against 14.4; 1536 slots 12.0 against 9.9 and 12.1 against 14.2.  d = 128 float32, 224 slots 14.5 against
+// 15.2 and 14.1 against 15.5; 512 slots 24.8 against 15.2 and 24.4 against 15.5.  Key heads that need two parts to fill the device keep it busy by themselves: 36 rows,
+// d = 64 bf16, 2048 slots 17.6 against 22.4 us; d = 128 float32, 1024 slots 43.3 against 57.9, but 2048 slots over an evicting cache 81.6 against 72.8.
+inline bool short_ring(const bla_window_params* p, long long slots, bool many)
+{
+    return slots <= (many ? 2048 : 1024) && slots * p->d * elem_bytes(p->io_dtype) <= (many ? 512 : 120) * 1024;
+}
 struct ShortStepPlan : StepPlan {
     int waves;
 };
@@ -99,7 +103,7 @@ inline ShortStepPlan short_step_plan(const bla_window_params* p)
     static_cast<StepPlan&>(s) = step_plan(p);
     s.waves = 4;
     const bool many = 2ll * p->B * p->H_kv * s.ngrp > kFill;
-    if (s.nsplit > 1 && ((long long)p->window + p->sinks + 31) / 32 <= (many ? kShortBlocksOfMany : kShortBlocks)) s.nsplit = 1, s.total = 0, s.waves = 8;
+    if (s.nsplit > 1 && short_ring(p, (long long)p->window + p->sinks, many)) s.nsplit = 1, s.total = 0, s.waves = 8;
     return s;
 }
 inline bool fits(const bla_window_params* p, const StepPlan& s) { return launchable((double)p->B * p->H_kv * s.ngrp * s.nsplit, 256); }

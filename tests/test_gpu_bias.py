@@ -209,8 +209,9 @@ def test_backward_against_differences():
     (40, 2, 128, 129, 3, [0, 131, 132, 133, 1 << 50], LOG + FAR),  # twenty heads to a key head: two groups
     (4, 2, 64, 3000, 70, [2999, 3069, 3070, 100000], LOG + FAR),   # parts of the ring, blocks of sinks alone
     (2, 2, 128, 300, 0, [-1, 5, 299, -(1 << 62)], LOG),            # rows without a token
-    (4, 2, 64, 1018, 6, [1023, 40, 1024, 90000], LOG + FAR),       # the longest ring of one launch, and the next
-    (4, 2, 64, 1019, 6, [1023, 40, 1025, 90000], LOG + FAR),
+    (4, 2, 64, 954, 6, [959, 40, 960, 90000], LOG + FAR),          # the longest ring of one launch, and the next
+    (4, 2, 64, 955, 6, [959, 40, 961, 90000], LOG + FAR),
+    (4, 2, 64, 474, 6, [479, 40, 480, 90000], LOG + FAR),          # in float32
     (4, 2, 64, 2040, 8, [2047, 40, 2048, 90000] * 17, LOG + FAR),  # with more rows
     (4, 2, 64, 2041, 8, [2047, 40, 2049, 90000] * 17, LOG + FAR),
     (3, 3, 64, 100, 40, [20, 39, 40, 200], tuple(range(1, 64))),

@@ -258,9 +258,11 @@ def check_step(B, H, Hkv, d, slots, recent, pos, dtype, seed=3, inplace=True, sc
     (40, 2, 128, 130, 129, [0, 129, 130, 131, 1 << 40]),       # twenty heads to a key head; one slot that can go
     (4, 2, 64, 3000, 70, [2999, 3000, 3001, 100000]),          # parts of the cache
     (2, 2, 128, 300, 0, [-1, 5, 299, 300, -(1 << 62)]),        # rows without a token
-    (4, 2, 64, 1024, 30, [1023, 1024, 40, 90000]),             # the longest cache of one launch, and the next
-    (4, 2, 64, 1025, 30, [1024, 1025, 40, 90000]),
-    (16, 2, 128, 1024, 30, [1023, 1024, 40, 90000]),           # the most scores that stay on the chip
+    (4, 2, 64, 960, 30, [959, 960, 40, 90000]),                # the longest cache of one launch, and the next
+    (4, 2, 64, 961, 30, [960, 961, 40, 90000]),
+    (4, 2, 64, 480, 30, [479, 480, 40, 90000]),                # in float32
+    (16, 2, 128, 1024, 30, [1023, 1024, 40, 90000] * 17),      # the most scores that stay on the chip, or more
+    (32, 2, 128, 240, 30, [239, 240, 40, 90000]),
     (4, 2, 64, 2048, 30, [2047, 2048, 40, 90000] * 17),        # with more rows
     (4, 2, 64, 2049, 30, [2048, 2049, 40, 90000] * 17),
     (100, 1, 32, 2100, 10, [2500, -1, 7]),                     # more heads than the sums take at a time

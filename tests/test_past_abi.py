@@ -98,7 +98,7 @@ def test_bias_refusals(lib):  # noqa: F811
     big = P(window=5000)
     need = lib.bla_bias_step_workspace_size(ctypes.byref(big))
     assert need > 0 and S(p=big, tail=(WS, need - 1)) == WORKSPACE
-    assert lib.bla_bias_step_workspace_size(ctypes.byref(P(window=1020))) == 0 < lib.bla_bias_step_workspace_size(ctypes.byref(P(window=1021)))  # 32 blocks of 32
+    assert lib.bla_bias_step_workspace_size(ctypes.byref(P(window=956))) == 0 < lib.bla_bias_step_workspace_size(ctypes.byref(P(window=957)))  # 120 KiB of keys
     for i in (0, 1, 2, 3, 4, 5, 6, 8, 9, 10, 11):
         assert B(drop=[i]) == INVALID
     for i in (3, 5, 7, 11):                                   # bias, lse, lengths, dbias
