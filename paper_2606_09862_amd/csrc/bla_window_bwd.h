@@ -11,6 +11,9 @@
 // forms it, whose delta is exact (EXACT), from dS before its rounding.  Where the pairs of a wave share a bucket a lane adds its own to a
 // register; elsewhere dS is summed along its diagonals, a distance to a lane, and then over the lanes of a bucket.  A wave's sums go out once for each head
 // and are added up by bias_bwd_sum_kernel in a fixed order.
+// Bound: issue and waits at two waves to a SIMD, whose 256 registers hold 32 keys' K, V, dK and dV (8 x 16 heads x 2048 queries, four heads to a key head, causal, d = 64,
+// bf16, 32 buckets to 128: key pass 300 us, query pass 180, sum 6; one bucket 421 in all, 64 to 2048 617.  dbias by float atomics in LDS, some 160 cycles each: 1200 where
+// diagonals take 497).
 #pragma once
 
 #include <algorithm>
