@@ -120,6 +120,7 @@ def check_step(B, G, H, Hkv, d, P, window, sinks, pos, dtype, plen=None, seed=3,
     (4, 2, 4, 2, 32, 777, 64, 4, [0, 67, 68, 500], [777, 33]),             # prefix and ring in one launch without parts, the last block of each in part
     (2, 1, 24, 1, 64, 448, 500, 12, [3, 900], None),                       # ... two groups of heads, as many blocks as it takes
     (2, 1, 2, 1, 64, 449, 500, 12, [3, 900], None),                        # ... and one more
+    (4, 2, 4, 2, 64, 100, 64, 4, [0, 67, 68, -1], [0, 100]),                # ... and a prefix without tokens
     (6, 6, 4, 2, 64, 0, 3000, 0, [2999, 3, 5000], None),                   # no prefix, a long ring
     (70, 2, 8, 2, 64, 200, 33, 0, [3, 40, -1, 0, 100], [200, 63]),          # queries in several blocks, the last in part
     (40, 1, 16, 4, 64, 1111, 20, 0, [10, 25], None),
