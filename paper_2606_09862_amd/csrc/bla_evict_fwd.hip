@@ -182,9 +182,9 @@ constexpr int kSelWaves = 16, kSelLds = 24 * 1024;  // entries whose keys are ke
 __global__ void __launch_bounds__(1024) evict_select_kernel(EvictSelectArgs a)
 {
     __shared__ unsigned keys[kSelLds];
-    __shared__ int hist[2048];
+    __shared__ int hist[3][2048];
     __shared__ int wsum[2][kSelWaves];
-    __shared__ int found[2];
+    __shared__ int found[3][3];
     __shared__ int index[kSliceSlots];  // the slice's entries
     const size_t bh = blockIdx.x / a.slices;
     const int slice = (int)(blockIdx.x % a.slices), each_slice = (a.slots + a.slices - 1) / a.slices;
@@ -204,27 +204,56 @@ __global__ void __launch_bounds__(1024) evict_select_kernel(EvictSelectArgs a)
     const float* score = a.score + bh * ((size_t)a.slots + a.L);
     const int64_t* at = a.at_in ? a.at_in + bh * a.slots : nullptr;
     const int64_t late = pos + len - a.recent;  // the first position that stays in any case
-    auto form = [&](int i) {
-        const bool is_old = i < n;
-        const int64_t p = is_old ? at[i] : pos + (i - n);
-        return p >= late ? 0xffffffffu : score_key(score[is_old ? i : a.slots + i - n]);
+    float es[4];
+    int64_t ep[4];
+    auto fetch = [&](int i0) {  // four entries, all loads in flight; one past the last is the last again
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = min(i0 + 1024 * k, total - 1);
+            es[k] = score[i < n ? i : a.slots + i - n];
+            ep[k] = pos + (i - n);
+        }
+        if (n > 0)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t old = at[min(i0 + 1024 * k, n - 1)];
+                ep[k] = i0 + 1024 * k < n ? old : ep[k];
+            }
     };
-    for (int i = tid; i < min(total, kSelLds); i += 1024) keys[i] = form(i);
-    auto key = [&](int i) { return i < kSelLds ? keys[i] : form(i); };
+    auto fetched = [&](int k) { return ep[k] >= late ? 0xffffffffu : score_key(es[k]); };
+    auto key = [&](int i) {
+        if (i < kSelLds) return keys[i];
+        const int64_t p = i < n ? at[i] : pos + (i - n);
+        return p >= late ? 0xffffffffu : score_key(score[i < n ? i : a.slots + i - n]);
+    };
+    fetch(tid);
+    for (int i = tid; i < 3 * 2048; i += 1024) (&hist[0][0])[i] = 0;
+    __syncthreads();
+    for (int i0 = tid; i0 < total;) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + 1024 * k;
+            if (i >= total) continue;
+            const unsigned x = fetched(k);
+            if (i < kSelLds) keys[i] = x;
+            atomicAdd(&hist[0][x >> 21], 1);
+        }
+        i0 += 4096;
+        if (i0 < total) fetch(i0);
+    }
 
     unsigned prefix = 0;    // the upper bits of the last key that stays
     int need = a.slots;     // entries that stay among those with these bits
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-        for (int i = tid; i < 2048; i += 1024) hist[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < total; i += 1024) {
-            const unsigned x = key(i);
-            if (pass == 0 || x >> (pass == 1 ? 21 : 10) == prefix) atomicAdd(&hist[(x >> shift) & (bins - 1)], 1);
-        }
+        if (pass > 0)
+            for (int i = tid; i < total; i += 1024) {
+                const unsigned x = key(i);
+                if (x >> (pass == 1 ? 21 : 10) == prefix) atomicAdd(&hist[pass][(x >> shift) & (bins - 1)], 1);
+            }
         __syncthreads();
         // the bin in which the count from above passes `need`: two bins a thread, the highest first
-        const int t0 = bins - 1 - 2 * tid, c0 = t0 >= 0 ? hist[t0] : 0, c1 = t0 >= 1 ? hist[t0 - 1] : 0;
+        const int t0 = bins - 1 - 2 * tid, c0 = t0 >= 0 ? hist[pass][t0] : 0, c1 = t0 >= 1 ? hist[pass][t0 - 1] : 0;
         int x = c0 + c1;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
@@ -237,12 +266,17 @@ __global__ void __launch_bounds__(1024) evict_select_kernel(EvictSelectArgs a)
         for (int w = 0; w < wave; ++w) above += wsum[0][w];
         if (above < need && above + c0 + c1 >= need) {
             const bool first = above + c0 >= need;
-            found[0] = first ? t0 : t0 - 1;
-            found[1] = need - above - (first ? 0 : c0);
+            found[pass][0] = first ? t0 : t0 - 1;
+            found[pass][1] = need - above - (first ? 0 : c0);
+            found[pass][2] = first ? c0 : c1;
         }
         __syncthreads();
-        prefix = pass == 2 ? prefix << 10 | (unsigned)found[0] : pass == 1 ? prefix << 11 | (unsigned)found[0] : (unsigned)found[0];
-        need = found[1];
+        prefix = pass == 2 ? prefix << 10 | (unsigned)found[pass][0] : pass == 1 ? prefix << 11 | (unsigned)found[pass][0] : (unsigned)found[pass][0];
+        need = found[pass][1];
+        if (pass < 2 && need == found[pass][2]) {  // every key with these bits stays, some below them do not, so the bits are not zeros
+            prefix = (prefix << shift) - 1, need = 0;
+            break;
+        }
     }
     const int each = ((total + kSelWaves - 1) / kSelWaves + 63) & ~63, i0 = wave * each, i1 = min(total, i0 + each);
     int more = 0, same = 0;

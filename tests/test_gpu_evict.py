@@ -184,6 +184,17 @@ def test_select_many():
     check_select(1, 1, 30000, 32, 555, 3, BF, score=base)
 
 
+def test_select_at_a_step():
+    """As many large scores as slots, told from the others by the first bits of their keys, by the next, or by the last; and one more or less."""
+    for low in (1.0, 2.0 - 2.0 ** -10, 2.0 - 2.0 ** -23, 0.0, -2.0, -math.inf):
+        for extra in (-1, 0, 1):
+            s = torch.full((1, 2, 60 + 200), low)
+            g = torch.Generator().manual_seed(extra + 5)
+            for h in range(2):
+                s[0, h, 60 + torch.randperm(200, generator=g)[:60 + extra]] = 2.0
+            check_select(1, 2, 200, 64, 60, 0, BF, score=s)
+
+
 def test_select_equal_and_special_scores():
     """Ties go to the lowest entry; zeros are one number, NaN is above infinity."""
     for pick in ([1.0], [0.0, -0.0], [math.inf, -math.inf, math.nan, 0.0, -0.0, -1.5, 1e-40, -1e-40, 3.0]):
