@@ -146,11 +146,11 @@ __global__ void __launch_bounds__(256) evict_sum_out_kernel(EvictSumArgs a)
 
 // Which entries stay, and their way to the cache.  A workgroup of 16 waves takes one key head of one row and moves a slice of the slots: several find the
 // same in parallel, which costs nothing where the key heads do not fill the device, and a second launch would cost more.  An entry's key is its score's place in the order of scores, the
-// largest of all for the newest `recent` tokens; three counts of its upper 11, next 11 and last 10 bits (by integer atomics in LDS, whose order does not
-// matter) find the key of the last entry that stays, of which the lowest entries fill the slots.  Then each wave walks a sixteenth of the entries
-// in order, first to count, then to number those that stay.
-// Bound: latency: three counts, as many scans and two dependent loads (1024 of 4096 entries for 32 key heads, d = 64: 14 us, 1.3 TB/s; a launch to choose and one to move
-// 18.7).
+// largest of all for the newest `recent` tokens; counts of its upper 11, next 11 and last 10 bits (by integer atomics in LDS, whose order does not
+// matter) find the key of the last entry that stays, of which the lowest entries fill the slots.  Once all entries with the bits found so far stay, no further bits are
+// looked at.  Then each wave walks a sixteenth of the entries in order, first to count, then to number those that stay.
+// Bound: latency: two or three counts, as many scans and two dependent loads (1024 of 4096 entries for 32 key heads, d = 64: 12.4 us, 1.5 TB/s; a launch to choose and one
+// to move 18.7; loads one by one and always three counts 14.1).  With as many key heads as compute units it is bound by memory (32 rows of 8, d = 128: 53 us, 5.1 TB/s).
 __device__ __forceinline__ void move_slice(const EvictSelectArgs& a, size_t bh, int64_t pos, int s0, int s1, const int* index)
 {
     const intx4 *ck = (const intx4*)a.ck + bh * a.slots * a.pieces, *cv = (const intx4*)a.cv + bh * a.slots * a.pieces;
