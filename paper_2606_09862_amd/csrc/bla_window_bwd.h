@@ -301,38 +301,7 @@ __global__ void __launch_bounds__(256) window_bwd_q_kernel(typename ExtBwdArgs<E
                 }
             }
             float sx = sc, bu = 0.f;
-            if constexpr (EXT == kBias) {
-                const int dmax = c + a0 + 16 * QT - 1 - i0 + (i0 < 0 ? far : 0);
-                const int ulo = lanes.bucket(c + a0 - i1), uhi = lanes.bucket(dmax);
-                bu = lanes.of(ulo);
-                if (ulo != uhi) {
-#pragma unroll
-                    for (int qt = 0; qt < QT; ++qt) {
-                        float bv[8];
-                        const int n = c + a0 + 16 * qt + r - i0 - 4 * g;  // of the lane's first key
-                        if (dmax < kNear && (i0 >= 0 || i1 < 0)) {
-                            const float* from = near + kPad + n + (i0 < 0 ? far : 0);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) bv[e] = from[-16 * (e >> 2) - (e & 3)];
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) bv[e] = bu;
-                            for (int w = ulo + 1; w <= uhi; ++w) {
-                                const int edge = lanes.first(w);
-                                const float x = lanes.of(w);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const int m = n - 16 * (e >> 2) - (e & 3), j = i0 + 4 * g + 16 * (e >> 2) + (e & 3);
-                                    bv[e] = m + (j < 0 ? far : 0) >= edge ? x : bv[e];
-                                }
-                            }
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) s[qt][e >> 2][e & 3] = __builtin_fmaf(s[qt][e >> 2][e & 3], sc, bv[e]);
-                    }
-                    sx = 1.f, bu = 0.f;
-                }
-            }
+            if constexpr (EXT == kBias) bias_scores<QT>(s, sx, bu, lanes, near, sc, c + a0, i0, far, g, r);
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt)
 #pragma unroll

@@ -1,9 +1,10 @@
-// Host-side view of the library's internals for the CPU tests: the launch plans (bla_api.hip) and
-// the slot order of the folded kernels (bla_device.h).  Compiled for the host only.
+// Host-side view of the library's internals for the CPU tests: the launch plans (bla_api.hip),
+// the slot order of the folded kernels (bla_device.h) and the spans of the learned bias (bla_bias.h).  Compiled for the host only.
 #include <stdio.h>
 #include <stdlib.h>
 
 #include "bla_api.hip"
+#include "bla_bias.h"
 #include "bla_device.h"
 
 // plan: reads lines "form B H L d M S bf16 chunk anchor", form f (forward), b (backward) or s (step),
@@ -90,11 +91,31 @@ static int products()
     return 0;
 }
 
+// bias: reads lines "first query, queries, first key, far"; prints the least and the largest distance and whether the table of near distances is read.
+// bias_table: reads last edges; prints where the table ends.
+static int bias_spans()
+{
+    int qi, queries, i0, far;
+    while (scanf("%d %d %d %d", &qi, &queries, &i0, &far) == 4) {
+        const BiasSpan d = bias_span(qi, queries, i0, far);
+        printf("%d %d %d\n", d.lo, d.hi, bias_near(d, i0));
+    }
+    return 0;
+}
+static int bias_tables()
+{
+    int last;
+    while (scanf("%d", &last) == 1) printf("%d\n", bias_table_end(last));
+    return 0;
+}
+
 int main(int argc, char** argv)
 {
     if (argc == 2 && !strcmp(argv[1], "products")) return products();
     if (argc == 2 && !strcmp(argv[1], "slots")) return slots();
     if (argc == 2 && !strcmp(argv[1], "records")) return records();
     if (argc == 2 && !strcmp(argv[1], "plan")) return plans();
+    if (argc == 2 && !strcmp(argv[1], "bias")) return bias_spans();
+    if (argc == 2 && !strcmp(argv[1], "bias_table")) return bias_tables();
     return 2;
 }
