@@ -153,7 +153,10 @@ bla_status bla_evict_select(const bla_evict_params* p, const void* k, const void
                             const int64_t* pos, const void* cache_k_in, const void* cache_v_in, const int64_t* at_in, void* cache_k_out,
                             void* cache_v_out, float* score_out, int64_t* at_out, void* stream)
 {
-    const bla_status st = check_evict(p, false);
+    if (!p) return BLA_ERR_INVALID_ARG;
+    bla_evict_params own = *p;  // query heads and the scale are no part of this call, whatever they hold
+    own.H = 0, own.scale = 0.f;
+    const bla_status st = check_evict(&own, false);
     if (st != BLA_OK) return st;
     if (!select_fits(p)) return BLA_ERR_UNSUPPORTED;
     if (p->B == 0 || p->H_kv == 0) return BLA_OK;

@@ -222,6 +222,14 @@ def test_evict_refusals(lib):  # noqa: F811
         assert lib.bla_evict_step_workspace_size(ctypes.byref(evict(L=L))) == need and T(evict(L=L), drop=[0]) == INVALID
 
 
+def test_select_takes_no_notice_of_query_heads_and_scale(lib):  # noqa: F811
+    S = lambda p, drop=(): call(lib.bla_evict_select, p, 12, drop)  # noqa: E731
+    for kw in (dict(H=3), dict(H=-1), dict(H=0), dict(H=1 << 30), dict(scale=float("nan")), dict(scale=3e6), dict(scale=1e-9)):
+        assert S(evict(B=0, **kw), range(12)) == OK, kw
+        assert S(evict(**kw), [2]) == INVALID, kw             # the missing scores, and nothing before them
+    assert lib.bla_evict_select(None, *addresses(12), None) == INVALID
+
+
 def test_launches(lib):  # noqa: F811
     """A launch holds fewer than 2^32 threads: refused before any launch, and without a workspace's size."""
     size = lambda name, p: getattr(lib, name)(ctypes.byref(p))  # noqa: E731
