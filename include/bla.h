@@ -446,8 +446,10 @@ bla_status bla_prefix_step(const bla_prefix_params* p, const void* q, const void
  * a token's score is the sum of the softmax weights that it has got, over the queries since it came and over the query heads of its key head.
  * A row at position pos (tokens before the call) has min(pos, slots) tokens, in the first slots.
  *   cache_k, cache_v: [B, H_kv, slots, d] in the io dtype   score: float32 [B, H_kv, slots]   at: int64 [B, H_kv, slots], the tokens' positions
- * The newest `recent` tokens are never given up.  Scores are compared as numbers (NaN above all of them); of equal ones the lowest entry goes
- * first into what stays, and is the first to be replaced by bla_evict_step.
+ * The newest `recent` tokens are never given up.  bla_evict_select counts the call's own among them (positions from pos + L - recent on stay); bla_evict_step counts
+ * those before its token (positions from pos - recent on stay, and the token itself), so it keeps one more than a call of one token and a selection after it would.
+ * Such a call also sees a full cache and its token, the step the cache in which its token has taken a slot: one token fewer.
+ * Scores are compared as numbers (NaN above all of them); of equal ones the lowest entry goes first into what stays, and is the first to be replaced by bla_evict_step.
  *   q, o: [B, H, L, d]   k, v: [B, H_kv, L, d]   lengths, pos: as for bla_window_forward, idle rows included (their caches stay as they are).
  * Slots that no token has reached are never read as tokens.  Supported: shapes and types of window attention; 1 <= slots <= 2^24, 0 <= recent < slots.
  */
@@ -479,7 +481,8 @@ bla_status bla_evict_forward(const bla_evict_params* p, const void* q, const voi
 /*
  * The cache after L tokens: of its tokens and the call's the newest `recent` stay and of the others those with the largest scores [B, H_kv, slots + L], slots
  * in all, in the order of their entries; their scores and positions go with them.  Slots without a token: zeros, at = -1.  cache_k_in, cache_v_in and
- * at_in: all or none.  p->H and p->scale are not used.
+ * at_in: all or none.  p->H and p->scale are not used.  Without a cache nothing before token 0 exists, at any position: a row at pos > 0 with fewer than `slots` tokens
+ * then gets a cache of its own tokens that no later call can take, since one at pos + L would find min(pos + L, slots) tokens in it.
  */
 bla_status bla_evict_select(const bla_evict_params* p, const void* k, const void* v, const float* score, const int32_t* lengths,
                             const int64_t* pos, const void* cache_k_in, const void* cache_v_in, const int64_t* at_in,

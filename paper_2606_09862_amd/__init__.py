@@ -916,7 +916,8 @@ def evict_select(k, v, score, slots: int, recent: int = 0, cache_k=None, cache_v
     with the largest score [B,H_kv,slots+L] (of equal ones the lowest entries), `slots` in all, in the order of their entries.
 
     cache_k / cache_v [B,H_kv,slots,d] and at [B,H_kv,slots] int64 (the tokens' positions): all or none.  Returns (cache_k, cache_v, score, at)
-    after the call, new tensors; slots without a token hold zeros and a position of -1.
+    after the call, new tensors; slots without a token hold zeros and a position of -1.  Without a cache a row should be at position 0 or have `slots` tokens
+    or more: a later call takes min(position, slots) of the slots as tokens.
     """
     B, Hkv, L, d = k.shape
     dt, dev = k.dtype, k.get_device()
@@ -940,8 +941,8 @@ def evict_select(k, v, score, slots: int, recent: int = 0, cache_k=None, cache_v
 def evict_step(q, k, v, cache_k, cache_v, score, at, recent: int = 0, pos=None, t0: int = 0, scale: float | None = None, workspace=None,
                out=None, score_out=None, at_out=None):
     """bla_evict_step: one decode token per row, q [B,H,d], k and v [B,H_kv,d], over a cache [B,H_kv,slots,d] that takes it in place: in slot pos while it is not
-    full, then in that of the least score among the tokens older than the newest `recent`.  score [B,H_kv,slots] float32 and at [B,H_kv,slots] int64 are updated in place,
-    or written to score_out and at_out.  A row with a negative pos is idle (zeros).  Returns (o, score after the call, at after the call)."""
+    full, then in that of the least score among the tokens older than the newest `recent` before it (evict_select counts the call's own among
+    them).  score [B,H_kv,slots] float32 and at [B,H_kv,slots] int64 are updated in place, or written to score_out and at_out.  A row with a negative pos is idle (zeros).  Returns (o, score after the call, at after the call)."""
     B, H, d = q.shape
     Hkv, dt, dev = k.shape[1], q.dtype, q.get_device()
     if cache_k.dim() != 4:
