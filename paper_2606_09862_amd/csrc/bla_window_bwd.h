@@ -812,10 +812,12 @@ template <typename T, int D, int EXT> hipError_t backward_d(const typename ExtBw
     typedef BwdGeo<T, D> G;
     // The bias's gradient is float32 and takes a delta that is not rounded.  (Putting only delta right for it in long rows, without the third product, took the
     // query pass of bla_bias_backward from 188 to 146 us but left dq an error of 0.0026 where this has 0.0024 and one rounding of dq 0.0017.)
+    const dim3 queries((unsigned)(8 * a.q_per));
+    constexpr bool exact = sizeof(T) == 2;
     if (EXT == kBias || std::min((long long)a.W + a.S, (long long)a.L) <= kExactKeys)
-        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, sizeof(T) == 2, EXT>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
-    else
-        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, EXT == kBias && sizeof(T) == 2, EXT>), dim3((unsigned)(8 * a.q_per)), dim3(G::NT), 0, s, a);
+        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, exact, EXT>), queries, dim3(G::NT), 0, s, a);
+    else if constexpr (EXT != kBias)
+        hipLaunchKernelGGL((window_bwd_q_kernel<T, D, false, EXT>), queries, dim3(G::NT), 0, s, a);
     hipLaunchKernelGGL((window_bwd_k_kernel<T, D, EXT>), dim3((unsigned)(8 * a.k_per) + a.s_units), dim3(G::NT), 0, s, a);
     if (a.ns > 0) {
         const long long n = (long long)a.B * a.Hkv * a.ns * (2 * D / 4);

@@ -157,7 +157,7 @@ __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>
         return qrow + i;
     };
 
-    int64_t pos;
+    int64_t pos = 0;  // kFew: of no row
     if (EXT != kFew && row_tokens(nullptr, a.pos, a.t0, b, 1, pos) == 0) {  // a row without a token
         for (int i = tid; i < nh * D; i += NT)
             if (whole) ((T*)a.o)[qrow * D + i] = (T)0.f;
