@@ -8,8 +8,8 @@ namespace {
 // Sums over the queries of P = exp(scale q k - lse).  Every lse has to be known first, so the scores are formed again, once for each head.  Wave w of a
 // workgroup owns 32 keys of one head's key block, whose K are operands in registers for the whole walk over 64-query tiles; S = Q K^T (accumulator rows:
 // queries) leaves each lane four queries of a key, whose weights it adds up in float32.  The heads of a group are added up by evict_sum_out_kernel, in order.
-// Bound: issue, of one product instead of two and as many exponentials as attention itself (2 x 16 heads x 4096 queries over themselves, d = 64, bf16: 62-65 us beside
-// 90 for the attention; the heads' sum 4).
+// Bound: issue, of one product instead of two and as many exponentials as attention itself (2 x 16 heads x 4096 queries over themselves, d = 64, bf16: 57 us beside
+// 102 for the attention; the heads' sum 5).
 template <typename T, int D> struct SumGeo {
     static constexpr int NT = 256, PE = 16 / (int)sizeof(T), CH = D / PE, RPP = NT / CH, NP = (64 + RPP - 1) / RPP;
     static constexpr int KT = 2, LD = nat_ld<T>(D);

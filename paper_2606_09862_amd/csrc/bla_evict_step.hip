@@ -7,7 +7,7 @@ namespace {
 // What is left where several workgroups share a key head's slots or heads.  The first workgroups form the sums of the weights, 256 slots to each: the maxima
 // and sums of up to 64 heads at a time are joined from their parts (a wave to a head, a part to a lane), then each thread adds its slot's weights up,
 // head by head.  The others join the outputs, four rows to each.
-// Bound: latency (16 heads of 4 key heads with 4096 slots, d = 128: 3.8 us behind the 7.9 of the parts; sums and joins in launches of their own 19.3 us a call, so 14.5).
+// Bound: latency (16 heads of 4 key heads with 4096 slots, d = 128: 3.9 us behind the 8.4 of the parts; sums and joins in launches of their own 19.3 us a call, so 14.5).
 template <typename T, int D> __global__ void __launch_bounds__(256) evict_finish_kernel(EvictStepArgs a)
 {
     __shared__ float sm[64], sinv[64];

@@ -8,9 +8,10 @@ namespace {
 // without a mask.  A workgroup takes 64 QT queries and a part of the prefix, in tiles of 64 tokens that pass through two LDS buffers, one barrier per
 // tile, as in window_forward_kernel; each fragment read from LDS serves QT products.  KG groups of four waves take every KG-th tile, wave w of a group the
 // 16 QT queries from 16 QT w on, and are joined through LDS, so that a workgroup fills half a compute unit and leaves one part for as many waves.  The parts are
-// joined with the ring's by window_join_kernel.  Bound: for one prefix of many tokens its bytes (16 rows x 16 heads on 2 behind 65536 tokens, d = 128, bf16: 26 us for 67 MB
-// read and 17 MB of parts, with 128 parts; 44 in all with 48 parts of one group, 29 now); with as many rows as fill the device also the rings' (256 rows x 16 heads on 4
-// behind 8192, rings of 512, d = 64: 30 us for 110 MB and 9 GFLOP).
+// joined with the ring's by window_join_kernel.  Bound: for one prefix of many tokens neither its bytes nor issue: a group walks four tiles or so, one ahead, so that
+// starting and ending weigh as much as the stream (16 rows x 16 heads on 2 behind 65536 tokens, d = 128, bf16: 26 us for 67 MB read and 17 MB of parts, 3.2 TB/s, with 128
+// parts; 44 in all with 48 parts of one group, 29 now); with as many rows as fill the device also the rings' (256 rows x 16 heads on 4
+// behind 8192, rings of 512, d = 64: 33 us for 110 MB and 9 GFLOP).
 // Few queries (kFewQueries) leave most of such a workgroup idle: they go as the heads of a ring do, in window_step_part.  Where prefix and ring are short as well
 // (short_ring), a workgroup of eight waves takes both for its key head's heads of one row: one launch, without parts, though each row reads the
 // prefix for itself (3 rows of float32 behind 777 tokens, d = 32: 14.3 us a call with parts, 9.5 without; the kernel takes 8.8).

@@ -11,8 +11,9 @@
 // forms it, whose delta is exact (EXACT), from dS before its rounding.  Where the pairs of a wave share a bucket a lane adds its own to a
 // register; elsewhere dS is summed along its diagonals, a distance to a lane, and then over the lanes of a bucket.  A wave's sums go out once for each head
 // and are added up by bias_bwd_sum_kernel in a fixed order.
-// Bound: issue and waits at two waves to a SIMD, whose 256 registers hold 32 keys' K, V, dK and dV (8 x 16 heads x 2048 queries, four heads to a key head, causal, d = 64,
-// bf16, 32 buckets to 128: key pass 300 us, query pass 180, sum 6; one bucket 421 in all, 64 to 2048 617.  dbias by float atomics in LDS, some 160 cycles each: 1200 where
+// Bound: the query pass by issue at two waves to a SIMD, the key pass by its longest walks: 256 registers hold 32 keys' K, V, dK and dV, and 512 workgroups start at once in as
+// many places, the first keys' with 16 times the last keys' queries, so that 1.3 waves of two are left on average (8 x 16 heads x 2048 queries, four heads to a key head,
+// causal, d = 64, bf16, 32 buckets to 128: key pass 281 us, query pass 166, sum 6; one bucket 421 in all, 64 to 2048 617.  dbias by float atomics in LDS, some 160 cycles each: 1200 where
 // diagonals take 497).
 #pragma once
 
@@ -811,7 +812,7 @@ template <typename T, int D, int EXT> hipError_t backward_d(const typename ExtBw
 {
     typedef BwdGeo<T, D> G;
     // The bias's gradient is float32 and takes a delta that is not rounded.  (Putting only delta right for it in long rows, without the third product, took the
-    // query pass of bla_bias_backward from 188 to 146 us but left dq an error of 0.0026 where this has 0.0024 and one rounding of dq 0.0017.)
+    // query pass of bla_bias_backward from 188 to 146 us, both with a cold clock, but left dq an error of 0.0026 where this has 0.0024 and one rounding of dq 0.0017.)
     const dim3 queries((unsigned)(8 * a.q_per));
     constexpr bool exact = sizeof(T) == 2;
     if (EXT == kBias || std::min((long long)a.W + a.S, (long long)a.L) <= kExactKeys)

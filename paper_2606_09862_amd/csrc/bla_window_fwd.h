@@ -98,7 +98,7 @@ constexpr float kLag = 8.f;
 // LDS, elsewhere from a selection at each edge.
 // A prefix (EXT = kPrefix) has tiles of its own ahead of the others.
 // QT tiles of 16 queries to a wave: with two each fragment read from LDS serves two products, and what a tile costs beside its pairs is shared.
-// Both are bound by issue as well.  4 x 16 heads x 4096 queries, four heads to a key head, causal, d = 64, bf16, 32 buckets to 128: 186-190 us, 725-740 TFLOP/s of
+// Both are bound by issue as well.  4 x 16 heads x 4096 queries, four heads to a key head, causal, d = 64, bf16, 32 buckets to 128: 186-191 us, 720-740 TFLOP/s of
 // visible pairs (208 with a tile to a wave, 235 with the blocks in order of the rows too).  16 rows x 16 heads x 512 queries of which 13 % are padding behind 4096
 // tokens: 175 us (650 TFLOP/s over all queries, 754 with 24 whole rows).
 template <typename T, int D, int NW, int QT, bool RING, int EXT>

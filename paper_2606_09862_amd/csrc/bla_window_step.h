@@ -118,8 +118,8 @@ template <typename T, int D, int NW = 4> struct StepGeo {
 // EXT = kEvict: the token's slot is found first, and the scores are kept until the softmax's sum is known.
 // EXT = kFew: not the ring but a part of the prefix, for 16 of the few queries that share it (heads of one row or of several).
 // EXT = kBoth: the blocks of the prefix, then the ring's, for the heads of one row.
-// 256 rows, four key heads of 1028 slots, d = 64, bf16: with a bias 46 us for 204 MB, 4.4 TB/s; 512 rows over caches of 1024 slots with their scores 98 us for 449 MB,
-// 4.6 TB/s (111 with the scores in memory, loaded one by one).  What a bias or a score costs a slot hides behind the ring's bytes.
+// 256 rows, four key heads of 1028 slots, d = 64, bf16: with a bias 46 us for 204 MB, 4.4 TB/s; 512 rows over caches of 1024 slots with their scores 99 us for 449 MB,
+// 4.5 TB/s (111 with the scores in memory, loaded one by one).  What a bias or a score costs a slot hides behind the ring's bytes.
 template <typename T, int D, int EXT, int NW = 4>
 __device__ __forceinline__ void window_step_part(const typename ExtStepArgs<EXT>::type& a, unsigned u, char* raw, float (&sml)[2][NW][16])
 {
