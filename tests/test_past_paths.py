@@ -155,3 +155,24 @@ def test_biased_backward_of_many_blocks(dtype, d):
     want = bla.bias_backward(*args, lengths=n, workspace=torch.zeros(need // 4, device="cuda").view(torch.uint8))
     got = bla.bias_backward(*args, lengths=n, workspace=torch.full((need // 4,), math.nan, device="cuda").view(torch.uint8))
     assert all(torch.isfinite(x).all() and torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("slots", [300, 3000])  # one launch, and parts
+def test_evicting_step_with_one_result_in_place(slots):
+    """Scores in place and positions elsewhere, and the other way round: the same results, and what is not in place stays as it was."""
+    B, H, Hkv, d = 4, 4, 2, 64
+    pos = torch.tensor([slots + 9, 5, -1, slots], device="cuda")
+    x = [normal(90 + i, *s).cuda() for i, s in enumerate(((B, H, d), (B, Hkv, d), (B, Hkv, d), (B, Hkv, slots, d), (B, Hkv, slots, d)))]
+    score, at = evict.weights(96, B, Hkv, slots).cuda(), torch.arange(slots, device="cuda").expand(B, Hkv, slots).contiguous()
+
+    def step(**more):
+        s, a = score.clone(), at.clone()
+        got = bla.evict_step(*x[:3], x[3].clone(), x[4].clone(), s, a, 7, pos=pos, **more)
+        return s, a, got
+
+    _, _, want = step()
+    s, a, got = step(at_out=torch.full_like(at, 9))
+    assert got[1] is s and torch.equal(a, at) and all(torch.equal(y, z) for y, z in zip(got, want))
+    s, a, got = step(score_out=torch.full_like(score, 9.0))
+    assert got[2] is a and torch.equal(s, score) and all(torch.equal(y, z) for y, z in zip(got, want))
